@@ -67,7 +67,8 @@ typedef enum {
     W4A16_ERR_ALIGNMENT = 3,     /* a pointer is not 16-byte aligned */
     W4A16_ERR_CUDA = 4,          /* a CUDA runtime/driver call or launch failed */
     W4A16_ERR_TIMEOUT = 5,       /* a kernel gave up on a bounded wait */
-    W4A16_ERR_INDEX = 6          /* an index check of a W4A16_DEBUG build failed */
+    W4A16_ERR_INDEX = 6,         /* an index check of a W4A16_DEBUG build failed */
+    W4A16_ERR_CAPACITY = 7       /* a key-value cache has too few free pages, or a list is full */
 } w4a16_status;
 
 /*
@@ -268,11 +269,147 @@ int w4a16_topk_smallest(const void* scores, int score_bits, int64_t n, int64_t k
                         void* out_index_i32, void* out_score_f32, void* stream);
 
 /*
+ * A paged key-value cache, for sequences that grow one token at a time and for
+ * prefixes that many sequences share: a protein's tokens are prefilled once and
+ * every ligand's sequence goes on from the same pages (the paper's workflow
+ * scores one target against many ligands, Sec. 3.3, Sec. 4.1).  The caller owns
+ * every buffer; all are device memory, 16-byte aligned, and none overlap.
+ *   pages       bf16 (kv_bits 16) or e4m3 (kv_bits 8)
+ *               [layers, 2, num_pages, kv_heads, page_tokens, head_dim]: keys
+ *               and values; a page index stands for one page of every layer
+ *   exponents   kv_bits 8: uint8 [layers, num_pages, kv_heads, page_tokens, 2],
+ *               for each token's key and value of a head a power of two, biased
+ *               by 127; kv_bits 16: NULL
+ *   page_table  int32 [num_slots, max_pages]: token t of slot s is in page
+ *               page_table[s][t / page_tokens], at t % page_tokens.  Entries past a
+ *               sequence's last page mean nothing and are left as they are.
+ *   seq_len     int32 [num_slots], tokens of each slot's sequence (0: none)
+ *   page_refs   int32 [num_pages], how many sequences have the page; 0: free
+ *   scratch     w4a16_kv_scratch_bytes bytes for the page operations, any contents
+ * Supported: head_dim 128; page_tokens 16, 32, 64 or 128; num_slots <= 65536;
+ * num_pages <= 2^24; a layer's rows (2 num_pages kv_heads page_tokens) < 2^31.
+ * An empty cache has seq_len and page_refs all zero.  The struct is a HOST
+ * object that each call reads before it returns.  Calls on one cache are
+ * ordered by the caller (one stream, or events): the operations below read and
+ * write its tables on the device, and none of them synchronises, so that they can
+ * be captured in a graph together.
+ *
+ * 8-bit rows: a row x of 128 values is held as codes RNE_e4m3(x / 2^e) with e the
+ * smallest integer for which every finite |x| <= 448 2^e (at least -120);
+ * infinities become +-448 2^e, a NaN stays one.
+ *
+ * Slot lists: entries of -1 are skipped (a batch padded to a captured graph's
+ * size); the other slots of one list are distinct.  The lists, and the tables
+ * they lead to, are checked on the device: a slot outside [0, num_slots) or twice
+ * in a list, a length or page index out of range record W4A16_ERR_INVALID_ARG
+ * in the device status word, and too few free pages W4A16_ERR_CAPACITY.  A page
+ * operation that records an error changes nothing; kv_write and
+ * attention_decode leave out the rows concerned.
+ */
+typedef struct {
+    void* pages;
+    void* exponents;
+    void* page_table;
+    void* seq_len;
+    void* page_refs;
+    void* scratch;
+    int64_t layers;
+    int64_t num_pages;
+    int64_t kv_heads;
+    int64_t page_tokens;
+    int64_t head_dim;
+    int64_t num_slots;
+    int64_t max_pages;
+    int64_t kv_bits;
+} w4a16_kv_cache;
+
+/* Bytes of a cache's scratch buffer; 0 for sizes that are not supported. */
+int64_t w4a16_kv_scratch_bytes(int64_t num_pages, int64_t num_slots);
+
+/*
+ * Grows the sequence of slots_i32[i] by add_i32[i] >= 0 tokens, i < n <= num_slots:
+ * allocates pages up to the new length and sets seq_len.  The tokens' keys and
+ * values are then written layer by layer (w4a16_kv_write, w4a16_attention_decode).
+ * A sequence whose last page is part full and shared with others first gets a
+ * copy of that page's tokens, in every layer (copy on write; each of several such
+ * sequences in one call gets its own).  Free pages are taken lowest index first,
+ * by the list's order, a sequence's copy before its new pages.
+ */
+int w4a16_kv_extend(const w4a16_kv_cache* cache, const void* slots_i32, const void* add_i32,
+                    int64_t n, void* stream);
+
+/*
+ * Gives the empty slot children_i32[i] the sequence of slot parents_i32[i], i < n <=
+ * num_slots: the same length and the same pages, whose reference counts grow; no
+ * page is copied.  Parents may repeat; a child is no parent of the same call.  An entry
+ * whose child is -1 is skipped.
+ */
+int w4a16_kv_fork(const w4a16_kv_cache* cache, const void* parents_i32, const void* children_i32,
+                  int64_t n, void* stream);
+
+/*
+ * Shortens the sequence of slots_i32[i] to keep_i32[i] tokens (0 <= keep <= its
+ * length; keep_i32 NULL: 0, which frees it), i < n <= num_slots: gives back the pages
+ * past the new length.
+ */
+int w4a16_kv_trim(const w4a16_kv_cache* cache, const void* slots_i32, const void* keep_i32,
+                  int64_t n, void* stream);
+
+/*
+ * Moves the pages in use to the front of the pool: with n_live of them, those
+ * at indices >= n_live move, in order, to the free pages below; tables and
+ * counts follow.  The memory behind the first n_live pages is then free.  What the
+ * pages that were left hold is unspecified.
+ */
+int w4a16_kv_compact(const w4a16_kv_cache* cache, void* stream);
+
+/*
+ * Stores the keys and values of a packed batch's tokens in one layer's pages.
+ *   qkv_bf16       [M, (H + 2 kv_heads) * 128] bf16: queries, keys and values by
+ *                  columns, as w4a16_attention_prefill reads them where H =
+ *                  kv_heads (the H * 128 query columns are not read; H >= 0)
+ *   seq_start_i32  [nseq + 1], as in w4a16_attention_prefill: rows
+ *                  [seq_start[i], seq_start[i+1]) are the LAST tokens of the
+ *                  sequence of slots_i32[i] (after w4a16_kv_extend); a table that
+ *                  decreases or leaves [0, M], or a sequence shorter than its rows,
+ *                  records W4A16_ERR_INVALID_ARG
+ *   layer          0 .. layers - 1
+ */
+int w4a16_kv_write(const w4a16_kv_cache* cache, int64_t layer, const void* qkv_bf16,
+                   const void* seq_start_i32, const void* slots_i32, int64_t nseq, int64_t M,
+                   int64_t H, void* stream);
+
+/*
+ * Attention of one new token per sequence over the cache, one layer:
+ *   out[i, h*128 + t] = sum_j softmax_j(q_i,h . k_j / sqrt(128)) v_j[t]
+ * over tokens j of slot slots_i32[i]'s sequence with len - window <= j < len,
+ * key and value head h / (H / kv_heads).  The new token is the sequence's last
+ * one (j = len - 1, after w4a16_kv_extend): its key and value come from the row of
+ * qkv, are stored in the cache, and count as the cache holds them.
+ *   qkv_bf16   [n, (H + 2 kv_heads) * 128] bf16, H a multiple of kv_heads
+ *   slots_i32  [n]; a row of slot -1, or of an empty sequence, gives zeros
+ *   out_bf16   [n, H * 128] bf16, written in full
+ *   workspace  w4a16_attention_decode_workspace bytes, zeroed by the caller
+ *              before its first use; calls leave it ready for the next one.  Calls
+ *              that may run at the same time need one each.
+ * Scores and sums in fp32; the softmax's weights are rounded to bf16 (kv_bits 16)
+ * or fp16 (kv_bits 8) for the product with the values; one bf16 rounding at the
+ * store.  Keys outside the range may hold anything, NaN included.
+ */
+int w4a16_attention_decode(const w4a16_kv_cache* cache, int64_t layer, const void* qkv_bf16,
+                           const void* slots_i32, int64_t n, int64_t H, int64_t window,
+                           void* out_bf16, void* workspace, void* stream);
+
+/* Bytes of the workspace on the current device, for any n and any cache of these heads. */
+int w4a16_attention_decode_workspace(int64_t H, int64_t kv_heads, int64_t* bytes);
+
+/*
  * Synchronises `stream`, then reads and clears the device status word.
  * Returns W4A16_OK, the first error a kernel recorded since the last read
  * (W4A16_ERR_TIMEOUT from a bounded wait that ran out, W4A16_ERR_INVALID_ARG
- * from a bad sequence table or gather index), or W4A16_ERR_CUDA if the
- * synchronisation or the copy failed.
+ * from a bad sequence table, gather index or slot, W4A16_ERR_CAPACITY from a cache
+ * with too few free pages), or W4A16_ERR_CUDA if the synchronisation or the copy
+ * failed.
  */
 int w4a16_get_device_error(void* stream);
 

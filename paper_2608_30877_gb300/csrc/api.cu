@@ -1,6 +1,7 @@
 // C ABI of the library (declared in include/w4a16.h): argument validation,
 // TMA descriptor encoding, kernel dispatch and the device status word.
 #include "internal.h"
+#include "kv.h"
 #include "ptx.cuh"
 #include "w4a16.h"
 
@@ -399,6 +400,27 @@ int launch_linear(const DeviceState& st, const void* x, const void* w, const voi
 
 uint64_t wait_limit_ns() { return g_wait_limit_ns.load(std::memory_order_relaxed); }
 
+int library_state(LibraryState* out) {
+    DeviceState* st = nullptr;
+    const int rc = device_state(&st);
+    if (rc != W4A16_OK) return rc;
+    *out = {st->sm_count, st->status};
+    return W4A16_OK;
+}
+
+int encode_3d(CUtensorMap* map, CUtensorMapDataType dtype, const void* base, const uint64_t dims[3],
+              const uint64_t strides[2], const uint32_t box[3]) {
+    const cuuint64_t d[3] = {dims[0], dims[1], dims[2]};
+    const cuuint64_t s[2] = {strides[0], strides[1]};
+    const cuuint32_t b[3] = {box[0], box[1], box[2]};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    const CUresult r = g_encode(map, dtype, 3, const_cast<void*>(base), d, s, b, estr,
+                                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? W4A16_OK : W4A16_ERR_CUDA;
+}
+
 }  // namespace w4a16
 
 using namespace w4a16;
@@ -739,6 +761,7 @@ extern "C" const char* w4a16_status_string(int status) {
         case W4A16_ERR_CUDA: return "CUDA error";
         case W4A16_ERR_TIMEOUT: return "kernel wait timed out";
         case W4A16_ERR_INDEX: return "index check failed (debug build)";
+        case W4A16_ERR_CAPACITY: return "too few free pages in the key-value cache";
         default: return "unknown status";
     }
 }

@@ -1,0 +1,61 @@
+// Rows of the key-value cache: where a token's key or value of one head lies, and the
+// 8-bit form of a row.
+#pragma once
+
+#include <cstdint>
+
+#include "kv.h"
+
+namespace w4a16 {
+
+// Row of (layer, key or value, page, head, token in the page), in rows of 128 values; a
+// long cache passes 32 bits.
+__device__ __forceinline__ int64_t kv_row(const KvView& kv, int layer, int which, int page, int head,
+                                          int at) {
+    return ((((static_cast<int64_t>(layer) * 2 + which) * kv.num_pages + page) * kv.kv_heads + head)
+            << kv.page_shift) + at;
+}
+// Its exponent byte.
+__device__ __forceinline__ int64_t kv_exponent(const KvView& kv, int layer, int which, int page,
+                                               int head, int at) {
+    return ((((static_cast<int64_t>(layer) * kv.num_pages + page) * kv.kv_heads + head)
+             << kv.page_shift) + at) * 2 + which;
+}
+
+// The 8-bit form takes a power of two per row, not amax / 448: a power of two scales
+// exactly, costs an e4m3 code no relative precision, and takes one byte.
+constexpr int kKvMinExp = -120;
+
+// The smallest e >= kKvMinExp with amax <= 448 * 2^e, amax finite and not negative:
+// 448 = 1.75 * 2^8, so e is amax's exponent less 8, one more if its mantissa is past 1.75.
+__device__ __forceinline__ int e4m3_row_exponent(float amax) {
+    const uint32_t b = __float_as_uint(amax);
+    const int e = static_cast<int>(b >> 23) - 127 - 8 + ((b & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+    return e < kKvMinExp ? kKvMinExp : e;
+}
+// |x| for the row's largest; what is not finite does not count.
+__device__ __forceinline__ float finite_abs(float x) {
+    const float a = fabsf(x);
+    return a < __int_as_float(0x7F800000) ? a : 0.0f;
+}
+// 2^e within the normal range.
+__device__ __forceinline__ float power_of_two(int e) {
+    return __uint_as_float(static_cast<uint32_t>(e + 127) << 23);
+}
+// Two values to e4m3, the first in the low byte; round to nearest even, infinities to 448.
+__device__ __forceinline__ uint32_t e4m3_pair(float lo, float hi) {
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ uint32_t e4m3_quad(float a, float b, float c, float d) {
+    return e4m3_pair(a, b) | (e4m3_pair(c, d) << 16);
+}
+// Two e4m3 codes to a pair of halves, exactly.
+__device__ __forceinline__ uint32_t e4m3_to_half2(uint16_t codes) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(codes));
+    return r;
+}
+
+}  // namespace w4a16

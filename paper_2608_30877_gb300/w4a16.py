@@ -7,6 +7,7 @@ missing, the call raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 import re
@@ -19,7 +20,8 @@ LIB_PATH = os.path.join(_PKG, "libw4a16_debug.so" if os.environ.get("W4A16_DEBUG
                         else "libw4a16.so")
 HEADER = os.path.join(os.path.dirname(_PKG), "include", "w4a16.h")
 
-OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_ALIGNMENT, ERR_CUDA, ERR_TIMEOUT, ERR_INDEX = range(7)
+OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_ALIGNMENT, ERR_CUDA, ERR_TIMEOUT, ERR_INDEX, \
+    ERR_CAPACITY = range(8)
 ACT_NONE, ACT_SWIGLU, ACT_GELU = range(3)
 
 _lib = None
@@ -35,6 +37,13 @@ class Layer(ctypes.Structure):
     _fields_ = [("x", ctypes.c_void_p), ("w_packed", ctypes.c_void_p),
                 ("scales", ctypes.c_void_p), ("out", ctypes.c_void_p),
                 ("N", ctypes.c_int64), ("K", ctypes.c_int64)]
+
+
+class KVCacheStruct(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("pages", "exponents", "page_table", "seq_len",
+                                               "page_refs", "scratch")] + \
+               [(n, ctypes.c_int64) for n in ("layers", "num_pages", "kv_heads", "page_tokens",
+                                              "head_dim", "num_slots", "max_pages", "kv_bits")]
 
 
 def header_functions() -> list[str]:
@@ -64,6 +73,16 @@ def lib() -> ctypes.CDLL:
         L.w4a16_attention_zero_outside.argtypes = [p, i64, i64, i64, i64, p, p]
         L.w4a16_topk_smallest.argtypes = [p, ctypes.c_int, i64, i64, p, p, p]
         L.w4a16_quantize.argtypes = [p, p, p, i64, i64, i64, p]
+        kv = ctypes.POINTER(KVCacheStruct)
+        L.w4a16_kv_scratch_bytes.argtypes = [i64, i64]
+        L.w4a16_kv_scratch_bytes.restype = i64
+        L.w4a16_kv_extend.argtypes = [kv, p, p, i64, p]
+        L.w4a16_kv_fork.argtypes = [kv, p, p, i64, p]
+        L.w4a16_kv_trim.argtypes = [kv, p, p, i64, p]
+        L.w4a16_kv_compact.argtypes = [kv, p]
+        L.w4a16_kv_write.argtypes = [kv, i64, p, p, p, i64, i64, i64, p]
+        L.w4a16_attention_decode.argtypes = [kv, i64, p, p, i64, i64, i64, p, p, p]
+        L.w4a16_attention_decode_workspace.argtypes = [i64, i64, ctypes.POINTER(i64)]
         L.w4a16_get_device_error.argtypes = [p]
         L.w4a16_selftest_wait_timeout.argtypes = [i64, p]
         L.w4a16_selftest_set_wait_limit.argtypes = [i64]
@@ -76,6 +95,8 @@ def lib() -> ctypes.CDLL:
                   "w4a16_gather_rows", "w4a16_topk_smallest", "w4a16_attention_prefill",
                   "w4a16_attention_zero_outside", "w4a16_stack_graph_create", "w4a16_stack_graph_launch",
                   "w4a16_stack_graph_destroy", "w4a16_dequant", "w4a16_quantize",
+                  "w4a16_kv_extend", "w4a16_kv_fork", "w4a16_kv_trim", "w4a16_kv_compact",
+                  "w4a16_kv_write", "w4a16_attention_decode", "w4a16_attention_decode_workspace",
                   "w4a16_get_device_error", "w4a16_selftest_wait_timeout",
                   "w4a16_selftest_set_wait_limit", "w4a16_selftest_route"):
             getattr(L, f).restype = ctypes.c_int
@@ -273,6 +294,178 @@ def quantize(w: torch.Tensor, g: int = 128, stream=None):
     _check("w4a16_quantize", lib().w4a16_quantize(w.data_ptr(), packed.data_ptr(),
                                                   scales.data_ptr(), N, K, g, _stream(stream)))
     return packed, scales
+
+
+def _allocating_on(stream):
+    """Context in which torch allocates (and fills) for use on `stream`."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(_stream(stream))
+    return torch.cuda.stream(stream)
+
+
+class KVCache:
+    """A paged key-value cache (include/w4a16.h): the tensors and the handle that the kv_*
+    functions and attention_decode take.  dtype torch.bfloat16, or torch.float8_e4m3fn with
+    a power-of-two exponent for each token's key and value of a head.  Calls on one cache
+    are ordered by the caller."""
+
+    def __init__(self, layers: int, num_pages: int, kv_heads: int, num_slots: int, max_pages: int,
+                 page_tokens: int = 64, dtype=torch.bfloat16, head_dim: int = 128, device="cuda"):
+        i32 = {"dtype": torch.int32, "device": device}
+        e4m3 = dtype == torch.float8_e4m3fn
+        self._bind(torch.empty((layers, 2, num_pages, kv_heads, page_tokens, head_dim), dtype=dtype,
+                               device=device),
+                   torch.zeros((num_slots, max_pages), **i32), torch.zeros(num_slots, **i32),
+                   torch.zeros(num_pages, **i32),
+                   torch.empty((layers, num_pages, kv_heads, page_tokens, 2), dtype=torch.uint8,
+                               device=device) if e4m3 else None)
+
+    @classmethod
+    def from_tensors(cls, pages: torch.Tensor, page_table: torch.Tensor, seq_len: torch.Tensor,
+                     page_refs: torch.Tensor, exponents: torch.Tensor | None = None) -> "KVCache":
+        """A cache over tensors that the caller keeps (shapes as in include/w4a16.h)."""
+        cache = cls.__new__(cls)
+        cache._bind(pages, page_table, seq_len, page_refs, exponents)
+        return cache
+
+    def _bind(self, pages, page_table, seq_len, page_refs, exponents):
+        given = (page_table, seq_len, page_refs) + (() if exponents is None else (exponents,))
+        _need_cuda(pages, *given)
+        if pages.dtype not in (torch.bfloat16, torch.float8_e4m3fn):
+            raise ValueError("a cache's pages are torch.bfloat16 or torch.float8_e4m3fn")
+        if pages.dim() != 6 or pages.shape[1] != 2 or page_table.dim() != 2:
+            raise ValueError("expected pages [layers, 2, num_pages, kv_heads, page_tokens, head_dim] "
+                             "and page_table [num_slots, max_pages]")
+        layers, _, num_pages, kv_heads, page_tokens, head_dim = pages.shape
+        num_slots, max_pages = page_table.shape
+        if (any(t.dtype != torch.int32 for t in (page_table, seq_len, page_refs))
+                or seq_len.shape != (num_slots,) or page_refs.shape != (num_pages,)):
+            raise ValueError("expected int32 page_table, seq_len [num_slots] and page_refs [num_pages]")
+        e4m3 = pages.dtype == torch.float8_e4m3fn
+        if e4m3 != (exponents is not None) or (e4m3 and (
+                exponents.dtype != torch.uint8
+                or exponents.shape != (layers, num_pages, kv_heads, page_tokens, 2))):
+            raise ValueError("exponents uint8 [layers, num_pages, kv_heads, page_tokens, 2] come with "
+                             "pages in e4m3, and only with them")
+        if any(t.device != pages.device for t in given):
+            raise ValueError("a cache's tensors are on one device")
+        self.pages, self.page_table, self.seq_len = pages, page_table, seq_len
+        self.page_refs, self.exponents = page_refs, exponents
+        self.layers, self.num_pages, self.kv_heads, self.page_tokens = layers, num_pages, kv_heads, page_tokens
+        self.num_slots, self.max_pages = num_slots, max_pages
+        size = lib().w4a16_kv_scratch_bytes(num_pages, num_slots)
+        if size == 0:
+            raise W4A16Error("w4a16_kv_scratch_bytes", ERR_UNSUPPORTED)
+        self._scratch = torch.empty(size, dtype=torch.uint8, device=pages.device)
+        self._workspaces, self._workspace_bytes = {}, {}
+        self._struct = KVCacheStruct(
+            pages.data_ptr(), None if exponents is None else exponents.data_ptr(), page_table.data_ptr(),
+            seq_len.data_ptr(), page_refs.data_ptr(), self._scratch.data_ptr(), layers, num_pages, kv_heads,
+            page_tokens, head_dim, num_slots, max_pages, 8 if e4m3 else 16)
+        self._ref = ctypes.byref(self._struct)
+
+    def new_workspace(self, H: int, stream=None) -> torch.Tensor:
+        """A workspace for attention_decode with H query heads, zeroed on `stream`."""
+        with _allocating_on(stream):
+            return torch.zeros(self.workspace_bytes(H), dtype=torch.uint8, device=self.pages.device)
+
+    def workspace_bytes(self, H: int) -> int:
+        if H not in self._workspace_bytes:
+            size = ctypes.c_int64()
+            _check("w4a16_attention_decode_workspace", lib().w4a16_attention_decode_workspace(
+                H, self.kv_heads, ctypes.byref(size)))
+            self._workspace_bytes[H] = size.value
+        return self._workspace_bytes[H]
+
+
+def _need_list(t: torch.Tensor, n: int | None = None) -> int:
+    if not (t.is_cuda and t.dtype == torch.int32 and t.dim() == 1 and t.is_contiguous()
+            and (n is None or t.shape[0] == n)):
+        raise ValueError("expected contiguous int32 CUDA lists of one length")
+    return t.shape[0]
+
+
+def kv_extend(cache: KVCache, slots: torch.Tensor, add: torch.Tensor, stream=None) -> None:
+    """Grows the sequences of `slots` by `add` tokens each (int32 lists): allocates pages, and
+    copies a part-full last page that others share (include/w4a16.h)."""
+    n = _need_list(slots)
+    _need_list(add, n)
+    _check("w4a16_kv_extend", lib().w4a16_kv_extend(cache._ref, slots.data_ptr(), add.data_ptr(), n,
+                                                    _stream(stream)))
+
+
+def kv_fork(cache: KVCache, parents: torch.Tensor, children: torch.Tensor, stream=None) -> None:
+    """Gives the empty slots `children` the sequences of `parents`, sharing their pages."""
+    n = _need_list(parents)
+    _need_list(children, n)
+    _check("w4a16_kv_fork", lib().w4a16_kv_fork(cache._ref, parents.data_ptr(), children.data_ptr(), n,
+                                                _stream(stream)))
+
+
+def kv_trim(cache: KVCache, slots: torch.Tensor, keep: torch.Tensor | None = None, stream=None) -> None:
+    """Shortens the sequences of `slots` to `keep` tokens each; None frees them."""
+    n = _need_list(slots)
+    if keep is not None:
+        _need_list(keep, n)
+    _check("w4a16_kv_trim", lib().w4a16_kv_trim(cache._ref, slots.data_ptr(),
+                                                None if keep is None else keep.data_ptr(), n,
+                                                _stream(stream)))
+
+
+def kv_compact(cache: KVCache, stream=None) -> None:
+    """Moves the pages in use to the front of the pool."""
+    _check("w4a16_kv_compact", lib().w4a16_kv_compact(cache._ref, _stream(stream)))
+
+
+def _need_qkv(cache: KVCache, qkv: torch.Tensor, H: int) -> None:
+    if not (qkv.is_cuda and qkv.dtype == torch.bfloat16 and qkv.dim() == 2 and qkv.is_contiguous()
+            and qkv.shape[1] == (H + 2 * cache.kv_heads) * cache.pages.shape[5]):
+        raise ValueError("expected a contiguous bf16 CUDA qkv [rows, (H + 2 kv_heads) * head_dim]")
+
+
+def kv_write(cache: KVCache, layer: int, qkv: torch.Tensor, seq_start: torch.Tensor, slots: torch.Tensor,
+             H: int, stream=None) -> None:
+    """Stores the keys and values of a packed batch in one layer's pages: rows
+    [seq_start[i], seq_start[i+1]) are the last tokens of slots[i]'s sequence."""
+    _need_qkv(cache, qkv, H)
+    n = _need_list(slots)
+    _need_list(seq_start, n + 1)
+    _check("w4a16_kv_write", lib().w4a16_kv_write(
+        cache._ref, layer, qkv.data_ptr(), seq_start.data_ptr(), slots.data_ptr(), n, qkv.shape[0], H,
+        _stream(stream)))
+
+
+def attention_decode(cache: KVCache, layer: int, qkv: torch.Tensor, slots: torch.Tensor, H: int,
+                     window: int = 32768, out: torch.Tensor | None = None,
+                     workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Attention of one new token per sequence over the cache, its key and value stored
+    (include/w4a16.h): qkv bf16 [n, (H + 2 kv_heads) 128], slots int32 [n] -> out bf16
+    [n, H 128].  Without `workspace` the cache's own is used, made on the first call: calls
+    on several streams at once need one each (KVCache.new_workspace)."""
+    _need_qkv(cache, qkv, H)
+    n = _need_list(slots, qkv.shape[0])
+    if workspace is None:
+        workspace = cache._workspaces.get(H)
+        if workspace is None:
+            workspace = cache._workspaces[H] = cache.new_workspace(H, stream)
+    elif not (workspace.is_cuda and workspace.is_contiguous()
+              and workspace.numel() * workspace.element_size() >= cache.workspace_bytes(H)):
+        raise ValueError("expected a workspace of KVCache.new_workspace(H)")
+    if out is None:
+        if stream is None:
+            out = torch.empty((n, H * 128), dtype=torch.bfloat16, device=qkv.device)
+        else:
+            with _allocating_on(stream):
+                out = torch.empty((n, H * 128), dtype=torch.bfloat16, device=qkv.device)
+    elif not (out.is_cuda and out.dtype == torch.bfloat16 and out.is_contiguous()
+              and out.shape == (n, H * 128)):
+        raise ValueError("expected a contiguous bf16 CUDA out [n, H * 128]")
+    _check("w4a16_attention_decode", lib().w4a16_attention_decode(
+        cache._ref, layer, qkv.data_ptr(), slots.data_ptr(), n, H, int(window), out.data_ptr(),
+        workspace.data_ptr(), _stream(stream)))
+    return out
 
 
 def selftest_wait_timeout(limit_ns: int, stream=None) -> None:
