@@ -303,8 +303,9 @@ int w4a16_topk_smallest(const void* scores, int score_bits, int64_t n, int64_t k
  * they lead to, are checked on the device: a slot outside [0, num_slots) or twice
  * in a list, a length or page index out of range record W4A16_ERR_INVALID_ARG
  * in the device status word, and too few free pages W4A16_ERR_CAPACITY.  A page
- * operation that records an error changes nothing; kv_write and
- * attention_decode leave out the rows concerned.
+ * operation that records an error changes nothing; kv_write leaves out the rows
+ * concerned, and in attention_decode they are zero (a bad page index may show
+ * after the row's own key and value were stored).
  */
 typedef struct {
     void* pages;
@@ -390,8 +391,9 @@ int w4a16_kv_write(const w4a16_kv_cache* cache, int64_t layer, const void* qkv_b
  *   slots_i32  [n]; a row of slot -1, or of an empty sequence, gives zeros
  *   out_bf16   [n, H * 128] bf16, written in full
  *   workspace  w4a16_attention_decode_workspace bytes, zeroed by the caller
- *              before its first use; calls leave it ready for the next one.  Calls
- *              that may run at the same time need one each.
+ *              before its first use and after a W4A16_ERR_TIMEOUT; calls leave it
+ *              ready for the next one.  Calls that may run at the same time need
+ *              one each.
  * Scores and sums in fp32; the softmax's weights are rounded to bf16 (kv_bits 16)
  * or fp16 (kv_bits 8) for the product with the values; one bf16 rounding at the
  * store.  Keys outside the range may hold anything, NaN included.

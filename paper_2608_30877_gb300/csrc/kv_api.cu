@@ -241,6 +241,9 @@ extern "C" int w4a16_attention_decode(const w4a16_kv_cache* cache, int64_t layer
     p.window = window > kMaxDim ? static_cast<int>(kMaxDim) : static_cast<int>(window);
     p.scale = 1.0f / sqrtf(static_cast<float>(kKvHeadDim));
     p.wait_ns = wait_limit_ns();
-    return status_of(launch_attention_decode(view_of(*cache, st.status), p, st.sm_count,
-                                             static_cast<cudaStream_t>(stream)));
+    const KvView view = view_of(*cache, st.status);
+    alignas(64) CUtensorMap map;
+    rc = encode_cache(&map, view, p.layer);
+    if (rc != W4A16_OK) return rc;
+    return status_of(launch_attention_decode(map, view, p, st.sm_count, static_cast<cudaStream_t>(stream)));
 }

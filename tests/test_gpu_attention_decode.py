@@ -218,7 +218,8 @@ def test_padding_rows_and_bad_slots(bits):
         assert (out[1] == 0).all(), what
         others = [0, 2, 3, 4, 5]
         assert torch.equal(out[others], want[others]), what
-        case.check_rest(before, rows=others)
+        # (a bad page index may show after the row's own token was stored)
+        case.check_rest(before, rows=others + ([1] if what == "page" else []))
 
 
 def test_unused_memory_of_any_kind_is_not_seen():
