@@ -6,9 +6,11 @@
 //
 //  * Units.  The keys that a row sees, cut into tiles of 32 KB of keys and values (64 tokens
 //    in bf16, 128 in e4m3), times the key heads, form one list over the whole batch, and
-//    each CTA takes an equal run of it.  A row's length is thus split over as many CTAs as
-//    its share of the bytes, and short rows share a CTA.  Everything follows from the
-//    lengths on the device, so that a captured graph serves growing sequences.
+//    each CTA takes a run of it with an equal share of the keys (rows end inside tiles: by
+//    equal numbers of tiles the 64 rows of 200 to 1024 tokens kept an SM busy 72% of the
+//    time).  A row's length is thus split over as many CTAs as its share of the bytes,
+//    and short rows share a CTA.  Everything follows from the lengths on the device, so
+//    that a captured graph serves growing sequences.
 //  * Stages.  One warp walks the run: it looks pages up in the table, and brings the pieces of
 //    a tile by TMA into a ring of three stages (192 KB in flight on an SM's two CTAs), with
 //    the row's queries and the new token's key and value.
@@ -46,6 +48,7 @@ constexpr int kStages = 3;
 constexpr int kHalfStage = 16384;            // a tile's keys, or its values
 constexpr int kStageBytes = 2 * kHalfStage;
 constexpr int kMaxCols = 64;                 // query columns of an item
+constexpr int kQueryStride = 272;            // bytes between rows of q, on other banks
 constexpr int kCtasPerSm = 2;
 constexpr int kInvalid = 1;                  // W4A16_ERR_INVALID_ARG
 // e4m3: fp16 weights go up to 2^12, so that the least of them is 2^-36 of the largest
@@ -70,7 +73,10 @@ __host__ __device__ inline int used_columns(int group) { return group < kMaxCols
 
 // A part in the workspace: the outputs of its columns, then their sums, maxima, and the
 // maxima that the outputs are relative to (e4m3; else the same).
-__host__ __device__ inline int part_floats(int cols) { return cols * (kKvHeadDim + 3); }
+__host__ __device__ inline int part_floats(int cols) { return (cols * (kKvHeadDim + 3) + 3) / 4 * 4; }
+
+// The workspace's counters, one for each CTA.
+__host__ __device__ inline int counter_bytes(int ctas) { return (ctas * 4 + 15) / 16 * 16; }
 
 // What the producer says about a stage.
 struct Unit {
@@ -83,19 +89,31 @@ struct Unit {
 };
 constexpr int kFirst = 1;    // the item's first unit in this CTA
 constexpr int kLast = 2;     // and its last
+constexpr int kEnd = 16;     // the CTA's last unit
 constexpr int kNew = 4;      // the tile has the new token
 constexpr int kBad = 8;      // a page index out of range
-constexpr int kQSlotShift = 4;
+constexpr int kQSlotShift = 5;
+
+// A row's slot and the keys it sees; no keys for padding, an empty sequence or bad data.
+struct Row {
+    int slot, len, low;
+    int first, tiles;  // its first tile, and how many
+    int skip;          // groups of 16 keys of the first tile that it does not see
+    int weight;        // of an item: the groups that it sees, and kItemWeight
+};
 
 struct Shared {
     uint64_t full[kStages], empty[kStages], met;
     Unit unit[kStages];
     alignas(16) uint16_t fresh[kStages][2][kKvHeadDim];           // the new token's key and value
     alignas(16) uint8_t exponents[kStages][2 * 128];  // e4m3: a tile's (key, value) pairs
-    float part_l[kWarps][16], part_m[kWarps][16], part_w[kWarps][16];
+    alignas(16) float part_l[kMaxCols][kWarps], part_m[kMaxCols][kWarps], part_w[kMaxCols][kWarps];
     int64_t warp_sum[kThreads / 32];
+    int64_t bound[2];
     int64_t start_base;
     int start_row;
+    Row start;
+    int empty_rows;
     int is_last;
     int abort;
 };
@@ -145,13 +163,13 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {
 template <bool E4M3>
 __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     if constexpr (E4M3)
-        asm volatile(
+        asm(
             "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
             "{%8, %9}, {%0, %1, %2, %3};"
             : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
             : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
     else
-        asm volatile(
+        asm(
             "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
             "{%8, %9}, {%0, %1, %2, %3};"
             : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
@@ -162,7 +180,10 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint3
 __device__ __forceinline__ bool consumers_meet(Shared& sh, uint32_t& phase, int* status, uint64_t wait_ns) {
     __syncwarp();
     if ((threadIdx.x & 31) == 0) mbar_arrive(smem_u32(&sh.met));
-    const bool ok = wait_warp(smem_u32(&sh.met), phase, &sh.abort, status, wait_ns);
+    // (the others are a few instructions away: polls that do not suspend the warp)
+    bool ok = false;
+    for (int i = 0; i < 64 && !ok; ++i) ok = __all_sync(0xffffffffu, mbar_test_wait(smem_u32(&sh.met), phase));
+    if (!ok) ok = wait_warp(smem_u32(&sh.met), phase, &sh.abort, status, wait_ns);
     phase ^= 1;
     return ok;
 }
@@ -185,14 +206,12 @@ __device__ __forceinline__ uint32_t tile_byte(int row, int unit) {
     return base + row * 128u + (((unit & 7) ^ (row & 7)) << 4);
 }
 
-// A row's slot and the keys it sees; no keys for padding, an empty sequence or bad data.
-struct Row {
-    int slot, len, low, first, tiles;  // first: its first tile
-};
+// An item costs about as much beside its keys as this many groups of 16.
+constexpr int kItemWeight = 2;
 template <bool E4M3>
 __device__ __forceinline__ Row row_of(const DecodeArgs& a, int i, bool* bad) {
-    constexpr int kTile = E4M3 ? 128 : 64;
-    Row r{a.p.slots[i], 0, 0, 0, 0};
+    constexpr int kGroups = E4M3 ? 8 : 4;  // of a tile
+    Row r{a.p.slots[i], 0, 0, 0, 0, 0, 0};
     *bad = r.slot < -1 || r.slot >= a.kv.num_slots;
     if (*bad || r.slot < 0) return r;
     const int len = a.kv.seq_len[r.slot];
@@ -200,19 +219,60 @@ __device__ __forceinline__ Row row_of(const DecodeArgs& a, int i, bool* bad) {
     if (*bad || len == 0) return r;
     r.len = len;
     r.low = len > a.window ? len - a.window : 0;
-    r.first = r.low / kTile;
-    r.tiles = (len - 1) / kTile + 1 - r.first;
+    const int begin = r.low / 16, end = (len - 1) / 16 + 1;
+    r.first = begin / kGroups;
+    r.tiles = (end - 1) / kGroups + 1 - r.first;
+    r.skip = begin - r.first * kGroups;
+    r.weight = end - begin + kItemWeight;
     return r;
 }
+// Where tile t of an item starts in its weight.
+template <bool E4M3>
+__device__ __forceinline__ int tile_start(const Row& r, int t) {
+    return t == 0 ? 0 : t * (E4M3 ? 8 : 4) - r.skip;
+}
 
-// The CTA whose run has unit u: runs start at c * units / ctas, rounded down.
-__device__ __forceinline__ int cta_of(int64_t u, int64_t units, int64_t ctas) {
-    return static_cast<int>(((u + 1) * ctas - 1) / units);
+// CTA c has the tiles that start in [bound(c), bound(c + 1)), bound(c) = c * weight / ctas rounded
+// down and, if that is at most kSnap groups from the start or the end of the item in which it
+// falls, moved there: a part costs more than so many groups.  kSnap is at least a tile and
+// kItemWeight, and so are the bounds apart before they move; so each part of an item has a tile.
+template <bool E4M3>
+struct Snap {
+    static constexpr int kGroups = E4M3 ? 8 : 4;  // of a tile
+    static constexpr int kMost = kGroups + kItemWeight;
+    static constexpr int kSnap = E4M3 ? 16 : 12;
+    static_assert(kSnap >= kMost);
+};
+// A bound within the items of a row, which start at `base`.
+template <bool E4M3>
+__device__ __forceinline__ int64_t snapped(int64_t bound, int64_t base, int item_weight) {
+    const int into = static_cast<int>((bound - base) % item_weight);
+    return into <= Snap<E4M3>::kSnap                 ? bound - into
+           : item_weight - into <= Snap<E4M3>::kSnap ? bound + (item_weight - into)
+                                                     : bound;
+}
+// The parts of an item [begin, end), and the CTA of the first if there are more.
+template <bool E4M3>
+__device__ __forceinline__ int parts_of(int64_t begin, int64_t end, int64_t weight, int64_t ctas, int* first_cta) {
+    // the bounds in (begin + kSnap, end - kSnap)
+    const int64_t lo = ((begin + Snap<E4M3>::kSnap + 1) * ctas + weight - 1) / weight;
+    const int64_t hi = ((end - Snap<E4M3>::kSnap) * ctas - 1) / weight;
+    *first_cta = static_cast<int>(lo) - 1;
+    return end - begin > 2 * Snap<E4M3>::kSnap && hi >= lo ? static_cast<int>(hi - lo) + 2 : 1;
+}
+
+// The next row with keys; without tiles if there is none.
+template <bool E4M3>
+__device__ __forceinline__ Row next_row(const DecodeArgs& a, int* row) {
+    Row r{};
+    bool bad;
+    while (r.tiles == 0 && *row + 1 < a.p.n) r = row_of<E4M3>(a, ++*row, &bad);
+    return r;
 }
 
 template <bool E4M3>
 __device__ void produce(const DecodeArgs& a, const CUtensorMap* map, Shared& sh, uint32_t stages,
-                        uint32_t queries, int64_t units, int64_t ctas, int64_t u0, int64_t u1) {
+                        uint32_t queries, int64_t weight, int64_t ctas, int64_t w0, int64_t w1) {
     constexpr int kTile = E4M3 ? 128 : 64;
     const KvView& kv = a.kv;
     const int lane = threadIdx.x & 31;
@@ -227,18 +287,31 @@ __device__ void produce(const DecodeArgs& a, const CUtensorMap* map, Shared& sh,
 
     int row = sh.start_row;
     int64_t base = sh.start_base;
-    bool bad;
-    Row r = row_of<E4M3>(a, row, &bad);
-    int item = static_cast<int>((u0 - base) / r.tiles);
-    int tile = static_cast<int>((u0 - base) - static_cast<int64_t>(item) * r.tiles);
+    Row r = sh.start;
+    int item = static_cast<int>((w0 - base) / max(r.weight, 1)), tile = 0;
+    const int rest = static_cast<int>((w0 - base) - static_cast<int64_t>(item) * r.weight);
+    while (tile < r.tiles && tile_start<E4M3>(r, tile) < rest) tile = max(tile + 1, (rest + r.skip) / (kTile / 16));
+    bool begun = false, more = true;
     int ids = 0, ids_from = -1, ids_row = -1;  // 32 entries of the row's page list, a lane each
     int slot = 0;             // of the item's queries
     int since[2] = {0, 0};    // units since the one that read each query slot; 0: none
     int st = 0;
     uint32_t phase = 0;       // of the stage's barriers
     int64_t issued = 0;
-    for (int64_t u = u0; u < u1; ++u, ++issued) {
-        const bool first = u == u0 || tile == 0;
+    if (item == items) {  // (a bound moved to the end of the row)
+        item = tile = 0;
+        base += static_cast<int64_t>(items) * r.weight;
+        r = next_row<E4M3>(a, &row);
+        more = r.tiles > 0;
+    }
+    if (!more || tile >= r.tiles) {  // (only if the lengths changed during the call)
+        sh.abort = 1;
+        record_status(kv.status, kInvalid);
+        return;
+    }
+    for (; more; ++issued) {
+        const bool first = !begun || tile == 0;
+        begun = true;
         if (issued >= kStages &&
             !wait_warp(smem_u32(&sh.empty[st]), phase ^ 1, &sh.abort, kv.status, a.p.wait_ns))
             break;
@@ -274,7 +347,10 @@ __device__ void produce(const DecodeArgs& a, const CUtensorMap* map, Shared& sh,
         const int loads = __popc(__ballot_sync(0xffffffffu, mine));
         const bool fresh = key0 + kTile >= r.len;
         const int last_id = __shfl_sync(0xffffffffu, ids, (((r.len - 1) >> kv.page_shift) - ids_from) & 31);
-        const bool last = u + 1 == u1 || tile + 1 == r.tiles;
+        // whether the item goes on in this CTA, and the CTA after it
+        const int64_t begin = base + static_cast<int64_t>(item) * r.weight;
+        const bool last = tile + 1 == r.tiles || begin + tile_start<E4M3>(r, tile + 1) >= w1;
+        more = !last || (tile + 1 == r.tiles && begin + r.weight < w1);
         const uint32_t bar = smem_u32(&sh.full[st]);
         const int q_cols = min(a.cols.block, a.cols.group - block * a.cols.block);
         if (lane == 0) {
@@ -286,29 +362,25 @@ __device__ void produce(const DecodeArgs& a, const CUtensorMap* map, Shared& sh,
             t.low = r.low;
             t.len = r.len;
             t.flags = (first ? kFirst : 0) | (last ? kLast : 0) | (fresh ? kNew : 0) | (tile_bad ? kBad : 0) |
-                      slot << kQSlotShift;
+                      (more ? 0 : kEnd) | slot << kQSlotShift;
             if (last) {
-                const int64_t begin = base + static_cast<int64_t>(item) * r.tiles;
-                t.first_cta = cta_of(begin, units, ctas);
-                t.parts = cta_of(begin + r.tiles - 1, units, ctas) - t.first_cta + 1;
+                t.parts = parts_of<E4M3>(begin, begin + r.weight, weight, ctas, &t.first_cta);
             }
             t.page = last_id >= 0 && last_id < kv.num_pages ? last_id : -1;
             t.at = (r.len - 1) & ((1 << kv.page_shift) - 1);
             mbar_arrive_expect_tx(bar, loads * (box_rows * 128u) + (first ? q_cols * 256u : 0u) +
                                            (fresh ? 512u : 0u));
-            const uint16_t* qkv = a.p.qkv + row * width;
-            if (first)
-                bulk_load(queries + slot * a.cols.block * 256,
-                          qkv + (static_cast<int64_t>(head) * a.cols.group + block * a.cols.block) * kKvHeadDim,
-                          q_cols * 256, bar);
-            if (fresh) {
-                bulk_load(smem_u32(sh.fresh[st][0]), qkv + (a.p.H + head) * static_cast<int64_t>(kKvHeadDim), 256,
-                          bar);
-                bulk_load(smem_u32(sh.fresh[st][1]),
-                          qkv + (a.p.H + kv.kv_heads + head) * static_cast<int64_t>(kKvHeadDim), 256, bar);
-            }
         }
         __syncwarp();
+        const uint16_t* const qkv = a.p.qkv + row * width;
+        if (first)
+            for (int i = lane; i < q_cols; i += 32)
+                bulk_load(queries + (slot * a.cols.block + i) * kQueryStride,
+                          qkv + (static_cast<int64_t>(head) * a.cols.group + block * a.cols.block + i) * kKvHeadDim,
+                          256, bar);
+        if (fresh && lane < 2)
+            bulk_load(smem_u32(sh.fresh[st][lane]),
+                      qkv + (a.p.H + lane * kv.kv_heads + head) * static_cast<int64_t>(kKvHeadDim), 256, bar);
         if (mine) {
             const int32_t at = key & ((1 << kv.page_shift) - 1);
             const int32_t c1 = static_cast<int32_t>(
@@ -348,17 +420,14 @@ __device__ void produce(const DecodeArgs& a, const CUtensorMap* map, Shared& sh,
         if (++tile == r.tiles) {
             tile = 0;
             slot ^= 1;
-            if (++item == items && u + 1 < u1) {
+            if (++item == items && more) {
                 item = 0;
-                base += static_cast<int64_t>(items) * r.tiles;
-                do {  // (there are units left, so that a row has them)
-                    r = row_of<E4M3>(a, ++row, &bad);
-                } while (r.tiles == 0 && row + 1 < a.p.n);
-                if (r.tiles == 0) {  // (unless the lengths changed during the call)
+                base += static_cast<int64_t>(items) * r.weight;
+                r = next_row<E4M3>(a, &row);
+                if (r.tiles == 0) {  // (only if the lengths changed during the call)
                     sh.abort = 1;
                     record_status(kv.status, kInvalid);
-                    ++issued;
-                    break;
+                    more = false;
                 }
             }
         }
@@ -366,6 +435,193 @@ __device__ void produce(const DecodeArgs& a, const CUtensorMap* map, Shared& sh,
     // the copies in flight, before the CTA may end (the consumers may have given up)
     for (int64_t i = issued > kStages ? issued - kStages : 0; i < issued; ++i)
         settle(smem_u32(&sh.full[i % kStages]), (i / kStages) & 1);
+}
+
+__device__ __forceinline__ float finite(float m) { return m == -INFINITY ? 0.0f : m; }
+// What makes an output of a sum relative to 2^w, with weights whose sum is l relative to 2^m.
+template <bool E4M3>
+__device__ __forceinline__ float output_scale(float l, float m, float w) {
+    // (in two steps: an exponent may be -120, and ex2 flushes below 2^-126)
+    return E4M3 ? 1.0f / l * ex2(-kWeightTop) * ex2(finite(w) - finite(m)) : 1.0f / l;
+}
+
+// Adds up an item's parts in their order: part 0 is its CTA's last item, the others their
+// CTAs' first.  A warp takes a column at a time: its lanes the parts' statistics, then four
+// outputs each, the loads of eight parts under way together.  (A thread per output that walked
+// columns and parts took 35 of 72 us with 13 parts of 8 columns.)
+template <bool E4M3>
+__device__ __noinline__ void join_parts(const float* parts, int64_t stride, int n, int cols, int max_cols, uint16_t* out,
+                           int warp, int lane, int* status) {
+    auto at = [&](int k) { return parts + (2 * static_cast<int64_t>(k) + (k == 0)) * stride; };
+    for (int col = warp; col < cols; col += kWarps) {
+        const int stats = max_cols * kKvHeadDim + col;
+        float m = -INFINITY, w = -INFINITY;
+        for (int k = lane; k < n; k += 32) {
+            m = fmaxf(m, __ldcg(at(k) + stats + max_cols));
+            w = fmaxf(w, __ldcg(at(k) + stats + 2 * max_cols));
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+            w = fmaxf(w, __shfl_xor_sync(0xffffffffu, w, o));
+        }
+        float l = 0.0f;
+        bool bad = false;
+        float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int k0 = 0; k0 < n; k0 += 32) {
+            float f = 0.0f, pl = 0.0f;
+            if (k0 + lane < n) {
+                const float* p = at(k0 + lane) + stats;
+                pl = __ldcg(p);
+                bad |= pl < 0.0f;
+                pl *= ex2(__ldcg(p + max_cols) - finite(m));
+                f = ex2(__ldcg(p + 2 * max_cols) - finite(w));
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) pl += __shfl_xor_sync(0xffffffffu, pl, o);
+            l += pl;
+            const int end = min(32, n - k0);
+            for (int k = 0; k < end; k += 8) {
+                float4 v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (k + i < end)
+                        v[i] = __ldcg(reinterpret_cast<const float4*>(at(k0 + k + i) + col * kKvHeadDim) + lane);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float a = __shfl_sync(0xffffffffu, f, (k + i) & 31);
+                    if (k + i < end) {
+                        sum.x += a * v[i].x;
+                        sum.y += a * v[i].y;
+                        sum.z += a * v[i].z;
+                        sum.w += a * v[i].w;
+                    }
+                }
+            }
+        }
+        bad = __any_sync(0xffffffffu, bad);
+        if (bad && lane == 0) record_status(status, kInvalid);
+        const float f = output_scale<E4M3>(l, m, w);
+        reinterpret_cast<uint2*>(out + col * kKvHeadDim)[lane] =
+            bad ? make_uint2(0, 0) : make_uint2(bf16_pair(sum.x * f, sum.y * f), bf16_pair(sum.z * f, sum.w * f));
+    }
+}
+
+// The tile's ends: the new token's row is put in place, as the cache holds it, and stored, and
+// values that no query sees become zero (a weight of 0 does not keep a NaN out of a product).
+template <bool E4M3>
+__device__ __forceinline__ void mend_tile(const DecodeArgs& a, Shared& sh, int st, uint8_t* tile, int warp, int lane,
+                                       bool store_ok) {
+    constexpr int kTile = E4M3 ? 128 : 64;
+    const KvView& kv = a.kv;
+    const Unit& t = sh.unit[st];
+    constexpr int kStep = kTile / kWarps;  // the keys that this warp mends
+    const int key = t.key0 + warp * kStep;
+    if (key < t.len && key + kStep > t.low) {
+        for (int i = lane; i < kStep * (E4M3 ? 8 : 16); i += 32) {
+            const int r = i >> (E4M3 ? 3 : 4), unit = i & (E4M3 ? 7 : 15);
+            if (key + r < t.low || key + r >= t.len)
+                *reinterpret_cast<uint4*>(tile + kHalfStage + tile_byte<E4M3>(warp * kStep + r, unit)) =
+                    make_uint4(0, 0, 0, 0);
+        }
+        const int fresh = t.len - 1 - key;
+        if (fresh < kStep && fresh >= 0) {
+            // half a warp has the key, the other half the value, eight dimensions a lane
+            const int r = warp * kStep + fresh, which = lane >> 4, unit = lane & 15;
+            const bool store = store_ok && t.block == 0 && t.page >= 0;
+            const int64_t row = kv_row(kv, a.p.layer, which, max(t.page, 0), t.head, t.at);
+            const uint4 v = reinterpret_cast<const uint4*>(sh.fresh[st][which])[unit];
+            if constexpr (!E4M3) {
+                *reinterpret_cast<uint4*>(tile + which * kHalfStage + tile_byte<E4M3>(r, unit)) = v;
+                if (store) reinterpret_cast<uint4*>(kv.pages)[row * 16 + unit] = v;
+            } else {
+                uint2 codes;
+                const int e = e4m3_row_of_16(v, &codes);
+                *reinterpret_cast<uint2*>(tile + which * kHalfStage + tile_byte<E4M3>(r, unit >> 1) + (unit & 1) * 8) =
+                    codes;
+                if (unit == 0) sh.exponents[st][r * 2 + which] = static_cast<uint8_t>(e + 127);
+                if (store) {
+                    reinterpret_cast<uint2*>(kv.pages)[row * 16 + unit] = codes;
+                    if (unit == 0)
+                        kv.exponents[kv_exponent(kv, a.p.layer, which, t.page, t.head, t.at)] =
+                            static_cast<uint8_t>(e + 127);
+                }
+            }
+        }
+    }
+    fence_proxy_async();  // (the stage's next contents come by TMA)
+    __syncwarp();
+}
+
+// The warps' parts of an item, met in shared memory, to the output or to the workspace and the
+// join; false if the CTA gave up.
+template <bool E4M3, int NT>
+__device__ __forceinline__ bool finish_item(const DecodeArgs& a, Shared& sh, const Unit& t, const float* meet, int warp,
+                                         int lane, bool bad, uint32_t& met) {
+    const KvView& kv = a.kv;
+    const int key_warps = kWarps / a.cols.warps;
+    const int tid = threadIdx.x - 32, d = tid;  // a thread to a dimension
+    const int cols = min(a.cols.block, a.cols.group - t.block * a.cols.block);
+    const int max_cols = used_columns(a.cols.group);
+    float* const parts = reinterpret_cast<float*>(
+        static_cast<uint8_t*>(a.p.workspace) + counter_bytes(gridDim.x));
+    const int64_t stride = part_floats(max_cols);
+    const bool whole = t.parts == 1;
+    float* const part =
+        parts + (2 * static_cast<int64_t>(blockIdx.x) + (t.first_cta == static_cast<int>(blockIdx.x))) * stride;
+    uint16_t* const out =
+        a.p.out + (static_cast<int64_t>(t.row) * a.p.H + static_cast<int64_t>(t.head) * a.cols.group +
+                   t.block * a.cols.block) * kKvHeadDim;
+    // (as many columns under way as the loop is unrolled: each is a chain of loads from shared
+    // memory and exponentials)
+#pragma unroll 4
+    for (int col = 0; col < cols; ++col) {
+        const int cw = col / (8 * NT), in = col - cw * 8 * NT;
+        const float4 ms = *reinterpret_cast<const float4*>(sh.part_m[col]);
+        const float4 ls = *reinterpret_cast<const float4*>(sh.part_l[col]);
+        const float4 ws = E4M3 ? *reinterpret_cast<const float4*>(sh.part_w[col]) : ms;
+        float x[kWarps];
+#pragma unroll
+        for (int k = 0; k < kWarps; ++k)
+            x[k] = k < key_warps ? meet[((k * a.cols.warps + cw) * 8 * NT + in) * kKvHeadDim + ((d + 8 * (in >> 1)) & 127)]
+                                 : 0.0f;
+        // (warps that have no keys of the column: a maximum of -inf and a sum of 0)
+        const float m = fmaxf(fmaxf(ms.x, ms.y), fmaxf(ms.z, ms.w)), base = finite(m);
+        const float w = E4M3 ? fmaxf(fmaxf(ws.x, ws.y), fmaxf(ws.z, ws.w)) : m, from = finite(w);
+        const float l = ex2(ms.x - base) * ls.x + ex2(ms.y - base) * ls.y + ex2(ms.z - base) * ls.z +
+                        ex2(ms.w - base) * ls.w;
+        const float o = ex2(ws.x - from) * x[0] + ex2(ws.y - from) * x[1] + ex2(ws.z - from) * x[2] +
+                        ex2(ws.w - from) * x[3];
+        if (whole) {
+            out[col * kKvHeadDim + d] =
+                bad ? 0 : static_cast<uint16_t>(bf16_pair(o * output_scale<E4M3>(l, m, w), 0.0f));
+        } else {
+            part[col * kKvHeadDim + d] = o;
+            if (d == 0) {
+                float* const stats = part + max_cols * kKvHeadDim + col;
+                stats[0] = bad ? -1.0f : l;  // (a sum is never negative: marks a bad page index)
+                stats[max_cols] = m;
+                stats[2 * max_cols] = w;
+            }
+        }
+    }
+    if (whole) {
+        if (bad && tid == 0) record_status(kv.status, kInvalid);
+    } else {
+        __threadfence();
+        if (!consumers_meet(sh, met, kv.status, a.p.wait_ns)) return false;
+        if (tid == 0) {
+            unsigned int* const count = static_cast<unsigned int*>(a.p.workspace) + t.first_cta;
+            sh.is_last = atomicInc(count, t.parts - 1) == static_cast<unsigned int>(t.parts - 1);
+        }
+        if (!consumers_meet(sh, met, kv.status, a.p.wait_ns)) return false;
+        if (sh.is_last) {
+            __threadfence();
+            join_parts<E4M3>(parts + 2 * t.first_cta * stride, stride, t.parts, cols, max_cols, out, warp, lane,
+                             kv.status);
+        }
+    }
+    return true;
 }
 
 // The running softmax of a warp: two columns a thread in each of NT tiles of eight.
@@ -377,400 +633,296 @@ struct State {
 };
 
 template <bool E4M3, int NT>
-__device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uint8_t* query_mem, int64_t u0,
-                        int64_t u1) {
+__device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uint8_t* query_mem) {
     constexpr int kTile = E4M3 ? 128 : 64;
+    constexpr int kStep = kTile / kWarps, kGroups = kStep / 16, kRows = 2 * kGroups;  // a warp's keys at a time
     const KvView& kv = a.kv;
     const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - 1;
     const int g = lane >> 2, c = lane & 3;
     const int col_warp = warp % a.cols.warps, key_warp = warp / a.cols.warps, key_warps = kWarps / a.cols.warps;
     const float scale = a.p.scale * 1.4426950408889634f;
-    State<NT> s;
-    uint32_t q[8][NT][2];
-    float q_scale[NT][2];  // of this thread's columns: the softmax's scale, and e4m3's of q
+    // This lane's row of an ldmatrix within a group of 16 keys.  Matrices of keys are (rows 0..7,
+    // unit 0), (8..15, 0), (0..7, 1), (8..15, 1); of transposed values the same in e4m3, and with
+    // the middle two exchanged in bf16.  Steps along the dimensions flip bits of the address.
+    const uint32_t key_off = tile_byte<E4M3>(lane & 15, lane >> 4);
+    const uint32_t value_off =
+        E4M3 ? key_off : tile_byte<E4M3>((lane & 7) + ((lane >> 4) << 3), lane >> 3 & 1);
     int st = 0;
     uint32_t phase = 0, met = 0;
-    for (int64_t u = u0; u < u1; ++u) {
-        if (!wait_warp(smem_u32(&sh.full[st]), phase, &sh.abort, kv.status, a.p.wait_ns)) return;
-        const Unit t = sh.unit[st];
-        uint8_t* const tile = stage_mem + st * kStageBytes;
-        const uint32_t keys = smem_u32(tile), values = keys + kHalfStage;
-        if (t.flags & kFirst) {
-            // Q as the B operand: column g of a tile of eight, in the order of K's dimensions
-            const uint8_t* rows = query_mem + (t.flags >> kQSlotShift & 1) * a.cols.block * 256;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                const uint8_t* row = rows + (col_warp * 8 * NT + nt * 8 + g) * 256;
-                if constexpr (!E4M3) {
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        q[k][nt][0] = *reinterpret_cast<const uint32_t*>(row + k * 32 + c * 4);
-                        q[k][nt][1] = *reinterpret_cast<const uint32_t*>(row + k * 32 + 16 + c * 4);
-                    }
-                    q_scale[nt][0] = q_scale[nt][1] = scale;
-                } else {
-                    uint2 v[8];
-                    float top = 0.0f;
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        v[k] = *reinterpret_cast<const uint2*>(row + k * 32 + c * 8);
-                        top = fmaxf(top, fmaxf(fmaxf(finite_abs(bf16_lo(v[k].x)), finite_abs(bf16_hi(v[k].x))),
-                                               fmaxf(finite_abs(bf16_lo(v[k].y)), finite_abs(bf16_hi(v[k].y)))));
-                    }
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                    // the largest to [2^14, 2^15): eight bits of mantissa stay exact down to 2^-31 of it
-                    int e = static_cast<int>(__float_as_uint(top) >> 23) - 127 - 14;
-                    e = e < -112 ? -112 : e;
-                    const float f = power_of_two(-e);
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        q[k][nt][0] = half_pair(bf16_lo(v[k].x) * f, bf16_hi(v[k].x) * f);
-                        q[k][nt][1] = half_pair(bf16_lo(v[k].y) * f, bf16_hi(v[k].y) * f);
-                    }
-                    // (column g's scale is needed by the threads of columns 2c and 2c + 1)
-#pragma unroll
-                    for (int j = 0; j < 2; ++j)
-                        q_scale[nt][j] = scale * power_of_two(__shfl_sync(0xffffffffu, e, (2 * c + j) * 4));
-                }
-            }
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) s.m[nt][j] = s.w[nt][j] = -INFINITY, s.l[nt][j] = 0.0f;
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) s.o[k][nt][j] = 0.0f;
-            s.bad = false;
-        }
-        s.bad |= (t.flags & kBad) != 0;
-        // The tile's ends: the new token's row is put in place, and values that no query sees
-        // become zero (a weight of 0 does not keep a NaN out of a product).
-        const bool edge = t.key0 < t.low || t.key0 + kTile >= t.len;
-        if (edge) {
-            for (int kg = warp; kg < kTile / 16; kg += kWarps) {
-                const int k16 = t.key0 + kg * 16;
-                if (k16 >= t.len || k16 + 16 <= t.low) continue;
-                for (int i = lane; i < 16 * (E4M3 ? 8 : 16); i += 32) {
-                    const int r = i >> (E4M3 ? 3 : 4), unit = i & (E4M3 ? 7 : 15);
-                    if (k16 + r < t.low || k16 + r >= t.len)
-                        *reinterpret_cast<uint4*>(tile + kHalfStage + tile_byte<E4M3>(kg * 16 + r, unit)) =
-                            make_uint4(0, 0, 0, 0);
-                }
-                const int fresh = t.len - 1 - k16;
-                if (fresh < 16 && fresh >= 0) {
-                    const int r = kg * 16 + fresh;
-                    const bool store = t.block == 0 && t.page >= 0 && !s.bad;
-                    if constexpr (!E4M3) {
-                        const int which = lane >> 4, unit = lane & 15;
-                        const uint4 v = reinterpret_cast<const uint4*>(sh.fresh[st][which])[unit];
-                        *reinterpret_cast<uint4*>(tile + which * kHalfStage + tile_byte<E4M3>(r, unit)) = v;
-                        if (store)
-                            reinterpret_cast<uint4*>(kv.pages)[kv_row(kv, a.p.layer, which, t.page, t.head, t.at) * 16 +
-                                                               unit] = v;
-                    } else {
-#pragma unroll
-                        for (int which = 0; which < 2; ++which) {
-                            const uint2 v = reinterpret_cast<const uint2*>(sh.fresh[st][which])[lane];
-                            float top = fmaxf(fmaxf(finite_abs(bf16_lo(v.x)), finite_abs(bf16_hi(v.x))),
-                                              fmaxf(finite_abs(bf16_lo(v.y)), finite_abs(bf16_hi(v.y))));
-#pragma unroll
-                            for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                            const int e = e4m3_row_exponent(top);
-                            const float f = power_of_two(-e);
-                            const uint32_t codes = e4m3_quad(bf16_lo(v.x) * f, bf16_hi(v.x) * f, bf16_lo(v.y) * f,
-                                                             bf16_hi(v.y) * f);
-                            *reinterpret_cast<uint32_t*>(tile + which * kHalfStage + tile_byte<E4M3>(r, lane >> 2) +
-                                                         (lane & 3) * 4) = codes;
-                            if (lane == 0) sh.exponents[st][r * 2 + which] = static_cast<uint8_t>(e + 127);
-                            if (store) {
-                                reinterpret_cast<uint32_t*>(
-                                    kv.pages)[kv_row(kv, a.p.layer, which, t.page, t.head, t.at) * 32 + lane] = codes;
-                                if (lane == 0)
-                                    kv.exponents[kv_exponent(kv, a.p.layer, which, t.page, t.head, t.at)] =
-                                        static_cast<uint8_t>(e + 127);
-                            }
-                        }
-                    }
-                }
-            }
-            fence_proxy_async();  // (the stage's next contents come by TMA)
-            __syncwarp();
-            // others read what this warp mended
-            if (a.cols.warps > 1 && !consumers_meet(sh, met, kv.status, a.p.wait_ns)) return;
-        }
-        for (int kg = key_warp; kg < kTile / 16; kg += key_warps) {
-            const int k16 = t.key0 + kg * 16;
-            if (k16 >= t.len || k16 + 16 <= t.low) continue;
-            // scores of 16 keys: rows g and g + 8, columns 2c and 2c + 1
-            float acc[2][NT][4];
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[i][nt][j] = 0.0f;
-            if constexpr (!E4M3) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    uint32_t f[4];
-                    ldsm_x4(keys + tile_byte<E4M3>(kg * 16 + (lane & 15), 2 * k + (lane >> 4)), f);
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) mma<E4M3>(acc[k & 1][nt], f, q[k][nt][0], q[k][nt][1]);
-                }
-            } else {
-                // a 16-byte unit is 16 dimensions, of which a thread gets 4c .. 4c + 3
-#pragma unroll
-                for (int k = 0; k < 8; k += 2) {
-                    uint32_t w[4];
-                    ldsm_x4(keys + tile_byte<E4M3>(kg * 16 + (lane & 15), k + (lane >> 4)), w);
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const uint32_t f[4] = {e4m3_to_half2(static_cast<uint16_t>(w[2 * i])),
-                                               e4m3_to_half2(static_cast<uint16_t>(w[2 * i + 1])),
-                                               e4m3_to_half2(static_cast<uint16_t>(w[2 * i] >> 16)),
-                                               e4m3_to_half2(static_cast<uint16_t>(w[2 * i + 1] >> 16))};
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) mma<E4M3>(acc[i][nt], f, q[k + i][nt][0], q[k + i][nt][1]);
-                    }
-                }
-            }
-            bool see[2] = {true, true};
-            if (edge) {
-                see[0] = k16 + g >= t.low && k16 + g < t.len;
-                see[1] = k16 + g + 8 >= t.low && k16 + g + 8 < t.len;
-            }
-            float key_scale[2] = {1.0f, 1.0f}, value_exp[2] = {0.0f, 0.0f};
-            if constexpr (E4M3) {
-                const uint8_t* pairs = sh.exponents[st] + (kg * 16 + g) * 2;
-                const uint32_t e0 = *reinterpret_cast<const uint16_t*>(pairs);
-                const uint32_t e1 = *reinterpret_cast<const uint16_t*>(pairs + 16);
-                key_scale[0] = __uint_as_float((e0 & 0xFFu) << 23);
-                key_scale[1] = __uint_as_float((e1 & 0xFFu) << 23);
-                value_exp[0] = static_cast<float>(static_cast<int>(e0 >> 8) - 127);
-                value_exp[1] = static_cast<float>(static_cast<int>(e1 >> 8) - 127);
-            }
-            float alpha[NT][2];  // what the new maxima make of o
-            uint32_t b[NT][2];
-            bool moved = false;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                float x[4], p[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float v = acc[0][nt][j] + acc[1][nt][j];
-                    x[j] = see[j >> 1] ? v * (E4M3 ? key_scale[j >> 1] * q_scale[nt][j & 1] : q_scale[nt][j & 1])
-                                       : -INFINITY;
-                }
-                // the running maximum of a column: v over the group's keys and what it was
-                auto raise = [&](float v, float& was, float* scale_old) {
-                    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 4));
-                    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
-                    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
-                    v = fmaxf(v, was);
-                    const float base = v == -INFINITY ? 0.0f : v;
-                    *scale_old = ex2(was - base);
-                    moved |= v != was;
-                    was = v;
-                    return base;
-                };
-                float scale_l[2];
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const float base = raise(fmaxf(x[j], x[j + 2]), s.m[nt][j], &scale_l[j]);
-                    p[j] = ex2(x[j] - base);
-                    p[j + 2] = ex2(x[j + 2] - base);
-                    alpha[nt][j] = scale_l[j];
-                }
-                // keys 2c, 2c + 1 of column g: the transpose of what this thread holds
-                uint32_t w0, w1;
-                if constexpr (!E4M3) {
-                    w0 = bf16_pair(p[0], p[1]);
-                    w1 = bf16_pair(p[2], p[3]);
-                    // (the sum of the rounded weights, so that they add up to one)
-                    s.l[nt][0] = s.l[nt][0] * scale_l[0] + (bf16_lo(w0) + bf16_lo(w1));
-                    s.l[nt][1] = s.l[nt][1] * scale_l[1] + (bf16_hi(w0) + bf16_hi(w1));
-                } else {
-                    s.l[nt][0] = s.l[nt][0] * scale_l[0] + (p[0] + p[2]);
-                    s.l[nt][1] = s.l[nt][1] * scale_l[1] + (p[1] + p[3]);
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        // (an unseen key's score is -inf whatever its exponent)
-                        const float y0 = x[j] + value_exp[0], y1 = x[j + 2] + value_exp[1];
-                        const float base = raise(fmaxf(y0, y1), s.w[nt][j], &alpha[nt][j]) - kWeightTop;
-                        p[j] = ex2(y0 - base);
-                        p[j + 2] = ex2(y1 - base);
-                    }
-                    w0 = half_pair(p[0], p[1]);
-                    w1 = half_pair(p[2], p[3]);
-                }
-                b[nt][0] = transpose_8x8(w0);
-                b[nt][1] = transpose_8x8(w1);
-            }
-            if (__any_sync(0xffffffffu, moved)) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) s.o[k][nt][j] *= alpha[nt][j & 1];
-            }
-            if constexpr (!E4M3) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    uint32_t f[4];
-                    ldsm_x4_trans(values + tile_byte<E4M3>(kg * 16 + (lane & 7) + ((lane >> 4) << 3),
-                                                           2 * k + (lane >> 3 & 1)), f);
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) mma<E4M3>(s.o[k][nt], f, b[nt][0], b[nt][1]);
-                }
-            } else {
-                // rows g and g + 8 of a tile are dimensions 2g and 2g + 1 of its 16
-#pragma unroll
-                for (int k = 0; k < 8; k += 2) {
-                    uint32_t w[4];
-                    ldsm_x4_trans(values + tile_byte<E4M3>(kg * 16 + (lane & 15), k + (lane >> 4)), w);
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const uint32_t lo = __byte_perm(w[2 * i], 0, 0x3120);
-                        const uint32_t hi = __byte_perm(w[2 * i + 1], 0, 0x3120);
-                        const uint32_t f[4] = {e4m3_to_half2(static_cast<uint16_t>(lo)),
-                                               e4m3_to_half2(static_cast<uint16_t>(lo >> 16)),
-                                               e4m3_to_half2(static_cast<uint16_t>(hi)),
-                                               e4m3_to_half2(static_cast<uint16_t>(hi >> 16))};
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) mma<E4M3>(s.o[k + i][nt], f, b[nt][0], b[nt][1]);
-                    }
-                }
-            }
-        }
-        if (t.flags & kLast) {
-            // The warps' parts meet in the stage, which all have read: [warp][16 columns][128],
-            // a column turned by eight values per pair so that a store's lanes hit all banks.
-            float* const meet = reinterpret_cast<float*>(tile);
-            if (!consumers_meet(sh, met, kv.status, a.p.wait_ns)) return;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    float l = s.l[nt][j];
-                    l += __shfl_xor_sync(0xffffffffu, l, 4);
-                    l += __shfl_xor_sync(0xffffffffu, l, 8);
-                    l += __shfl_xor_sync(0xffffffffu, l, 16);
-                    const int col = nt * 8 + 2 * c + j;
-                    if (g == 0) {
-                        sh.part_l[warp][col] = l;
-                        sh.part_m[warp][col] = s.m[nt][j];
-                        sh.part_w[warp][col] = E4M3 ? s.w[nt][j] : s.m[nt][j];
-                    }
-#pragma unroll
-                    for (int k = 0; k < 8; ++k)
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const int d = E4M3 ? 16 * k + 2 * g + i : 16 * k + g + 8 * i;
-                            meet[(warp * 8 * NT + col) * kKvHeadDim + ((d + 8 * (col >> 1)) & 127)] =
-                                s.o[k][nt][2 * i + j];
-                        }
-                }
-            if (!consumers_meet(sh, met, kv.status, a.p.wait_ns)) return;
-            const int tid = threadIdx.x - 32, d = tid;  // a thread to a dimension
-            const int cols = min(a.cols.block, a.cols.group - t.block * a.cols.block);
-            const int max_cols = used_columns(a.cols.group);
-            float* const parts = reinterpret_cast<float*>(
-                static_cast<uint8_t*>(a.p.workspace) + static_cast<int64_t>(gridDim.x) * 4);
-            const int64_t stride = part_floats(max_cols);
-            const bool whole = t.parts == 1;
-            float* const part =
-                parts + (2 * static_cast<int64_t>(blockIdx.x) + (t.first_cta == static_cast<int>(blockIdx.x))) * stride;
-            uint16_t* const out =
-                a.p.out + (static_cast<int64_t>(t.row) * a.p.H + static_cast<int64_t>(t.head) * a.cols.group +
-                           t.block * a.cols.block) * kKvHeadDim;
-            auto finite = [](float m) { return m == -INFINITY ? 0.0f : m; };
-            // an output from its sum, relative to 2^w, and the weights' sum, relative to 2^m
-            auto output = [&](float o, float l, float m, float w, bool bad) {
-                float v = o / l;
-                // (in two steps: an exponent may be -120, and ex2 flushes below 2^-126)
-                if constexpr (E4M3) v = v * ex2(-kWeightTop) * ex2(finite(w) - finite(m));
-                return bad ? uint16_t{0} : static_cast<uint16_t>(bf16_pair(v, 0.0f));
-            };
-            for (int col = 0; col < cols; ++col) {
-                const int cw = col / (8 * NT), in = col - cw * 8 * NT;
-                float m = -INFINITY, w = -INFINITY, l = 0.0f, o = 0.0f;
-                for (int k = 0; k < key_warps; ++k) {
-                    m = fmaxf(m, sh.part_m[k * a.cols.warps + cw][in]);
-                    w = fmaxf(w, sh.part_w[k * a.cols.warps + cw][in]);
-                }
-                for (int k = 0; k < key_warps; ++k) {
-                    const int i = k * a.cols.warps + cw;
-                    l += ex2(sh.part_m[i][in] - finite(m)) * sh.part_l[i][in];
-                    o += ex2(sh.part_w[i][in] - finite(w)) *
-                         meet[(i * 8 * NT + in) * kKvHeadDim + ((d + 8 * (in >> 1)) & 127)];
-                }
-                if (whole) {
-                    out[col * kKvHeadDim + d] = output(o, l, m, w, s.bad);
-                } else {
-                    part[col * kKvHeadDim + d] = o;
-                    if (d == 0) {
-                        float* const stats = part + max_cols * kKvHeadDim + col;
-                        stats[0] = s.bad ? -1.0f : l;  // (a sum is never negative: marks a bad page index)
-                        stats[max_cols] = m;
-                        stats[2 * max_cols] = w;
-                    }
-                }
-            }
-            if (whole) {
-                if (s.bad && tid == 0) record_status(kv.status, kInvalid);
-            } else {
-                __threadfence();
-                if (!consumers_meet(sh, met, kv.status, a.p.wait_ns)) return;
-                if (tid == 0) {
-                    unsigned int* const count = static_cast<unsigned int*>(a.p.workspace) + t.first_cta;
-                    sh.is_last = atomicInc(count, t.parts - 1) == static_cast<unsigned int>(t.parts - 1);
-                }
-                if (!consumers_meet(sh, met, kv.status, a.p.wait_ns)) return;
-                if (sh.is_last) {
-                    __threadfence();
-                    // part k is of CTA first_cta + k: its last item for k = 0, else its first
-                    auto at = [&](int k) {
-                        return parts + (2 * static_cast<int64_t>(t.first_cta + k) + (k == 0)) * stride;
-                    };
-                    for (int col = 0; col < cols; ++col) {
-                        const int stats = max_cols * kKvHeadDim + col;
-                        float m = -INFINITY, w = -INFINITY, l = 0.0f, o = 0.0f;
-                        bool bad = false;
-                        for (int k = 0; k < t.parts; ++k) {
-                            m = fmaxf(m, __ldcg(at(k) + stats + max_cols));
-                            w = fmaxf(w, __ldcg(at(k) + stats + 2 * max_cols));
-                        }
-                        for (int k = 0; k < t.parts; ++k) {
-                            const float pl = __ldcg(at(k) + stats);
-                            bad |= pl < 0.0f;
-                            l += ex2(__ldcg(at(k) + stats + max_cols) - finite(m)) * pl;
-                            o += ex2(__ldcg(at(k) + stats + 2 * max_cols) - finite(w)) *
-                                 __ldcg(at(k) + col * kKvHeadDim + d);
-                        }
-                        out[col * kKvHeadDim + d] = output(o, l, m, w, bad);
-                        if (bad && tid == 0) record_status(kv.status, kInvalid);
-                    }
-                }
-            }
-            fence_proxy_async();
-        }
+    auto wait = [&]() { return wait_warp(smem_u32(&sh.full[st]), phase, &sh.abort, kv.status, a.p.wait_ns); };
+    auto release = [&]() {
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&sh.empty[st]));
         if (++st == kStages) {
             st = 0;
             phase ^= 1;
         }
+    };
+    for (;;) {  // an item
+        if (!wait()) return;
+        State<NT> s;
+        uint32_t q[8][NT][2];
+        float q_scale[NT][2];  // e4m3: of this thread's columns, the softmax's scale and that of q
+        // Q as the B operand: column g of a tile of eight, in the order of K's dimensions
+        const uint8_t* rows = query_mem + (sh.unit[st].flags >> kQSlotShift & 1) * a.cols.block * kQueryStride;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const uint8_t* row = rows + (col_warp * 8 * NT + nt * 8 + g) * kQueryStride;
+            if constexpr (!E4M3) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    q[k][nt][0] = *reinterpret_cast<const uint32_t*>(row + k * 32 + c * 4);
+                    q[k][nt][1] = *reinterpret_cast<const uint32_t*>(row + k * 32 + 16 + c * 4);
+                }
+            } else {
+                uint2 v[8];
+                float top = 0.0f;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    v[k] = *reinterpret_cast<const uint2*>(row + k * 32 + c * 8);
+                    top = fmaxf(top, fmaxf(fmaxf(finite_abs(bf16_lo(v[k].x)), finite_abs(bf16_hi(v[k].x))),
+                                           fmaxf(finite_abs(bf16_lo(v[k].y)), finite_abs(bf16_hi(v[k].y)))));
+                }
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                // the largest to [2^14, 2^15): eight bits of mantissa stay exact down to 2^-31 of it
+                int e = static_cast<int>(__float_as_uint(top) >> 23) - 127 - 14;
+                e = e < -112 ? -112 : e;
+                const float f = power_of_two(-e);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    q[k][nt][0] = half_pair(bf16_lo(v[k].x) * f, bf16_hi(v[k].x) * f);
+                    q[k][nt][1] = half_pair(bf16_lo(v[k].y) * f, bf16_hi(v[k].y) * f);
+                }
+                // (column g's scale is needed by the threads of columns 2c and 2c + 1)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    q_scale[nt][j] = scale * power_of_two(__shfl_sync(0xffffffffu, e, (2 * c + j) * 4));
+            }
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) s.m[nt][j] = s.w[nt][j] = -INFINITY, s.l[nt][j] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s.o[k][nt][j] = 0.0f;
+        s.bad = false;
+        int flags;
+        uint8_t* tile;
+        for (;;) {  // a unit of it
+            flags = sh.unit[st].flags;
+            const int key0 = sh.unit[st].key0, low = sh.unit[st].low, len = sh.unit[st].len;
+            tile = stage_mem + st * kStageBytes;
+            const uint32_t keys = smem_u32(tile), values = keys + kHalfStage;
+            s.bad |= (flags & kBad) != 0;
+            const bool edge = key0 < low || key0 + kTile >= len;
+            if (edge) {
+                mend_tile<E4M3>(a, sh, st, tile, warp, lane, !s.bad);
+                // others read what this warp mended
+                if (a.cols.warps > 1 && !consumers_meet(sh, met, kv.status, a.p.wait_ns)) return;
+            }
+            for (int step = key_warp; step < kWarps; step += key_warps) {
+                const int key = key0 + step * kStep;
+                if (key >= len || key + kStep <= low) continue;
+                // scores of the step's groups of 16 keys: rows g and g + 8, columns 2c and 2c + 1
+                float acc[2][NT][4];  // e4m3: of two groups; bf16: of even and odd dimensions
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) acc[i][nt][j] = 0.0f;
+                if constexpr (!E4M3) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        uint32_t f[4];
+                        ldsm_x4(((keys + key_off + step * 2048) ^ ((k & 3) << 5)) + (k >> 2) * 8192, f);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) mma<E4M3>(acc[k & 1][nt], f, q[k][nt][0], q[k][nt][1]);
+                    }
+                } else {
+                    // a 16-byte unit is 16 dimensions, of which a thread gets 4c .. 4c + 3
+#pragma unroll
+                    for (int k = 0; k < 8; k += 2) {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            uint32_t w[4];
+                            ldsm_x4((keys + key_off + step * 4096 + i * 2048) ^ (k << 4), w);
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                const uint32_t f[4] = {e4m3_to_half2(static_cast<uint16_t>(w[2 * h])),
+                                                       e4m3_to_half2(static_cast<uint16_t>(w[2 * h + 1])),
+                                                       e4m3_to_half2(static_cast<uint16_t>(w[2 * h] >> 16)),
+                                                       e4m3_to_half2(static_cast<uint16_t>(w[2 * h + 1] >> 16))};
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt)
+                                    mma<E4M3>(acc[i][nt], f, q[k + h][nt][0], q[k + h][nt][1]);
+                            }
+                        }
+                    }
+                }
+                bool see[kRows];  // keys g and g + 8 of each group
+#pragma unroll
+                for (int i = 0; i < kRows; ++i) {
+                    const int at = key + g + 8 * i;
+                    see[i] = !edge || (at >= low && at < len);
+                }
+                float key_scale[kRows], value_exp[kRows];
+                if constexpr (E4M3) {
+#pragma unroll
+                    for (int i = 0; i < kRows; ++i) {
+                        const uint32_t e =
+                            *reinterpret_cast<const uint16_t*>(sh.exponents[st] + (step * kStep + g + 8 * i) * 2);
+                        key_scale[i] = __uint_as_float((e & 0xFFu) << 23);
+                        value_exp[i] = static_cast<float>(static_cast<int>(e >> 8) - 127);
+                    }
+                }
+                float alpha[NT][2];  // what the new maxima make of o
+                uint32_t b[kGroups][NT][2];
+                bool moved = false;
+                // the running maximum of a column: v over the keys of this thread, and what it was
+                auto raise = [&](float v, float& was, float* scale_old) {
+                    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 4));
+                    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
+                    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
+                    v = fmaxf(v, was);
+                    const float base = finite(v);
+                    *scale_old = ex2(was - base);
+                    moved |= v != was;
+                    was = v;
+                    return base;
+                };
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    float x[kRows][2], p[kRows][2], scale_l[2];
+#pragma unroll
+                    for (int i = 0; i < kRows; ++i)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const float v = E4M3 ? acc[i >> 1][nt][(i & 1) * 2 + j] * (key_scale[i] * q_scale[nt][j])
+                                                 : (acc[0][nt][i * 2 + j] + acc[1][nt][i * 2 + j]) * scale;
+                            x[i][j] = see[i] ? v : -INFINITY;
+                        }
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        float top = fmaxf(x[0][j], x[1][j]);
+                        if constexpr (E4M3) top = fmaxf(top, fmaxf(x[2][j], x[kRows - 1][j]));
+                        const float base = raise(top, s.m[nt][j], &scale_l[j]);
+                        float sum = 0.0f;
+#pragma unroll
+                        for (int i = 0; i < kRows; ++i) {
+                            p[i][j] = ex2(x[i][j] - base);
+                            sum += p[i][j];
+                        }
+                        s.l[nt][j] = s.l[nt][j] * scale_l[j] + (E4M3 ? sum : 0.0f);
+                        alpha[nt][j] = scale_l[j];
+                        if constexpr (E4M3) {
+                            // (an unseen key's score is -inf whatever its exponent)
+#pragma unroll
+                            for (int i = 0; i < kRows; ++i) x[i][j] += value_exp[i];
+                            top = fmaxf(fmaxf(x[0][j], x[1][j]), fmaxf(x[2][j], x[kRows - 1][j]));
+                            const float to = raise(top, s.w[nt][j], &alpha[nt][j]) - kWeightTop;
+#pragma unroll
+                            for (int i = 0; i < kRows; ++i) p[i][j] = ex2(x[i][j] - to);
+                        }
+                    }
+                    // keys 2c, 2c + 1 of column g: the transpose of what this thread holds
+#pragma unroll
+                    for (int i = 0; i < kRows; ++i) {
+                        const uint32_t w = E4M3 ? half_pair(p[i][0], p[i][1]) : bf16_pair(p[i][0], p[i][1]);
+                        if constexpr (!E4M3) {  // (the rounded weights' sum, so that they add up to one)
+                            s.l[nt][0] += bf16_lo(w);
+                            s.l[nt][1] += bf16_hi(w);
+                        }
+                        b[i >> 1][nt][i & 1] = transpose_8x8(w);
+                    }
+                }
+                if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) s.o[k][nt][j] *= alpha[nt][j & 1];
+                }
+                if constexpr (!E4M3) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        uint32_t f[4];
+                        ldsm_x4_trans(((values + value_off + step * 2048) ^ ((k & 3) << 5)) + (k >> 2) * 8192, f);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) mma<E4M3>(s.o[k][nt], f, b[0][nt][0], b[0][nt][1]);
+                    }
+                } else {
+                    // rows g and g + 8 of a tile are dimensions 2g and 2g + 1 of its 16
+#pragma unroll
+                    for (int k = 0; k < 8; k += 2) {
+#pragma unroll
+                        for (int i = 0; i < kGroups; ++i) {
+                            uint32_t w[4];
+                            ldsm_x4_trans((values + value_off + step * 4096 + i * 2048) ^ (k << 4), w);
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                const uint32_t lo = __byte_perm(w[2 * h], 0, 0x3120);
+                                const uint32_t hi = __byte_perm(w[2 * h + 1], 0, 0x3120);
+                                const uint32_t f[4] = {e4m3_to_half2(static_cast<uint16_t>(lo)),
+                                                       e4m3_to_half2(static_cast<uint16_t>(lo >> 16)),
+                                                       e4m3_to_half2(static_cast<uint16_t>(hi)),
+                                                       e4m3_to_half2(static_cast<uint16_t>(hi >> 16))};
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt) mma<E4M3>(s.o[k + h][nt], f, b[i][nt][0], b[i][nt][1]);
+                            }
+                        }
+                    }
+                }
+            }
+            if (flags & kLast) break;
+            release();
+            if (!wait()) return;
+        }
+        // The warps' parts meet in the stage, which all have read: [warp][16 columns][128],
+        // a column turned by eight values per pair so that a store's lanes hit all banks.
+        float* const meet = reinterpret_cast<float*>(tile);
+        if (!consumers_meet(sh, met, kv.status, a.p.wait_ns)) return;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                float l = s.l[nt][j];
+                l += __shfl_xor_sync(0xffffffffu, l, 4);
+                l += __shfl_xor_sync(0xffffffffu, l, 8);
+                l += __shfl_xor_sync(0xffffffffu, l, 16);
+                const int col = nt * 8 + 2 * c + j;
+                if (g == 0) {
+                    const int at = col_warp * 8 * NT + col;
+                    sh.part_l[at][key_warp] = l;
+                    sh.part_m[at][key_warp] = s.m[nt][j];
+                    if constexpr (E4M3) sh.part_w[at][key_warp] = s.w[nt][j];
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int d = E4M3 ? 16 * k + 2 * g + i : 16 * k + g + 8 * i;
+                        meet[(warp * 8 * NT + col) * kKvHeadDim + ((d + 8 * (col >> 1)) & 127)] =
+                            s.o[k][nt][2 * i + j];
+                    }
+            }
+        if (!consumers_meet(sh, met, kv.status, a.p.wait_ns)) return;
+        if (!finish_item<E4M3, NT>(a, sh, sh.unit[st], meet, warp, lane, s.bad, met)) return;
+        fence_proxy_async();
+        release();
+        if (flags & kEnd) return;
     }
 }
 
 template <bool E4M3, int NT>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm)
-    attention_decode_kernel(const __grid_constant__ CUtensorMap map, const DecodeArgs a) {
+    attention_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ DecodeArgs a) {
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ Shared sh;
     // (the dynamic part starts past the static one: rounded up to the swizzle's 1024 bytes)
@@ -785,80 +937,107 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
             mbar_init(smem_u32(&sh.empty[i]), kWarps);
         }
         mbar_init(smem_u32(&sh.met), kWarps);
+        sh.start_base = sh.start_row = sh.empty_rows = 0;
+        sh.bound[0] = sh.bound[1] = 0;
+        sh.start = Row{};
         sh.abort = 0;
         fence_mbar_init();
+    }
+    for (int i = tid; i < kMaxCols * kWarps; i += kThreads) {  // (of warps without keys of a column)
+        sh.part_l[i / kWarps][i % kWarps] = 0.0f;
+        sh.part_m[i / kWarps][i % kWarps] = sh.part_w[i / kWarps][i % kWarps] = -INFINITY;
     }
     grid_launch_dependents();
     grid_wait();
     __syncthreads();
 
-    // the batch's units, this CTA's run of them, and the row and its first unit where it starts
+    // The batch's weight, this CTA's share of it, and the row where it starts.  (Each load is
+    // a microsecond's part: a batch of up to kThreads rows is read once.)
     const int items = a.kv.kv_heads * a.cols.blocks;
-    int64_t units = 0;
-    for (int i0 = 0; i0 < a.p.n; i0 += kThreads) {
-        const int i = i0 + tid;
-        int64_t v = 0;
-        if (i < a.p.n) {
-            bool bad;
-            const Row r = row_of<E4M3>(a, i, &bad);
-            v = static_cast<int64_t>(r.tiles) * items;
-            if (i % gridDim.x == blockIdx.x && bad) record_status(a.kv.status, kInvalid);
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-        if (lane == 0) sh.warp_sum[warp] = v;
-        __syncthreads();
-        for (int w = 0; w < kThreads / 32; ++w) units += sh.warp_sum[w];
-        __syncthreads();
-    }
-    // rows without keys are zero
-    for (int i = blockIdx.x; i < a.p.n; i += gridDim.x) {
+    auto weigh = [&](int i, Row* r) -> int64_t {
+        *r = Row{};
+        if (i >= a.p.n) return 0;
         bool bad;
-        if (row_of<E4M3>(a, i, &bad).tiles > 0) continue;
-        uint4* const out = reinterpret_cast<uint4*>(a.p.out + static_cast<int64_t>(i) * a.p.H * kKvHeadDim);
-        for (int j = tid; j < a.p.H * (kKvHeadDim / 8); j += kThreads) out[j] = make_uint4(0, 0, 0, 0);
-    }
-    const int64_t ctas = units < gridDim.x ? units : gridDim.x;
-    if (blockIdx.x >= ctas) return;
-    const int64_t u0 = blockIdx.x * units / ctas, u1 = (blockIdx.x + 1) * units / ctas;
-    int64_t before = 0;
-    for (int i0 = 0; i0 < a.p.n && before <= u0; i0 += kThreads) {
-        const int i = i0 + tid;
-        int64_t v = 0;
-        if (i < a.p.n) {
-            bool bad;
-            v = static_cast<int64_t>(row_of<E4M3>(a, i, &bad).tiles) * items;
+        *r = row_of<E4M3>(a, i, &bad);
+        if (r->tiles == 0 && i % gridDim.x == blockIdx.x) {
+            sh.empty_rows = 1;
+            if (bad) record_status(a.kv.status, kInvalid);
         }
-        int64_t sum = v;
+        return static_cast<int64_t>(r->weight) * items;
+    };
+    // the sum of v over the threads before this one and its own, and over all
+    auto scan = [&](int64_t v, int64_t* all) {
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int64_t t = __shfl_up_sync(0xffffffffu, sum, o);
-            if (lane >= o) sum += t;
+            const int64_t t = __shfl_up_sync(0xffffffffu, v, o);
+            if (lane >= o) v += t;
         }
-        if (lane == 31) sh.warp_sum[warp] = sum;
+        if (lane == 31) sh.warp_sum[warp] = v;
         __syncthreads();
-        int64_t all = 0;
+        *all = 0;
         for (int w = 0; w < kThreads / 32; ++w) {
-            if (w == warp) sum += all + before;
-            all += sh.warp_sum[w];
+            if (w == warp) v += *all;
+            *all += sh.warp_sum[w];
         }
-        if (u0 < sum && u0 >= sum - v) {
-            sh.start_row = i;
-            sh.start_base = sum - v;
+        return v;
+    };
+    Row r;
+    int64_t all, weight = 0, v = weigh(tid, &r), upto = scan(v, &all);
+    weight = all;
+    for (int i0 = kThreads; i0 < a.p.n; i0 += kThreads) {
+        __syncthreads();
+        Row other;
+        scan(weigh(i0 + tid, &other), &all);
+        weight += all;
+    }
+    // rows without keys are zero
+    if (sh.empty_rows)
+        for (int i = blockIdx.x; i < a.p.n; i += gridDim.x) {
+            bool bad;
+            if (row_of<E4M3>(a, i, &bad).tiles > 0) continue;
+            uint4* const out = reinterpret_cast<uint4*>(a.p.out + static_cast<int64_t>(i) * a.p.H * kKvHeadDim);
+            for (int j = tid; j < a.p.H * (kKvHeadDim / 8); j += kThreads) out[j] = make_uint4(0, 0, 0, 0);
+        }
+    if (weight == 0) return;
+    // as many CTAs as leave each at least the most that lies between two tiles' starts
+    const int64_t most = weight / Snap<E4M3>::kMost;
+    const int64_t ctas = most < 1 ? 1 : most < gridDim.x ? most : gridDim.x;
+    if (blockIdx.x >= ctas) return;
+    const int64_t w0 = blockIdx.x * weight / ctas, w1 = (blockIdx.x + 1) * weight / ctas;
+    int64_t before = 0;
+    for (int i0 = 0;;) {
+        const int64_t begin = before + upto - v, end = before + upto;
+        if (begin <= w0 && w0 < end) {
+            sh.bound[0] = snapped<E4M3>(w0, begin, r.weight);
+            sh.start_row = i0 + tid;
+            sh.start_base = begin;
+            sh.start = r;
+        }
+        if (begin <= w1 && w1 < end) sh.bound[1] = snapped<E4M3>(w1, begin, r.weight);
+        if (w1 == weight) sh.bound[1] = weight;
+        if (i0 == 0 && a.p.n > kThreads) {
+            __syncthreads();
+            scan(v, &all);  // (the first block's again)
         }
         before += all;
+        i0 += kThreads;
+        if (i0 >= a.p.n || before > w1) break;
         __syncthreads();
+        v = weigh(i0 + tid, &r);
+        upto = scan(v, &all);
     }
+    __syncthreads();
+    if (sh.bound[0] == sh.bound[1]) return;
     if (warp == 0)
-        produce<E4M3>(a, &map, sh, smem_u32(stage_mem), smem_u32(query_mem), units, ctas, u0, u1);
+        produce<E4M3>(a, &map, sh, smem_u32(stage_mem), smem_u32(query_mem), weight, ctas, sh.bound[0], sh.bound[1]);
     else
-        consume<E4M3, NT>(a, sh, stage_mem, query_mem, u0, u1);
+        consume<E4M3, NT>(a, sh, stage_mem, query_mem);
 }
 
 template <bool E4M3, int NT>
 cudaError_t launch(const CUtensorMap& map, const DecodeArgs& a, int grid, cudaStream_t stream) {
     auto kern = attention_decode_kernel<E4M3, NT>;
-    const int bytes = 1024 + kStages * kStageBytes + 2 * a.cols.block * 256;
+    const int bytes = 1024 + kStages * kStageBytes + 2 * a.cols.block * kQueryStride;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
@@ -880,8 +1059,7 @@ cudaError_t launch(const CUtensorMap& map, const DecodeArgs& a, int grid, cudaSt
 // A counter for each CTA, then two parts for each.
 int64_t decode_workspace_bytes(int H, int kv_heads, int sm_count) {
     const int64_t ctas = static_cast<int64_t>(sm_count) * kCtasPerSm;
-    const int64_t bytes = ctas * 4 + ctas * 2 * part_floats(used_columns(H / kv_heads)) * 4;
-    return (bytes + 15) / 16 * 16;
+    return counter_bytes(static_cast<int>(ctas)) + ctas * 2 * part_floats(used_columns(H / kv_heads)) * 4;
 }
 
 int encode_cache(CUtensorMap* map, const KvView& kv, int layer) {

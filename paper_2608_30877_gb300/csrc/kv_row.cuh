@@ -51,6 +51,26 @@ __device__ __forceinline__ uint32_t e4m3_pair(float lo, float hi) {
 __device__ __forceinline__ uint32_t e4m3_quad(float a, float b, float c, float d) {
     return e4m3_pair(a, b) | (e4m3_pair(c, d) << 16);
 }
+// A row of 128 bf16 values to codes and its exponent: sixteen lanes (an aligned half of a warp,
+// all of them here) with eight values each.
+__device__ __forceinline__ int e4m3_row_of_16(uint4 v, uint2* codes) {
+    const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+    float f[8], top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[2 * i] = __uint_as_float(u[i] << 16);
+        f[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+        top = fmaxf(top, fmaxf(finite_abs(f[2 * i]), finite_abs(f[2 * i + 1])));
+    }
+    const uint32_t half = 0xFFFFu << (threadIdx.x & 16);
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(half, top, o));
+    const int e = e4m3_row_exponent(top);
+    const float s = power_of_two(-e);
+    codes->x = e4m3_quad(f[0] * s, f[1] * s, f[2] * s, f[3] * s);
+    codes->y = e4m3_quad(f[4] * s, f[5] * s, f[6] * s, f[7] * s);
+    return e;
+}
 // Two e4m3 codes to a pair of halves, exactly.
 __device__ __forceinline__ uint32_t e4m3_to_half2(uint16_t codes) {
     uint32_t r;

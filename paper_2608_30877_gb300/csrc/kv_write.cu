@@ -73,23 +73,8 @@ __global__ void __launch_bounds__(kThreads) kv_write_kernel(const KvView kv, con
         if constexpr (!E4M3) {
             reinterpret_cast<uint4*>(kv.pages)[row * 16 + lane16] = v;
         } else {
-            float f[8];
-            const uint32_t u[4] = {v.x, v.y, v.z, v.w};
-            float top = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                f[2 * i] = __uint_as_float(u[i] << 16);
-                f[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
-                top = fmaxf(top, fmaxf(finite_abs(f[2 * i]), finite_abs(f[2 * i + 1])));
-            }
-            const uint32_t half = 0xFFFFu << (threadIdx.x & 16);
-#pragma unroll
-            for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(half, top, o));
-            const int e = e4m3_row_exponent(top);
-            const float s = power_of_two(-e);
             uint2 codes;
-            codes.x = e4m3_quad(f[0] * s, f[1] * s, f[2] * s, f[3] * s);
-            codes.y = e4m3_quad(f[4] * s, f[5] * s, f[6] * s, f[7] * s);
+            const int e = e4m3_row_of_16(v, &codes);
             reinterpret_cast<uint2*>(kv.pages)[row * 16 + lane16] = codes;
             if (lane16 == 0)
                 kv.exponents[kv_exponent(kv, p.layer, which, pages[t], head, places[t])] =
