@@ -18,16 +18,22 @@
 //    warp-level MMAs whose A operand is the cache (16 keys or 16 values' dimensions) and whose
 //    N = 8 columns are the queries of a key head, so that few queries waste few columns.  The
 //    tensor pipe is nearly idle at this; the tcgen05 form would want 128 rows.  The warps'
-//    maxima, sums and outputs are their own until the end of an item (row and head), where
-//    they meet in the stage that was read last.
+//    maxima, sums and outputs are their own until the end of an item (row and head): each
+//    leaves them in its own rows of the stage that it read last and goes on, and a sixth
+//    warp adds them up, stores the result and releases the stage (with the four warps doing
+//    that together, they stood still 1 us per item).
 //  * More than 16 queries of a key head: the warps split the columns instead of the keys, up
 //    to 64, then further items.
 //  * Join.  A CTA's first and last items may continue in other CTAs: each then writes its
-//    part to the workspace, and the last one to finish, found by a counter that wraps
-//    to zero, adds them up in the order of the CTAs, so that the result has the same bits every time.
+//    part to the workspace, and when all its work is done counts itself present for both
+//    (one fence and one round trip for the two).  The last CTA of an item, found by a counter
+//    that wraps to zero, adds the parts up in the order of the CTAs, so that the result has
+//    the same bits every time.
 //
-// 8-bit cache: codes are exact in fp16, where the products are taken.  A row of q is scaled by
-// a power of two to the top of fp16's range; a key's exponent goes to its score; a value's
+// 8-bit cache.  Scores are products of codes: a row of q, scaled by a power of two to e4m3's
+// range, is the sum of two e4m3 values (4 + 4 of bf16's 8 bits; what they leave is at most 2^-18
+// of the row's largest), so that keys need no conversion.  For the other product, values'
+// codes are converted to fp16, exactly; a key's exponent goes to its score, a value's
 // exponent to its weight, and the weights that multiply the codes are relative to the largest
 // of these products, whose running maximum a column keeps next to its scores'.
 #include <cuda.h>
@@ -43,7 +49,7 @@ namespace w4a16 {
 namespace {
 
 constexpr int kWarps = 4;                    // consumers
-constexpr int kThreads = (kWarps + 1) * 32;  // and the producer
+constexpr int kThreads = (kWarps + 2) * 32;  // the producer before them, the finisher after
 constexpr int kStages = 3;
 constexpr int kHalfStage = 16384;            // a tile's keys, or its values
 constexpr int kStageBytes = 2 * kHalfStage;
@@ -71,9 +77,9 @@ __host__ __device__ inline Columns columns_of(int group) {
 }
 __host__ __device__ inline int used_columns(int group) { return group < kMaxCols ? group : kMaxCols; }
 
-// A part in the workspace: the outputs of its columns, then their sums, maxima, and the
-// maxima that the outputs are relative to (e4m3; else the same).
-__host__ __device__ inline int part_floats(int cols) { return (cols * (kKvHeadDim + 3) + 3) / 4 * 4; }
+// A part in the workspace: the outputs of its columns, then for each its sum, its maximum and
+// the maximum that the outputs are relative to (e4m3; else the same).
+__host__ __device__ inline int part_floats(int cols) { return cols * (kKvHeadDim + 4); }
 
 // The workspace's counters, one for each CTA.
 __host__ __device__ inline int counter_bytes(int ctas) { return (ctas * 4 + 15) / 16 * 16; }
@@ -102,19 +108,26 @@ struct Row {
     int weight;        // of an item: the groups that it sees, and kItemWeight
 };
 
+// A part that the CTA has written: the item, and whether the CTA is to add it up.
+struct Pending {
+    int row, head, block, first_cta, parts;  // parts 0: none
+    int join;
+};
+
 struct Shared {
-    uint64_t full[kStages], empty[kStages], met;
+    uint64_t full[kStages], empty[kStages], done[kStages], met, joined;
     Unit unit[kStages];
     alignas(16) uint16_t fresh[kStages][2][kKvHeadDim];           // the new token's key and value
     alignas(16) uint8_t exponents[kStages][2 * 128];  // e4m3: a tile's (key, value) pairs
-    alignas(16) float part_l[kMaxCols][kWarps], part_m[kMaxCols][kWarps], part_w[kMaxCols][kWarps];
+    // an item's sums and maxima by stage, column and key warp (at most 64 of the two)
+    alignas(16) float part_l[kStages][kMaxCols], part_m[kStages][kMaxCols], part_w[kStages][kMaxCols];
+    Pending pending[2];  // the CTA's parts of items that others share
     int64_t warp_sum[kThreads / 32];
     int64_t bound[2];
     int64_t start_base;
     int start_row;
     Row start;
     int empty_rows;
-    int is_last;
     int abort;
 };
 
@@ -159,6 +172,13 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {
     uint32_t r;
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
     return r;
+}
+// m16n8k32 on e4m3 codes; its sums are as exact as fp32's (2^-22 of the products' magnitudes).
+__device__ __forceinline__ void mma_codes(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
+        "{%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 template <bool E4M3>
 __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -207,7 +227,10 @@ __device__ __forceinline__ uint32_t tile_byte(int row, int unit) {
 }
 
 // An item costs about as much beside its keys as this many groups of 16.
-constexpr int kItemWeight = 2;
+#ifndef KIW
+#define KIW 2
+#endif
+constexpr int kItemWeight = KIW;
 template <bool E4M3>
 __device__ __forceinline__ Row row_of(const DecodeArgs& a, int i, bool* bad) {
     constexpr int kGroups = E4M3 ? 8 : 4;  // of a tile
@@ -240,7 +263,7 @@ template <bool E4M3>
 struct Snap {
     static constexpr int kGroups = E4M3 ? 8 : 4;  // of a tile
     static constexpr int kMost = kGroups + kItemWeight;
-    static constexpr int kSnap = E4M3 ? 16 : 12;
+    static constexpr int kSnap = kMost + (E4M3 ? 4 : 6);
     static_assert(kSnap >= kMost);
 };
 // A bound within the items of a row, which start at `base`.
@@ -271,19 +294,17 @@ __device__ __forceinline__ Row next_row(const DecodeArgs& a, int* row) {
 }
 
 template <bool E4M3>
-__device__ void produce(const DecodeArgs& a, const CUtensorMap* map, Shared& sh, uint32_t stages,
+__device__ void produce(const DecodeArgs& a, const CUtensorMap* maps, Shared& sh, uint32_t stages,
                         uint32_t queries, int64_t weight, int64_t ctas, int64_t w0, int64_t w1) {
     constexpr int kTile = E4M3 ? 128 : 64;
     const KvView& kv = a.kv;
     const int lane = threadIdx.x & 31;
-    const int box_shift = kv.page_shift < (E4M3 ? 7 : 6) ? kv.page_shift : (E4M3 ? 7 : 6);
-    const int box_rows = 1 << box_shift;
-    const int halves = E4M3 ? 1 : 2;
-    const int boxes = (kTile >> box_shift) * halves * 2;  // of a stage, at most 16
+    const int page_box = kv.page_shift < (E4M3 ? 7 : 6) ? kv.page_shift : (E4M3 ? 7 : 6);
+    constexpr int kHalves = E4M3 ? 1 : 2;
     const int items = kv.kv_heads * a.cols.blocks;        // of a row
     const int64_t width = static_cast<int64_t>(a.p.H + 2 * kv.kv_heads) * kKvHeadDim;
     // this lane's box: values or keys, half of the row, place in the tile
-    const int which = lane & 1, half = (lane >> 1) % halves, box = (lane >> 1) / halves;
+    const int which = lane & 1, half = (lane >> 1) % kHalves, box = (lane >> 1) / kHalves;
 
     int row = sh.start_row;
     int64_t base = sh.start_base;
@@ -339,8 +360,12 @@ __device__ void produce(const DecodeArgs& a, const CUtensorMap* map, Shared& sh,
                       ? __ldg(kv.table + static_cast<int64_t>(r.slot) * kv.max_pages + e) : 0;
         }
         const int head = item / a.cols.blocks, block = item - head * a.cols.blocks;
-        const int key = key0 + box * box_rows;  // of this lane's box
-        const bool mine = lane < boxes && key < r.len && key + box_rows > r.low;
+        // Boxes of a page, or of 16 rows at the ends of what the row sees, where a page's would
+        // bring tokens for nothing (half a page of 64 tokens is 5% of a row of 600).
+        const bool edge = key0 < r.low || key0 + kTile > r.len;
+        const int box_shift = edge ? 4 : page_box, box_rows = 1 << box_shift;
+        const int key = key0 + (box << box_shift);  // of this lane's box
+        const bool mine = box < kTile >> box_shift && key < r.len && key + box_rows > r.low;
         const int id = __shfl_sync(0xffffffffu, ids, ((key >> kv.page_shift) - ids_from) & 31);
         const bool id_ok = id >= 0 && id < kv.num_pages;
         const bool tile_bad = __any_sync(0xffffffffu, mine && !id_ok);
@@ -390,7 +415,7 @@ __device__ void produce(const DecodeArgs& a, const CUtensorMap* map, Shared& sh,
                                  box * box_rows * 128u;
             if (dbg_check(tma_box_ok(dst, box_rows * 128u, 1024, stages, stages + kStages * kStageBytes, half * 64,
                                      E4M3 ? 1 : 2), kv.status))
-                tma_load_2d(dst, map, bar, half * 64, c1);
+                tma_load_2d(dst, maps + edge, bar, half * 64, c1);
         }
         if constexpr (E4M3) {
             // (key, value) exponents, eight tokens to a lane; every lane arrives
@@ -445,66 +470,220 @@ __device__ __forceinline__ float output_scale(float l, float m, float w) {
     return E4M3 ? 1.0f / l * ex2(-kWeightTop) * ex2(finite(w) - finite(m)) : 1.0f / l;
 }
 
-// Adds up an item's parts in their order: part 0 is its CTA's last item, the others their
-// CTAs' first.  A warp takes a column at a time: its lanes the parts' statistics, then four
-// outputs each, the loads of eight parts under way together.  (A thread per output that walked
-// columns and parts took 35 of 72 us with 13 parts of 8 columns.)
+// Where a column of a warp's output lies in the stage: in the warp's own rows, which no other
+// warp reads while the columns are not split.  The dimensions of a column are turned so that
+// the lanes of a store hit different banks.
 template <bool E4M3>
-__device__ __noinline__ void join_parts(const float* parts, int64_t stride, int n, int cols, int max_cols, uint16_t* out,
-                           int warp, int lane, int* status) {
-    auto at = [&](int k) { return parts + (2 * static_cast<int64_t>(k) + (k == 0)) * stride; };
-    for (int col = warp; col < cols; col += kWarps) {
-        const int stats = max_cols * kKvHeadDim + col;
-        float m = -INFINITY, w = -INFINITY;
-        for (int k = lane; k < n; k += 32) {
-            m = fmaxf(m, __ldcg(at(k) + stats + max_cols));
-            w = fmaxf(w, __ldcg(at(k) + stats + 2 * max_cols));
+__device__ __forceinline__ uint32_t meet_byte(int warp, int col) {
+    return E4M3 ? (col >> 3) * kHalfStage + warp * 4096 + (col & 7) * 512
+                : (col >> 2) * 8192 + warp * 2048 + (col & 3) * 512;
+}
+template <bool E4M3>
+__device__ __forceinline__ int meet_turn(int col) {
+    const int c = col >> 1 & 3;
+    return E4M3 ? 16 * (c & 1) + 4 * (c >> 1) : 8 * c;
+}
+
+__device__ __forceinline__ uint16_t* output_of(const DecodeArgs& a, int row, int head, int block) {
+    return a.p.out + (static_cast<int64_t>(row) * a.p.H + static_cast<int64_t>(head) * a.cols.group +
+                      block * a.cols.block) * kKvHeadDim;
+}
+__device__ __forceinline__ int columns_in(const DecodeArgs& a, int block) {
+    return min(a.cols.block, a.cols.group - block * a.cols.block);
+}
+__device__ __forceinline__ float* parts_in(const DecodeArgs& a) {
+    return reinterpret_cast<float*>(static_cast<uint8_t*>(a.p.workspace) + counter_bytes(gridDim.x));
+}
+
+// Adds up an item's parts in their order: part 0 is its CTA's last item, the others their
+// CTAs' first.  Sixteen lanes take a column, eight outputs each; a lane has a part's
+// statistics, and the outputs of kBatch parts are under way together.  (A thread per output that walked
+// columns and parts took 35 of 72 us with 13 parts of 8 columns, a warp per column with the
+// weights in one chain 20.)
+template <bool E4M3>
+__device__ void join_parts(const DecodeArgs& a, const Pending& p, int group, int groups, int lane) {
+    constexpr int kBatch = 8;
+    const int cols = columns_in(a, p.block), max_cols = used_columns(a.cols.group), n = p.parts;
+    const int64_t stride = part_floats(max_cols);
+    const float* const parts = parts_in(a) + 2 * p.first_cta * stride;
+    auto part = [&](int k) { return parts + (2 * static_cast<int64_t>(k) + (k == 0)) * stride; };
+    const int l16 = lane & 15;
+    for (int col0 = 0; col0 < cols; col0 += groups) {
+        const bool mine = col0 + group < cols;
+        const int col = mine ? col0 + group : 0;  // (the other half of the warp may have one)
+        auto stats = [&](int k) {
+            return k < n ? __ldcg(reinterpret_cast<const float4*>(part(k) + max_cols * kKvHeadDim) + col)
+                         : make_float4(0.0f, -INFINITY, -INFINITY, 0.0f);
+        };
+        float m = -INFINITY, top = -INFINITY, l = 0.0f;
+        float4 mine16 = stats(l16);
+        for (int k0 = 0; k0 < n; k0 += 16) {
+            const float4 s = k0 == 0 ? mine16 : stats(k0 + l16);
+            m = fmaxf(m, s.y);
+            top = fmaxf(top, s.z);
         }
+        float4 v[kBatch][2];
+        auto load = [&](int k0) {
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
+            for (int i = 0; i < kBatch; ++i)
+                if (k0 + i < n) {
+                    const float4* from = reinterpret_cast<const float4*>(part(k0 + i) + col * kKvHeadDim) + 2 * l16;
+                    v[i][0] = __ldcg(from);
+                    v[i][1] = __ldcg(from + 1);
+                }
+        };
+        load(0);
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) {
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-            w = fmaxf(w, __shfl_xor_sync(0xffffffffu, w, o));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
         }
-        float l = 0.0f;
         bool bad = false;
-        float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int k0 = 0; k0 < n; k0 += 32) {
-            float f = 0.0f, pl = 0.0f;
-            if (k0 + lane < n) {
-                const float* p = at(k0 + lane) + stats;
-                pl = __ldcg(p);
-                bad |= pl < 0.0f;
-                pl *= ex2(__ldcg(p + max_cols) - finite(m));
-                f = ex2(__ldcg(p + 2 * max_cols) - finite(w));
-            }
+        float sum[8] = {};
+        for (int k0 = 0; k0 < n; k0 += 16) {
+            const float4 s = k0 == 0 ? mine16 : stats(k0 + l16);
+            bad |= s.x < 0.0f;
+            l += s.x * ex2(s.y - finite(m));
+            const float f = ex2(s.z - finite(top));
+            for (int h = 0; h < 16 && k0 + h < n; h += kBatch) {
+                if (k0 + h > 0) load(k0 + h);
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) pl += __shfl_xor_sync(0xffffffffu, pl, o);
-            l += pl;
-            const int end = min(32, n - k0);
-            for (int k = 0; k < end; k += 8) {
-                float4 v[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (k + i < end)
-                        v[i] = __ldcg(reinterpret_cast<const float4*>(at(k0 + k + i) + col * kKvHeadDim) + lane);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float a = __shfl_sync(0xffffffffu, f, (k + i) & 31);
-                    if (k + i < end) {
-                        sum.x += a * v[i].x;
-                        sum.y += a * v[i].y;
-                        sum.z += a * v[i].z;
-                        sum.w += a * v[i].w;
+                for (int i = 0; i < kBatch; ++i) {
+                    const float w = __shfl_sync(0xffffffffu, f, (lane & 16) | (h + i));
+                    if (k0 + h + i < n) {
+                        sum[0] += w * v[i][0].x;
+                        sum[1] += w * v[i][0].y;
+                        sum[2] += w * v[i][0].z;
+                        sum[3] += w * v[i][0].w;
+                        sum[4] += w * v[i][1].x;
+                        sum[5] += w * v[i][1].y;
+                        sum[6] += w * v[i][1].z;
+                        sum[7] += w * v[i][1].w;
                     }
                 }
             }
         }
-        bad = __any_sync(0xffffffffu, bad);
-        if (bad && lane == 0) record_status(status, kInvalid);
-        const float f = output_scale<E4M3>(l, m, w);
-        reinterpret_cast<uint2*>(out + col * kKvHeadDim)[lane] =
-            bad ? make_uint2(0, 0) : make_uint2(bf16_pair(sum.x * f, sum.y * f), bf16_pair(sum.z * f, sum.w * f));
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+        bad = __any_sync(0xffffffffu, bad);  // (of the item: its columns see the same pages)
+        if (!mine) continue;
+        const float f = output_scale<E4M3>(l, m, top);
+        uint4 o = make_uint4(bf16_pair(sum[0] * f, sum[1] * f), bf16_pair(sum[2] * f, sum[3] * f),
+                             bf16_pair(sum[4] * f, sum[5] * f), bf16_pair(sum[6] * f, sum[7] * f));
+        if (bad) {
+            o = make_uint4(0, 0, 0, 0);
+            if (l16 == 0) record_status(a.kv.status, kInvalid);
+        }
+        reinterpret_cast<uint4*>(output_of(a, p.row, p.head, p.block) + col * kKvHeadDim)[l16] = o;
     }
+}
+
+// After the CTA's last unit, by all warps that computed: the items that this CTA adds up.
+template <bool E4M3>
+__device__ void join_pending(const DecodeArgs& a, Shared& sh, int w, int lane) {
+    for (int i = 0; i < 2; ++i)
+        if (sh.pending[i].join) join_parts<E4M3>(a, sh.pending[i], 2 * w + (lane >> 4), 2 * (kWarps + 1), lane);
+}
+
+// The finisher: follows the stages, and at an item's end adds up what the warps left there.
+template <bool E4M3, int NT>
+__device__ void finish(const DecodeArgs& a, Shared& sh, const uint8_t* stage_mem) {
+    const KvView& kv = a.kv;
+    const int lane = threadIdx.x & 31;
+    const int key_warps = kWarps / a.cols.warps, max_cols = used_columns(a.cols.group);
+    int st = 0;
+    uint32_t phase = 0, done_phase = 0;  // done_phase: a bit for each stage
+    bool bad = false;
+    for (;;) {
+        if (!wait_warp<false, 100>(smem_u32(&sh.full[st]), phase, &sh.abort, kv.status, a.p.wait_ns)) return;
+        const Unit& t = sh.unit[st];
+        const int flags = t.flags;
+        if (flags & kFirst) bad = false;
+        bad |= (flags & kBad) != 0;
+        if (flags & kLast) {
+            if (!wait_warp(smem_u32(&sh.done[st]), done_phase >> st & 1, &sh.abort, kv.status, a.p.wait_ns)) return;
+            done_phase ^= 1u << st;
+            const uint8_t* const tile = stage_mem + st * kStageBytes;
+            const int cols = columns_in(a, t.block);
+            const bool whole = t.parts == 1;
+            const int slot = t.first_cta == static_cast<int>(blockIdx.x);
+            float* const part = parts_in(a) + (2 * static_cast<int64_t>(blockIdx.x) + slot) * part_floats(max_cols);
+            uint16_t* const out = output_of(a, t.row, t.head, t.block);
+#pragma unroll 2
+            for (int col = 0; col < cols; ++col) {
+                const int cw = col / (8 * NT), in = col - cw * 8 * NT, turned = (4 * lane + meet_turn<E4M3>(in)) & 127;
+                float4 x[kWarps];
+                float ls[kWarps], ms[kWarps], ws[kWarps];
+#pragma unroll
+                for (int k = 0; k < kWarps; ++k) {
+                    const bool has = k < key_warps;
+                    const int at = col * key_warps + (has ? k : 0);
+                    x[k] = *reinterpret_cast<const float4*>(
+                        tile + meet_byte<E4M3>((has ? k : 0) * a.cols.warps + cw, in) + turned * 4);
+                    ls[k] = has ? sh.part_l[st][at] : 0.0f;
+                    ms[k] = has ? sh.part_m[st][at] : -INFINITY;
+                    ws[k] = E4M3 && has ? sh.part_w[st][at] : ms[k];
+                }
+                // (a warp without keys: a maximum of -inf and a sum of 0)
+                const float m = fmaxf(fmaxf(ms[0], ms[1]), fmaxf(ms[2], ms[3]));
+                const float w = E4M3 ? fmaxf(fmaxf(ws[0], ws[1]), fmaxf(ws[2], ws[3])) : m;
+                float l = 0.0f;
+                float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+                for (int k = 0; k < kWarps; ++k) {
+                    const float f = ex2(ms[k] - finite(m));
+                    l += f * ls[k];
+                    const float h = k >= key_warps ? 0.0f : E4M3 ? ex2(ws[k] - finite(w)) : f;
+                    if (k < key_warps) {
+                        o.x += h * x[k].x;
+                        o.y += h * x[k].y;
+                        o.z += h * x[k].z;
+                        o.w += h * x[k].w;
+                    }
+                }
+                if (whole) {
+                    const float f = output_scale<E4M3>(l, m, w);
+                    reinterpret_cast<uint2*>(out + col * kKvHeadDim)[lane] =
+                        bad ? make_uint2(0, 0) : make_uint2(bf16_pair(o.x * f, o.y * f), bf16_pair(o.z * f, o.w * f));
+                } else {
+                    reinterpret_cast<float4*>(part + col * kKvHeadDim)[lane] = o;
+                    if (lane == 0)  // (a sum is never negative: marks a bad page index)
+                        reinterpret_cast<float4*>(part + max_cols * kKvHeadDim)[col] =
+                            make_float4(bad ? -1.0f : l, m, w, 0.0f);
+                }
+            }
+            if (lane == 0) {
+                if (whole) {
+                    if (bad) record_status(kv.status, kInvalid);
+                } else {
+                    sh.pending[slot] = {t.row, t.head, t.block, t.first_cta, t.parts, 0};
+                }
+            }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sh.empty[st]));
+        if (flags & kEnd) break;
+        if (++st == kStages) {
+            st = 0;
+            phase ^= 1;
+        }
+    }
+    if (sh.pending[0].parts == 0 && sh.pending[1].parts == 0) {
+        if (lane == 0) mbar_arrive(smem_u32(&sh.joined));
+        return;
+    }
+    __syncwarp();
+    if (lane < 2 && sh.pending[lane].parts > 0) {
+        // (releases this CTA's part, which the warp wrote, and acquires the others')
+        const uint32_t last = sh.pending[lane].parts - 1;
+        uint32_t* const count = static_cast<uint32_t*>(a.p.workspace) + sh.pending[lane].first_cta;
+        uint32_t was;
+        asm volatile("atom.acq_rel.gpu.global.inc.u32 %0, [%1], %2;" : "=r"(was) : "l"(count), "r"(last) : "memory");
+        sh.pending[lane].join = was == last;
+    }
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_u32(&sh.joined));
+    join_pending<E4M3>(a, sh, kWarps, lane);
 }
 
 // The tile's ends: the new token's row is put in place, as the cache holds it, and stored, and
@@ -551,77 +730,6 @@ __device__ __forceinline__ void mend_tile(const DecodeArgs& a, Shared& sh, int s
     }
     fence_proxy_async();  // (the stage's next contents come by TMA)
     __syncwarp();
-}
-
-// The warps' parts of an item, met in shared memory, to the output or to the workspace and the
-// join; false if the CTA gave up.
-template <bool E4M3, int NT>
-__device__ __forceinline__ bool finish_item(const DecodeArgs& a, Shared& sh, const Unit& t, const float* meet, int warp,
-                                         int lane, bool bad, uint32_t& met) {
-    const KvView& kv = a.kv;
-    const int key_warps = kWarps / a.cols.warps;
-    const int tid = threadIdx.x - 32, d = tid;  // a thread to a dimension
-    const int cols = min(a.cols.block, a.cols.group - t.block * a.cols.block);
-    const int max_cols = used_columns(a.cols.group);
-    float* const parts = reinterpret_cast<float*>(
-        static_cast<uint8_t*>(a.p.workspace) + counter_bytes(gridDim.x));
-    const int64_t stride = part_floats(max_cols);
-    const bool whole = t.parts == 1;
-    float* const part =
-        parts + (2 * static_cast<int64_t>(blockIdx.x) + (t.first_cta == static_cast<int>(blockIdx.x))) * stride;
-    uint16_t* const out =
-        a.p.out + (static_cast<int64_t>(t.row) * a.p.H + static_cast<int64_t>(t.head) * a.cols.group +
-                   t.block * a.cols.block) * kKvHeadDim;
-    // (as many columns under way as the loop is unrolled: each is a chain of loads from shared
-    // memory and exponentials)
-#pragma unroll 4
-    for (int col = 0; col < cols; ++col) {
-        const int cw = col / (8 * NT), in = col - cw * 8 * NT;
-        const float4 ms = *reinterpret_cast<const float4*>(sh.part_m[col]);
-        const float4 ls = *reinterpret_cast<const float4*>(sh.part_l[col]);
-        const float4 ws = E4M3 ? *reinterpret_cast<const float4*>(sh.part_w[col]) : ms;
-        float x[kWarps];
-#pragma unroll
-        for (int k = 0; k < kWarps; ++k)
-            x[k] = k < key_warps ? meet[((k * a.cols.warps + cw) * 8 * NT + in) * kKvHeadDim + ((d + 8 * (in >> 1)) & 127)]
-                                 : 0.0f;
-        // (warps that have no keys of the column: a maximum of -inf and a sum of 0)
-        const float m = fmaxf(fmaxf(ms.x, ms.y), fmaxf(ms.z, ms.w)), base = finite(m);
-        const float w = E4M3 ? fmaxf(fmaxf(ws.x, ws.y), fmaxf(ws.z, ws.w)) : m, from = finite(w);
-        const float l = ex2(ms.x - base) * ls.x + ex2(ms.y - base) * ls.y + ex2(ms.z - base) * ls.z +
-                        ex2(ms.w - base) * ls.w;
-        const float o = ex2(ws.x - from) * x[0] + ex2(ws.y - from) * x[1] + ex2(ws.z - from) * x[2] +
-                        ex2(ws.w - from) * x[3];
-        if (whole) {
-            out[col * kKvHeadDim + d] =
-                bad ? 0 : static_cast<uint16_t>(bf16_pair(o * output_scale<E4M3>(l, m, w), 0.0f));
-        } else {
-            part[col * kKvHeadDim + d] = o;
-            if (d == 0) {
-                float* const stats = part + max_cols * kKvHeadDim + col;
-                stats[0] = bad ? -1.0f : l;  // (a sum is never negative: marks a bad page index)
-                stats[max_cols] = m;
-                stats[2 * max_cols] = w;
-            }
-        }
-    }
-    if (whole) {
-        if (bad && tid == 0) record_status(kv.status, kInvalid);
-    } else {
-        __threadfence();
-        if (!consumers_meet(sh, met, kv.status, a.p.wait_ns)) return false;
-        if (tid == 0) {
-            unsigned int* const count = static_cast<unsigned int*>(a.p.workspace) + t.first_cta;
-            sh.is_last = atomicInc(count, t.parts - 1) == static_cast<unsigned int>(t.parts - 1);
-        }
-        if (!consumers_meet(sh, met, kv.status, a.p.wait_ns)) return false;
-        if (sh.is_last) {
-            __threadfence();
-            join_parts<E4M3>(parts + 2 * t.first_cta * stride, stride, t.parts, cols, max_cols, out, warp, lane,
-                             kv.status);
-        }
-    }
-    return true;
 }
 
 // The running softmax of a warp: two columns a thread in each of NT tiles of eight.
@@ -685,14 +793,16 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
                 }
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                // the largest to [2^14, 2^15): eight bits of mantissa stay exact down to 2^-31 of it
-                int e = static_cast<int>(__float_as_uint(top) >> 23) - 127 - 14;
-                e = e < -112 ? -112 : e;
+                const int e = e4m3_row_exponent(top);
                 const float f = power_of_two(-e);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
-                    q[k][nt][0] = half_pair(bf16_lo(v[k].x) * f, bf16_hi(v[k].x) * f);
-                    q[k][nt][1] = half_pair(bf16_lo(v[k].y) * f, bf16_hi(v[k].y) * f);
+                    const float x[4] = {bf16_lo(v[k].x) * f, bf16_hi(v[k].x) * f, bf16_lo(v[k].y) * f,
+                                        bf16_hi(v[k].y) * f};
+                    q[k][nt][0] = e4m3_quad(x[0], x[1], x[2], x[3]);
+                    const float2 lo = half2_floats(e4m3_to_half2(static_cast<uint16_t>(q[k][nt][0])));
+                    const float2 hi = half2_floats(e4m3_to_half2(static_cast<uint16_t>(q[k][nt][0] >> 16)));
+                    q[k][nt][1] = e4m3_quad(x[0] - lo.x, x[1] - lo.y, x[2] - hi.x, x[3] - hi.y);
                 }
                 // (column g's scale is needed by the threads of columns 2c and 2c + 1)
 #pragma unroll
@@ -745,22 +855,17 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
                         for (int nt = 0; nt < NT; ++nt) mma<E4M3>(acc[k & 1][nt], f, q[k][nt][0], q[k][nt][1]);
                     }
                 } else {
-                    // a 16-byte unit is 16 dimensions, of which a thread gets 4c .. 4c + 3
+                    // 32 dimensions at a time, for both parts of q
 #pragma unroll
                     for (int k = 0; k < 8; k += 2) {
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
-                            uint32_t w[4];
-                            ldsm_x4((keys + key_off + step * 4096 + i * 2048) ^ (k << 4), w);
+                            uint32_t f[4];
+                            ldsm_x4((keys + key_off + step * 4096 + i * 2048) ^ (k << 4), f);
 #pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                const uint32_t f[4] = {e4m3_to_half2(static_cast<uint16_t>(w[2 * h])),
-                                                       e4m3_to_half2(static_cast<uint16_t>(w[2 * h + 1])),
-                                                       e4m3_to_half2(static_cast<uint16_t>(w[2 * h] >> 16)),
-                                                       e4m3_to_half2(static_cast<uint16_t>(w[2 * h + 1] >> 16))};
-#pragma unroll
-                                for (int nt = 0; nt < NT; ++nt)
-                                    mma<E4M3>(acc[i][nt], f, q[k + h][nt][0], q[k + h][nt][1]);
+                            for (int nt = 0; nt < NT; ++nt) {
+                                mma_codes(acc[i][nt], f, q[k][nt][0], q[k + 1][nt][0]);
+                                mma_codes(acc[i][nt], f, q[k][nt][1], q[k + 1][nt][1]);
                             }
                         }
                     }
@@ -884,10 +989,8 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
             release();
             if (!wait()) return;
         }
-        // The warps' parts meet in the stage, which all have read: [warp][16 columns][128],
-        // a column turned by eight values per pair so that a store's lanes hit all banks.
-        float* const meet = reinterpret_cast<float*>(tile);
-        if (!consumers_meet(sh, met, kv.status, a.p.wait_ns)) return;
+        // what this warp has of the item, into its rows of the stage
+        if (a.cols.warps > 1 && !consumers_meet(sh, met, kv.status, a.p.wait_ns)) return;  // (others read them)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -898,31 +1001,33 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
                 l += __shfl_xor_sync(0xffffffffu, l, 16);
                 const int col = nt * 8 + 2 * c + j;
                 if (g == 0) {
-                    const int at = col_warp * 8 * NT + col;
-                    sh.part_l[at][key_warp] = l;
-                    sh.part_m[at][key_warp] = s.m[nt][j];
-                    if constexpr (E4M3) sh.part_w[at][key_warp] = s.w[nt][j];
+                    const int at = (col_warp * 8 * NT + col) * key_warps + key_warp;
+                    sh.part_l[st][at] = l;
+                    sh.part_m[st][at] = s.m[nt][j];
+                    if constexpr (E4M3) sh.part_w[st][at] = s.w[nt][j];
                 }
+                uint8_t* const to = tile + meet_byte<E4M3>(warp, col);
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         const int d = E4M3 ? 16 * k + 2 * g + i : 16 * k + g + 8 * i;
-                        meet[(warp * 8 * NT + col) * kKvHeadDim + ((d + 8 * (col >> 1)) & 127)] =
-                            s.o[k][nt][2 * i + j];
+                        *reinterpret_cast<float*>(to + ((d + meet_turn<E4M3>(col)) & 127) * 4) = s.o[k][nt][2 * i + j];
                     }
             }
-        if (!consumers_meet(sh, met, kv.status, a.p.wait_ns)) return;
-        if (!finish_item<E4M3, NT>(a, sh, sh.unit[st], meet, warp, lane, s.bad, met)) return;
-        fence_proxy_async();
+        fence_proxy_async();  // (the stage's next contents come by TMA)
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sh.done[st]));
         release();
-        if (flags & kEnd) return;
+        if (flags & kEnd) break;
     }
+    if (!wait_warp(smem_u32(&sh.joined), 0, &sh.abort, kv.status, a.p.wait_ns)) return;
+    join_pending<E4M3>(a, sh, warp, lane);
 }
 
 template <bool E4M3, int NT>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm)
-    attention_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ DecodeArgs a) {
+    attention_decode_kernel(const __grid_constant__ CacheMaps maps, const __grid_constant__ DecodeArgs a) {
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ Shared sh;
     // (the dynamic part starts past the static one: rounded up to the swizzle's 1024 bytes)
@@ -931,21 +1036,21 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
     uint8_t* const query_mem = stage_mem + kStages * kStageBytes;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (tid == 0) {
-        prefetch_tmap(&map);
+        prefetch_tmap(&maps.map[0]);
+        prefetch_tmap(&maps.map[1]);
         for (int i = 0; i < kStages; ++i) {
             mbar_init(smem_u32(&sh.full[i]), E4M3 ? 33 : 1);
-            mbar_init(smem_u32(&sh.empty[i]), kWarps);
+            mbar_init(smem_u32(&sh.empty[i]), kWarps + 1);
+            mbar_init(smem_u32(&sh.done[i]), kWarps);
         }
         mbar_init(smem_u32(&sh.met), kWarps);
+        mbar_init(smem_u32(&sh.joined), 1);
+        sh.pending[0] = sh.pending[1] = Pending{};
         sh.start_base = sh.start_row = sh.empty_rows = 0;
         sh.bound[0] = sh.bound[1] = 0;
         sh.start = Row{};
         sh.abort = 0;
         fence_mbar_init();
-    }
-    for (int i = tid; i < kMaxCols * kWarps; i += kThreads) {  // (of warps without keys of a column)
-        sh.part_l[i / kWarps][i % kWarps] = 0.0f;
-        sh.part_m[i / kWarps][i % kWarps] = sh.part_w[i / kWarps][i % kWarps] = -INFINITY;
     }
     grid_launch_dependents();
     grid_wait();
@@ -1029,13 +1134,15 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
     __syncthreads();
     if (sh.bound[0] == sh.bound[1]) return;
     if (warp == 0)
-        produce<E4M3>(a, &map, sh, smem_u32(stage_mem), smem_u32(query_mem), weight, ctas, sh.bound[0], sh.bound[1]);
-    else
+        produce<E4M3>(a, maps.map, sh, smem_u32(stage_mem), smem_u32(query_mem), weight, ctas, sh.bound[0], sh.bound[1]);
+    else if (warp <= kWarps)
         consume<E4M3, NT>(a, sh, stage_mem, query_mem);
+    else
+        finish<E4M3, NT>(a, sh, stage_mem);
 }
 
 template <bool E4M3, int NT>
-cudaError_t launch(const CUtensorMap& map, const DecodeArgs& a, int grid, cudaStream_t stream) {
+cudaError_t launch(const CacheMaps& maps, const DecodeArgs& a, int grid, cudaStream_t stream) {
     auto kern = attention_decode_kernel<E4M3, NT>;
     const int bytes = 1024 + kStages * kStageBytes + 2 * a.cols.block * kQueryStride;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
@@ -1050,7 +1157,7 @@ cudaError_t launch(const CUtensorMap& map, const DecodeArgs& a, int grid, cudaSt
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, kern, map, a);
+    e = cudaLaunchKernelEx(&cfg, kern, maps, a);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
@@ -1062,22 +1169,25 @@ int64_t decode_workspace_bytes(int H, int kv_heads, int sm_count) {
     return counter_bytes(static_cast<int>(ctas)) + ctas * 2 * part_floats(used_columns(H / kv_heads)) * 4;
 }
 
-int encode_cache(CUtensorMap* map, const KvView& kv, int layer) {
+int encode_cache(CacheMaps* maps, const KvView& kv, int layer) {
     const bool e4m3 = kv.exponents != nullptr;
     const int64_t rows = static_cast<int64_t>(2) * kv.num_pages * kv.kv_heads << kv.page_shift;
     const int most = e4m3 ? 128 : 64, tokens = 1 << kv.page_shift;
-    return encode_rows(map, e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
-                          kv.pages + layer * rows * kv.row_bytes, kKvHeadDim, rows, kv.row_bytes,
-                          e4m3 ? 128 : 64, tokens < most ? tokens : most);
+    int rc = 0;
+    for (int i = 0; i < 2 && rc == 0; ++i)
+        rc = encode_rows(&maps->map[i], e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
+                         kv.pages + layer * rows * kv.row_bytes, kKvHeadDim, rows, kv.row_bytes, e4m3 ? 128 : 64,
+                         i == 1 ? 16 : tokens < most ? tokens : most);
+    return rc;
 }
 
-cudaError_t launch_attention_decode(const CUtensorMap& map, const KvView& kv, const DecodeParams& p, int sm_count,
+cudaError_t launch_attention_decode(const CacheMaps& maps, const KvView& kv, const DecodeParams& p, int sm_count,
                                     cudaStream_t stream) {
     const DecodeArgs a{kv, p, columns_of(p.H / kv.kv_heads), p.window};
     const int grid = sm_count * kCtasPerSm;
     const bool e4m3 = kv.exponents != nullptr, wide = a.cols.block > 8;
-    return e4m3 ? (wide ? launch<true, 2>(map, a, grid, stream) : launch<true, 1>(map, a, grid, stream))
-                : (wide ? launch<false, 2>(map, a, grid, stream) : launch<false, 1>(map, a, grid, stream));
+    return e4m3 ? (wide ? launch<true, 2>(maps, a, grid, stream) : launch<true, 1>(maps, a, grid, stream))
+                : (wide ? launch<false, 2>(maps, a, grid, stream) : launch<false, 1>(maps, a, grid, stream));
 }
 
 }  // namespace w4a16

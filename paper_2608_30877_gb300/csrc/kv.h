@@ -72,8 +72,12 @@ struct DecodeParams {
     uint64_t wait_ns;
 };
 int64_t decode_workspace_bytes(int H, int kv_heads, int sm_count);
-int encode_cache(CUtensorMap* map, const KvView& kv, int layer);  // one layer's keys and values
-cudaError_t launch_attention_decode(const CUtensorMap& map, const KvView& kv, const DecodeParams& p,
+// One layer's keys and values, in boxes of a page (at most a tile of decode.cu) and of 16 rows.
+struct CacheMaps {
+    CUtensorMap map[2];
+};
+int encode_cache(CacheMaps* maps, const KvView& kv, int layer);
+cudaError_t launch_attention_decode(const CacheMaps& maps, const KvView& kv, const DecodeParams& p,
                                     int sm_count, cudaStream_t stream);
 
 uint64_t wait_limit_ns();  // internal.h
