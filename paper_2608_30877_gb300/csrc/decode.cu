@@ -226,11 +226,10 @@ __device__ __forceinline__ uint32_t tile_byte(int row, int unit) {
     return base + row * 128u + (((unit & 7) ^ (row & 7)) << 4);
 }
 
-// An item costs about as much beside its keys as this many groups of 16.
-#ifndef KIW
-#define KIW 2
-#endif
-constexpr int kItemWeight = KIW;
+// An item costs about as much beside its keys as this many groups of 16 (its queries, the
+// half-filled last tile, its end): 64 rows of 200 to 1024 tokens, 96 heads, with 2 / 4 / 6 / 9 of them
+// 292 / 288 / 287 / 290 us in bf16, in e4m3 193 / 185 / 181 / 173.
+__host__ __device__ constexpr int item_weight(bool e4m3) { return e4m3 ? 9 : 5; }
 template <bool E4M3>
 __device__ __forceinline__ Row row_of(const DecodeArgs& a, int i, bool* bad) {
     constexpr int kGroups = E4M3 ? 8 : 4;  // of a tile
@@ -246,7 +245,7 @@ __device__ __forceinline__ Row row_of(const DecodeArgs& a, int i, bool* bad) {
     r.first = begin / kGroups;
     r.tiles = (end - 1) / kGroups + 1 - r.first;
     r.skip = begin - r.first * kGroups;
-    r.weight = end - begin + kItemWeight;
+    r.weight = end - begin + item_weight(E4M3);
     return r;
 }
 // Where tile t of an item starts in its weight.
@@ -258,11 +257,11 @@ __device__ __forceinline__ int tile_start(const Row& r, int t) {
 // CTA c has the tiles that start in [bound(c), bound(c + 1)), bound(c) = c * weight / ctas rounded
 // down and, if that is at most kSnap groups from the start or the end of the item in which it
 // falls, moved there: a part costs more than so many groups.  kSnap is at least a tile and
-// kItemWeight, and so are the bounds apart before they move; so each part of an item has a tile.
+// an item's weight, and so are the bounds apart before they move; so each part of an item has a tile.
 template <bool E4M3>
 struct Snap {
     static constexpr int kGroups = E4M3 ? 8 : 4;  // of a tile
-    static constexpr int kMost = kGroups + kItemWeight;
+    static constexpr int kMost = kGroups + item_weight(E4M3);
     static constexpr int kSnap = kMost + (E4M3 ? 4 : 6);
     static_assert(kSnap >= kMost);
 };
@@ -740,7 +739,7 @@ struct State {
     bool bad;        // a page index was out of range
 };
 
-template <bool E4M3, int NT>
+template <bool E4M3, int NT, bool ONE>
 __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uint8_t* query_mem) {
     constexpr int kTile = E4M3 ? 128 : 64;
     constexpr int kStep = kTile / kWarps, kGroups = kStep / 16, kRows = 2 * kGroups;  // a warp's keys at a time
@@ -775,7 +774,7 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
         const uint8_t* rows = query_mem + (sh.unit[st].flags >> kQSlotShift & 1) * a.cols.block * kQueryStride;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const uint8_t* row = rows + (col_warp * 8 * NT + nt * 8 + g) * kQueryStride;
+            const uint8_t* row = rows + (ONE ? 0 : col_warp * 8 * NT + nt * 8 + g) * kQueryStride;
             if constexpr (!E4M3) {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
@@ -870,80 +869,123 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
                         }
                     }
                 }
-                bool see[kRows];  // keys g and g + 8 of each group
-#pragma unroll
-                for (int i = 0; i < kRows; ++i) {
-                    const int at = key + g + 8 * i;
-                    see[i] = !edge || (at >= low && at < len);
-                }
-                float key_scale[kRows], value_exp[kRows];
-                if constexpr (E4M3) {
-#pragma unroll
-                    for (int i = 0; i < kRows; ++i) {
-                        const uint32_t e =
-                            *reinterpret_cast<const uint16_t*>(sh.exponents[st] + (step * kStep + g + 8 * i) * 2);
-                        key_scale[i] = __uint_as_float((e & 0xFFu) << 23);
-                        value_exp[i] = static_cast<float>(static_cast<int>(e >> 8) - 127);
-                    }
-                }
                 float alpha[NT][2];  // what the new maxima make of o
                 uint32_t b[kGroups][NT][2];
                 bool moved = false;
-                // the running maximum of a column: v over the keys of this thread, and what it was
-                auto raise = [&](float v, float& was, float* scale_old) {
-                    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 4));
-                    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
-                    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
-                    v = fmaxf(v, was);
-                    const float base = finite(v);
-                    *scale_old = ex2(was - base);
-                    moved |= v != was;
-                    was = v;
-                    return base;
-                };
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    float x[kRows][2], p[kRows][2], scale_l[2];
-#pragma unroll
-                    for (int i = 0; i < kRows; ++i)
-#pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            const float v = E4M3 ? acc[i >> 1][nt][(i & 1) * 2 + j] * (key_scale[i] * q_scale[nt][j])
-                                                 : (acc[0][nt][i * 2 + j] + acc[1][nt][i * 2 + j]) * scale;
-                            x[i][j] = see[i] ? v : -INFINITY;
-                        }
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        float top = fmaxf(x[0][j], x[1][j]);
-                        if constexpr (E4M3) top = fmaxf(top, fmaxf(x[2][j], x[kRows - 1][j]));
-                        const float base = raise(top, s.m[nt][j], &scale_l[j]);
-                        float sum = 0.0f;
-#pragma unroll
-                        for (int i = 0; i < kRows; ++i) {
-                            p[i][j] = ex2(x[i][j] - base);
-                            sum += p[i][j];
-                        }
-                        s.l[nt][j] = s.l[nt][j] * scale_l[j] + (E4M3 ? sum : 0.0f);
-                        alpha[nt][j] = scale_l[j];
-                        if constexpr (E4M3) {
-                            // (an unseen key's score is -inf whatever its exponent)
-#pragma unroll
-                            for (int i = 0; i < kRows; ++i) x[i][j] += value_exp[i];
-                            top = fmaxf(fmaxf(x[0][j], x[1][j]), fmaxf(x[2][j], x[kRows - 1][j]));
-                            const float to = raise(top, s.w[nt][j], &alpha[nt][j]) - kWeightTop;
-#pragma unroll
-                            for (int i = 0; i < kRows; ++i) p[i][j] = ex2(x[i][j] - to);
-                        }
+                if constexpr (ONE) {
+                    // One query, the same in every column: lane (g, c) has all of keys g + 8 r, and
+                    // takes that of r = c (bf16: r = c % 2, in two lanes alike).
+                    const int r = c % kRows, at = key + g + 8 * r;
+                    float x = acc[0][0][0] + (E4M3 ? 0.0f : acc[1][0][0]);
+                    const float x1 = acc[0][0][2] + (E4M3 ? 0.0f : acc[1][0][2]);
+                    if (r == 1) x = x1;
+                    if (E4M3 && r == 2) x = acc[1][0][0];
+                    if (E4M3 && r == 3) x = acc[1][0][2];
+                    uint32_t e = 0;
+                    if constexpr (E4M3)
+                        e = *reinterpret_cast<const uint16_t*>(sh.exponents[st] + (step * kStep + g + 8 * r) * 2);
+                    x *= E4M3 ? __uint_as_float((e & 0xFFu) << 23) * q_scale[0][0] : scale;
+                    if (edge && (at < low || at >= len)) x = -INFINITY;
+                    auto raise = [&](float v, float& was, float* scale_old) {
+                        v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 1));
+                        if constexpr (E4M3) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 2));
+                        v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 4));
+                        v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
+                        v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
+                        v = fmaxf(v, was);
+                        const float base = finite(v);
+                        *scale_old = ex2(was - base);
+                        moved |= v != was;
+                        was = v;
+                        return base;
+                    };
+                    float p = ex2(x - raise(x, s.m[0][0], &alpha[0][0]));
+                    if constexpr (E4M3) {
+                        s.l[0][0] = s.l[0][0] * alpha[0][0] + p;
+                        x += static_cast<float>(static_cast<int>(e >> 8) - 127);
+                        p = ex2(x - raise(x, s.w[0][0], &alpha[0][0]) + kWeightTop);
+                    } else {
+                        // (the rounded weights' sum, so that they add up to one)
+                        s.l[0][0] = s.l[0][0] * alpha[0][0] + bf16_lo(bf16_pair(p, 0.0f));
                     }
-                    // keys 2c, 2c + 1 of column g: the transpose of what this thread holds
+                    // keys g and g + 1 in the lanes of even g, then keys 2c and 2c + 1 everywhere
+                    const float next = __shfl_xor_sync(0xffffffffu, p, 4);
+                    const uint32_t pair = E4M3 ? half_pair(p, next) : bf16_pair(p, next);
+#pragma unroll
+                    for (int i = 0; i < kRows; ++i) b[i >> 1][0][i & 1] = __shfl_sync(0xffffffffu, pair, 8 * c + i);
+                } else {
+                    bool see[kRows];  // keys g and g + 8 of each group
 #pragma unroll
                     for (int i = 0; i < kRows; ++i) {
-                        const uint32_t w = E4M3 ? half_pair(p[i][0], p[i][1]) : bf16_pair(p[i][0], p[i][1]);
-                        if constexpr (!E4M3) {  // (the rounded weights' sum, so that they add up to one)
-                            s.l[nt][0] += bf16_lo(w);
-                            s.l[nt][1] += bf16_hi(w);
+                        const int at = key + g + 8 * i;
+                        see[i] = !edge || (at >= low && at < len);
+                    }
+                    float key_scale[kRows], value_exp[kRows];
+                    if constexpr (E4M3) {
+#pragma unroll
+                        for (int i = 0; i < kRows; ++i) {
+                            const uint32_t e =
+                                *reinterpret_cast<const uint16_t*>(sh.exponents[st] + (step * kStep + g + 8 * i) * 2);
+                            key_scale[i] = __uint_as_float((e & 0xFFu) << 23);
+                            value_exp[i] = static_cast<float>(static_cast<int>(e >> 8) - 127);
                         }
-                        b[i >> 1][nt][i & 1] = transpose_8x8(w);
+                    }
+                    // the running maximum of a column: v over the keys of this thread, and what it was
+                    auto raise = [&](float v, float& was, float* scale_old) {
+                        v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 4));
+                        v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
+                        v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
+                        v = fmaxf(v, was);
+                        const float base = finite(v);
+                        *scale_old = ex2(was - base);
+                        moved |= v != was;
+                        was = v;
+                        return base;
+                    };
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        float x[kRows][2], p[kRows][2], scale_l[2];
+#pragma unroll
+                        for (int i = 0; i < kRows; ++i)
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) {
+                                const float v = E4M3 ? acc[i >> 1][nt][(i & 1) * 2 + j] * (key_scale[i] * q_scale[nt][j])
+                                                     : (acc[0][nt][i * 2 + j] + acc[1][nt][i * 2 + j]) * scale;
+                                x[i][j] = see[i] ? v : -INFINITY;
+                            }
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            float top = fmaxf(x[0][j], x[1][j]);
+                            if constexpr (E4M3) top = fmaxf(top, fmaxf(x[2][j], x[kRows - 1][j]));
+                            const float base = raise(top, s.m[nt][j], &scale_l[j]);
+                            float sum = 0.0f;
+#pragma unroll
+                            for (int i = 0; i < kRows; ++i) {
+                                p[i][j] = ex2(x[i][j] - base);
+                                sum += p[i][j];
+                            }
+                            s.l[nt][j] = s.l[nt][j] * scale_l[j] + (E4M3 ? sum : 0.0f);
+                            alpha[nt][j] = scale_l[j];
+                            if constexpr (E4M3) {
+                                // (an unseen key's score is -inf whatever its exponent)
+#pragma unroll
+                                for (int i = 0; i < kRows; ++i) x[i][j] += value_exp[i];
+                                top = fmaxf(fmaxf(x[0][j], x[1][j]), fmaxf(x[2][j], x[kRows - 1][j]));
+                                const float to = raise(top, s.w[nt][j], &alpha[nt][j]) - kWeightTop;
+#pragma unroll
+                                for (int i = 0; i < kRows; ++i) p[i][j] = ex2(x[i][j] - to);
+                            }
+                        }
+                        // keys 2c, 2c + 1 of column g: the transpose of what this thread holds
+#pragma unroll
+                        for (int i = 0; i < kRows; ++i) {
+                            const uint32_t w = E4M3 ? half_pair(p[i][0], p[i][1]) : bf16_pair(p[i][0], p[i][1]);
+                            if constexpr (!E4M3) {  // (the rounded weights' sum, so that they add up to one)
+                                s.l[nt][0] += bf16_lo(w);
+                                s.l[nt][1] += bf16_hi(w);
+                            }
+                            b[i >> 1][nt][i & 1] = transpose_8x8(w);
+                        }
                     }
                 }
                 if (__any_sync(0xffffffffu, moved)) {
@@ -952,7 +994,7 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) s.o[k][nt][j] *= alpha[nt][j & 1];
+                            for (int j = 0; j < 4; j += ONE ? 2 : 1) s.o[k][nt][j] *= alpha[nt][j & 1];
                 }
                 if constexpr (!E4M3) {
 #pragma unroll
@@ -994,8 +1036,12 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
+            for (int j = 0; j < (ONE ? 1 : 2); ++j) {
                 float l = s.l[nt][j];
+                if constexpr (ONE) {
+                    l += __shfl_xor_sync(0xffffffffu, l, 1);
+                    if constexpr (E4M3) l += __shfl_xor_sync(0xffffffffu, l, 2);
+                }
                 l += __shfl_xor_sync(0xffffffffu, l, 4);
                 l += __shfl_xor_sync(0xffffffffu, l, 8);
                 l += __shfl_xor_sync(0xffffffffu, l, 16);
@@ -1006,6 +1052,7 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
                     sh.part_m[st][at] = s.m[nt][j];
                     if constexpr (E4M3) sh.part_w[st][at] = s.w[nt][j];
                 }
+                if (ONE && c > 0) continue;
                 uint8_t* const to = tile + meet_byte<E4M3>(warp, col);
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
@@ -1025,7 +1072,7 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
     join_pending<E4M3>(a, sh, warp, lane);
 }
 
-template <bool E4M3, int NT>
+template <bool E4M3, int NT, bool ONE>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm)
     attention_decode_kernel(const __grid_constant__ CacheMaps maps, const __grid_constant__ DecodeArgs a) {
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -1136,29 +1183,18 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
     if (warp == 0)
         produce<E4M3>(a, maps.map, sh, smem_u32(stage_mem), smem_u32(query_mem), weight, ctas, sh.bound[0], sh.bound[1]);
     else if (warp <= kWarps)
-        consume<E4M3, NT>(a, sh, stage_mem, query_mem);
+        consume<E4M3, NT, ONE>(a, sh, stage_mem, query_mem);
     else
         finish<E4M3, NT>(a, sh, stage_mem);
 }
 
-template <bool E4M3, int NT>
+template <bool E4M3, int NT, bool ONE>
 cudaError_t launch(const CacheMaps& maps, const DecodeArgs& a, int grid, cudaStream_t stream) {
-    auto kern = attention_decode_kernel<E4M3, NT>;
+    auto kern = attention_decode_kernel<E4M3, NT, ONE>;
     const int bytes = 1024 + kStages * kStageBytes + 2 * a.cols.block * kQueryStride;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = kThreads;
-    cfg.dynamicSmemBytes = bytes;
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, kern, maps, a);
-    return e != cudaSuccess ? e : cudaGetLastError();
+    return launch_overlapped(kern, grid, kThreads, bytes, stream, maps, a);
 }
 
 }  // namespace
@@ -1186,8 +1222,9 @@ cudaError_t launch_attention_decode(const CacheMaps& maps, const KvView& kv, con
     const DecodeArgs a{kv, p, columns_of(p.H / kv.kv_heads), p.window};
     const int grid = sm_count * kCtasPerSm;
     const bool e4m3 = kv.exponents != nullptr, wide = a.cols.block > 8;
-    return e4m3 ? (wide ? launch<true, 2>(maps, a, grid, stream) : launch<true, 1>(maps, a, grid, stream))
-                : (wide ? launch<false, 2>(maps, a, grid, stream) : launch<false, 1>(maps, a, grid, stream));
+    if (p.H == kv.kv_heads) return e4m3 ? launch<true, 1, true>(maps, a, grid, stream) : launch<false, 1, true>(maps, a, grid, stream);
+    if (wide) return e4m3 ? launch<true, 2, false>(maps, a, grid, stream) : launch<false, 2, false>(maps, a, grid, stream);
+    return e4m3 ? launch<true, 1, false>(maps, a, grid, stream) : launch<false, 1, false>(maps, a, grid, stream);
 }
 
 }  // namespace w4a16

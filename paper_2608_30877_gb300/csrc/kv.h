@@ -82,4 +82,23 @@ cudaError_t launch_attention_decode(const CacheMaps& maps, const KvView& kv, con
 
 uint64_t wait_limit_ns();  // internal.h
 
+// A launch that may begin while the kernel before it in the stream ends; the kernel calls
+// grid_wait (ptx.cuh) before it touches global memory.
+template <typename... P, typename... A>
+cudaError_t launch_overlapped(void (*kernel)(P...), int grid, int block, int smem, cudaStream_t stream,
+                              const A&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+    return e != cudaSuccess ? e : cudaGetLastError();
+}
+
 }  // namespace w4a16

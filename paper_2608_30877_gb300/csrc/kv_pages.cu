@@ -77,6 +77,8 @@ __device__ __forceinline__ void plan_begin(const KvView& kv, PlanShared& sh) {
     for (int i = threadIdx.x; i < (kv.num_slots + 31) / 32; i += kThreads) sh.seen[i] = 0;
     if (threadIdx.x == 0) sh.error = sh.copies = 0;
     __syncthreads();
+    grid_launch_dependents();
+    grid_wait();
 }
 // Whether the slot is within range and new to the call.
 __device__ __forceinline__ bool claim_slot(const KvView& kv, PlanShared& sh, int slot) {
@@ -147,12 +149,24 @@ __global__ void __launch_bounds__(kThreads)
     // the lowest free pages, in order (list b)
     int found = 0;
     if (!too_many) {
-        for (int p0 = 0; p0 < kv.num_pages && found < need_all; p0 += kThreads) {
-            const int p = p0 + tid;
-            const int free = p < kv.num_pages && kv.refs[p] == 0;
+        // kRun counts a thread and pass, which a pool of 16000 pages takes once
+        constexpr int kRun = 16;
+        for (int p0 = 0; p0 < kv.num_pages && found < need_all; p0 += kThreads * kRun) {
+            const int begin = p0 + tid * kRun;
+            uint32_t free = 0;
+            if (begin + kRun <= kv.num_pages) {
+                int4 v[kRun / 4];
+#pragma unroll
+                for (int k = 0; k < kRun / 4; ++k) v[k] = reinterpret_cast<const int4*>(kv.refs + begin)[k];
+#pragma unroll
+                for (int k = 0; k < kRun / 4; ++k)
+                    free |= ((v[k].x == 0) | (v[k].y == 0) << 1 | (v[k].z == 0) << 2 | (v[k].w == 0) << 3) << 4 * k;
+            } else {
+                for (int k = 0; begin + k < kv.num_pages; ++k) free |= (kv.refs[begin + k] == 0) << k;
+            }
             int sum;
-            const int rank = found + block_scan(free, sh, &sum);
-            if (free && rank < need_all) ls.b[rank] = p;
+            int rank = found + block_scan(__popc(free), sh, &sum);
+            for (; free != 0 && rank < need_all; free &= free - 1, ++rank) ls.b[rank] = begin + __ffs(free) - 1;
             found += sum;
         }
     }
@@ -339,7 +353,10 @@ __global__ void __launch_bounds__(kThreads) kv_compact_kernel(const KvView kv) {
 // The listed pages' tokens in every layer, and after a compaction the tables' entries.  A
 // warp copies a head's tokens of one layer's keys or values, which lie in one run.
 __global__ void __launch_bounds__(256) kv_copy_kernel(const KvView kv) {
+    constexpr int kBatch = 8;  // 16-byte pieces that a thread has under way
     const Lists ls = lists_of(kv);
+    grid_launch_dependents();
+    grid_wait();
     const int lane = threadIdx.x & 31, T = 1 << kv.page_shift;
     const int64_t warp = blockIdx.x * 8 + (threadIdx.x >> 5), warps = gridDim.x * 8;
     const int copies = ls.head->copies, moved = ls.head->moved;
@@ -357,7 +374,15 @@ __global__ void __launch_bounds__(256) kv_copy_kernel(const KvView kv) {
         uint4* to = reinterpret_cast<uint4*>(
             kv.pages + kv_row(kv, layer, which, ls.dst[c], head, 0) * kv.row_bytes);
         const int units = tokens * (kv.row_bytes / 16);
-        for (int u = lane; u < units; u += 32) to[u] = from[u];
+        for (int u0 = lane; u0 < units; u0 += 32 * kBatch) {
+            uint4 v[kBatch];
+#pragma unroll
+            for (int b = 0; b < kBatch; ++b)
+                if (u0 + 32 * b < units) v[b] = __ldcs(from + u0 + 32 * b);
+#pragma unroll
+            for (int b = 0; b < kBatch; ++b)
+                if (u0 + 32 * b < units) __stcs(to + u0 + 32 * b, v[b]);
+        }
         if (kv.exponents != nullptr && which == 0) {
             const uint16_t* ef = reinterpret_cast<const uint16_t*>(
                 kv.exponents + kv_exponent(kv, layer, 0, page, head, 0));
@@ -376,34 +401,29 @@ __global__ void __launch_bounds__(256) kv_copy_kernel(const KvView kv) {
 }
 
 cudaError_t launch_copies(const KvView& kv, int sm_count, cudaStream_t stream) {
-    kv_copy_kernel<<<sm_count * 8, 256, 0, stream>>>(kv);
-    return cudaGetLastError();
+    return launch_overlapped(kv_copy_kernel, sm_count * 8, 256, 0, stream, kv);
 }
 
 }  // namespace
 
 cudaError_t launch_kv_extend(const KvView& kv, const int32_t* slots, const int32_t* add, int n,
                              int sm_count, cudaStream_t stream) {
-    kv_extend_kernel<<<1, kThreads, 0, stream>>>(kv, slots, add, n);
-    const cudaError_t e = cudaGetLastError();
+    const cudaError_t e = launch_overlapped(kv_extend_kernel, 1, kThreads, 0, stream, kv, slots, add, n);
     return e != cudaSuccess ? e : launch_copies(kv, sm_count, stream);
 }
 
 cudaError_t launch_kv_fork(const KvView& kv, const int32_t* parents, const int32_t* children, int n,
                            cudaStream_t stream) {
-    kv_fork_kernel<<<1, kThreads, 0, stream>>>(kv, parents, children, n);
-    return cudaGetLastError();
+    return launch_overlapped(kv_fork_kernel, 1, kThreads, 0, stream, kv, parents, children, n);
 }
 
 cudaError_t launch_kv_trim(const KvView& kv, const int32_t* slots, const int32_t* keep, int n,
                            cudaStream_t stream) {
-    kv_trim_kernel<<<1, kThreads, 0, stream>>>(kv, slots, keep, n);
-    return cudaGetLastError();
+    return launch_overlapped(kv_trim_kernel, 1, kThreads, 0, stream, kv, slots, keep, n);
 }
 
 cudaError_t launch_kv_compact(const KvView& kv, int sm_count, cudaStream_t stream) {
-    kv_compact_kernel<<<1, kThreads, 0, stream>>>(kv);
-    const cudaError_t e = cudaGetLastError();
+    const cudaError_t e = launch_overlapped(kv_compact_kernel, 1, kThreads, 0, stream, kv);
     return e != cudaSuccess ? e : launch_copies(kv, sm_count, stream);
 }
 

@@ -17,6 +17,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kTokens = 16;  // tokens of a CTA
+constexpr int kBatch = 4;    // rows that 16 threads have under way
 
 // Where token m of the packed batch goes: its page and place there; page -1 outside every
 // sequence or for an entry of -1, -2 for an error.
@@ -48,6 +49,8 @@ template <bool E4M3>
 __global__ void __launch_bounds__(kThreads) kv_write_kernel(const KvView kv, const KvWriteParams p) {
     __shared__ int pages[kTokens], places[kTokens];
     const int m0 = blockIdx.x * kTokens;
+    grid_launch_dependents();
+    grid_wait();
     if (threadIdx.x < kTokens) {
         int page = -1, at = 0;
         if (m0 + threadIdx.x < p.M) token_place(kv, p, m0 + threadIdx.x, &page, &at);
@@ -64,21 +67,34 @@ __global__ void __launch_bounds__(kThreads) kv_write_kernel(const KvView kv, con
     const int lane16 = threadIdx.x & 15;
     const int rows = 2 * kv.kv_heads;  // of a token
     const int64_t width = static_cast<int64_t>(p.H + rows) * kKvHeadDim;
-    for (int r = threadIdx.x >> 4; r < kTokens * rows; r += kThreads / 16) {
-        const int t = r / rows, which = (r - t * rows) / kv.kv_heads, head = r - t * rows - which * kv.kv_heads;
-        if (pages[t] < 0) continue;  // (the same for the row's 16 threads)
-        const uint4 v = __ldg(reinterpret_cast<const uint4*>(
-            p.qkv + (m0 + t) * width + (p.H + which * kv.kv_heads + head) * static_cast<int64_t>(kKvHeadDim)) + lane16);
-        const int64_t row = kv_row(kv, p.layer, which, pages[t], head, places[t]);
-        if constexpr (!E4M3) {
-            reinterpret_cast<uint4*>(kv.pages)[row * 16 + lane16] = v;
-        } else {
-            uint2 codes;
-            const int e = e4m3_row_of_16(v, &codes);
-            reinterpret_cast<uint2*>(kv.pages)[row * 16 + lane16] = codes;
-            if (lane16 == 0)
-                kv.exponents[kv_exponent(kv, p.layer, which, pages[t], head, places[t])] =
-                    static_cast<uint8_t>(e + 127);
+    // (kBatch rows' loads under way together: one at a time, 13000 tokens of 8 heads took 32 us)
+    for (int r0 = threadIdx.x >> 4; r0 < kTokens * rows; r0 += kBatch * (kThreads / 16)) {
+        uint4 v[kBatch];
+        int64_t row[kBatch], exponent[kBatch];
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) {
+            const int r = r0 + b * (kThreads / 16);
+            const int t = r < kTokens * rows ? r / rows : 0;
+            const int which = (r - t * rows) / kv.kv_heads, head = r - t * rows - which * kv.kv_heads;
+            row[b] = -1;
+            if (r >= kTokens * rows || pages[t] < 0) continue;  // (the same for the row's 16 threads)
+            v[b] = __ldg(reinterpret_cast<const uint4*>(
+                p.qkv + (m0 + t) * width +
+                (p.H + which * kv.kv_heads + head) * static_cast<int64_t>(kKvHeadDim)) + lane16);
+            row[b] = kv_row(kv, p.layer, which, pages[t], head, places[t]);
+            exponent[b] = kv_exponent(kv, p.layer, which, pages[t], head, places[t]);
+        }
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) {
+            if (row[b] < 0) continue;
+            if constexpr (!E4M3) {
+                reinterpret_cast<uint4*>(kv.pages)[row[b] * 16 + lane16] = v[b];
+            } else {
+                uint2 codes;
+                const int e = e4m3_row_of_16(v[b], &codes);
+                reinterpret_cast<uint2*>(kv.pages)[row[b] * 16 + lane16] = codes;
+                if (lane16 == 0) kv.exponents[exponent[b]] = static_cast<uint8_t>(e + 127);
+            }
         }
     }
 }
@@ -87,11 +103,8 @@ __global__ void __launch_bounds__(kThreads) kv_write_kernel(const KvView kv, con
 
 cudaError_t launch_kv_write(const KvView& kv, const KvWriteParams& p, cudaStream_t stream) {
     const int grid = (p.M + kTokens - 1) / kTokens;
-    if (kv.exponents != nullptr)
-        kv_write_kernel<true><<<grid, kThreads, 0, stream>>>(kv, p);
-    else
-        kv_write_kernel<false><<<grid, kThreads, 0, stream>>>(kv, p);
-    return cudaGetLastError();
+    return launch_overlapped(kv.exponents != nullptr ? kv_write_kernel<true> : kv_write_kernel<false>, grid, kThreads,
+                             0, stream, kv, p);
 }
 
 }  // namespace w4a16
