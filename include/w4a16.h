@@ -287,7 +287,8 @@ int w4a16_topk_smallest(const void* scores, int score_bits, int64_t n, int64_t k
  *   page_refs   int32 [num_pages], how many sequences have the page; 0: free
  *   scratch     w4a16_kv_scratch_bytes bytes for the page operations, any contents
  * Supported: head_dim 128; page_tokens 16, 32, 64 or 128; num_slots <= 65536;
- * num_pages <= 2^24; a layer's rows (2 num_pages kv_heads page_tokens) < 2^31.
+ * num_pages <= 2^24; a layer's rows (2 num_pages kv_heads page_tokens), the page
+ * table's entries and a sequence's tokens (max_pages page_tokens) < 2^31.
  * An empty cache has seq_len and page_refs all zero.  The struct is a HOST
  * object that each call reads before it returns.  Calls on one cache are
  * ordered by the caller (one stream, or events): the operations below read and

@@ -35,10 +35,11 @@ struct KvView {
     int row_bytes;       // of a token's key: 256 or 128
 };
 
-// The scratch buffer: a header, then four lists of max(num_pages, num_slots) entries.
+// The scratch buffer: a header, then kKvScratchLists lists of max(num_pages, num_slots) entries.
+constexpr int kKvScratchLists = 5;
 struct KvScratch {
     int32_t copies;  // entries of src / dst / tokens
-    int32_t moved;   // compaction: pages from this index on have moved (map says where), else -1
+    int32_t moved;   // compaction: pages from this index on have moved (a list says where), else -1
     int32_t pad[14];
 };
 constexpr int kKvScratchHeader = sizeof(KvScratch) / sizeof(int32_t);

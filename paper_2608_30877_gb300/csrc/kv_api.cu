@@ -31,8 +31,8 @@ bool scratch_sizes_ok(int64_t num_pages, int64_t num_slots) {
     return num_pages > 0 && num_pages <= kKvMaxPages && num_slots > 0 && num_slots <= kKvMaxSlots;
 }
 int64_t scratch_bytes(int64_t num_pages, int64_t num_slots) {
-    return 4 * (kKvScratchHeader + 4 * static_cast<int64_t>(kv_scratch_list(
-                                           static_cast<int>(num_pages), static_cast<int>(num_slots))));
+    const int list = kv_scratch_list(static_cast<int>(num_pages), static_cast<int>(num_slots));
+    return (4 * (kKvScratchHeader + kKvScratchLists * static_cast<int64_t>(list)) + 15) / 16 * 16;
 }
 
 // A cache's buffers, for the overlap checks.
@@ -53,7 +53,7 @@ int check_cache(const w4a16_kv_cache* c, CacheSpans* spans) {
     if (c->page_tokens != 16 && c->page_tokens != 32 && c->page_tokens != 64 && c->page_tokens != 128)
         return W4A16_ERR_UNSUPPORTED;
     if (!scratch_sizes_ok(c->num_pages, c->num_slots) || c->layers > 65535 || c->kv_heads > 65535 ||
-        c->max_pages > kMaxDim / c->page_tokens ||
+        c->max_pages > kMaxDim / c->page_tokens || c->num_slots * c->max_pages > kMaxDim ||
         2 * c->num_pages * c->kv_heads > kMaxDim / c->page_tokens)
         return W4A16_ERR_UNSUPPORTED;
     const void* all[6] = {c->pages, c->exponents, c->page_table, c->seq_len, c->page_refs, c->scratch};

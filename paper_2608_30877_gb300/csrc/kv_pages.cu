@@ -7,7 +7,10 @@
 // operation runs its checks before its first change, so an error leaves the cache as it was.
 // One CTA plans; what has to be copied (an extend's shared last pages, a compaction's
 // moved pages) goes to a list in the scratch buffer that a second kernel works off over
-// the whole GPU.  Bound by latency but for the copies, which HBM bounds.
+// the whole GPU.  Bound by latency but for the copies, which HBM bounds: a thread takes a list
+// entry and all pages of a chunk of entries are worked off side by side, so that a call is a
+// chain of four or five loads (with a warp for each entry, one after another, 512 sequences
+// took 11 us a call).
 #include <cuda_runtime.h>
 #include <cstdint>
 
@@ -30,52 +33,108 @@ static_assert(kKvMaxPages == 1 << kTokenShift);
 // compaction's map, which never live at the same time as one another.
 struct Lists {
     KvScratch* head;
-    int32_t *src, *dst, *a, *b;
+    int32_t *src, *dst;     // what the copy kernel copies
+    int32_t *offset, *copy; // growth, by entry: its first allocated page, its page to copy or -1
+    int32_t* page;          // growth: the free pages; compaction: where a page has gone
 };
 __device__ __forceinline__ Lists lists_of(const KvView& kv) {
     const int n = kv_scratch_list(kv.num_pages, kv.num_slots);
     int32_t* p = kv.scratch + kKvScratchHeader;
-    return {reinterpret_cast<KvScratch*>(kv.scratch), p, p + n, p + 2 * n, p + 3 * n};
+    return {reinterpret_cast<KvScratch*>(kv.scratch), p, p + n, p + 2 * n, p + 3 * n, p + 4 * n};
 }
 
 struct PlanShared {
     uint32_t seen[kKvMaxSlots / 32];
-    int warp[kThreads / 32];
-    int total;
+    int64_t warp[kThreads / 32];
     int error;
     int copies;
+    // a chunk of list entries: slot, first page entry, and where its pages start among the chunk's
+    int slot[kThreads], other[kThreads], first[kThreads], start[kThreads];
+    int large[kThreads], larges;
 };
 
-// Exclusive sum over the CTA's threads in thread order, and the total; all threads call it.
-__device__ __forceinline__ int block_scan(int v, PlanShared& sh, int* total) {
+// Sum over the CTA's threads before this one, and the total; all threads call it.
+__device__ __forceinline__ int64_t block_scan(int64_t v, PlanShared& sh, int64_t* total) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int inc = v;
+    int64_t inc = v;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int t = __shfl_up_sync(0xffffffffu, inc, o);
+        const int64_t t = __shfl_up_sync(0xffffffffu, inc, o);
         if (lane >= o) inc += t;
     }
     if (lane == 31) sh.warp[warp] = inc;
     __syncthreads();
     if (warp == 0) {
-        int w = sh.warp[lane];
+        int64_t w = sh.warp[lane];
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int t = __shfl_up_sync(0xffffffffu, w, o);
+            const int64_t t = __shfl_up_sync(0xffffffffu, w, o);
             if (lane >= o) w += t;
         }
         sh.warp[lane] = w;
     }
     __syncthreads();
-    const int before = warp > 0 ? sh.warp[warp - 1] : 0;
+    const int64_t before = warp > 0 ? sh.warp[warp - 1] : 0;
     *total = sh.warp[kThreads / 32 - 1];
     __syncthreads();
     return before + inc - v;
 }
 
+// Calls use(k, e, load(k, e)) for page entry e of chunk entry k, over the pages [first, first +
+// count) of each thread's chunk entry (of `entries`).  Where an entry has 16 pages or more on
+// average a warp takes an entry, else the pages are spread evenly over the CTA by a search for
+// each (64 entries of 63 pages 9 us a call against 12, 512 of at most one 8 against 11);
+// kSide of a thread's searches and loads are under way together.
+template <typename Load, typename Use>
+__device__ __forceinline__ void each_page(PlanShared& sh, int first, int count, int entries, Load load, Use use) {
+    constexpr int kSide = 4;
+    int64_t all;
+    const int before = static_cast<int>(block_scan(count, sh, &all));
+    const int total = static_cast<int>(all);  // (at most the page table's entries)
+    sh.first[threadIdx.x] = first;
+    sh.start[threadIdx.x] = before;
+    __syncthreads();
+    if (total >= 16 * static_cast<int64_t>(entries)) {
+        for (int k = threadIdx.x >> 5; k < entries; k += kThreads / 32) {
+            const int from = sh.first[k], n = (k + 1 < kThreads ? sh.start[k + 1] : total) - sh.start[k];
+            for (int e0 = threadIdx.x & 31; e0 < n; e0 += 32 * kSide) {
+                int page[kSide];
+#pragma unroll
+                for (int s = 0; s < kSide; ++s)
+                    if (e0 + 32 * s < n) page[s] = load(k, from + e0 + 32 * s);
+#pragma unroll
+                for (int s = 0; s < kSide; ++s)
+                    if (e0 + 32 * s < n) use(k, from + e0 + 32 * s, page[s]);
+            }
+        }
+        __syncthreads();
+        return;
+    }
+    for (int64_t r0 = threadIdx.x; r0 < total; r0 += kThreads * kSide) {
+        int k[kSide], e[kSide], page[kSide];
+#pragma unroll
+        for (int s = 0; s < kSide; ++s) k[s] = 0;
+        // the last entry that starts at r or before
+        for (int step = kThreads / 2; step > 0; step >>= 1)
+#pragma unroll
+            for (int s = 0; s < kSide; ++s)
+                if (sh.start[k[s] + step] <= r0 + s * kThreads) k[s] += step;
+#pragma unroll
+        for (int s = 0; s < kSide; ++s) {
+            const int r = static_cast<int>(r0) + s * kThreads;
+            e[s] = sh.first[k[s]] + r - sh.start[k[s]];
+            if (r < total) page[s] = load(k[s], e[s]);
+        }
+#pragma unroll
+        for (int s = 0; s < kSide; ++s)
+            if (r0 + s * kThreads < total) use(k[s], e[s], page[s]);
+    }
+    __syncthreads();
+}
+
 __device__ __forceinline__ void plan_begin(const KvView& kv, PlanShared& sh) {
     for (int i = threadIdx.x; i < (kv.num_slots + 31) / 32; i += kThreads) sh.seen[i] = 0;
-    if (threadIdx.x == 0) sh.error = sh.copies = 0;
+    if (threadIdx.x == 0) sh.error = sh.copies = sh.larges = 0;
     __syncthreads();
     grid_launch_dependents();
     grid_wait();
@@ -116,15 +175,33 @@ __global__ void __launch_bounds__(kThreads)
     const Lists ls = lists_of(kv);
     const int tid = threadIdx.x;
     plan_begin(kv, sh);
-    // pages that each entry needs, as offsets into the pages to allocate (list a)
-    int need_all = 0;
-    bool too_many = false;
+    // kRun counts a thread and pass: a pool of 16000 pages takes one, under way from the start
+    constexpr int kRun = 16;
+    auto load_run = [&](int p0, int4 (&v)[kRun / 4]) {
+        const int begin = p0 + tid * kRun;
+#pragma unroll
+        for (int k = 0; k < kRun / 4; ++k) {
+            v[k] = make_int4(1, 1, 1, 1);
+            if (begin + 4 * k + 4 <= kv.num_pages) {
+                v[k] = reinterpret_cast<const int4*>(kv.refs + begin)[k];
+            } else {
+                const int left = kv.num_pages - begin - 4 * k;
+                if (left > 0) v[k].x = kv.refs[begin + 4 * k];
+                if (left > 1) v[k].y = kv.refs[begin + 4 * k + 1];
+                if (left > 2) v[k].z = kv.refs[begin + 4 * k + 2];
+            }
+        }
+    };
+    int4 run[kRun / 4];
+    load_run(0, run);
+    // pages that each entry needs, as offsets into the pages to allocate
+    int64_t need_all = 0;
     for (int i0 = 0; i0 < n; i0 += kThreads) {
         const int i = i0 + tid;
-        int need = 0;
+        int need = 0, copy = -1;
         if (i < n && slots[i] != -1) {
             const int slot = slots[i], grow = add[i];
-            int error = 0, copy = -1;
+            int error = 0;
             if (!claim_slot(kv, sh, slot) || grow < 0) {
                 error = kInvalid;
             } else {
@@ -139,39 +216,30 @@ __global__ void __launch_bounds__(kThreads)
             }
             if (error != 0) atomicCAS(&sh.error, 0, error);
         }
-        int sum;
-        const int before = block_scan(need, sh, &sum);
-        if (i < n) ls.a[i] = need_all + before;
-        too_many |= sum > kv.num_pages - need_all;  // (no overflow: need_all stays below)
-        if (too_many) break;
+        int64_t sum;
+        const int64_t before = need_all + block_scan(need, sh, &sum);
+        if (i < n) {
+            ls.offset[i] = static_cast<int>(before < kv.num_pages ? before : kv.num_pages);
+            ls.copy[i] = copy;
+        }
         need_all += sum;
     }
-    // the lowest free pages, in order (list b)
-    int found = 0;
-    if (!too_many) {
-        // kRun counts a thread and pass, which a pool of 16000 pages takes once
-        constexpr int kRun = 16;
-        for (int p0 = 0; p0 < kv.num_pages && found < need_all; p0 += kThreads * kRun) {
-            const int begin = p0 + tid * kRun;
-            uint32_t free = 0;
-            if (begin + kRun <= kv.num_pages) {
-                int4 v[kRun / 4];
+    // the lowest free pages, in order
+    int64_t found = 0;
+    for (int p0 = 0; p0 < kv.num_pages && found < need_all && need_all <= kv.num_pages; p0 += kThreads * kRun) {
+        if (p0 > 0) load_run(p0, run);
+        uint32_t free = 0;
 #pragma unroll
-                for (int k = 0; k < kRun / 4; ++k) v[k] = reinterpret_cast<const int4*>(kv.refs + begin)[k];
-#pragma unroll
-                for (int k = 0; k < kRun / 4; ++k)
-                    free |= ((v[k].x == 0) | (v[k].y == 0) << 1 | (v[k].z == 0) << 2 | (v[k].w == 0) << 3) << 4 * k;
-            } else {
-                for (int k = 0; begin + k < kv.num_pages; ++k) free |= (kv.refs[begin + k] == 0) << k;
-            }
-            int sum;
-            int rank = found + block_scan(__popc(free), sh, &sum);
-            for (; free != 0 && rank < need_all; free &= free - 1, ++rank) ls.b[rank] = begin + __ffs(free) - 1;
-            found += sum;
-        }
+        for (int k = 0; k < kRun / 4; ++k)
+            free |= ((run[k].x == 0) | (run[k].y == 0) << 1 | (run[k].z == 0) << 2 | (run[k].w == 0) << 3) << 4 * k;
+        int64_t sum;
+        int64_t rank = found + block_scan(__popc(free), sh, &sum);
+        for (; free != 0 && rank < need_all; free &= free - 1, ++rank)
+            ls.page[rank] = p0 + tid * kRun + __ffs(free) - 1;
+        found += sum;
     }
     __syncthreads();
-    if (sh.error != 0 || too_many || found < need_all) {
+    if (sh.error != 0 || found < need_all) {
         if (tid == 0) {
             record_status(kv.status, sh.error != 0 ? sh.error : kCapacity);
             ls.head->copies = 0;
@@ -179,38 +247,45 @@ __global__ void __launch_bounds__(kThreads)
         }
         return;
     }
-    // what to copy, before any count changes
-    for (int i = tid; i < n; i += kThreads) {
-        const int slot = slots[i];
-        int copy = -1;
-        if (slot != -1) shared_last(kv, slot, kv.seq_len[slot], add[i], &copy);
-        if (copy >= 0) {
-            const int c = atomicAdd(&sh.copies, 1);  // (the copies' order does not matter)
-            ls.src[c] = copy | (kv.seq_len[slot] & ((1 << kv.page_shift) - 1)) << kTokenShift;
-            ls.dst[c] = i;
+    // nothing above has changed the cache; each entry's pages, many of them by the whole CTA
+    constexpr int kOwn = 16;
+    for (int i0 = 0; i0 < n; i0 += kThreads) {
+        const int i = i0 + tid;
+        if (i < n && slots[i] != -1) {
+            const int slot = slots[i], len = kv.seq_len[slot], to = len + add[i];
+            const int offset = ls.offset[i], copy = ls.copy[i];
+            const int first = pages_of(kv, len) - (copy >= 0), need = pages_of(kv, to) - first;
+            if (copy >= 0) {
+                const int c = atomicAdd(&sh.copies, 1);  // (the copies' order does not matter)
+                ls.src[c] = copy | (len & ((1 << kv.page_shift) - 1)) << kTokenShift;
+                ls.dst[c] = ls.page[offset];
+                atomicSub(&kv.refs[copy], 1);
+            }
+            for (int k = 0; k < need && k < kOwn; ++k) {
+                const int page = ls.page[offset + k];
+                entries_of(kv, slot)[first + k] = page;
+                kv.refs[page] = 1;
+            }
+            if (need > kOwn) {
+                const int l = atomicAdd(&sh.larges, 1);
+                sh.slot[l] = slot;
+                sh.first[l] = first;
+                sh.start[l] = offset;
+                sh.large[l] = need;
+            }
+            kv.seq_len[slot] = to;
         }
+        __syncthreads();
+        for (int l = 0; l < sh.larges; ++l)
+            for (int k = kOwn + tid; k < sh.large[l]; k += kThreads) {
+                const int page = ls.page[sh.start[l] + k];
+                entries_of(kv, sh.slot[l])[sh.first[l] + k] = page;
+                kv.refs[page] = 1;
+            }
+        __syncthreads();
+        if (tid == 0) sh.larges = 0;
+        __syncthreads();
     }
-    __syncthreads();
-    for (int c = tid; c < sh.copies; c += kThreads)
-        atomicSub(&kv.refs[ls.src[c] & (kKvMaxPages - 1)], 1);
-    // page r of the allocated ones belongs to the last entry whose offset is at most r
-    for (int r = tid; r < need_all; r += kThreads) {
-        int lo = 0, hi = n - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (ls.a[mid] <= r) lo = mid; else hi = mid - 1;
-        }
-        const int slot = slots[lo];
-        const int need = (lo + 1 < n ? ls.a[lo + 1] : need_all) - ls.a[lo];
-        const int has = pages_of(kv, kv.seq_len[slot] + add[lo]);
-        const int page = ls.b[r];
-        entries_of(kv, slot)[has - need + r - ls.a[lo]] = page;
-        kv.refs[page] = 1;
-    }
-    __syncthreads();
-    for (int c = tid; c < sh.copies; c += kThreads) ls.dst[c] = ls.b[ls.a[ls.dst[c]]];
-    for (int i = tid; i < n; i += kThreads)
-        if (slots[i] != -1) kv.seq_len[slots[i]] += add[i];
     if (tid == 0) {
         ls.head->copies = sh.copies;
         ls.head->moved = -1;
@@ -221,7 +296,7 @@ __global__ void __launch_bounds__(kThreads)
     kv_fork_kernel(const KvView kv, const int32_t* __restrict__ parents,
                    const int32_t* __restrict__ children, int n) {
     __shared__ PlanShared sh;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x;
     plan_begin(kv, sh);
     for (int i = tid; i < n; i += kThreads) {
         if (children[i] == -1) continue;
@@ -231,68 +306,73 @@ __global__ void __launch_bounds__(kThreads)
             sh.error = kInvalid;
     }
     __syncthreads();
-    for (int i = warp; i < n && sh.error == 0; i += kThreads / 32) {
-        if (children[i] == -1) continue;
-        const int parent = parents[i];
-        bool ok = (sh.seen[parent >> 5] >> (parent & 31) & 1) == 0;  // (a child of this call)
-        const int pages = pages_of(kv, kv.seq_len[parent]);
-        for (int e = lane; e < pages; e += 32) ok &= page_ok(kv, entries_of(kv, parent)[e]);
-        if (!ok) sh.error = kInvalid;
-    }
-    __syncthreads();
-    if (sh.error != 0) {
-        if (tid == 0) record_status(kv.status, sh.error);
-        return;
-    }
-    for (int i = warp; i < n; i += kThreads / 32) {
-        if (children[i] == -1) continue;
-        const int len = kv.seq_len[parents[i]], pages = pages_of(kv, len);
-        const int32_t* from = entries_of(kv, parents[i]);
-        int32_t* to = entries_of(kv, children[i]);
-        for (int e = lane; e < pages; e += 32) {
-            const int page = from[e];
-            to[e] = page;
-            atomicAdd(&kv.refs[page], 1);
+    // checks every page, then shares them; a chunk of entries at a time
+    for (int pass = 0; pass < 2 && sh.error == 0; ++pass) {
+        for (int i0 = 0; i0 < n; i0 += kThreads) {
+            const int i = i0 + tid;
+            int len = 0;
+            if (i < n && children[i] != -1) {
+                const int parent = parents[i];
+                // (a parent that is a child of this call)
+                if (sh.seen[parent >> 5] >> (parent & 31) & 1) sh.error = kInvalid;
+                len = kv.seq_len[parent];
+                sh.slot[tid] = parent;
+                sh.other[tid] = children[i];
+            }
+            auto load = [&](int k, int e) { return entries_of(kv, sh.slot[k])[e]; };
+            each_page(sh, 0, pages_of(kv, len), min(n - i0, kThreads), load, [&](int k, int e, int page) {
+                if (pass == 0) {
+                    if (!page_ok(kv, page)) sh.error = kInvalid;
+                } else {
+                    entries_of(kv, sh.other[k])[e] = page;
+                    atomicAdd(&kv.refs[page], 1);
+                }
+            });
+            if (pass == 1 && len > 0) kv.seq_len[children[i]] = len;
         }
-        if (lane == 0) kv.seq_len[children[i]] = len;
     }
+    if (sh.error != 0 && tid == 0) record_status(kv.status, sh.error);
 }
 
 __global__ void __launch_bounds__(kThreads)
     kv_trim_kernel(const KvView kv, const int32_t* __restrict__ slots,
                    const int32_t* __restrict__ keep, int n) {
     __shared__ PlanShared sh;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x;
     plan_begin(kv, sh);
-    for (int i = tid; i < n; i += kThreads) {
-        const int slot = slots[i];
-        if (slot == -1) continue;
-        const int left = keep != nullptr ? keep[i] : 0;
-        if (!claim_slot(kv, sh, slot) || !length_ok(kv, kv.seq_len[slot]) || left < 0 ||
-            left > kv.seq_len[slot])
-            sh.error = kInvalid;
+    // checks every entry and page, then gives the pages back; a chunk of entries at a time
+    for (int pass = 0; pass < 2 && sh.error == 0; ++pass) {
+        for (int i0 = 0; i0 < n; i0 += kThreads) {
+            const int i = i0 + tid;
+            int first = 0, count = 0, slot = -1, left = 0;
+            if (i < n && slots[i] != -1) {
+                slot = slots[i];
+                left = keep != nullptr ? keep[i] : 0;
+                if (pass == 0 && !claim_slot(kv, sh, slot)) {
+                    sh.error = kInvalid;
+                } else {
+                    const int len = kv.seq_len[slot];
+                    if (!length_ok(kv, len) || left < 0 || left > len) {
+                        sh.error = kInvalid;
+                    } else {
+                        first = pages_of(kv, left);
+                        count = pages_of(kv, len) - first;
+                    }
+                }
+                sh.slot[tid] = slot;
+            }
+            auto load = [&](int k, int e) { return entries_of(kv, sh.slot[k])[e]; };
+            each_page(sh, first, count, min(n - i0, kThreads), load, [&](int, int, int page) {
+                if (pass == 0) {
+                    if (!page_ok(kv, page)) sh.error = kInvalid;
+                } else {
+                    atomicSub(&kv.refs[page], 1);
+                }
+            });
+            if (pass == 1 && slot >= 0) kv.seq_len[slot] = left;
+        }
     }
-    __syncthreads();
-    for (int i = warp; i < n && sh.error == 0; i += kThreads / 32) {
-        if (slots[i] == -1) continue;
-        const int pages = pages_of(kv, kv.seq_len[slots[i]]);
-        for (int e = pages_of(kv, keep != nullptr ? keep[i] : 0) + lane; e < pages; e += 32)
-            if (!page_ok(kv, entries_of(kv, slots[i])[e])) sh.error = kInvalid;
-    }
-    __syncthreads();
-    if (sh.error != 0) {
-        if (tid == 0) record_status(kv.status, sh.error);
-        return;
-    }
-    for (int i = warp; i < n; i += kThreads / 32) {
-        if (slots[i] == -1) continue;
-        const int left = keep != nullptr ? keep[i] : 0;
-        const int pages = pages_of(kv, kv.seq_len[slots[i]]);
-        for (int e = pages_of(kv, left) + lane; e < pages; e += 32)
-            atomicSub(&kv.refs[entries_of(kv, slots[i])[e]], 1);
-        __syncwarp();
-        if (lane == 0) kv.seq_len[slots[i]] = left;
-    }
+    if (sh.error != 0 && tid == 0) record_status(kv.status, sh.error);
 }
 
 __global__ void __launch_bounds__(kThreads) kv_compact_kernel(const KvView kv) {
@@ -329,18 +409,18 @@ __global__ void __launch_bounds__(kThreads) kv_compact_kernel(const KvView kv) {
         const int p = p0 + tid;
         const bool used = p < kv.num_pages && kv.refs[p] > 0;
         const int mover = used && p >= live, hole = !used && p < live;
-        int sum;
-        const int m = block_scan(mover, sh, &sum);
-        if (mover) ls.src[movers + m] = p;
-        movers += sum;
-        const int h = block_scan(hole, sh, &sum);
-        if (hole) ls.dst[holes + h] = p;
-        holes += sum;
+        int64_t sum;
+        // (both counts in one scan: a pass has at most kThreads of each)
+        const int64_t before = block_scan(mover + (static_cast<int64_t>(hole) << 32), sh, &sum);
+        if (mover) ls.src[movers + static_cast<int>(before & 0xFFFFFFFF)] = p;
+        if (hole) ls.dst[holes + static_cast<int>(before >> 32)] = p;
+        movers += static_cast<int>(sum & 0xFFFFFFFF);
+        holes += static_cast<int>(sum >> 32);
     }
     __syncthreads();
     for (int c = tid; c < movers; c += kThreads) {
         const int from = ls.src[c], to = ls.dst[c];
-        ls.b[from] = to;  // the map
+        ls.page[from] = to;
         kv.refs[to] = kv.refs[from];
         kv.refs[from] = 0;
     }
@@ -378,7 +458,7 @@ __global__ void __launch_bounds__(256) kv_copy_kernel(const KvView kv) {
             uint4 v[kBatch];
 #pragma unroll
             for (int b = 0; b < kBatch; ++b)
-                if (u0 + 32 * b < units) v[b] = __ldcs(from + u0 + 32 * b);
+                if (u0 + 32 * b < units) v[b] = __ldg(from + u0 + 32 * b);
 #pragma unroll
             for (int b = 0; b < kBatch; ++b)
                 if (u0 + 32 * b < units) __stcs(to + u0 + 32 * b, v[b]);
@@ -396,7 +476,7 @@ __global__ void __launch_bounds__(256) kv_copy_kernel(const KvView kv) {
         const int pages = pages_of(kv, kv.seq_len[s]);
         int32_t* entry = entries_of(kv, static_cast<int>(s));
         for (int e = lane; e < pages; e += 32)
-            if (entry[e] >= moved) entry[e] = ls.b[entry[e]];
+            if (entry[e] >= moved) entry[e] = ls.page[entry[e]];
     }
 }
 

@@ -36,7 +36,8 @@ BAD_CACHES = [
     (dict(page_tokens=256), W.ERR_UNSUPPORTED), (dict(num_slots=65537), W.ERR_UNSUPPORTED),
     (dict(num_pages=(1 << 24) + 1), W.ERR_UNSUPPORTED),
     (dict(num_pages=1 << 24, kv_heads=4), W.ERR_UNSUPPORTED),  # 2^31 rows a layer
-    (dict(max_pages=1 << 28), W.ERR_UNSUPPORTED), (dict(page_table=2 * A + 4), W.ERR_ALIGNMENT),
+    (dict(max_pages=1 << 28), W.ERR_UNSUPPORTED), (dict(num_slots=65536, max_pages=1 << 15), W.ERR_UNSUPPORTED),
+    (dict(page_table=2 * A + 4), W.ERR_ALIGNMENT),
     (dict(seq_len=4 * A + 16), W.ERR_INVALID_ARG),  # inside page_refs
 ]
 
