@@ -230,16 +230,14 @@ __device__ __forceinline__ uint32_t tile_byte(int row, int unit) {
 // half-filled last tile, its end): 64 rows of 200 to 1024 tokens, 96 heads, with 2 / 4 / 6 / 9 of them
 // 292 / 288 / 287 / 290 us in bf16, in e4m3 193 / 185 / 181 / 173.
 __host__ __device__ constexpr int item_weight(bool e4m3) { return e4m3 ? 9 : 5; }
+__device__ __forceinline__ bool length_ok(const DecodeArgs& a, int len) {
+    return len >= 0 && len <= static_cast<int64_t>(a.kv.max_pages) << a.kv.page_shift;
+}
 template <bool E4M3>
-__device__ __forceinline__ Row row_of(const DecodeArgs& a, int i, bool* bad) {
+__device__ __forceinline__ Row row_from(const DecodeArgs& a, int slot, int len) {
     constexpr int kGroups = E4M3 ? 8 : 4;  // of a tile
-    Row r{a.p.slots[i], 0, 0, 0, 0, 0, 0};
-    *bad = r.slot < -1 || r.slot >= a.kv.num_slots;
-    if (*bad || r.slot < 0) return r;
-    const int len = a.kv.seq_len[r.slot];
-    *bad = len < 0 || len > static_cast<int64_t>(a.kv.max_pages) << a.kv.page_shift;
-    if (*bad || len == 0) return r;
-    r.len = len;
+    Row r{slot, len, 0, 0, 0, 0, 0};
+    if (len == 0) return r;
     r.low = len > a.window ? len - a.window : 0;
     const int begin = r.low / 16, end = (len - 1) / 16 + 1;
     r.first = begin / kGroups;
@@ -247,6 +245,15 @@ __device__ __forceinline__ Row row_of(const DecodeArgs& a, int i, bool* bad) {
     r.skip = begin - r.first * kGroups;
     r.weight = end - begin + item_weight(E4M3);
     return r;
+}
+template <bool E4M3>
+__device__ __forceinline__ Row row_of(const DecodeArgs& a, int i, bool* bad) {
+    const int slot = a.p.slots[i];
+    *bad = slot < -1 || slot >= a.kv.num_slots;
+    if (*bad || slot < 0) return Row{};
+    const int len = a.kv.seq_len[slot];
+    *bad = !length_ok(a, len);
+    return *bad ? Row{} : row_from<E4M3>(a, slot, len);
 }
 // Where tile t of an item starts in its weight.
 template <bool E4M3>
@@ -283,15 +290,6 @@ __device__ __forceinline__ int parts_of(int64_t begin, int64_t end, int64_t weig
     return end - begin > 2 * Snap<E4M3>::kSnap && hi >= lo ? static_cast<int>(hi - lo) + 2 : 1;
 }
 
-// The next row with keys; without tiles if there is none.
-template <bool E4M3>
-__device__ __forceinline__ Row next_row(const DecodeArgs& a, int* row) {
-    Row r{};
-    bool bad;
-    while (r.tiles == 0 && *row + 1 < a.p.n) r = row_of<E4M3>(a, ++*row, &bad);
-    return r;
-}
-
 template <bool E4M3>
 __device__ void produce(const DecodeArgs& a, const CUtensorMap* maps, Shared& sh, uint32_t stages,
                         uint32_t queries, int64_t weight, int64_t ctas, int64_t w0, int64_t w1) {
@@ -312,23 +310,56 @@ __device__ void produce(const DecodeArgs& a, const CUtensorMap* maps, Shared& sh
     const int rest = static_cast<int>((w0 - base) - static_cast<int64_t>(item) * r.weight);
     while (tile < r.tiles && tile_start<E4M3>(r, tile) < rest) tile = max(tile + 1, (rest + r.skip) / (kTile / 16));
     bool begun = false, more = true;
-    int ids = 0, ids_from = -1, ids_row = -1;  // 32 entries of the row's page list, a lane each
+    // Page list entries, a lane each: the row's first 32, the 32 that the tiles are in, and the
+    // 32 after them; and the same of the rows that follow.  All are loaded ahead of their use:
+    // a stop for each would be a microsecond, of the 1.5 that a tile takes.
+    auto load_ids = [&](const Row& of, int from) {
+        const int e = from + lane;
+        return e <= (of.len - 1) >> kv.page_shift
+                   ? __ldcg(kv.table + static_cast<int64_t>(of.slot) * kv.max_pages + e) : 0;
+    };
+    auto first_entry = [&](const Row& of) { return of.first * kTile >> kv.page_shift; };
+    constexpr int kUnknown = -2, kNone = -1;
+    int next_index = kUnknown, next_ids = 0, rows_from = kNone, slot_of = -1, len_of = 0;
+    Row next{};
+    auto find_next = [&]() {  // the next row with keys
+        next_index = kNone;
+        for (int from = row + 1; from < a.p.n && next_index == kNone; from = rows_from + 32) {
+            if (rows_from == kNone || from >= rows_from + 32) {
+                rows_from = from;
+                slot_of = from + lane < a.p.n ? __ldcg(a.p.slots + from + lane) : -1;
+                len_of = slot_of >= 0 && slot_of < kv.num_slots ? __ldcg(kv.seq_len + slot_of) : 0;
+                if (!length_ok(a, len_of)) len_of = 0;
+            }
+            const uint32_t have = __ballot_sync(0xffffffffu, len_of > 0 && rows_from + lane >= from);
+            if (have == 0) continue;
+            const int l = __ffs(have) - 1;
+            next_index = rows_from + l;
+            next = row_from<E4M3>(a, __shfl_sync(0xffffffffu, slot_of, l), __shfl_sync(0xffffffffu, len_of, l));
+            next_ids = load_ids(next, first_entry(next));
+        }
+    };
     int slot = 0;             // of the item's queries
     int since[2] = {0, 0};    // units since the one that read each query slot; 0: none
     int st = 0;
     uint32_t phase = 0;       // of the stage's barriers
     int64_t issued = 0;
     if (item == items) {  // (a bound moved to the end of the row)
+        find_next();
         item = tile = 0;
         base += static_cast<int64_t>(items) * r.weight;
-        r = next_row<E4M3>(a, &row);
-        more = r.tiles > 0;
+        row = next_index;
+        r = next;
+        more = next_index != kNone;
+        next_index = kUnknown;
     }
     if (!more || tile >= r.tiles) {  // (only if the lengths changed during the call)
         sh.abort = 1;
         record_status(kv.status, kInvalid);
         return;
     }
+    int ids_from = ((r.first + tile) * kTile) >> kv.page_shift;
+    int ids = load_ids(r, ids_from), ids_first = load_ids(r, first_entry(r)), ids_after = load_ids(r, ids_from + 32);
     for (; more; ++issued) {
         const bool first = !begun || tile == 0;
         begun = true;
@@ -348,15 +379,11 @@ __device__ void produce(const DecodeArgs& a, const CUtensorMap* maps, Shared& sh
             since[slot] = 0;
         }
         const int key0 = (r.first + tile) * kTile;
-        // page list entries of the tile; a page's boxes never cross it
-        const int e0 = key0 >> kv.page_shift;
-        const int e1 = (min(key0 + kTile, r.len) - 1) >> kv.page_shift;
-        if (ids_row != row || e0 < ids_from || e1 >= ids_from + 32) {
-            ids_row = row;
-            ids_from = e0;
-            const int e = e0 + lane;
-            ids = e <= (r.len - 1) >> kv.page_shift
-                      ? __ldg(kv.table + static_cast<int64_t>(r.slot) * kv.max_pages + e) : 0;
+        // (32 entries are whole tiles, and a page's boxes never cross it)
+        if (key0 >> kv.page_shift >= ids_from + 32) {
+            ids = ids_after;
+            ids_from += 32;
+            ids_after = load_ids(r, ids_from + 32);
         }
         const int head = item / a.cols.blocks, block = item - head * a.cols.blocks;
         // Boxes of a page, or of 16 rows at the ends of what the row sees, where a page's would
@@ -445,16 +472,29 @@ __device__ void produce(const DecodeArgs& a, const CUtensorMap* maps, Shared& sh
             tile = 0;
             slot ^= 1;
             if (++item == items && more) {
-                item = 0;
-                base += static_cast<int64_t>(items) * r.weight;
-                r = next_row<E4M3>(a, &row);
-                if (r.tiles == 0) {  // (only if the lengths changed during the call)
+                if (next_index == kUnknown) find_next();
+                if (next_index == kNone) {  // (only if the lengths changed during the call)
                     sh.abort = 1;
                     record_status(kv.status, kInvalid);
-                    more = false;
+                    ++issued;
+                    break;
                 }
+                item = 0;
+                base += static_cast<int64_t>(items) * r.weight;
+                row = next_index;
+                r = next;
+                next_index = kUnknown;
+                ids_first = next_ids;
+                ids_from = kNone;
+            }
+            if (ids_from != first_entry(r)) {
+                ids = ids_first;
+                ids_from = first_entry(r);
+                ids_after = load_ids(r, ids_from + 32);
             }
         }
+        // (once the stages are all under way)
+        if (next_index == kUnknown && issued + 1 >= kStages) find_next();
     }
     // the copies in flight, before the CTA may end (the consumers may have given up)
     for (int64_t i = issued > kStages ? issued - kStages : 0; i < issued; ++i)
@@ -494,94 +534,99 @@ __device__ __forceinline__ float* parts_in(const DecodeArgs& a) {
     return reinterpret_cast<float*>(static_cast<uint8_t*>(a.p.workspace) + counter_bytes(gridDim.x));
 }
 
-// Adds up an item's parts in their order: part 0 is its CTA's last item, the others their
-// CTAs' first.  Sixteen lanes take a column, eight outputs each; a lane has a part's
-// statistics, and the outputs of kBatch parts are under way together.  (A thread per output that walked
-// columns and parts took 35 of 72 us with 13 parts of 8 columns, a warp per column with the
-// weights in one chain 20.)
+// The items that this CTA adds up, after its last unit, by all warps that computed.  Part 0 of
+// an item is its CTA's last item, the others their CTAs' first, and they are added in this
+// order.  Sixteen lanes take a column, eight outputs each; a lane has a part's statistics, and the
+// outputs of kBatch parts are under way together.  One compact copy of the code: every CTA runs
+// it once at most, and fetching it is a good part of its time (13 parts of 8 columns: a thread per output
+// that walked columns and parts 35 us, a warp per column 20, this inlined and with 16 parts 6).
 template <bool E4M3>
-__device__ void join_parts(const DecodeArgs& a, const Pending& p, int group, int groups, int lane) {
+__device__ __noinline__ void join_pending(const float* parts, uint16_t* out, int H, int group, int block,
+                                          const Pending* pending, int* status, int mine, int groups) {
     constexpr int kBatch = 8;
-    const int cols = columns_in(a, p.block), max_cols = used_columns(a.cols.group), n = p.parts;
+    const int lane = threadIdx.x & 31, l16 = lane & 15, max_cols = used_columns(group);
     const int64_t stride = part_floats(max_cols);
-    const float* const parts = parts_in(a) + 2 * p.first_cta * stride;
-    auto part = [&](int k) { return parts + (2 * static_cast<int64_t>(k) + (k == 0)) * stride; };
-    const int l16 = lane & 15;
-    for (int col0 = 0; col0 < cols; col0 += groups) {
-        const bool mine = col0 + group < cols;
-        const int col = mine ? col0 + group : 0;  // (the other half of the warp may have one)
+    int cols[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) cols[i] = pending[i].join ? min(block, group - pending[i].block * block) : 0;
+#pragma unroll 1
+    for (int i0 = 0; i0 < cols[0] + cols[1]; i0 += groups) {
+        // (a warp's halves may have columns of two items, or one of them none)
+        const int i = i0 + mine;
+        const Pending& p = pending[i >= cols[0]];
+        const int col = i < cols[0] ? i : i - cols[0], n = i < cols[0] + cols[1] ? p.parts : 0;
+        const int longest = max(n, __shfl_xor_sync(0xffffffffu, n, 16));
+        const float* const first = parts + (2 * p.first_cta + 1) * stride;  // then every second, from one before
+        auto part = [&](int k) { return k == 0 ? first : first + (2 * k - 1) * stride; };
         auto stats = [&](int k) {
             return k < n ? __ldcg(reinterpret_cast<const float4*>(part(k) + max_cols * kKvHeadDim) + col)
                          : make_float4(0.0f, -INFINITY, -INFINITY, 0.0f);
         };
         float m = -INFINITY, top = -INFINITY, l = 0.0f;
-        float4 mine16 = stats(l16);
-        for (int k0 = 0; k0 < n; k0 += 16) {
-            const float4 s = k0 == 0 ? mine16 : stats(k0 + l16);
-            m = fmaxf(m, s.y);
-            top = fmaxf(top, s.z);
-        }
-        float4 v[kBatch][2];
-        auto load = [&](int k0) {
-#pragma unroll
-            for (int i = 0; i < kBatch; ++i)
-                if (k0 + i < n) {
-                    const float4* from = reinterpret_cast<const float4*>(part(k0 + i) + col * kKvHeadDim) + 2 * l16;
-                    v[i][0] = __ldcg(from);
-                    v[i][1] = __ldcg(from + 1);
-                }
-        };
-        load(0);
-#pragma unroll
-        for (int o = 8; o > 0; o >>= 1) {
-            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        }
+        float4 s = stats(l16);
         bool bad = false;
-        float sum[8] = {};
-        for (int k0 = 0; k0 < n; k0 += 16) {
-            const float4 s = k0 == 0 ? mine16 : stats(k0 + l16);
-            bad |= s.x < 0.0f;
-            l += s.x * ex2(s.y - finite(m));
-            const float f = ex2(s.z - finite(top));
-            for (int h = 0; h < 16 && k0 + h < n; h += kBatch) {
-                if (k0 + h > 0) load(k0 + h);
+        float sum[8] = {}, f = 0.0f;
+#pragma unroll 1
+        for (int k0 = 0; k0 < longest; k0 += kBatch) {
+            float4 v[kBatch][2];
 #pragma unroll
-                for (int i = 0; i < kBatch; ++i) {
-                    const float w = __shfl_sync(0xffffffffu, f, (lane & 16) | (h + i));
-                    if (k0 + h + i < n) {
-                        sum[0] += w * v[i][0].x;
-                        sum[1] += w * v[i][0].y;
-                        sum[2] += w * v[i][0].z;
-                        sum[3] += w * v[i][0].w;
-                        sum[4] += w * v[i][1].x;
-                        sum[5] += w * v[i][1].y;
-                        sum[6] += w * v[i][1].z;
-                        sum[7] += w * v[i][1].w;
-                    }
+            for (int b = 0; b < kBatch; ++b)
+                if (k0 + b < n) {
+                    const float4* from = reinterpret_cast<const float4*>(part(k0 + b) + col * kKvHeadDim) + 2 * l16;
+                    v[b][0] = __ldcg(from);
+                    v[b][1] = __ldcg(from + 1);
+                }
+            if (k0 == 0) {  // (with the first outputs on their way)
+                m = s.y;
+                top = s.z;
+#pragma unroll 1
+                for (int k = 16; k < longest; k += 16) {
+                    const float4 t = stats(k + l16);
+                    m = fmaxf(m, t.y);
+                    top = fmaxf(top, t.z);
+                }
+#pragma unroll
+                for (int o = 8; o > 0; o >>= 1) {
+                    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                }
+            }
+            if (k0 % 16 == 0) {
+                if (k0 > 0) s = stats(k0 + l16);
+                bad |= s.x < 0.0f;
+                l += s.x * ex2(s.y - finite(m));
+                f = ex2(s.z - finite(top));
+            }
+#pragma unroll
+            for (int b = 0; b < kBatch; ++b) {
+                const float w = __shfl_sync(0xffffffffu, f, (lane & 16) | ((k0 + b) & 15));
+                if (k0 + b < n) {
+                    sum[0] += w * v[b][0].x;
+                    sum[1] += w * v[b][0].y;
+                    sum[2] += w * v[b][0].z;
+                    sum[3] += w * v[b][0].w;
+                    sum[4] += w * v[b][1].x;
+                    sum[5] += w * v[b][1].y;
+                    sum[6] += w * v[b][1].z;
+                    sum[7] += w * v[b][1].w;
                 }
             }
         }
 #pragma unroll
         for (int o = 8; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-        bad = __any_sync(0xffffffffu, bad);  // (of the item: its columns see the same pages)
-        if (!mine) continue;
-        const float f = output_scale<E4M3>(l, m, top);
-        uint4 o = make_uint4(bf16_pair(sum[0] * f, sum[1] * f), bf16_pair(sum[2] * f, sum[3] * f),
-                             bf16_pair(sum[4] * f, sum[5] * f), bf16_pair(sum[6] * f, sum[7] * f));
+        bad = (__ballot_sync(0xffffffffu, bad) >> (lane & 16) & 0xFFFFu) != 0;
+        if (n == 0) continue;
+        const float scale = output_scale<E4M3>(l, m, top);
+        uint4 o = make_uint4(bf16_pair(sum[0] * scale, sum[1] * scale), bf16_pair(sum[2] * scale, sum[3] * scale),
+                             bf16_pair(sum[4] * scale, sum[5] * scale), bf16_pair(sum[6] * scale, sum[7] * scale));
         if (bad) {
             o = make_uint4(0, 0, 0, 0);
-            if (l16 == 0) record_status(a.kv.status, kInvalid);
+            if (l16 == 0) record_status(status, kInvalid);
         }
-        reinterpret_cast<uint4*>(output_of(a, p.row, p.head, p.block) + col * kKvHeadDim)[l16] = o;
+        reinterpret_cast<uint4*>(
+            out + (static_cast<int64_t>(p.row) * H + static_cast<int64_t>(p.head) * group + p.block * block + col) *
+                      kKvHeadDim)[l16] = o;
     }
-}
-
-// After the CTA's last unit, by all warps that computed: the items that this CTA adds up.
-template <bool E4M3>
-__device__ void join_pending(const DecodeArgs& a, Shared& sh, int w, int lane) {
-    for (int i = 0; i < 2; ++i)
-        if (sh.pending[i].join) join_parts<E4M3>(a, sh.pending[i], 2 * w + (lane >> 4), 2 * (kWarps + 1), lane);
 }
 
 // The finisher: follows the stages, and at an item's end adds up what the warps left there.
@@ -682,7 +727,9 @@ __device__ void finish(const DecodeArgs& a, Shared& sh, const uint8_t* stage_mem
     }
     __syncwarp();
     if (lane == 0) mbar_arrive(smem_u32(&sh.joined));
-    join_pending<E4M3>(a, sh, kWarps, lane);
+    if (sh.pending[0].join || sh.pending[1].join)
+        join_pending<E4M3>(parts_in(a), a.p.out, a.p.H, a.cols.group, a.cols.block, sh.pending, kv.status,
+                           2 * kWarps + (lane >> 4), 2 * (kWarps + 1));
 }
 
 // The tile's ends: the new token's row is put in place, as the cache holds it, and stored, and
@@ -1069,7 +1116,9 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
         if (flags & kEnd) break;
     }
     if (!wait_warp(smem_u32(&sh.joined), 0, &sh.abort, kv.status, a.p.wait_ns)) return;
-    join_pending<E4M3>(a, sh, warp, lane);
+    if (sh.pending[0].join || sh.pending[1].join)
+        join_pending<E4M3>(parts_in(a), a.p.out, a.p.H, a.cols.group, a.cols.block, sh.pending, kv.status,
+                           2 * warp + (lane >> 4), 2 * (kWarps + 1));
 }
 
 template <bool E4M3, int NT, bool ONE>

@@ -169,8 +169,8 @@ __device__ __forceinline__ bool shared_last(const KvView& kv, int slot, int len,
 }
 
 __global__ void __launch_bounds__(kThreads)
-    kv_extend_kernel(const KvView kv, const int32_t* __restrict__ slots,
-                     const int32_t* __restrict__ add, int n) {
+    kv_extend_kernel(const KvView kv, const int32_t* slots,
+                     const int32_t* add, int n) {
     __shared__ PlanShared sh;
     const Lists ls = lists_of(kv);
     const int tid = threadIdx.x;
@@ -293,8 +293,8 @@ __global__ void __launch_bounds__(kThreads)
 }
 
 __global__ void __launch_bounds__(kThreads)
-    kv_fork_kernel(const KvView kv, const int32_t* __restrict__ parents,
-                   const int32_t* __restrict__ children, int n) {
+    kv_fork_kernel(const KvView kv, const int32_t* parents,
+                   const int32_t* children, int n) {
     __shared__ PlanShared sh;
     const int tid = threadIdx.x;
     plan_begin(kv, sh);
@@ -335,8 +335,8 @@ __global__ void __launch_bounds__(kThreads)
 }
 
 __global__ void __launch_bounds__(kThreads)
-    kv_trim_kernel(const KvView kv, const int32_t* __restrict__ slots,
-                   const int32_t* __restrict__ keep, int n) {
+    kv_trim_kernel(const KvView kv, const int32_t* slots,
+                   const int32_t* keep, int n) {
     __shared__ PlanShared sh;
     const int tid = threadIdx.x;
     plan_begin(kv, sh);
@@ -458,7 +458,7 @@ __global__ void __launch_bounds__(256) kv_copy_kernel(const KvView kv) {
             uint4 v[kBatch];
 #pragma unroll
             for (int b = 0; b < kBatch; ++b)
-                if (u0 + 32 * b < units) v[b] = __ldg(from + u0 + 32 * b);
+                if (u0 + 32 * b < units) v[b] = __ldcg(from + u0 + 32 * b);
 #pragma unroll
             for (int b = 0; b < kBatch; ++b)
                 if (u0 + 32 * b < units) __stcs(to + u0 + 32 * b, v[b]);
