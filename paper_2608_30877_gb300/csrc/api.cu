@@ -408,10 +408,17 @@ int library_state(LibraryState* out) {
     return W4A16_OK;
 }
 
-int encode_rows(CUtensorMap* map, CUtensorMapDataType dtype, const void* base, uint64_t inner,
-                uint64_t rows, uint64_t row_bytes, uint32_t box_inner, uint32_t box_rows) {
-    return encode_2d(map, dtype, base, inner, rows, row_bytes, box_inner, box_rows,
-                     CU_TENSOR_MAP_SWIZZLE_128B);
+int encode_3d(CUtensorMap* map, CUtensorMapDataType dtype, const void* base, const uint64_t dims[3],
+              const uint64_t strides[2], const uint32_t box[3]) {
+    const cuuint64_t d[3] = {dims[0], dims[1], dims[2]};
+    const cuuint64_t s[2] = {strides[0], strides[1]};
+    const cuuint32_t b[3] = {box[0], box[1], box[2]};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    const CUresult r = g_encode(map, dtype, 3, const_cast<void*>(base), d, s, b, estr,
+                                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? W4A16_OK : W4A16_ERR_CUDA;
 }
 
 }  // namespace w4a16

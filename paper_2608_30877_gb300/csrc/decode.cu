@@ -51,8 +51,9 @@ namespace {
 constexpr int kWarps = 4;                    // consumers
 constexpr int kThreads = (kWarps + 2) * 32;  // the producer before them, the finisher after
 constexpr int kStages = 3;
-constexpr int kHalfStage = 16384;            // a tile's keys, or its values
-constexpr int kStageBytes = 2 * kHalfStage;
+constexpr int kStageBytes = 32768;           // a tile's keys and values
+constexpr int kWarpBytes = kStageBytes / kWarps;
+constexpr int kValueOffset = 2048;           // from 16 keys' rows of 128 bytes to their values'
 constexpr int kMaxCols = 64;                 // query columns of an item
 constexpr int kQueryStride = 272;            // bytes between rows of q, on other banks
 constexpr int kCtasPerSm = 2;
@@ -131,7 +132,7 @@ struct Shared {
     int64_t warp_sum[kThreads / 32];
     int64_t bound[2];
     int64_t start_base;
-    int start_row;
+    int start_row, start_item, start_into;
     Row start;
     int empty_rows;
     int abort;
@@ -144,6 +145,7 @@ struct DecodeArgs {
     int window;
     int item_weight;  // groups of 16 keys that an item costs as much as, beside its own
     int snap;         // groups from an item's end within which no part begins
+    uint64_t grid_reciprocal;  // 2^64 / CTAs, rounded up
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -226,12 +228,27 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
         : "memory");
 }
 
-// Byte of 16-byte unit `unit` of a tile's row in the 128-byte swizzle; a bf16 row is two
-// halves of 128 bytes, a half tile of 64 rows apart.
+// A stage holds boxes of 16 tokens' keys and values, 128 bytes of each row: in bf16 a group of
+// 16 tokens is two boxes (the halves of its rows), in e4m3 one.  Byte of 16-byte unit `unit`
+// of a tile's key row, in the 128-byte swizzle.
 template <bool E4M3>
 __device__ __forceinline__ uint32_t tile_byte(int row, int unit) {
-    const uint32_t base = E4M3 ? 0 : static_cast<uint32_t>(unit >> 3) * 8192u;
-    return base + row * 128u + (((unit & 7) ^ (row & 7)) << 4);
+    const uint32_t box = E4M3 ? (row >> 4) * 4096u : (row >> 4) * 8192u + (unit >> 3) * 4096u;
+    return box + (row & 15) * 128u + (((unit & 7) ^ (row & 7)) << 4);
+}
+// One box; completion is signalled on `bar` as transaction bytes.
+__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, uint32_t bar, int32_t c0, int32_t row) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(row), "r"(0), "r"(bar)
+        : "memory");
+}
+// Quotient of numbers that are not negative: in 32 bits where they fit (a 64-bit division takes
+// 300 clocks, and a short row's call had eight of them in a row).
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+    if (((a | b) >> 32) == 0) return static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
+    return a / b;
 }
 
 __device__ __forceinline__ bool length_ok(const DecodeArgs& a, int len) {
@@ -269,39 +286,41 @@ __device__ __forceinline__ int tile_start(const Row& r, int t) {
 // down and, if that is at most `snap` groups from the start or the end of the item in which it
 // falls, moved there: a part costs more than so many groups.  `snap` is at least a tile and
 // an item's weight, and so are the bounds apart before they move; so each part of an item has a tile.
-// A bound within the items of a row, which start at `base`.
-__device__ __forceinline__ int64_t snapped(int64_t bound, int64_t base, int weight, int snap) {
-    const int into = static_cast<int>((bound - base) % weight);
-    return into <= snap ? bound - into : weight - into <= snap ? bound + (weight - into) : bound;
+// A bound `into` groups into an item, moved.
+__device__ __forceinline__ int snapped(int into, int weight, int snap) {
+    return into <= snap ? 0 : weight - into <= snap ? weight : into;
 }
 // The parts of an item [begin, end), and the CTA of the first if there are more.
 __device__ __forceinline__ int parts_of(int64_t begin, int64_t end, int64_t weight, int64_t ctas, int snap,
                                         int* first_cta) {
     // the bounds in (begin + snap, end - snap)
-    const int64_t lo = ((begin + snap + 1) * ctas + weight - 1) / weight;
-    const int64_t hi = ((end - snap) * ctas - 1) / weight;
+    if (end - begin <= 2 * snap) {
+        *first_cta = 0;
+        return 1;
+    }
+    const int64_t lo = quotient((begin + snap + 1) * ctas + weight - 1, weight);
+    const int64_t hi = quotient((end - snap) * ctas - 1, weight);
     *first_cta = static_cast<int>(lo) - 1;
-    return end - begin > 2 * snap && hi >= lo ? static_cast<int>(hi - lo) + 2 : 1;
+    return hi >= lo ? static_cast<int>(hi - lo) + 2 : 1;
 }
 
 template <bool E4M3>
-__device__ void produce(const DecodeArgs& a, const CUtensorMap* maps, Shared& sh, uint32_t stages,
-                        uint32_t queries, int64_t weight, int64_t ctas, int64_t w0, int64_t w1) {
+__device__ void produce(const DecodeArgs& a, const CUtensorMap* map, Shared& sh, uint32_t stages,
+                        uint32_t queries, int64_t weight, int64_t ctas, int64_t w1) {
     constexpr int kTile = E4M3 ? 128 : 64;
     const KvView& kv = a.kv;
     const int lane = threadIdx.x & 31;
-    const int page_box = kv.page_shift < (E4M3 ? 7 : 6) ? kv.page_shift : (E4M3 ? 7 : 6);
-    constexpr int kHalves = E4M3 ? 1 : 2;
+    constexpr int kHalves = E4M3 ? 1 : 2, kBoxBytes = 4096;  // of 16 tokens' keys and values
     const int items = kv.kv_heads * a.cols.blocks;        // of a row
     const int64_t width = static_cast<int64_t>(a.p.H + 2 * kv.kv_heads) * kKvHeadDim;
-    // this lane's box: values or keys, half of the row, place in the tile
-    const int which = lane & 1, half = (lane >> 1) % kHalves, box = (lane >> 1) / kHalves;
+    // this lane's box of a tile's eight: group of tokens, half of the row
+    const int half = lane % kHalves, box = lane / kHalves;
 
     int row = sh.start_row;
     int64_t base = sh.start_base;
     Row r = sh.start;
-    int item = static_cast<int>((w0 - base) / max(r.weight, 1)), tile = 0;
-    const int rest = static_cast<int>((w0 - base) - static_cast<int64_t>(item) * r.weight);
+    int item = sh.start_item, tile = 0;
+    const int rest = sh.start_into;
     while (tile < r.tiles && tile_start<E4M3>(r, tile) < rest) tile = max(tile + 1, (rest + r.skip) / (kTile / 16));
     bool begun = false, more = true;
     // Page list entries, a lane each: the row's first 32, the 32 that the tiles are in, and the
@@ -380,24 +399,39 @@ __device__ void produce(const DecodeArgs& a, const CUtensorMap* maps, Shared& sh
             ids_after = load_ids(r, ids_from + 32);
         }
         const int head = item / a.cols.blocks, block = item - head * a.cols.blocks;
-        // Boxes of a page, or of 16 rows at the ends of what the row sees, where a page's would
-        // bring tokens for nothing (half a page of 64 tokens is 5% of a row of 600).
-        const bool edge = key0 < r.low || key0 + kTile > r.len;
-        const int box_shift = edge ? 4 : page_box, box_rows = 1 << box_shift;
-        const int key = key0 + (box << box_shift);  // of this lane's box
-        const bool mine = box < kTile >> box_shift && key < r.len && key + box_rows > r.low;
+        const uint32_t bar = smem_u32(&sh.full[st]);
+        // The boxes with tokens that the row sees.  (Boxes of a whole page, with fewer to
+        // issue, brought 5% more for a row of 600 tokens in pages of 64.)
+        const int key = key0 + box * 16;  // of this lane's box
+        const bool mine = lane < 8 && key < r.len && key + 16 > r.low;
         const int id = __shfl_sync(0xffffffffu, ids, ((key >> kv.page_shift) - ids_from) & 31);
         const bool id_ok = id >= 0 && id < kv.num_pages;
         const bool tile_bad = __any_sync(0xffffffffu, mine && !id_ok);
         const int loads = __popc(__ballot_sync(0xffffffffu, mine));
+        if (mine) {
+            const int32_t at = key & ((1 << kv.page_shift) - 1);
+            const int32_t row_at = (((id_ok ? id : 0) * kv.kv_heads + head) << kv.page_shift) + at;
+            const uint32_t dst = stages + st * kStageBytes + lane * kBoxBytes;
+            if (dbg_check(tma_box_ok(dst, kBoxBytes, 1024, stages, stages + kStages * kStageBytes, half * 64,
+                                     E4M3 ? 1 : 2), kv.status))
+                load_box(dst, map, bar, half * 64, row_at);
+        }
+        const int q_cols = min(a.cols.block, a.cols.group - block * a.cols.block);
+        const uint16_t* const qkv = a.p.qkv + row * width;
+        if (first)
+            for (int i = lane; i < q_cols; i += 32)
+                bulk_load(queries + (slot * a.cols.block + i) * kQueryStride,
+                          qkv + (static_cast<int64_t>(head) * a.cols.group + block * a.cols.block + i) * kKvHeadDim,
+                          256, bar);
         const bool fresh = key0 + kTile >= r.len;
+        if (fresh && lane < 2)
+            bulk_load(smem_u32(sh.fresh[st][lane]),
+                      qkv + (a.p.H + lane * kv.kv_heads + head) * static_cast<int64_t>(kKvHeadDim), 256, bar);
         const int last_id = __shfl_sync(0xffffffffu, ids, (((r.len - 1) >> kv.page_shift) - ids_from) & 31);
         // whether the item goes on in this CTA, and the CTA after it
         const int64_t begin = base + static_cast<int64_t>(item) * r.weight;
         const bool last = tile + 1 == r.tiles || begin + tile_start<E4M3>(r, tile + 1) >= w1;
         more = !last || (tile + 1 == r.tiles && begin + r.weight < w1);
-        const uint32_t bar = smem_u32(&sh.full[st]);
-        const int q_cols = min(a.cols.block, a.cols.group - block * a.cols.block);
         if (lane == 0) {
             Unit& t = sh.unit[st];
             t.row = row;
@@ -408,35 +442,13 @@ __device__ void produce(const DecodeArgs& a, const CUtensorMap* maps, Shared& sh
             t.len = r.len;
             t.flags = (first ? kFirst : 0) | (last ? kLast : 0) | (fresh ? kNew : 0) | (tile_bad ? kBad : 0) |
                       (more ? 0 : kEnd) | slot << kQSlotShift;
-            if (last) {
-                t.parts = parts_of(begin, begin + r.weight, weight, ctas, a.snap, &t.first_cta);
-            }
+            if (last) t.parts = parts_of(begin, begin + r.weight, weight, ctas, a.snap, &t.first_cta);
             t.page = last_id >= 0 && last_id < kv.num_pages ? last_id : -1;
             t.at = (r.len - 1) & ((1 << kv.page_shift) - 1);
-            mbar_arrive_expect_tx(bar, loads * (box_rows * 128u) + (first ? q_cols * 256u : 0u) +
-                                           (fresh ? 512u : 0u));
+            // (after the copies: the phase waits for this arrival)
+            mbar_arrive_expect_tx(bar, loads * kBoxBytes + (first ? q_cols * 256u : 0u) + (fresh ? 512u : 0u));
         }
         __syncwarp();
-        const uint16_t* const qkv = a.p.qkv + row * width;
-        if (first)
-            for (int i = lane; i < q_cols; i += 32)
-                bulk_load(queries + (slot * a.cols.block + i) * kQueryStride,
-                          qkv + (static_cast<int64_t>(head) * a.cols.group + block * a.cols.block + i) * kKvHeadDim,
-                          256, bar);
-        if (fresh && lane < 2)
-            bulk_load(smem_u32(sh.fresh[st][lane]),
-                      qkv + (a.p.H + lane * kv.kv_heads + head) * static_cast<int64_t>(kKvHeadDim), 256, bar);
-        if (mine) {
-            const int32_t at = key & ((1 << kv.page_shift) - 1);
-            const int32_t c1 = static_cast<int32_t>(
-                (((static_cast<int64_t>(which) * kv.num_pages + (id_ok ? id : 0)) * kv.kv_heads + head)
-                 << kv.page_shift) + at);
-            const uint32_t dst = stages + st * kStageBytes + which * kHalfStage + half * 8192u +
-                                 box * box_rows * 128u;
-            if (dbg_check(tma_box_ok(dst, box_rows * 128u, 1024, stages, stages + kStages * kStageBytes, half * 64,
-                                     E4M3 ? 1 : 2), kv.status))
-                tma_load_2d(dst, maps + edge, bar, half * 64, c1);
-        }
         if constexpr (E4M3) {
             // (key, value) exponents, eight tokens to a lane; every lane arrives
             const int k8 = key0 + lane * 8;
@@ -502,14 +514,10 @@ __device__ __forceinline__ float output_scale(float l, float m, float w) {
     return E4M3 ? 1.0f / l * ex2(-kWeightTop) * ex2(w - m) : 1.0f / l;
 }
 
-// Where a column of a warp's output lies in the stage: in the warp's own rows, which no other
-// warp reads while the columns are not split.  The dimensions of a column are turned so that
-// the lanes of a store hit different banks.
-template <bool E4M3>
-__device__ __forceinline__ uint32_t meet_byte(int warp, int col) {
-    return E4M3 ? (col >> 3) * kHalfStage + warp * 4096 + (col & 7) * 512
-                : (col >> 2) * 8192 + warp * 2048 + (col & 3) * 512;
-}
+// A column of a warp's output lies in the warp's own rows of the stage, which no other warp
+// reads while the columns are not split; its dimensions are turned so that the lanes of
+// a store hit different banks.
+__device__ __forceinline__ uint32_t meet_byte(int warp, int col) { return warp * kWarpBytes + col * 512; }
 template <bool E4M3>
 __device__ __forceinline__ int meet_turn(int col) {
     const int c = col >> 1 & 3;
@@ -632,7 +640,7 @@ __device__ void finish(const DecodeArgs& a, Shared& sh, const uint8_t* stage_mem
     uint32_t phase = 0, done_phase = 0;  // done_phase: a bit for each stage
     bool bad = false;
     for (;;) {
-        if (!wait_warp<false, 100>(smem_u32(&sh.full[st]), phase, &sh.abort, kv.status, a.p.wait_ns)) return;
+        if (!wait_warp(smem_u32(&sh.full[st]), phase, &sh.abort, kv.status, a.p.wait_ns)) return;
         const Unit& t = sh.unit[st];
         const int flags = t.flags;
         if (flags & kFirst) bad = false;
@@ -656,7 +664,7 @@ __device__ void finish(const DecodeArgs& a, Shared& sh, const uint8_t* stage_mem
                     const bool has = k < key_warps;
                     const int at = col * key_warps + (has ? k : 0);
                     x[k] = *reinterpret_cast<const float4*>(
-                        tile + meet_byte<E4M3>((has ? k : 0) * a.cols.warps + cw, in) + turned * 4);
+                        tile + meet_byte((has ? k : 0) * a.cols.warps + cw, in) + turned * 4);
                     ls[k] = has ? sh.part_l[st][at] : 0.0f;
                     ms[k] = has ? sh.part_m[st][at] : kLeast;
                     ws[k] = E4M3 && has ? sh.part_w[st][at] : ms[k];
@@ -739,7 +747,7 @@ __device__ __forceinline__ void mend_tile(const DecodeArgs& a, Shared& sh, int s
         for (int i = lane; i < kStep * (E4M3 ? 8 : 16); i += 32) {
             const int r = i >> (E4M3 ? 3 : 4), unit = i & (E4M3 ? 7 : 15);
             if (key + r < t.low || key + r >= t.len)
-                *reinterpret_cast<uint4*>(tile + kHalfStage + tile_byte<E4M3>(warp * kStep + r, unit)) =
+                *reinterpret_cast<uint4*>(tile + kValueOffset + tile_byte<E4M3>(warp * kStep + r, unit)) =
                     make_uint4(0, 0, 0, 0);
         }
         const int fresh = t.len - 1 - key;
@@ -750,12 +758,12 @@ __device__ __forceinline__ void mend_tile(const DecodeArgs& a, Shared& sh, int s
             const int64_t row = kv_row(kv, a.p.layer, which, max(t.page, 0), t.head, t.at);
             const uint4 v = reinterpret_cast<const uint4*>(sh.fresh[st][which])[unit];
             if constexpr (!E4M3) {
-                *reinterpret_cast<uint4*>(tile + which * kHalfStage + tile_byte<E4M3>(r, unit)) = v;
+                *reinterpret_cast<uint4*>(tile + which * kValueOffset + tile_byte<E4M3>(r, unit)) = v;
                 if (store) reinterpret_cast<uint4*>(kv.pages)[row * 16 + unit] = v;
             } else {
                 uint2 codes;
                 const int e = e4m3_row_of_16(v, &codes);
-                *reinterpret_cast<uint2*>(tile + which * kHalfStage + tile_byte<E4M3>(r, unit >> 1) + (unit & 1) * 8) =
+                *reinterpret_cast<uint2*>(tile + which * kValueOffset + tile_byte<E4M3>(r, unit >> 1) + (unit & 1) * 8) =
                     codes;
                 if (unit == 0) sh.exponents[st][r * 2 + which] = static_cast<uint8_t>(e + 127);
                 if (store) {
@@ -866,7 +874,7 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
             flags = sh.unit[st].flags;
             const int key0 = sh.unit[st].key0, low = sh.unit[st].low, len = sh.unit[st].len;
             tile = stage_mem + st * kStageBytes;
-            const uint32_t keys = smem_u32(tile), values = keys + kHalfStage;
+            const uint32_t keys = smem_u32(tile), values = keys + kValueOffset;
             s.bad |= (flags & kBad) != 0;
             const bool edge = key0 < low || key0 + kTile >= len;
             if (edge) {
@@ -889,7 +897,7 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
                         uint32_t f[4];
-                        ldsm_x4(((keys + key_off + step * 2048) ^ ((k & 3) << 5)) + (k >> 2) * 8192, f);
+                        ldsm_x4(((keys + key_off + step * kWarpBytes) ^ ((k & 3) << 5)) + (k >> 2) * 4096, f);
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) mma<E4M3>(acc[k & 1][nt], f, q[k][nt][0], q[k][nt][1]);
                     }
@@ -900,7 +908,7 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
                             uint32_t f[4];
-                            ldsm_x4((keys + key_off + step * 4096 + i * 2048) ^ (k << 4), f);
+                            ldsm_x4((keys + key_off + step * kWarpBytes + i * 4096) ^ (k << 4), f);
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt) {
                                 mma_codes(acc[i][nt], f, q[k][nt][0], q[k + 1][nt][0]);
@@ -1061,7 +1069,7 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
                         uint32_t f[4];
-                        ldsm_x4_trans(((values + value_off + step * 2048) ^ ((k & 3) << 5)) + (k >> 2) * 8192, f);
+                        ldsm_x4_trans(((values + value_off + step * kWarpBytes) ^ ((k & 3) << 5)) + (k >> 2) * 4096, f);
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) mma<E4M3>(s.o[k][nt], f, b[0][nt][0], b[0][nt][1]);
                     }
@@ -1072,7 +1080,7 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
 #pragma unroll
                         for (int i = 0; i < kGroups; ++i) {
                             uint32_t w[4];
-                            ldsm_x4_trans((values + value_off + step * 4096 + i * 2048) ^ (k << 4), w);
+                            ldsm_x4_trans((values + value_off + step * kWarpBytes + i * 4096) ^ (k << 4), w);
 #pragma unroll
                             for (int h = 0; h < 2; ++h) {
                                 const uint32_t lo = __byte_perm(w[2 * h], 0, 0x3120);
@@ -1114,7 +1122,7 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
                     if constexpr (E4M3) sh.part_w[st][at] = s.w[nt][j];
                 }
                 if (ONE && c > 0) continue;
-                uint8_t* const to = tile + meet_byte<E4M3>(warp, col);
+                uint8_t* const to = tile + meet_byte(warp, col);
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
 #pragma unroll
@@ -1137,7 +1145,7 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
 
 template <bool E4M3, int NT, bool ONE>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm)
-    attention_decode_kernel(const __grid_constant__ CacheMaps maps, const __grid_constant__ DecodeArgs a) {
+    attention_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ DecodeArgs a) {
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ Shared sh;
     // (the dynamic part starts past the static one: rounded up to the swizzle's 1024 bytes)
@@ -1146,8 +1154,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
     uint8_t* const query_mem = stage_mem + kStages * kStageBytes;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (tid == 0) {
-        prefetch_tmap(&maps.map[0]);
-        prefetch_tmap(&maps.map[1]);
+        prefetch_tmap(&map);
         for (int i = 0; i < kStages; ++i) {
             mbar_init(smem_u32(&sh.full[i]), E4M3 ? 33 : 1);
             mbar_init(smem_u32(&sh.empty[i]), kWarps + 1);
@@ -1156,7 +1163,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
         mbar_init(smem_u32(&sh.met), kWarps);
         mbar_init(smem_u32(&sh.joined), 1);
         sh.pending[0] = sh.pending[1] = Pending{};
-        sh.start_base = sh.start_row = sh.empty_rows = 0;
+        sh.start_base = sh.start_row = sh.start_item = sh.start_into = sh.empty_rows = 0;
         sh.bound[0] = sh.bound[1] = 0;
         sh.start = Row{};
         sh.abort = 0;
@@ -1215,20 +1222,31 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
         }
     if (weight == 0) return;
     // as many CTAs as leave each at least the most that lies between two tiles' starts
-    const int64_t most = weight / ((E4M3 ? 8 : 4) + a.item_weight);
-    const int64_t ctas = most < 1 ? 1 : most < gridDim.x ? most : gridDim.x;
+    const int apart = (E4M3 ? 8 : 4) + a.item_weight;
+    const bool full = weight >= static_cast<int64_t>(apart) * gridDim.x;
+    const int64_t ctas = full ? gridDim.x : weight < apart ? 1 : quotient(weight, apart);
     if (blockIdx.x >= ctas) return;
-    const int64_t w0 = blockIdx.x * weight / ctas, w1 = (blockIdx.x + 1) * weight / ctas;
+    // (a batch of any size: less than 2^48 groups, so the multiplication is exact)
+    const int64_t w0 = full ? __umul64hi(blockIdx.x * weight, a.grid_reciprocal) : quotient(blockIdx.x * weight, ctas);
+    const int64_t w1 = full ? __umul64hi((blockIdx.x + 1) * weight, a.grid_reciprocal)
+                            : quotient((blockIdx.x + 1) * weight, ctas);
     int64_t before = 0;
     for (int i0 = 0;;) {
         const int64_t begin = before + upto - v, end = before + upto;
         if (begin <= w0 && w0 < end) {
-            sh.bound[0] = snapped(w0, begin, r.weight, a.snap);
+            const int64_t item = quotient(w0 - begin, r.weight), at = begin + item * r.weight;
+            const int into = snapped(static_cast<int>(w0 - at), r.weight, a.snap);
+            sh.bound[0] = at + into;
             sh.start_row = i0 + tid;
             sh.start_base = begin;
             sh.start = r;
+            sh.start_item = static_cast<int>(item) + (into == r.weight);
+            sh.start_into = into == r.weight ? 0 : into;
         }
-        if (begin <= w1 && w1 < end) sh.bound[1] = snapped(w1, begin, r.weight, a.snap);
+        if (begin <= w1 && w1 < end) {
+            const int64_t at = begin + quotient(w1 - begin, r.weight) * r.weight;
+            sh.bound[1] = at + snapped(static_cast<int>(w1 - at), r.weight, a.snap);
+        }
         if (w1 == weight) sh.bound[1] = weight;
         if (i0 == 0 && a.p.n > kThreads) {
             __syncthreads();
@@ -1244,7 +1262,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
     __syncthreads();
     if (sh.bound[0] == sh.bound[1]) return;
     if (warp == 0)
-        produce<E4M3>(a, maps.map, sh, smem_u32(stage_mem), smem_u32(query_mem), weight, ctas, sh.bound[0], sh.bound[1]);
+        produce<E4M3>(a, &map, sh, smem_u32(stage_mem), smem_u32(query_mem), weight, ctas, sh.bound[1]);
     else if (warp <= kWarps)
         consume<E4M3, NT, ONE>(a, sh, stage_mem, query_mem);
     else
@@ -1252,12 +1270,12 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
 }
 
 template <bool E4M3, int NT, bool ONE>
-cudaError_t launch(const CacheMaps& maps, const DecodeArgs& a, int grid, cudaStream_t stream) {
+cudaError_t launch(const CUtensorMap& map, const DecodeArgs& a, int grid, cudaStream_t stream) {
     auto kern = attention_decode_kernel<E4M3, NT, ONE>;
     const int bytes = 1024 + kStages * kStageBytes + 2 * a.cols.block * kQueryStride;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != cudaSuccess) return e;
-    return launch_overlapped(kern, grid, kThreads, bytes, stream, maps, a);
+    return launch_overlapped(kern, grid, kThreads, bytes, stream, map, a);
 }
 
 }  // namespace
@@ -1268,30 +1286,29 @@ int64_t decode_workspace_bytes(int H, int kv_heads, int sm_count) {
     return counter_bytes(static_cast<int>(ctas)) + ctas * 2 * part_floats(used_columns(H / kv_heads)) * 4;
 }
 
-int encode_cache(CacheMaps* maps, const KvView& kv, int layer) {
+int encode_cache(CUtensorMap* map, const KvView& kv, int layer) {
     const bool e4m3 = kv.exponents != nullptr;
-    const int64_t rows = static_cast<int64_t>(2) * kv.num_pages * kv.kv_heads << kv.page_shift;
-    const int most = e4m3 ? 128 : 64, tokens = 1 << kv.page_shift;
-    int rc = 0;
-    for (int i = 0; i < 2 && rc == 0; ++i)
-        rc = encode_rows(&maps->map[i], e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
-                         kv.pages + layer * rows * kv.row_bytes, kKvHeadDim, rows, kv.row_bytes, e4m3 ? 128 : 64,
-                         i == 1 ? 16 : tokens < most ? tokens : most);
-    return rc;
+    const uint64_t rows = static_cast<uint64_t>(kv.num_pages) * kv.kv_heads << kv.page_shift;
+    const uint64_t dims[3] = {kKvHeadDim, rows, 2};
+    const uint64_t strides[2] = {static_cast<uint64_t>(kv.row_bytes), rows * kv.row_bytes};
+    const uint32_t box[3] = {e4m3 ? 128u : 64u, 16, 2};
+    return encode_3d(map, e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
+                     kv.pages + 2 * rows * kv.row_bytes * layer, dims, strides, box);
 }
 
-cudaError_t launch_attention_decode(const CacheMaps& maps, const KvView& kv, const DecodeParams& p, int sm_count,
+cudaError_t launch_attention_decode(const CUtensorMap& map, const KvView& kv, const DecodeParams& p, int sm_count,
                                     cudaStream_t stream) {
-    DecodeArgs a{kv, p, columns_of(p.H / kv.kv_heads), p.window, 0, 0};
+    DecodeArgs a{kv, p, columns_of(p.H / kv.kv_heads), p.window, 0, 0, 0};
     const int grid = sm_count * kCtasPerSm;
     const bool e4m3 = kv.exponents != nullptr, wide = a.cols.block > 8;
     // (measured on ragged batches of 200 to 1024 and 1 to 8192 tokens, with 3 / 5 / 8 / 12 / 16: bf16 best at 5
     // with up to 8 queries of a key head, 8 with more; e4m3 at 12, but 3% worse at 3)
     a.item_weight = e4m3 ? 12 : wide ? 8 : 5;
     a.snap = a.item_weight + (e4m3 ? 12 : 10);
-    if (p.H == kv.kv_heads) return e4m3 ? launch<true, 1, true>(maps, a, grid, stream) : launch<false, 1, true>(maps, a, grid, stream);
-    if (wide) return e4m3 ? launch<true, 2, false>(maps, a, grid, stream) : launch<false, 2, false>(maps, a, grid, stream);
-    return e4m3 ? launch<true, 1, false>(maps, a, grid, stream) : launch<false, 1, false>(maps, a, grid, stream);
+    a.grid_reciprocal = ~uint64_t{0} / grid + 1;
+    if (p.H == kv.kv_heads) return e4m3 ? launch<true, 1, true>(map, a, grid, stream) : launch<false, 1, true>(map, a, grid, stream);
+    if (wide) return e4m3 ? launch<true, 2, false>(map, a, grid, stream) : launch<false, 2, false>(map, a, grid, stream);
+    return e4m3 ? launch<true, 1, false>(map, a, grid, stream) : launch<false, 1, false>(map, a, grid, stream);
 }
 
 }  // namespace w4a16

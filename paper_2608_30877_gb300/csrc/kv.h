@@ -8,15 +8,14 @@
 
 namespace w4a16 {
 
-// api.cu: the current device's state, and the encoder of tensor maps of rows, in boxes of
-// box_rows rows with the 128-byte swizzle.
+// api.cu: the current device's state, and the encoder of tensor maps (128-byte swizzle).
 struct LibraryState {
     int sm_count;
     int* status;  // device status word
 };
 int library_state(LibraryState* out);
-int encode_rows(CUtensorMap* map, CUtensorMapDataType dtype, const void* base, uint64_t inner,
-                uint64_t rows, uint64_t row_bytes, uint32_t box_inner, uint32_t box_rows);
+int encode_3d(CUtensorMap* map, CUtensorMapDataType dtype, const void* base, const uint64_t dims[3],
+              const uint64_t strides[2], const uint32_t box[3]);
 
 constexpr int kKvHeadDim = 128;
 constexpr int kKvMaxSlots = 1 << 16;
@@ -73,12 +72,9 @@ struct DecodeParams {
     uint64_t wait_ns;
 };
 int64_t decode_workspace_bytes(int H, int kv_heads, int sm_count);
-// One layer's keys and values, in boxes of a page (at most a tile of decode.cu) and of 16 rows.
-struct CacheMaps {
-    CUtensorMap map[2];
-};
-int encode_cache(CacheMaps* maps, const KvView& kv, int layer);
-cudaError_t launch_attention_decode(const CacheMaps& maps, const KvView& kv, const DecodeParams& p,
+// One layer's keys and values as rows, in boxes of 16 rows of both, 128 bytes wide.
+int encode_cache(CUtensorMap* map, const KvView& kv, int layer);
+cudaError_t launch_attention_decode(const CUtensorMap& map, const KvView& kv, const DecodeParams& p,
                                     int sm_count, cudaStream_t stream);
 
 uint64_t wait_limit_ns();  // internal.h
