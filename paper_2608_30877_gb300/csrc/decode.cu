@@ -112,7 +112,7 @@ struct Row {
     int slot, len, low;
     int first, tiles;  // its first tile, and how many
     int skip;          // groups of 16 keys of the first tile that it does not see
-    int weight;        // of an item: the groups that it sees, and kItemWeight
+    int weight;        // of an item: the groups that it sees, and item_weight
 };
 
 // A part that the CTA has written: the item, and whether the CTA is to add it up.
