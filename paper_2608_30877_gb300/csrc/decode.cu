@@ -30,12 +30,12 @@
 //    that wraps to zero, adds the parts up in the order of the CTAs, so that the result has
 //    the same bits every time.
 //
-// 8-bit cache.  Scores are products of codes: a row of q, scaled by a power of two to e4m3's
-// range, is the sum of two e4m3 values (4 + 4 of bf16's 8 bits; what they leave is at most 2^-18
-// of the row's largest), so that keys need no conversion.  For the other product, values'
-// codes are converted to fp16, exactly; a key's exponent goes to its score, a value's
-// exponent to its weight, and the weights that multiply the codes are relative to the largest
-// of these products, whose running maximum a column keeps next to its scores'.
+// 8-bit cache.  Keys' and values' codes are converted to fp16, exactly, and multiplied with
+// the queries in fp16 (scaled by a power of two, which keeps all their bits) and the weights in
+// fp16.  (Warp-level MMAs on e4m3 are no way around that: on this machine each takes 2 fp16 MMAs
+// and the conversion of both operands.)  A key's exponent goes to its score, a value's exponent
+// to its weight, and the weights that multiply the codes are relative to the largest of these
+// products, whose running maximum a column keeps next to its scores'.
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <cstdint>
@@ -183,12 +183,20 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
     return r;
 }
-// m16n8k32 on e4m3 codes; its sums are as exact as fp32's (2^-22 of the products' magnitudes).
-__device__ __forceinline__ void mma_codes(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
-        "{%8, %9}, {%0, %1, %2, %3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+// Sixteen rows of 32 bytes' columns, transposed: register r of lane (g, c) has column
+// g + 8 (r % 2) of rows 4c .. 4c + 3, + 16 from r = 2 on; a lane gives a row's address.
+__device__ __forceinline__ void ldsm_bytes_trans(uint32_t addr, uint32_t (&v)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m16n16.x2.trans.shared.b8 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
+                 : "r"(addr)
+                 : "memory");
+}
+// The A operand from rows g and g + 8, four codes each: columns 2c, 2c + 1 and 2c + 8, 2c + 9.
+__device__ __forceinline__ void codes_to_halves(uint32_t row, uint32_t row8, uint32_t (&f)[4]) {
+    f[0] = e4m3_to_half2(static_cast<uint16_t>(row));
+    f[1] = e4m3_to_half2(static_cast<uint16_t>(row8));
+    f[2] = e4m3_to_half2(static_cast<uint16_t>(row >> 16));
+    f[3] = e4m3_to_half2(static_cast<uint16_t>(row8 >> 16));
 }
 template <bool E4M3>
 __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -235,6 +243,12 @@ template <bool E4M3>
 __device__ __forceinline__ uint32_t tile_byte(int row, int unit) {
     const uint32_t box = E4M3 ? (row >> 4) * 4096u : (row >> 4) * 8192u + (unit >> 3) * 4096u;
     return box + (row & 15) * 128u + (((unit & 7) ^ (row & 7)) << 4);
+}
+// Key of row `row` of a step's matrix `i` of 8 keys; e4m3: turned, so that both ways in which
+// ldmatrix reads keys and values are without bank conflicts.
+template <bool E4M3>
+__device__ __forceinline__ int key_at(int row, int i) {
+    return 8 * i + (E4M3 ? row ^ 4 * (i & 1) : row);
 }
 // One box; completion is signalled on `bar` as transaction bytes.
 __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, uint32_t bar, int32_t c0, int32_t row) {
@@ -518,11 +532,7 @@ __device__ __forceinline__ float output_scale(float l, float m, float w) {
 // reads while the columns are not split; its dimensions are turned so that the lanes of
 // a store hit different banks.
 __device__ __forceinline__ uint32_t meet_byte(int warp, int col) { return warp * kWarpBytes + col * 512; }
-template <bool E4M3>
-__device__ __forceinline__ int meet_turn(int col) {
-    const int c = col >> 1 & 3;
-    return E4M3 ? 16 * (c & 1) + 4 * (c >> 1) : 8 * c;
-}
+__device__ __forceinline__ int meet_turn(int col) { return 8 * (col >> 1 & 3); }
 
 __device__ __forceinline__ uint16_t* output_of(const DecodeArgs& a, int row, int head, int block) {
     return a.p.out + (static_cast<int64_t>(row) * a.p.H + static_cast<int64_t>(head) * a.cols.group +
@@ -656,7 +666,7 @@ __device__ void finish(const DecodeArgs& a, Shared& sh, const uint8_t* stage_mem
             uint16_t* const out = output_of(a, t.row, t.head, t.block);
 #pragma unroll 2
             for (int col = 0; col < cols; ++col) {
-                const int cw = col / (8 * NT), in = col - cw * 8 * NT, turned = (4 * lane + meet_turn<E4M3>(in)) & 127;
+                const int cw = col / (8 * NT), in = col - cw * 8 * NT, turned = (4 * lane + meet_turn(in)) & 127;
                 float4 x[kWarps];
                 float ls[kWarps], ms[kWarps], ws[kWarps];
 #pragma unroll
@@ -796,12 +806,15 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
     const int g = lane >> 2, c = lane & 3;
     const int col_warp = warp % a.cols.warps, key_warp = warp / a.cols.warps, key_warps = kWarps / a.cols.warps;
     const float scale = a.p.scale * 1.4426950408889634f;
-    // This lane's row of an ldmatrix within a group of 16 keys.  Matrices of keys are (rows 0..7,
-    // unit 0), (8..15, 0), (0..7, 1), (8..15, 1); of transposed values the same in e4m3, and with
-    // the middle two exchanged in bf16.  Steps along the dimensions flip bits of the address.
-    const uint32_t key_off = tile_byte<E4M3>(lane & 15, lane >> 4);
+    // This lane's row of an ldmatrix within a group of 16 keys (bytes, transposed: of the step's 32
+    // keys).  Matrices of keys are (rows 0 .. 7, unit 0), (8 .. 15, 0), (0 .. 7, 1), (8 .. 15, 1); of
+    // transposed values with the middle two exchanged; of transposed bytes rows 4c .. 4c + 3
+    // are keys 2c, 2c + 1 of one matrix of 8 and of the next, in the order that the weights have.
+    // Steps along the dimensions flip bits of the address.
+    const uint32_t key_off = tile_byte<E4M3>(key_at<E4M3>(lane & 7, lane >> 3 & 1), lane >> 4);
     const uint32_t value_off =
-        E4M3 ? key_off : tile_byte<E4M3>((lane & 7) + ((lane >> 4) << 3), lane >> 3 & 1);
+        E4M3 ? tile_byte<E4M3>(key_at<E4M3>((lane >> 1 & 6) + (lane & 1), 2 * (lane >> 4) + (lane >> 1 & 1)), 0)
+             : tile_byte<E4M3>((lane & 7) + ((lane >> 4) << 3), lane >> 3 & 1);
     int st = 0;
     uint32_t phase = 0, met = 0;
     auto wait = [&]() { return wait_warp(smem_u32(&sh.full[st]), phase, &sh.abort, kv.status, a.p.wait_ns); };
@@ -846,10 +859,8 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
                 for (int k = 0; k < 8; ++k) {
                     const float x[4] = {bf16_lo(v[k].x) * f, bf16_hi(v[k].x) * f, bf16_lo(v[k].y) * f,
                                         bf16_hi(v[k].y) * f};
-                    q[k][nt][0] = e4m3_quad(x[0], x[1], x[2], x[3]);
-                    const float2 lo = half2_floats(e4m3_to_half2(static_cast<uint16_t>(q[k][nt][0])));
-                    const float2 hi = half2_floats(e4m3_to_half2(static_cast<uint16_t>(q[k][nt][0] >> 16)));
-                    q[k][nt][1] = e4m3_quad(x[0] - lo.x, x[1] - lo.y, x[2] - hi.x, x[3] - hi.y);
+                    q[k][nt][0] = half_pair(x[0], x[1]);
+                    q[k][nt][1] = half_pair(x[2], x[3]);
                 }
                 // (column g's scale is needed by the threads of columns 2c and 2c + 1)
 #pragma unroll
@@ -885,7 +896,7 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
             for (int step = key_warp; step < kWarps; step += key_warps) {
                 const int key = key0 + step * kStep;
                 if (key >= len || key + kStep <= low) continue;
-                // scores of the step's groups of 16 keys: rows g and g + 8, columns 2c and 2c + 1
+                // scores of the step's matrices of 8 keys: row g, columns 2c and 2c + 1
                 float acc[2][NT][4];  // e4m3: of two groups; bf16: of even and odd dimensions
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
@@ -902,20 +913,20 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
                         for (int nt = 0; nt < NT; ++nt) mma<E4M3>(acc[k & 1][nt], f, q[k][nt][0], q[k][nt][1]);
                     }
                 } else {
-                    // 32 dimensions at a time, for both parts of q
 #pragma unroll
-                    for (int k = 0; k < 8; k += 2) {
+                    for (int k = 0; k < 8; k += 2)
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
-                            uint32_t f[4];
-                            ldsm_x4((keys + key_off + step * kWarpBytes + i * 4096) ^ (k << 4), f);
+                            uint32_t w[4], f[4];
+                            ldsm_x4((keys + key_off + step * kWarpBytes + i * 4096) ^ (k << 4), w);
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) {
-                                mma_codes(acc[i][nt], f, q[k][nt][0], q[k + 1][nt][0]);
-                                mma_codes(acc[i][nt], f, q[k][nt][1], q[k + 1][nt][1]);
+                            for (int h = 0; h < 2; ++h) {
+                                codes_to_halves(w[2 * h], w[2 * h + 1], f);
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt)
+                                    mma<E4M3>(acc[i][nt], f, q[k + h][nt][0], q[k + h][nt][1]);
                             }
                         }
-                    }
                 }
                 constexpr float kSlack = E4M3 ? kSlackE4m3 : kSlackBf16;
                 uint32_t b[kGroups][NT][2];
@@ -934,9 +945,9 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
                     return f;
                 };
                 if constexpr (ONE) {
-                    // One query, the same in every column: lane (g, c) has all of keys g + 8 r, and
-                    // takes that of r = c (bf16: r = c % 2, in two lanes alike).
-                    const int r = c % kRows, at = key + g + 8 * r;
+                    // One query, the same in every column: lane (g, c) has row g of all matrices, and
+                    // takes that of matrix c (bf16: c % 2, in two lanes alike).
+                    const int r = c % kRows, in = key_at<E4M3>(g, r), at = key + in;
                     float x = acc[0][0][0] + (E4M3 ? 0.0f : acc[1][0][0]);
                     const float x1 = acc[0][0][2] + (E4M3 ? 0.0f : acc[1][0][2]);
                     if (r == 1) x = x1;
@@ -945,7 +956,7 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
                     float y = 0.0f;
                     if constexpr (E4M3) {
                         const uint32_t e =
-                            *reinterpret_cast<const uint16_t*>(sh.exponents[st] + (step * kStep + g + 8 * r) * 2);
+                            *reinterpret_cast<const uint16_t*>(sh.exponents[st] + (step * kStep + in) * 2);
                         x *= __uint_as_float((e & 0xFFu) << 23) * q_scale[0][0];
                         y = static_cast<float>(static_cast<int>(e >> 8) - 127);
                     } else {
@@ -971,21 +982,21 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
                         // (the rounded weights' sum, so that they add up to one)
                         s.l[0][0] += bf16_lo(bf16_pair(p, 0.0f));
                     }
-                    // keys g and g + 1 in the lanes of even g, then keys 2c and 2c + 1 everywhere
+                    // rows g and g + 1 in the lanes of even g, then rows 2c and 2c + 1 everywhere
                     const float next = __shfl_xor_sync(0xffffffffu, p, 4);
                     const uint32_t pair = E4M3 ? half_pair(p, next) : bf16_pair(p, next);
 #pragma unroll
                     for (int i = 0; i < kRows; ++i) b[i >> 1][0][i & 1] = __shfl_sync(0xffffffffu, pair, 8 * c + i);
                 } else {
-                    // keys g and g + 8 of each group, as they come out of the products: e4m3 with
-                    // their exponents, before the columns' factors
+                    // row g of each matrix, as it comes out of the products: e4m3 with the keys'
+                    // exponents, before the columns' factors
                     float x[NT][kRows][2], value_exp[kRows] = {};
 #pragma unroll
                     for (int i = 0; i < kRows; ++i) {
                         float key_scale = 1.0f;
                         if constexpr (E4M3) {
                             const uint32_t e =
-                                *reinterpret_cast<const uint16_t*>(sh.exponents[st] + (step * kStep + g + 8 * i) * 2);
+                                *reinterpret_cast<const uint16_t*>(sh.exponents[st] + (step * kStep + key_at<E4M3>(g, i)) * 2);
                             key_scale = __uint_as_float((e & 0xFFu) << 23);
                             value_exp[i] = static_cast<float>(static_cast<int>(e >> 8) - 127);
                         }
@@ -999,7 +1010,7 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
                     if (edge) {
 #pragma unroll
                         for (int i = 0; i < kRows; ++i) {
-                            const int at = key + g + 8 * i;
+                            const int at = key + key_at<E4M3>(g, i);
                             if (at >= low && at < len) continue;
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt) x[nt][i][0] = x[nt][i][1] = -INFINITY;
@@ -1061,7 +1072,7 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
                                 s.l[nt][0] += bf16_lo(w);
                                 s.l[nt][1] += bf16_hi(w);
                             }
-                            // keys 2c, 2c + 1 of column g: the transpose of what this thread holds
+                            // rows 2c, 2c + 1 of column g: the transpose of what this thread holds
                             b[i >> 1][nt][i & 1] = transpose_8x8(w);
                         }
                 }
@@ -1074,24 +1085,15 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
                         for (int nt = 0; nt < NT; ++nt) mma<E4M3>(s.o[k][nt], f, b[0][nt][0], b[0][nt][1]);
                     }
                 } else {
-                    // rows g and g + 8 of a tile are dimensions 2g and 2g + 1 of its 16
 #pragma unroll
-                    for (int k = 0; k < 8; k += 2) {
+                    for (int k = 0; k < 8; ++k) {
+                        uint32_t w[4], f[4];
+                        ldsm_bytes_trans((values + value_off + step * kWarpBytes) ^ (k << 4), w);
 #pragma unroll
                         for (int i = 0; i < kGroups; ++i) {
-                            uint32_t w[4];
-                            ldsm_x4_trans((values + value_off + step * kWarpBytes + i * 4096) ^ (k << 4), w);
+                            codes_to_halves(w[2 * i], w[2 * i + 1], f);
 #pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                const uint32_t lo = __byte_perm(w[2 * h], 0, 0x3120);
-                                const uint32_t hi = __byte_perm(w[2 * h + 1], 0, 0x3120);
-                                const uint32_t f[4] = {e4m3_to_half2(static_cast<uint16_t>(lo)),
-                                                       e4m3_to_half2(static_cast<uint16_t>(lo >> 16)),
-                                                       e4m3_to_half2(static_cast<uint16_t>(hi)),
-                                                       e4m3_to_half2(static_cast<uint16_t>(hi >> 16))};
-#pragma unroll
-                                for (int nt = 0; nt < NT; ++nt) mma<E4M3>(s.o[k + h][nt], f, b[i][nt][0], b[i][nt][1]);
-                            }
+                            for (int nt = 0; nt < NT; ++nt) mma<E4M3>(s.o[k][nt], f, b[i][nt][0], b[i][nt][1]);
                         }
                     }
                 }
@@ -1127,8 +1129,8 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
                 for (int k = 0; k < 8; ++k)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        const int d = E4M3 ? 16 * k + 2 * g + i : 16 * k + g + 8 * i;
-                        *reinterpret_cast<float*>(to + ((d + meet_turn<E4M3>(col)) & 127) * 4) = s.o[k][nt][2 * i + j];
+                        const int d = 16 * k + g + 8 * i;
+                        *reinterpret_cast<float*>(to + ((d + meet_turn(col)) & 127) * 4) = s.o[k][nt][2 * i + j];
                     }
             }
         fence_proxy_async();  // (the stage's next contents come by TMA)

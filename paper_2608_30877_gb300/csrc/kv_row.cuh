@@ -78,12 +78,4 @@ __device__ __forceinline__ uint32_t e4m3_to_half2(uint16_t codes) {
     return r;
 }
 
-__device__ __forceinline__ float2 half2_floats(uint32_t h) {
-    float2 r;
-    asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.f32.f16 %0, lo;\n\tcvt.f32.f16 %1, hi;\n\t}"
-        : "=f"(r.x), "=f"(r.y)
-        : "r"(h));
-    return r;
-}
-
 }  // namespace w4a16
