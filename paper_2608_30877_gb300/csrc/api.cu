@@ -408,13 +408,17 @@ int library_state(LibraryState* out) {
     return W4A16_OK;
 }
 
-int encode_3d(CUtensorMap* map, CUtensorMapDataType dtype, const void* base, const uint64_t dims[3],
-              const uint64_t strides[2], const uint32_t box[3]) {
-    const cuuint64_t d[3] = {dims[0], dims[1], dims[2]};
-    const cuuint64_t s[2] = {strides[0], strides[1]};
-    const cuuint32_t b[3] = {box[0], box[1], box[2]};
-    const cuuint32_t estr[3] = {1, 1, 1};
-    const CUresult r = g_encode(map, dtype, 3, const_cast<void*>(base), d, s, b, estr,
+int encode_5d(CUtensorMap* map, CUtensorMapDataType dtype, const void* base, const uint64_t dims[5],
+              const uint64_t strides[4], const uint32_t box[5]) {
+    cuuint64_t d[5], s[4];
+    cuuint32_t b[5];
+    for (int i = 0; i < 5; ++i) {
+        d[i] = dims[i];
+        b[i] = box[i];
+        if (i < 4) s[i] = strides[i];
+    }
+    const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+    const CUresult r = g_encode(map, dtype, 5, const_cast<void*>(base), d, s, b, estr,
                                 CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                                 CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);

@@ -92,13 +92,11 @@ __host__ __device__ inline int part_floats(int cols) { return cols * (kKvHeadDim
 __host__ __device__ inline int counter_bytes(int ctas) { return (ctas * 4 + 15) / 16 * 16; }
 
 // What the producer says about a stage.
-struct Unit {
-    int row, head, block, key0;  // the tile's first key
-    int low, len;                // keys that the row sees
-    int flags;
-    int first_cta, parts;        // of the item, with kLast
-    int page, at;                // the new token's place, with kNew
-    int pad;
+struct alignas(16) Unit {
+    int row, head, block, key0;       // the tile's first key
+    int low, len, flags;              // keys that the row sees
+    int parts, first_cta;             // of the item, with kLast
+    int page, at;                     // the new token's place, with kNew
 };
 constexpr int kFirst = 1;    // the item's first unit in this CTA
 constexpr int kLast = 2;     // and its last
@@ -236,9 +234,9 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
         : "memory");
 }
 
-// A stage holds boxes of 16 tokens' keys and values, 128 bytes of each row: in bf16 a group of
-// 16 tokens is two boxes (the halves of its rows), in e4m3 one.  Byte of 16-byte unit `unit`
-// of a tile's key row, in the 128-byte swizzle.
+// A stage holds groups of 16 tokens; in each, for each half of the rows in bf16, the keys' 128
+// bytes, then the values'.  A box is a number of groups of one page.  Byte of 16-byte unit
+// `unit` of a tile's key row, in the 128-byte swizzle.
 template <bool E4M3>
 __device__ __forceinline__ uint32_t tile_byte(int row, int unit) {
     const uint32_t box = E4M3 ? (row >> 4) * 4096u : (row >> 4) * 8192u + (unit >> 3) * 4096u;
@@ -251,11 +249,11 @@ __device__ __forceinline__ int key_at(int row, int i) {
     return 8 * i + (E4M3 ? row ^ 4 * (i & 1) : row);
 }
 // One box; completion is signalled on `bar` as transaction bytes.
-__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, uint32_t bar, int32_t c0, int32_t row) {
+__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, uint32_t bar, int32_t group) {
     asm volatile(
-        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes"
-        " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
-        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(row), "r"(0), "r"(bar)
+        "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%2, %2, %2, %2, %3}], [%4];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(group), "r"(bar)
         : "memory");
 }
 // Quotient of numbers that are not negative: in 32 bits where they fit (a 64-bit division takes
@@ -319,16 +317,20 @@ __device__ __forceinline__ int parts_of(int64_t begin, int64_t end, int64_t weig
 }
 
 template <bool E4M3>
-__device__ void produce(const DecodeArgs& a, const CUtensorMap* map, Shared& sh, uint32_t stages,
+__device__ void produce(const DecodeArgs& a, const CacheMaps& maps, Shared& sh, uint32_t stages,
                         uint32_t queries, int64_t weight, int64_t ctas, int64_t w1) {
     constexpr int kTile = E4M3 ? 128 : 64;
     const KvView& kv = a.kv;
     const int lane = threadIdx.x & 31;
-    constexpr int kHalves = E4M3 ? 1 : 2, kBoxBytes = 4096;  // of 16 tokens' keys and values
+    constexpr int kGroupBytes = kStageBytes / (kTile / 16);  // 16 tokens' keys and values
     const int items = kv.kv_heads * a.cols.blocks;        // of a row
     const int64_t width = static_cast<int64_t>(a.p.H + 2 * kv.kv_heads) * kKvHeadDim;
-    // this lane's box of a tile's eight: group of tokens, half of the row
-    const int half = lane % kHalves, box = lane / kHalves;
+    // This lane's tokens of a tile: a group of 16, or in e4m3 eight, whose exponents it copies
+    // (of a group the even lane loads the codes).
+    constexpr int kLaneTokens = E4M3 ? 8 : 16;
+    const bool has_tokens = lane < kTile / kLaneTokens, has_group = has_tokens && lane * kLaneTokens % 16 == 0;
+    const int group = lane * kLaneTokens / 16, of_box = group & (maps.groups - 1);
+    const uint8_t* const exponents = E4M3 ? kv.exponents + kv_exponent(kv, a.p.layer, 0, 0, 0, 0) : nullptr;
 
     int row = sh.start_row;
     int64_t base = sh.start_base;
@@ -371,6 +373,7 @@ __device__ void produce(const DecodeArgs& a, const CUtensorMap* map, Shared& sh,
     int st = 0;
     uint32_t phase = 0;       // of the stage's barriers
     int64_t issued = 0;
+    bool cut = rest > 0;      // the item began in another CTA
     if (item == items) {  // (a bound moved to the end of the row)
         find_next();
         item = tile = 0;
@@ -385,6 +388,8 @@ __device__ void produce(const DecodeArgs& a, const CUtensorMap* map, Shared& sh,
         record_status(kv.status, kInvalid);
         return;
     }
+    int head = item / a.cols.blocks, block = item - head * a.cols.blocks;
+    int64_t begin = base + static_cast<int64_t>(item) * r.weight;  // of the item
     int ids_from = ((r.first + tile) * kTile) >> kv.page_shift;
     int ids = load_ids(r, ids_from), ids_first = load_ids(r, first_entry(r)), ids_after = load_ids(r, ids_from + 32);
     for (; more; ++issued) {
@@ -412,40 +417,56 @@ __device__ void produce(const DecodeArgs& a, const CUtensorMap* map, Shared& sh,
             ids_from += 32;
             ids_after = load_ids(r, ids_from + 32);
         }
-        const int head = item / a.cols.blocks, block = item - head * a.cols.blocks;
         const uint32_t bar = smem_u32(&sh.full[st]);
-        // The boxes with tokens that the row sees.  (Boxes of a whole page, with fewer to
-        // issue, brought 5% more for a row of 600 tokens in pages of 64.)
-        const int key = key0 + box * 16;  // of this lane's box
-        const bool mine = lane < 8 && key < r.len && key + 16 > r.low;
+        // The groups that the row sees, by boxes as large as a page allows, or each by itself at
+        // the row's ends.
+        const int key = key0 + lane * kLaneTokens;  // of this lane's tokens
         const int id = __shfl_sync(0xffffffffu, ids, ((key >> kv.page_shift) - ids_from) & 31);
         const bool id_ok = id >= 0 && id < kv.num_pages;
-        const bool tile_bad = __any_sync(0xffffffffu, mine && !id_ok);
-        const int loads = __popc(__ballot_sync(0xffffffffu, mine));
-        if (mine) {
-            const int32_t at = key & ((1 << kv.page_shift) - 1);
-            const int32_t row_at = (((id_ok ? id : 0) * kv.kv_heads + head) << kv.page_shift) + at;
-            const uint32_t dst = stages + st * kStageBytes + lane * kBoxBytes;
-            if (dbg_check(tma_box_ok(dst, kBoxBytes, 1024, stages, stages + kStages * kStageBytes, half * 64,
-                                     E4M3 ? 1 : 2), kv.status))
-                load_box(dst, map, bar, half * 64, row_at);
+        const int32_t row_at = (((id_ok ? id : 0) * kv.kv_heads + head) << kv.page_shift) +
+                               (key & ((1 << kv.page_shift) - 1));
+        const bool mine = has_group && key < r.len && key + 16 > r.low;
+        const bool whole = mine && key - (of_box - 1) * 16 > r.low && key + (maps.groups - 1 - of_box) * 16 < r.len;
+        if (mine && (!whole || of_box == 0)) {
+            const uint32_t dst = stages + st * kStageBytes + group * kGroupBytes;
+            const int box_bytes = whole ? maps.groups * kGroupBytes : kGroupBytes;
+            if (dbg_check(tma_box_ok(dst, box_bytes, 1024, stages, stages + kStages * kStageBytes, 0, 1), kv.status))
+                load_box(dst, whole ? &maps.box : &maps.group, bar, row_at >> 4);
         }
-        const int q_cols = min(a.cols.block, a.cols.group - block * a.cols.block);
+        if constexpr (E4M3) {  // (key, value) exponents; every lane arrives
+            if (has_tokens && key < r.len && key + 8 > r.low)
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(
+                                 smem_u32(&sh.exponents[st][lane * 16])),
+                             "l"(exponents + 2 * static_cast<int64_t>(row_at))
+                             : "memory");
+            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+        }
+        const int loads = __popc(__ballot_sync(0xffffffffu, mine));
+        const bool tile_bad = __any_sync(0xffffffffu, mine && !id_ok);
+        uint32_t bytes = loads * kGroupBytes;
         const uint16_t* const qkv = a.p.qkv + row * width;
-        if (first)
+        if (first) {
+            const int q_cols = min(a.cols.block, a.cols.group - block * a.cols.block);
             for (int i = lane; i < q_cols; i += 32)
                 bulk_load(queries + (slot * a.cols.block + i) * kQueryStride,
                           qkv + (static_cast<int64_t>(head) * a.cols.group + block * a.cols.block + i) * kKvHeadDim,
                           256, bar);
+            bytes += q_cols * 256;
+        }
         const bool fresh = key0 + kTile >= r.len;
-        if (fresh && lane < 2)
-            bulk_load(smem_u32(sh.fresh[st][lane]),
-                      qkv + (a.p.H + lane * kv.kv_heads + head) * static_cast<int64_t>(kKvHeadDim), 256, bar);
-        const int last_id = __shfl_sync(0xffffffffu, ids, (((r.len - 1) >> kv.page_shift) - ids_from) & 31);
+        int page = -1;
+        if (fresh) {
+            if (lane < 2)
+                bulk_load(smem_u32(sh.fresh[st][lane]),
+                          qkv + (a.p.H + lane * kv.kv_heads + head) * static_cast<int64_t>(kKvHeadDim), 256, bar);
+            bytes += 512;
+            page = __shfl_sync(0xffffffffu, ids, (((r.len - 1) >> kv.page_shift) - ids_from) & 31);
+            if (page >= kv.num_pages) page = -1;
+        }
         // whether the item goes on in this CTA, and the CTA after it
-        const int64_t begin = base + static_cast<int64_t>(item) * r.weight;
-        const bool last = tile + 1 == r.tiles || begin + tile_start<E4M3>(r, tile + 1) >= w1;
-        more = !last || (tile + 1 == r.tiles && begin + r.weight < w1);
+        const bool ends = begin + r.weight <= w1;
+        const bool last = tile + 1 == r.tiles || (!ends && begin + tile_start<E4M3>(r, tile + 1) >= w1);
+        more = !last || begin + r.weight < w1;
         if (lane == 0) {
             Unit& t = sh.unit[st];
             t.row = row;
@@ -456,27 +477,15 @@ __device__ void produce(const DecodeArgs& a, const CUtensorMap* map, Shared& sh,
             t.len = r.len;
             t.flags = (first ? kFirst : 0) | (last ? kLast : 0) | (fresh ? kNew : 0) | (tile_bad ? kBad : 0) |
                       (more ? 0 : kEnd) | slot << kQSlotShift;
-            if (last) t.parts = parts_of(begin, begin + r.weight, weight, ctas, a.snap, &t.first_cta);
-            t.page = last_id >= 0 && last_id < kv.num_pages ? last_id : -1;
+            t.parts = 1;
+            t.first_cta = 0;
+            if (last && (cut || !ends)) t.parts = parts_of(begin, begin + r.weight, weight, ctas, a.snap, &t.first_cta);
+            t.page = page;
             t.at = (r.len - 1) & ((1 << kv.page_shift) - 1);
             // (after the copies: the phase waits for this arrival)
-            mbar_arrive_expect_tx(bar, loads * kBoxBytes + (first ? q_cols * 256u : 0u) + (fresh ? 512u : 0u));
+            mbar_arrive_expect_tx(bar, bytes);
         }
         __syncwarp();
-        if constexpr (E4M3) {
-            // (key, value) exponents, eight tokens to a lane; every lane arrives
-            const int k8 = key0 + lane * 8;
-            const int id8 = __shfl_sync(0xffffffffu, ids, ((k8 >> kv.page_shift) - ids_from) & 31);
-            if (lane < kTile / 8 && k8 < r.len && k8 + 8 > r.low) {
-                const int64_t from = kv_exponent(kv, a.p.layer, 0, id8 >= 0 && id8 < kv.num_pages ? id8 : 0, head,
-                                                 k8 & ((1 << kv.page_shift) - 1));
-                asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(
-                                 smem_u32(&sh.exponents[st][lane * 16])),
-                             "l"(kv.exponents + from)
-                             : "memory");
-            }
-            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
-        }
         if (issued == 0 && !short_limit_ok(bar, 0, &sh.abort, kv.status, a.p.wait_ns)) {
             ++issued;
             break;
@@ -491,6 +500,12 @@ __device__ void produce(const DecodeArgs& a, const CUtensorMap* map, Shared& sh,
         if (++tile == r.tiles) {
             tile = 0;
             slot ^= 1;
+            cut = false;
+            begin += r.weight;
+            if (++block == a.cols.blocks) {
+                block = 0;
+                ++head;
+            }
             if (++item == items && more) {
                 if (next_index == kUnknown) find_next();
                 if (next_index == kNone) {  // (only if the lengths changed during the call)
@@ -499,8 +514,7 @@ __device__ void produce(const DecodeArgs& a, const CUtensorMap* map, Shared& sh,
                     ++issued;
                     break;
                 }
-                item = 0;
-                base += static_cast<int64_t>(items) * r.weight;
+                item = head = 0;
                 row = next_index;
                 r = next;
                 next_index = kUnknown;
@@ -1147,7 +1161,7 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
 
 template <bool E4M3, int NT, bool ONE>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm)
-    attention_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ DecodeArgs a) {
+    attention_decode_kernel(const __grid_constant__ CacheMaps maps, const __grid_constant__ DecodeArgs a) {
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ Shared sh;
     // (the dynamic part starts past the static one: rounded up to the swizzle's 1024 bytes)
@@ -1156,7 +1170,8 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
     uint8_t* const query_mem = stage_mem + kStages * kStageBytes;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (tid == 0) {
-        prefetch_tmap(&map);
+        prefetch_tmap(&maps.box);
+        prefetch_tmap(&maps.group);
         for (int i = 0; i < kStages; ++i) {
             mbar_init(smem_u32(&sh.full[i]), E4M3 ? 33 : 1);
             mbar_init(smem_u32(&sh.empty[i]), kWarps + 1);
@@ -1264,7 +1279,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
     __syncthreads();
     if (sh.bound[0] == sh.bound[1]) return;
     if (warp == 0)
-        produce<E4M3>(a, &map, sh, smem_u32(stage_mem), smem_u32(query_mem), weight, ctas, sh.bound[1]);
+        produce<E4M3>(a, maps, sh, smem_u32(stage_mem), smem_u32(query_mem), weight, ctas, sh.bound[1]);
     else if (warp <= kWarps)
         consume<E4M3, NT, ONE>(a, sh, stage_mem, query_mem);
     else
@@ -1272,12 +1287,12 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
 }
 
 template <bool E4M3, int NT, bool ONE>
-cudaError_t launch(const CUtensorMap& map, const DecodeArgs& a, int grid, cudaStream_t stream) {
+cudaError_t launch(const CacheMaps& maps, const DecodeArgs& a, int grid, cudaStream_t stream) {
     auto kern = attention_decode_kernel<E4M3, NT, ONE>;
     const int bytes = 1024 + kStages * kStageBytes + 2 * a.cols.block * kQueryStride;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != cudaSuccess) return e;
-    return launch_overlapped(kern, grid, kThreads, bytes, stream, map, a);
+    return launch_overlapped(kern, grid, kThreads, bytes, stream, maps, a);
 }
 
 }  // namespace
@@ -1288,17 +1303,25 @@ int64_t decode_workspace_bytes(int H, int kv_heads, int sm_count) {
     return counter_bytes(static_cast<int>(ctas)) + ctas * 2 * part_floats(used_columns(H / kv_heads)) * 4;
 }
 
-int encode_cache(CUtensorMap* map, const KvView& kv, int layer) {
+int encode_cache(CacheMaps* maps, const KvView& kv, int layer) {
     const bool e4m3 = kv.exponents != nullptr;
-    const uint64_t rows = static_cast<uint64_t>(kv.num_pages) * kv.kv_heads << kv.page_shift;
-    const uint64_t dims[3] = {kKvHeadDim, rows, 2};
-    const uint64_t strides[2] = {static_cast<uint64_t>(kv.row_bytes), rows * kv.row_bytes};
-    const uint32_t box[3] = {e4m3 ? 128u : 64u, 16, 2};
-    return encode_3d(map, e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
-                     kv.pages + 2 * rows * kv.row_bytes * layer, dims, strides, box);
+    const uint64_t row = kv.row_bytes, groups = (static_cast<uint64_t>(kv.num_pages) * kv.kv_heads << kv.page_shift) / 16;
+    const uint32_t halves = e4m3 ? 1 : 2, tile_groups = e4m3 ? 8 : 4, page_groups = (1u << kv.page_shift) / 16;
+    maps->groups = static_cast<int>(page_groups < tile_groups ? page_groups : tile_groups);
+    // elements of half a row, the rows of a group, keys and values, halves, groups
+    const uint64_t dims[5] = {row / halves / (e4m3 ? 1 : 2), 16, 2, halves, groups};
+    const uint64_t strides[4] = {row, groups * 16 * row, row / halves, 16 * row};
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t box[5] = {static_cast<uint32_t>(dims[0]), 16, 2, halves, i == 0 ? static_cast<uint32_t>(maps->groups) : 1u};
+        const int rc = encode_5d(i == 0 ? &maps->box : &maps->group,
+                                 e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
+                                 kv.pages + 2 * groups * 16 * row * layer, dims, strides, box);
+        if (rc != 0) return rc;
+    }
+    return 0;
 }
 
-cudaError_t launch_attention_decode(const CUtensorMap& map, const KvView& kv, const DecodeParams& p, int sm_count,
+cudaError_t launch_attention_decode(const CacheMaps& maps, const KvView& kv, const DecodeParams& p, int sm_count,
                                     cudaStream_t stream) {
     DecodeArgs a{kv, p, columns_of(p.H / kv.kv_heads), p.window, 0, 0, 0};
     const int grid = sm_count * kCtasPerSm;
@@ -1308,9 +1331,9 @@ cudaError_t launch_attention_decode(const CUtensorMap& map, const KvView& kv, co
     a.item_weight = e4m3 ? 12 : wide ? 8 : 5;
     a.snap = a.item_weight + (e4m3 ? 12 : 10);
     a.grid_reciprocal = ~uint64_t{0} / grid + 1;
-    if (p.H == kv.kv_heads) return e4m3 ? launch<true, 1, true>(map, a, grid, stream) : launch<false, 1, true>(map, a, grid, stream);
-    if (wide) return e4m3 ? launch<true, 2, false>(map, a, grid, stream) : launch<false, 2, false>(map, a, grid, stream);
-    return e4m3 ? launch<true, 1, false>(map, a, grid, stream) : launch<false, 1, false>(map, a, grid, stream);
+    if (p.H == kv.kv_heads) return e4m3 ? launch<true, 1, true>(maps, a, grid, stream) : launch<false, 1, true>(maps, a, grid, stream);
+    if (wide) return e4m3 ? launch<true, 2, false>(maps, a, grid, stream) : launch<false, 2, false>(maps, a, grid, stream);
+    return e4m3 ? launch<true, 1, false>(maps, a, grid, stream) : launch<false, 1, false>(maps, a, grid, stream);
 }
 
 }  // namespace w4a16

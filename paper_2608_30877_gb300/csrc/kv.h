@@ -14,8 +14,8 @@ struct LibraryState {
     int* status;  // device status word
 };
 int library_state(LibraryState* out);
-int encode_3d(CUtensorMap* map, CUtensorMapDataType dtype, const void* base, const uint64_t dims[3],
-              const uint64_t strides[2], const uint32_t box[3]);
+int encode_5d(CUtensorMap* map, CUtensorMapDataType dtype, const void* base, const uint64_t dims[5],
+              const uint64_t strides[4], const uint32_t box[5]);
 
 constexpr int kKvHeadDim = 128;
 constexpr int kKvMaxSlots = 1 << 16;
@@ -72,9 +72,14 @@ struct DecodeParams {
     uint64_t wait_ns;
 };
 int64_t decode_workspace_bytes(int H, int kv_heads, int sm_count);
-// One layer's keys and values as rows, in boxes of 16 rows of both, 128 bytes wide.
-int encode_cache(CUtensorMap* map, const KvView& kv, int layer);
-cudaError_t launch_attention_decode(const CUtensorMap& map, const KvView& kv, const DecodeParams& p,
+// Tensor maps of a layer's keys and values: of a page's groups of 16 tokens, or as many as a tile
+// has, and of one group.
+struct CacheMaps {
+    CUtensorMap box, group;
+    int groups;  // of `box`: a power of two
+};
+int encode_cache(CacheMaps* maps, const KvView& kv, int layer);
+cudaError_t launch_attention_decode(const CacheMaps& maps, const KvView& kv, const DecodeParams& p,
                                     int sm_count, cudaStream_t stream);
 
 uint64_t wait_limit_ns();  // internal.h

@@ -242,8 +242,8 @@ extern "C" int w4a16_attention_decode(const w4a16_kv_cache* cache, int64_t layer
     p.scale = 1.0f / sqrtf(static_cast<float>(kKvHeadDim));
     p.wait_ns = wait_limit_ns();
     const KvView view = view_of(*cache, st.status);
-    alignas(64) CUtensorMap map;
-    rc = encode_cache(&map, view, p.layer);
+    CacheMaps maps;
+    rc = encode_cache(&maps, view, p.layer);
     if (rc != W4A16_OK) return rc;
-    return status_of(launch_attention_decode(map, view, p, st.sm_count, static_cast<cudaStream_t>(stream)));
+    return status_of(launch_attention_decode(maps, view, p, st.sm_count, static_cast<cudaStream_t>(stream)));
 }
