@@ -22,8 +22,10 @@
 //    leaves them in its own rows of the stage that it read last and goes on, and a sixth
 //    warp adds them up, stores the result and releases the stage (with the four warps doing
 //    that together, they stood still 1 us per item).
-//  * More than 16 queries of a key head: the warps split the columns instead of the keys, up
-//    to 64, then further items.
+//  * More than 8 queries of a key head: the warps split the columns before the keys, up to 32
+//    columns, then further items.  (16 columns in a warp passed the registers' limit on the 8-bit
+//    cache: 12 queries of a head 86 us, and 69 with 8; in bf16 100 either way, 32 queries 71
+//    and 75, 64 queries 80 and 74.)
 //  * Join.  A CTA's first and last items may continue in other CTAs: each then writes its
 //    part to the workspace, and when all its work is done counts itself present for both
 //    (one fence and one round trip for the two).  The last CTA of an item, found by a counter
@@ -54,7 +56,7 @@ constexpr int kStages = 3;
 constexpr int kStageBytes = 32768;           // a tile's keys and values
 constexpr int kWarpBytes = kStageBytes / kWarps;
 constexpr int kValueOffset = 2048;           // from 16 keys' rows of 128 bytes to their values'
-constexpr int kMaxCols = 64;                 // query columns of an item
+constexpr int kMaxCols = 32;                 // query columns of an item: eight a warp
 constexpr int kQueryStride = 272;            // bytes between rows of q, on other banks
 constexpr int kCtasPerSm = 2;
 constexpr int kInvalid = 1;                  // W4A16_ERR_INVALID_ARG
@@ -70,16 +72,16 @@ constexpr float kLeast = -3.0e38f;
 // How the queries of a key head (the group) are laid over columns and warps.
 struct Columns {
     int group;  // queries of a key head
-    int block;  // columns of an item: 8, 16, 32 or 64
+    int block;  // columns of an item: 8, 16 or 32
     int blocks; // items of a key head
     int warps;  // warps side by side in the columns: 1, 2 or 4
 };
-__host__ __device__ inline Columns columns_of(int group) {
+inline Columns columns_of(int group) {
     Columns c;
     c.group = group;
-    c.block = group <= 8 ? 8 : group <= 16 ? 16 : group <= 32 ? 32 : kMaxCols;
+    c.block = group <= 8 ? 8 : group <= 16 ? 16 : kMaxCols;
     c.blocks = (group + c.block - 1) / c.block;
-    c.warps = c.block <= 16 ? 1 : c.block / 16;
+    c.warps = c.block / 8;
     return c;
 }
 __host__ __device__ inline int used_columns(int group) { return group < kMaxCols ? group : kMaxCols; }
@@ -655,7 +657,7 @@ __device__ __noinline__ void join_pending(const float* parts, uint16_t* out, int
 }
 
 // The finisher: follows the stages, and at an item's end adds up what the warps left there.
-template <bool E4M3, int NT>
+template <bool E4M3>
 __device__ void finish(const DecodeArgs& a, Shared& sh, const uint8_t* stage_mem) {
     const KvView& kv = a.kv;
     const int lane = threadIdx.x & 31;
@@ -680,7 +682,7 @@ __device__ void finish(const DecodeArgs& a, Shared& sh, const uint8_t* stage_mem
             uint16_t* const out = output_of(a, t.row, t.head, t.block);
 #pragma unroll 2
             for (int col = 0; col < cols; ++col) {
-                const int cw = col / (8 * NT), in = col - cw * 8 * NT, turned = (4 * lane + meet_turn(in)) & 127;
+                const int cw = col / 8, in = col % 8, turned = (4 * lane + meet_turn(in)) & 127;
                 float4 x[kWarps];
                 float ls[kWarps], ms[kWarps], ws[kWarps];
 #pragma unroll
@@ -803,15 +805,14 @@ __device__ __forceinline__ void mend_tile(const DecodeArgs& a, Shared& sh, int s
     __syncwarp();
 }
 
-// The running softmax of a warp: two columns a thread in each of NT tiles of eight.
-template <int NT>
+// The running softmax of a warp's eight columns: two a thread.
 struct State {
-    float m[NT][2], l[NT][2], o[8][NT][4];
-    float w[NT][2];  // e4m3: the largest score and value's exponent, which o is relative to
-    bool bad;        // a page index was out of range
+    float m[2], l[2], o[8][4];
+    float w[2];  // e4m3: the largest score and value's exponent, which o is relative to
+    bool bad;    // a page index was out of range
 };
 
-template <bool E4M3, int NT, bool ONE>
+template <bool E4M3, bool ONE>
 __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uint8_t* query_mem) {
     constexpr int kTile = E4M3 ? 128 : 64;
     constexpr int kStep = kTile / kWarps, kGroups = kStep / 16, kRows = 2 * kGroups;  // a warp's keys at a time
@@ -842,56 +843,49 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
     };
     for (;;) {  // an item
         if (!wait()) return;
-        State<NT> s;
-        uint32_t q[8][NT][2];
-        float q_scale[NT][2];  // e4m3: of this thread's columns, the softmax's scale and that of q
+        State s;
+        uint32_t q[8][2];
+        float q_scale[2];  // e4m3: of this thread's columns, the softmax's scale and that of q
         // Q as the B operand: column g of a tile of eight, in the order of K's dimensions
-        const uint8_t* rows = query_mem + (sh.unit[st].flags >> kQSlotShift & 1) * a.cols.block * kQueryStride;
+        const uint8_t* const row = query_mem + ((sh.unit[st].flags >> kQSlotShift & 1) * a.cols.block +
+                                                (ONE ? 0 : col_warp * 8 + g)) * kQueryStride;
+        if constexpr (!E4M3) {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const uint8_t* row = rows + (ONE ? 0 : col_warp * 8 * NT + nt * 8 + g) * kQueryStride;
-            if constexpr (!E4M3) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    q[k][nt][0] = *reinterpret_cast<const uint32_t*>(row + k * 32 + c * 4);
-                    q[k][nt][1] = *reinterpret_cast<const uint32_t*>(row + k * 32 + 16 + c * 4);
-                }
-            } else {
-                uint2 v[8];
-                float top = 0.0f;
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    v[k] = *reinterpret_cast<const uint2*>(row + k * 32 + c * 8);
-                    top = fmaxf(top, fmaxf(fmaxf(finite_abs(bf16_lo(v[k].x)), finite_abs(bf16_hi(v[k].x))),
-                                           fmaxf(finite_abs(bf16_lo(v[k].y)), finite_abs(bf16_hi(v[k].y)))));
-                }
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                const int e = e4m3_row_exponent(top);
-                const float f = power_of_two(-e);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const float x[4] = {bf16_lo(v[k].x) * f, bf16_hi(v[k].x) * f, bf16_lo(v[k].y) * f,
-                                        bf16_hi(v[k].y) * f};
-                    q[k][nt][0] = half_pair(x[0], x[1]);
-                    q[k][nt][1] = half_pair(x[2], x[3]);
-                }
-                // (column g's scale is needed by the threads of columns 2c and 2c + 1)
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    q_scale[nt][j] = scale * power_of_two(__shfl_sync(0xffffffffu, e, (2 * c + j) * 4));
+            for (int k = 0; k < 8; ++k) {
+                q[k][0] = *reinterpret_cast<const uint32_t*>(row + k * 32 + c * 4);
+                q[k][1] = *reinterpret_cast<const uint32_t*>(row + k * 32 + 16 + c * 4);
             }
+        } else {
+            uint2 v[8];
+            float top = 0.0f;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                v[k] = *reinterpret_cast<const uint2*>(row + k * 32 + c * 8);
+                top = fmaxf(top, fmaxf(fmaxf(finite_abs(bf16_lo(v[k].x)), finite_abs(bf16_hi(v[k].x))),
+                                       fmaxf(finite_abs(bf16_lo(v[k].y)), finite_abs(bf16_hi(v[k].y)))));
+            }
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            const int e = e4m3_row_exponent(top);
+            const float f = power_of_two(-e);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float x[4] = {bf16_lo(v[k].x) * f, bf16_hi(v[k].x) * f, bf16_lo(v[k].y) * f,
+                                    bf16_hi(v[k].y) * f};
+                q[k][0] = half_pair(x[0], x[1]);
+                q[k][1] = half_pair(x[2], x[3]);
+            }
+            // (column g's scale is needed by the threads of columns 2c and 2c + 1)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                q_scale[j] = scale * power_of_two(__shfl_sync(0xffffffffu, e, (2 * c + j) * 4));
         }
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) s.m[nt][j] = s.w[nt][j] = kLeast, s.l[nt][j] = 0.0f;
+        for (int j = 0; j < 2; ++j) s.m[j] = s.w[j] = kLeast, s.l[j] = 0.0f;
 #pragma unroll
         for (int k = 0; k < 8; ++k)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) s.o[k][nt][j] = 0.0f;
+            for (int j = 0; j < 4; ++j) s.o[k][j] = 0.0f;
         s.bad = false;
         int flags;
         uint8_t* tile;
@@ -911,20 +905,17 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
                 const int key = key0 + step * kStep;
                 if (key >= len || key + kStep <= low) continue;
                 // scores of the step's matrices of 8 keys: row g, columns 2c and 2c + 1
-                float acc[2][NT][4];  // e4m3: of two groups; bf16: of even and odd dimensions
+                float acc[2][4];  // e4m3: of two groups; bf16: of even and odd dimensions
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) acc[i][nt][j] = 0.0f;
+                    for (int j = 0; j < 4; ++j) acc[i][j] = 0.0f;
                 if constexpr (!E4M3) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
                         uint32_t f[4];
                         ldsm_x4(((keys + key_off + step * kWarpBytes) ^ ((k & 3) << 5)) + (k >> 2) * 4096, f);
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) mma<E4M3>(acc[k & 1][nt], f, q[k][nt][0], q[k][nt][1]);
+                        mma<E4M3>(acc[k & 1], f, q[k][0], q[k][1]);
                     }
                 } else {
 #pragma unroll
@@ -936,14 +927,12 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
 #pragma unroll
                             for (int h = 0; h < 2; ++h) {
                                 codes_to_halves(w[2 * h], w[2 * h + 1], f);
-#pragma unroll
-                                for (int nt = 0; nt < NT; ++nt)
-                                    mma<E4M3>(acc[i][nt], f, q[k + h][nt][0], q[k + h][nt][1]);
+                                mma<E4M3>(acc[i], f, q[k + h][0], q[k + h][1]);
                             }
                         }
                 }
                 constexpr float kSlack = E4M3 ? kSlackE4m3 : kSlackBf16;
-                uint32_t b[kGroups][NT][2];
+                uint32_t b[kGroups][2];
                 // a column's maximum over its lanes, if that passes what it was; the factor for what
                 // is relative to the old one
                 auto raise = [&](float v, float& was) {
@@ -962,49 +951,49 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
                     // One query, the same in every column: lane (g, c) has row g of all matrices, and
                     // takes that of matrix c (bf16: c % 2, in two lanes alike).
                     const int r = c % kRows, in = key_at<E4M3>(g, r), at = key + in;
-                    float x = acc[0][0][0] + (E4M3 ? 0.0f : acc[1][0][0]);
-                    const float x1 = acc[0][0][2] + (E4M3 ? 0.0f : acc[1][0][2]);
+                    float x = acc[0][0] + (E4M3 ? 0.0f : acc[1][0]);
+                    const float x1 = acc[0][2] + (E4M3 ? 0.0f : acc[1][2]);
                     if (r == 1) x = x1;
-                    if (E4M3 && r == 2) x = acc[1][0][0];
-                    if (E4M3 && r == 3) x = acc[1][0][2];
+                    if (E4M3 && r == 2) x = acc[1][0];
+                    if (E4M3 && r == 3) x = acc[1][2];
                     float y = 0.0f;
                     if constexpr (E4M3) {
                         const uint32_t e =
                             *reinterpret_cast<const uint16_t*>(sh.exponents[st] + (step * kStep + in) * 2);
-                        x *= __uint_as_float((e & 0xFFu) << 23) * q_scale[0][0];
+                        x *= __uint_as_float((e & 0xFFu) << 23) * q_scale[0];
                         y = static_cast<float>(static_cast<int>(e >> 8) - 127);
                     } else {
                         x *= scale;
                     }
                     if (edge && (at < low || at >= len)) x = -INFINITY;
                     y += x;
-                    if (__any_sync(0xffffffffu, x > s.m[0][0] + kSlack || (E4M3 && y > s.w[0][0] + kSlack))) {
-                        float f = raise(x, s.m[0][0]);
-                        s.l[0][0] *= f;
-                        if constexpr (E4M3) f = raise(y, s.w[0][0]);
+                    if (__any_sync(0xffffffffu, x > s.m[0] + kSlack || (E4M3 && y > s.w[0] + kSlack))) {
+                        float f = raise(x, s.m[0]);
+                        s.l[0] *= f;
+                        if constexpr (E4M3) f = raise(y, s.w[0]);
 #pragma unroll
                         for (int k = 0; k < 8; ++k) {
-                            s.o[k][0][0] *= f;
-                            s.o[k][0][2] *= f;
+                            s.o[k][0] *= f;
+                            s.o[k][2] *= f;
                         }
                     }
-                    float p = ex2(x - s.m[0][0]);
+                    float p = ex2(x - s.m[0]);
                     if constexpr (E4M3) {
-                        s.l[0][0] += p;
-                        p = ex2(y - s.w[0][0] + kWeightTop);
+                        s.l[0] += p;
+                        p = ex2(y - s.w[0] + kWeightTop);
                     } else {
                         // (the rounded weights' sum, so that they add up to one)
-                        s.l[0][0] += bf16_lo(bf16_pair(p, 0.0f));
+                        s.l[0] += bf16_lo(bf16_pair(p, 0.0f));
                     }
                     // rows g and g + 1 in the lanes of even g, then rows 2c and 2c + 1 everywhere
                     const float next = __shfl_xor_sync(0xffffffffu, p, 4);
                     const uint32_t pair = E4M3 ? half_pair(p, next) : bf16_pair(p, next);
 #pragma unroll
-                    for (int i = 0; i < kRows; ++i) b[i >> 1][0][i & 1] = __shfl_sync(0xffffffffu, pair, 8 * c + i);
+                    for (int i = 0; i < kRows; ++i) b[i >> 1][i & 1] = __shfl_sync(0xffffffffu, pair, 8 * c + i);
                 } else {
                     // row g of each matrix, as it comes out of the products: e4m3 with the keys'
                     // exponents, before the columns' factors
-                    float x[NT][kRows][2], value_exp[kRows] = {};
+                    float x[kRows][2], value_exp[kRows] = {};
 #pragma unroll
                     for (int i = 0; i < kRows; ++i) {
                         float key_scale = 1.0f;
@@ -1015,88 +1004,77 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
                             value_exp[i] = static_cast<float>(static_cast<int>(e >> 8) - 127);
                         }
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int j = 0; j < 2; ++j)
-                                x[nt][i][j] = E4M3 ? acc[i >> 1][nt][(i & 1) * 2 + j] * key_scale
-                                                   : acc[0][nt][i * 2 + j] + acc[1][nt][i * 2 + j];
+                        for (int j = 0; j < 2; ++j)
+                            x[i][j] = E4M3 ? acc[i >> 1][(i & 1) * 2 + j] * key_scale
+                                           : acc[0][i * 2 + j] + acc[1][i * 2 + j];
                     }
                     if (edge) {
 #pragma unroll
                         for (int i = 0; i < kRows; ++i) {
                             const int at = key + key_at<E4M3>(g, i);
                             if (at >= low && at < len) continue;
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) x[nt][i][0] = x[nt][i][1] = -INFINITY;
+                            x[i][0] = x[i][1] = -INFINITY;
                         }
                     }
-                    auto factor = [&](int nt, int j) { return E4M3 ? q_scale[nt][j] : scale; };
+                    auto factor = [&](int j) { return E4M3 ? q_scale[j] : scale; };
                     // this thread's largest score of a column, and with the value's exponent
-                    auto largest = [&](int nt, int j) {
-                        float v = x[nt][0][j];
+                    auto largest = [&](int j) {
+                        float v = x[0][j];
 #pragma unroll
-                        for (int i = 1; i < kRows; ++i) v = fmaxf(v, x[nt][i][j]);
-                        return v * factor(nt, j);
+                        for (int i = 1; i < kRows; ++i) v = fmaxf(v, x[i][j]);
+                        return v * factor(j);
                     };
-                    auto largest_value = [&](int nt, int j) {
-                        float v = fmaf(x[nt][0][j], factor(nt, j), value_exp[0]);
+                    auto largest_value = [&](int j) {
+                        float v = fmaf(x[0][j], factor(j), value_exp[0]);
 #pragma unroll
-                        for (int i = 1; i < kRows; ++i) v = fmaxf(v, fmaf(x[nt][i][j], factor(nt, j), value_exp[i]));
+                        for (int i = 1; i < kRows; ++i) v = fmaxf(v, fmaf(x[i][j], factor(j), value_exp[i]));
                         return v;
                     };
                     bool over = false;
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            over |= largest(nt, j) > s.m[nt][j] + kSlack;
-                            if constexpr (E4M3) over |= largest_value(nt, j) > s.w[nt][j] + kSlack;
-                        }
+                    for (int j = 0; j < 2; ++j) {
+                        over |= largest(j) > s.m[j] + kSlack;
+                        if constexpr (E4M3) over |= largest_value(j) > s.w[j] + kSlack;
+                    }
                     if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
+                        for (int j = 0; j < 2; ++j) {
+                            float f = raise(largest(j), s.m[j]);
+                            s.l[j] *= f;
+                            if constexpr (E4M3) f = raise(largest_value(j), s.w[j]);
 #pragma unroll
-                            for (int j = 0; j < 2; ++j) {
-                                float f = raise(largest(nt, j), s.m[nt][j]);
-                                s.l[nt][j] *= f;
-                                if constexpr (E4M3) f = raise(largest_value(nt, j), s.w[nt][j]);
-#pragma unroll
-                                for (int k = 0; k < 8; ++k) {
-                                    s.o[k][nt][j] *= f;
-                                    s.o[k][nt][j + 2] *= f;
-                                }
+                            for (int k = 0; k < 8; ++k) {
+                                s.o[k][j] *= f;
+                                s.o[k][j + 2] *= f;
                             }
+                        }
                     }
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                    for (int i = 0; i < kRows; ++i) {
+                        float p[2];
 #pragma unroll
-                        for (int i = 0; i < kRows; ++i) {
-                            float p[2];
-#pragma unroll
-                            for (int j = 0; j < 2; ++j) {
-                                p[j] = ex2(fmaf(x[nt][i][j], factor(nt, j), -s.m[nt][j]));
-                                if constexpr (E4M3) {
-                                    s.l[nt][j] += p[j];
-                                    p[j] = ex2(fmaf(x[nt][i][j], factor(nt, j), value_exp[i]) +
-                                               (kWeightTop - s.w[nt][j]));
-                                }
+                        for (int j = 0; j < 2; ++j) {
+                            p[j] = ex2(fmaf(x[i][j], factor(j), -s.m[j]));
+                            if constexpr (E4M3) {
+                                s.l[j] += p[j];
+                                p[j] = ex2(fmaf(x[i][j], factor(j), value_exp[i]) + (kWeightTop - s.w[j]));
                             }
-                            const uint32_t w = E4M3 ? half_pair(p[0], p[1]) : bf16_pair(p[0], p[1]);
-                            if constexpr (!E4M3) {  // (the rounded weights' sum, so that they add up to one)
-                                s.l[nt][0] += bf16_lo(w);
-                                s.l[nt][1] += bf16_hi(w);
-                            }
-                            // rows 2c, 2c + 1 of column g: the transpose of what this thread holds
-                            b[i >> 1][nt][i & 1] = transpose_8x8(w);
                         }
+                        const uint32_t w = E4M3 ? half_pair(p[0], p[1]) : bf16_pair(p[0], p[1]);
+                        if constexpr (!E4M3) {  // (the rounded weights' sum, so that they add up to one)
+                            s.l[0] += bf16_lo(w);
+                            s.l[1] += bf16_hi(w);
+                        }
+                        // rows 2c, 2c + 1 of column g: the transpose of what this thread holds
+                        b[i >> 1][i & 1] = transpose_8x8(w);
+                    }
                 }
                 if constexpr (!E4M3) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
                         uint32_t f[4];
                         ldsm_x4_trans(((values + value_off + step * kWarpBytes) ^ ((k & 3) << 5)) + (k >> 2) * 4096, f);
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) mma<E4M3>(s.o[k][nt], f, b[0][nt][0], b[0][nt][1]);
+                        mma<E4M3>(s.o[k], f, b[0][0], b[0][1]);
                     }
                 } else {
 #pragma unroll
@@ -1106,8 +1084,7 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
 #pragma unroll
                         for (int i = 0; i < kGroups; ++i) {
                             codes_to_halves(w[2 * i], w[2 * i + 1], f);
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) mma<E4M3>(s.o[k][nt], f, b[i][nt][0], b[i][nt][1]);
+                            mma<E4M3>(s.o[k], f, b[i][0], b[i][1]);
                         }
                     }
                 }
@@ -1119,34 +1096,32 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
         // what this warp has of the item, into its rows of the stage
         if (a.cols.warps > 1 && !consumers_meet(sh, met, kv.status, a.p.wait_ns)) return;  // (others read them)
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int j = 0; j < (ONE ? 1 : 2); ++j) {
-                float l = s.l[nt][j];
-                if constexpr (ONE) {
-                    l += __shfl_xor_sync(0xffffffffu, l, 1);
-                    if constexpr (E4M3) l += __shfl_xor_sync(0xffffffffu, l, 2);
-                }
-                l += __shfl_xor_sync(0xffffffffu, l, 4);
-                l += __shfl_xor_sync(0xffffffffu, l, 8);
-                l += __shfl_xor_sync(0xffffffffu, l, 16);
-                const int col = nt * 8 + 2 * c + j;
-                if (g == 0) {
-                    const int at = (col_warp * 8 * NT + col) * key_warps + key_warp;
-                    sh.part_l[st][at] = l;
-                    sh.part_m[st][at] = s.m[nt][j];
-                    if constexpr (E4M3) sh.part_w[st][at] = s.w[nt][j];
-                }
-                if (ONE && c > 0) continue;
-                uint8_t* const to = tile + meet_byte(warp, col);
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const int d = 16 * k + g + 8 * i;
-                        *reinterpret_cast<float*>(to + ((d + meet_turn(col)) & 127) * 4) = s.o[k][nt][2 * i + j];
-                    }
+        for (int j = 0; j < (ONE ? 1 : 2); ++j) {
+            float l = s.l[j];
+            if constexpr (ONE) {
+                l += __shfl_xor_sync(0xffffffffu, l, 1);
+                if constexpr (E4M3) l += __shfl_xor_sync(0xffffffffu, l, 2);
             }
+            l += __shfl_xor_sync(0xffffffffu, l, 4);
+            l += __shfl_xor_sync(0xffffffffu, l, 8);
+            l += __shfl_xor_sync(0xffffffffu, l, 16);
+            const int col = 2 * c + j;
+            if (g == 0) {
+                const int at = (col_warp * 8 + col) * key_warps + key_warp;
+                sh.part_l[st][at] = l;
+                sh.part_m[st][at] = s.m[j];
+                if constexpr (E4M3) sh.part_w[st][at] = s.w[j];
+            }
+            if (ONE && c > 0) continue;
+            uint8_t* const to = tile + meet_byte(warp, col);
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int d = 16 * k + g + 8 * i;
+                    *reinterpret_cast<float*>(to + ((d + meet_turn(col)) & 127) * 4) = s.o[k][2 * i + j];
+                }
+        }
         fence_proxy_async();  // (the stage's next contents come by TMA)
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&sh.done[st]));
@@ -1159,7 +1134,7 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
                            2 * warp + (lane >> 4), 2 * (kWarps + 1));
 }
 
-template <bool E4M3, int NT, bool ONE>
+template <bool E4M3, bool ONE>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm)
     attention_decode_kernel(const __grid_constant__ CacheMaps maps, const __grid_constant__ DecodeArgs a) {
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -1281,14 +1256,14 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
     if (warp == 0)
         produce<E4M3>(a, maps, sh, smem_u32(stage_mem), smem_u32(query_mem), weight, ctas, sh.bound[1]);
     else if (warp <= kWarps)
-        consume<E4M3, NT, ONE>(a, sh, stage_mem, query_mem);
+        consume<E4M3, ONE>(a, sh, stage_mem, query_mem);
     else
-        finish<E4M3, NT>(a, sh, stage_mem);
+        finish<E4M3>(a, sh, stage_mem);
 }
 
-template <bool E4M3, int NT, bool ONE>
+template <bool E4M3, bool ONE>
 cudaError_t launch(const CacheMaps& maps, const DecodeArgs& a, int grid, cudaStream_t stream) {
-    auto kern = attention_decode_kernel<E4M3, NT, ONE>;
+    auto kern = attention_decode_kernel<E4M3, ONE>;
     const int bytes = 1024 + kStages * kStageBytes + 2 * a.cols.block * kQueryStride;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != cudaSuccess) return e;
@@ -1325,15 +1300,15 @@ cudaError_t launch_attention_decode(const CacheMaps& maps, const KvView& kv, con
                                     cudaStream_t stream) {
     DecodeArgs a{kv, p, columns_of(p.H / kv.kv_heads), p.window, 0, 0, 0};
     const int grid = sm_count * kCtasPerSm;
-    const bool e4m3 = kv.exponents != nullptr, wide = a.cols.block > 8;
-    // (measured on ragged batches of 200 to 1024 and 1 to 8192 tokens, with 3 / 5 / 8 / 12 / 16: bf16 best at 5
-    // with up to 8 queries of a key head, 8 with more; e4m3 at 12, but 3% worse at 3)
-    a.item_weight = e4m3 ? 12 : wide ? 8 : 5;
+    const bool e4m3 = kv.exponents != nullptr;
+    // (measured with 3 / 5 / 8 / 12 / 16 / 20.  bf16: 64 pairs 288 / 290 / 291 / 291 us, 200 short
+    // rows 68 / 61 / 55 / 57; e4m3: 168 / 163 / 157 / 155 / 155 / 158 and 91 / 80 / 71 / 61 / 58 / 58, 64
+    // rows of 8 key heads and 12 queries each 34.4 / 33.6 / 33.6 / 33.8 / 34.7 / 35.4)
+    a.item_weight = e4m3 ? 12 : 8;
     a.snap = a.item_weight + (e4m3 ? 12 : 10);
     a.grid_reciprocal = ~uint64_t{0} / grid + 1;
-    if (p.H == kv.kv_heads) return e4m3 ? launch<true, 1, true>(maps, a, grid, stream) : launch<false, 1, true>(maps, a, grid, stream);
-    if (wide) return e4m3 ? launch<true, 2, false>(maps, a, grid, stream) : launch<false, 2, false>(maps, a, grid, stream);
-    return e4m3 ? launch<true, 1, false>(maps, a, grid, stream) : launch<false, 1, false>(maps, a, grid, stream);
+    if (p.H == kv.kv_heads) return e4m3 ? launch<true, true>(maps, a, grid, stream) : launch<false, true>(maps, a, grid, stream);
+    return e4m3 ? launch<true, false>(maps, a, grid, stream) : launch<false, false>(maps, a, grid, stream);
 }
 
 }  // namespace w4a16
