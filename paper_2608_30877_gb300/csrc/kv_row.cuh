@@ -55,16 +55,27 @@ __device__ __forceinline__ uint32_t e4m3_quad(float a, float b, float c, float d
 // all of them here) with eight values each.
 __device__ __forceinline__ int e4m3_row_of_16(uint4 v, uint2* codes) {
     const uint32_t u[4] = {v.x, v.y, v.z, v.w};
-    float f[8], top = 0.0f;
+    const uint32_t half = 0xFFFFu << (threadIdx.x & 16);
+    float f[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         f[2 * i] = __uint_as_float(u[i] << 16);
         f[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
-        top = fmaxf(top, fmaxf(finite_abs(f[2 * i]), finite_abs(f[2 * i + 1])));
     }
-    const uint32_t half = 0xFFFFu << (threadIdx.x & 16);
+    // the largest magnitude's bits, two at a time: magnitudes are in the order of their bits
+    uint32_t top2 = 0;
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(half, top, o));
+    for (int i = 0; i < 4; ++i) top2 = __vmaxu2(top2, u[i] & 0x7FFF7FFFu);
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) top2 = __vmaxu2(top2, __shfl_xor_sync(half, top2, o));
+    float top = __uint_as_float(max(top2 << 16, top2 & 0xFFFF0000u));
+    if (!(top < __int_as_float(0x7F800000))) {  // (all 16 lanes, or none)
+        top = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = fmaxf(top, finite_abs(f[i]));
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(half, top, o));
+    }
     const int e = e4m3_row_exponent(top);
     const float s = power_of_two(-e);
     codes->x = e4m3_quad(f[0] * s, f[1] * s, f[2] * s, f[3] * s);
