@@ -60,7 +60,7 @@ struct KvWriteParams {
     const int32_t* slots;
     int layer, nseq, M, H;
 };
-cudaError_t launch_kv_write(const KvView& kv, const KvWriteParams& p, cudaStream_t stream);
+cudaError_t launch_kv_write(const KvView& kv, const KvWriteParams& p, int sm_count, cudaStream_t stream);
 
 struct DecodeParams {
     const uint16_t* qkv;  // [n, (H + 2 kv_heads) * 128]

@@ -191,7 +191,7 @@ extern "C" int w4a16_kv_write(const w4a16_kv_cache* cache, int64_t layer, const 
     const KvWriteParams p{static_cast<const uint16_t*>(qkv_bf16), static_cast<const int32_t*>(seq_start_i32),
                           static_cast<const int32_t*>(slots_i32), static_cast<int>(layer),
                           static_cast<int>(nseq), static_cast<int>(M), static_cast<int>(H)};
-    return status_of(launch_kv_write(view_of(*cache, st.status), p, static_cast<cudaStream_t>(stream)));
+    return status_of(launch_kv_write(view_of(*cache, st.status), p, st.sm_count, static_cast<cudaStream_t>(stream)));
 }
 
 extern "C" int w4a16_attention_decode_workspace(int64_t H, int64_t kv_heads, int64_t* bytes) {

@@ -1,13 +1,16 @@
 // Keys and values of a packed batch's tokens into the cache's pages.
 //
 // Rows of the fused projection hold a token's keys and values of all heads in one run;
-// in a page a head's tokens lie in one run.  A CTA takes 8 tokens; 16 threads move a row of 128
-// values in 16-byte pieces (and reduce its largest value for the 8-bit form), several rows
-// under way together.  Bound by HBM: each value is read once and written once.  A row's
-// addresses are sums of 32-bit offsets: with divisions and 64-bit products per row the
-// issue slots were the bound (13000 tokens of 8 heads in 8 bits 32 us, now 22; 39000 of 96 heads
-// in bf16 600, now 576, 97% of the copy bandwidth).  Tokens / rows under way / CTAs an SM, both
-// in us: 8 / 4 / 6 576 and 24, 16 / 4 / 4 577 and 23, 8 / 2 / 8 593 and 22, 32 / 4 / 4 622 and 28.
+// in a page a head's tokens lie in one run.  A CTA takes 1 to 32 tokens (few heads, many tokens);
+// 16 threads move a row of 128 values in 16-byte pieces (and reduce its largest value for the 8-bit
+// form), several rows under way together.  Bound by HBM: each value is read once and written
+// once; 39000 tokens of 96 heads take 561 us (6.8 TB/s, the copy bandwidth), in 8 bits 508 (83%).  Short
+// calls are bound by the way to a token's place: three loads in a row before the first row (13000
+// tokens of 8 heads in 8 bits 20 us, 13 at the copy bandwidth).  A row's addresses are sums of
+// 32-bit offsets: with divisions and 64-bit products per row the issue slots were the bound.
+// Rows under way / CTAs an SM in 8 bits, 13000 tokens of 8 heads and 39000 of 96: 2 / 8 20 and
+// 505 us, 4 / 6 22 and 541, 4 / 5 21 and 522, 2 / 6 21 and 552; in bf16 4 / 6 576, 2 / 8 593.  The first
+// rows loaded ahead of the places took registers and time (22.9, 560).
 #include <cuda_runtime.h>
 #include <cstdint>
 
@@ -20,7 +23,7 @@ namespace w4a16 {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kTokens = 8;  // tokens of a CTA
+constexpr int kTokens = 32;  // of a CTA, at most
 constexpr int kStarts = 1024;  // a sequence table of up to so many sequences is searched in shared memory
 
 // Where token m of the packed batch goes: its page and place there; page -1 outside every
@@ -50,11 +53,12 @@ __device__ __forceinline__ void token_place(const KvView& kv, const KvWriteParam
 }
 
 template <bool E4M3>
-__global__ void __launch_bounds__(kThreads, E4M3 ? 8 : 6) kv_write_kernel(const KvView kv, const KvWriteParams p) {
+__global__ void __launch_bounds__(kThreads, E4M3 ? 8 : 6) kv_write_kernel(const KvView kv, const KvWriteParams p,
+                                                                             const int tokens) {
     constexpr int kBatch = E4M3 ? 2 : 4;  // rows that 16 threads have under way
     __shared__ int rows_at[kTokens];       // of a token: its row of head 0, -1 if it is left out
     __shared__ int32_t starts[kStarts + 1];
-    const int m0 = blockIdx.x * kTokens;
+    const int m0 = blockIdx.x * tokens;
     grid_launch_dependents();
     grid_wait();
     const bool staged = p.nseq <= kStarts;
@@ -62,7 +66,7 @@ __global__ void __launch_bounds__(kThreads, E4M3 ? 8 : 6) kv_write_kernel(const 
         for (int i = threadIdx.x; i <= p.nseq; i += kThreads) starts[i] = p.seq_start[i];
         __syncthreads();
     }
-    if (threadIdx.x < kTokens) {
+    if (threadIdx.x < tokens) {
         int page = -1, at = 0;
         if (m0 + threadIdx.x < p.M)
             token_place(kv, p, staged ? starts : p.seq_start, m0 + threadIdx.x, &page, &at);
@@ -86,19 +90,19 @@ __global__ void __launch_bounds__(kThreads, E4M3 ? 8 : 6) kv_write_kernel(const 
         E4M3 ? kv.exponents + 2 * static_cast<int64_t>(p.layer) * value_rows : nullptr;
     // these 16 threads' next row: row r of token t, keys of all heads and then values
     int t = (threadIdx.x >> 4) / rows, r = (threadIdx.x >> 4) - t * rows;
-    while (t < kTokens) {
+    while (t < tokens) {
         uint4 v[kBatch];
         int row[kBatch], which[kBatch];
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
             row[b] = -1;
-            if (t < kTokens && rows_at[t] >= 0) {
+            if (t < tokens && rows_at[t] >= 0) {
                 v[b] = __ldcs(src + t * width + r * (kKvHeadDim / 8));
                 which[b] = r >= kv.kv_heads;
                 row[b] = rows_at[t] + ((r - (which[b] ? kv.kv_heads : 0)) << kv.page_shift);
             }
             r += kThreads / 16;
-            while (r >= rows && t < kTokens) {
+            while (r >= rows && t < tokens) {
                 r -= rows;
                 ++t;
             }
@@ -121,10 +125,16 @@ __global__ void __launch_bounds__(kThreads, E4M3 ? 8 : 6) kv_write_kernel(const 
 
 }  // namespace
 
-cudaError_t launch_kv_write(const KvView& kv, const KvWriteParams& p, cudaStream_t stream) {
-    const int grid = (p.M + kTokens - 1) / kTokens;
+cudaError_t launch_kv_write(const KvView& kv, const KvWriteParams& p, int sm_count, cudaStream_t stream) {
+    // At most 64 pairs of rows to a CTA, and a CTA for each SM if there are tokens for it.  (us, with 64 /
+    // 128 / 768 pairs: 39000 tokens of 96 heads 561 / 561 / 576, in 8 bits 508 / 508 / 505, 40 of 32
+    // heads 4.2 / 5.7 / 8.9, one of 96 4.7 / 4.7 / 13; with 32 pairs 13000 of 8 heads in 8 bits 21.2
+    // and not 20.1.  One head, 64000 tokens: 32 tokens to a CTA 11.6, 8 21.8.)
+    int tokens = kTokens;
+    while (tokens > 1 && (tokens * kv.kv_heads > 64 || static_cast<int64_t>(tokens) * sm_count > p.M)) tokens /= 2;
+    const int grid = static_cast<int>((static_cast<int64_t>(p.M) + tokens - 1) / tokens);
     return launch_overlapped(kv.exponents != nullptr ? kv_write_kernel<true> : kv_write_kernel<false>, grid, kThreads,
-                             0, stream, kv, p);
+                             0, stream, kv, p, tokens);
 }
 
 }  // namespace w4a16
