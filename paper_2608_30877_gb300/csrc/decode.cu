@@ -24,7 +24,7 @@
 //    that together, they stood still 1 us per item).
 //  * More than 8 queries of a key head: the warps split the columns before the keys, up to 32
 //    columns, then further items.  (16 columns in a warp passed the registers' limit on the 8-bit
-//    cache: 12 queries of a head 86 us, and 69 with 8; in bf16 100 either way, 32 queries 71
+//    cache: 12 queries of a head 86 us, and 69 with 8, before small weights had products of their own; in bf16 100 either way, 32 queries 71
 //    and 75, 64 queries 80 and 74.)
 //  * Join.  A CTA's first and last items may continue in other CTAs: each then writes its
 //    part to the workspace, and when all its work is done counts itself present for both
@@ -33,10 +33,10 @@
 //    the same bits every time.
 //
 // Measured: 64 rows of 200 to 1024 tokens and 96 heads in pages of 64 tokens 288 us (6.6 TB/s, 97%
-// of the copy bandwidth), in 8 bits 154 (6.3 TB/s, 92%); 37 rows of 1 to 8192 tokens, 12 queries to
+// of the copy bandwidth), in 8 bits 155 (6.2 TB/s, 91%); 37 rows of 1 to 8192 tokens, 12 queries to
 // each of 8 key heads 99 us (88%).  Calls of less than 50 us are bound by the way to the first
 // tile (lengths, table, keys: four loads in a row, 3.5 us), by CTAs that end apart, and by the join
-// (2 to 4 us): three contexts of 131072 tokens in 8 bits 42 us (30 at the copy bandwidth), one
+// (2 to 4 us): three contexts of 131072 tokens in 8 bits 43.5 us (30 at the copy bandwidth), one
 // row of 333 tokens 9.4 (2.4).
 //
 // 8-bit cache.  Keys' and values' codes are converted to fp16, exactly, and multiplied with
@@ -44,7 +44,8 @@
 // fp16.  (Warp-level MMAs on e4m3 are no way around that: on this machine each takes 2 fp16 MMAs
 // and the conversion of both operands.)  A key's exponent goes to its score, a value's exponent
 // to its weight, and the weights that multiply the codes are relative to the largest of these
-// products, whose running maximum a column keeps next to its scores'.
+// products, whose running maximum a column keeps next to its scores'; small ones have MMAs of
+// their own.
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <cstdint>
@@ -70,9 +71,17 @@ constexpr int kInvalid = 1;                  // W4A16_ERR_INVALID_ARG
 // A column's maximum is raised, and what it has so far scaled down, only where a score passes
 // it by this much (powers of two): rarely, and until then a warp's lanes need not agree on the
 // largest score.
-constexpr float kSlackBf16 = 8.0f, kSlackE4m3 = 5.0f;
-// e4m3: fp16 weights go up to 2^(10 + 5), so that the least of them is 2^-34 of the largest.
-constexpr float kWeightTop = 10.0f;
+constexpr float kSlackBf16 = 8.0f, kSlackE4m3 = 3.0f;
+// e4m3: fp16 weights go up to 2^(12.9 + 3).  Those below 2^-16, where fp16 has fewer bits than bf16, get
+// products of their own, 2^24 times as large: where the keys with the large weights have values
+// of 0 in a dimension, the small weights are all there is.  (One query: in the odd columns, at
+// no cost.  Several: with weights over more than 2^29 in every step 64 rows of 8 key heads take 29
+// us and not 26.)  What is less than 2^-61 of the largest vanishes.
+constexpr float kWeightTop = 12.9f;
+constexpr float kSmallScale = 16777216.0f;
+__device__ __forceinline__ bool small_weight(float p) {  // 0 < p < 2^-16
+    return __float_as_uint(p) - 1u < 0x377FFFFFu;
+}
 // The maximum of no scores.  (Not -inf, whose differences would be NaN.)
 constexpr float kLeast = -3.0e38f;
 
@@ -893,6 +902,9 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
 #pragma unroll
             for (int j = 0; j < 4; ++j) s.o[k][j] = 0.0f;
         s.bad = false;
+        // whether this thread's columns are of queries
+        const int queries = columns_in(a, sh.unit[st].block) - col_warp * 8;
+        const bool used[2] = {2 * c < queries, 2 * c + 1 < queries};
         int flags;
         uint8_t* tile;
         for (;;) {  // a unit of it
@@ -938,7 +950,8 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
                         }
                 }
                 constexpr float kSlack = E4M3 ? kSlackE4m3 : kSlackBf16;
-                uint32_t b[kGroups][2];
+                uint32_t b[kGroups][2];  // the weights as the B operand
+                bool added = false;      // products with values done
                 // a column's maximum over its lanes, if that passes what it was; the factor for what
                 // is relative to the old one
                 auto raise = [&](float v, float& was) {
@@ -981,6 +994,10 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
                         for (int k = 0; k < 8; ++k) {
                             s.o[k][0] *= f;
                             s.o[k][2] *= f;
+                            if constexpr (E4M3) {
+                                s.o[k][1] *= f;
+                                s.o[k][3] *= f;
+                            }
                         }
                     }
                     float p = ex2(x - s.m[0]);
@@ -992,10 +1009,30 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
                         s.l[0] += bf16_lo(bf16_pair(p, 0.0f));
                     }
                     // rows g and g + 1 in the lanes of even g, then rows 2c and 2c + 1 everywhere
-                    const float next = __shfl_xor_sync(0xffffffffu, p, 4);
-                    const uint32_t pair = E4M3 ? half_pair(p, next) : bf16_pair(p, next);
+                    if constexpr (E4M3) {  // (the small ones to the odd columns)
+                        const bool small = small_weight(p);
+                        const float next = __shfl_xor_sync(0xffffffffu, p, 4);
+                        const bool next_small = small_weight(next);
+                        const uint32_t pair = half_pair(small ? 0.0f : p, next_small ? 0.0f : next);
 #pragma unroll
-                    for (int i = 0; i < kRows; ++i) b[i >> 1][i & 1] = __shfl_sync(0xffffffffu, pair, 8 * c + i);
+                        for (int i = 0; i < kRows; ++i) b[i >> 1][i & 1] = __shfl_sync(0xffffffffu, pair, 8 * c + i);
+                        if (__any_sync(0xffffffffu, small)) {
+                            const uint32_t low = half_pair(small ? p * kSmallScale : 0.0f,
+                                                           next_small ? next * kSmallScale : 0.0f);
+#pragma unroll
+                            for (int i = 0; i < kRows; ++i) {
+                                const uint32_t l = __shfl_sync(0xffffffffu, low, 8 * c + i);
+                                if (g & 1) b[i >> 1][i & 1] = l;
+                            }
+                        } else if (g & 1) {
+#pragma unroll
+                            for (int i = 0; i < kRows; ++i) b[i >> 1][i & 1] = 0;
+                        }
+                    } else {
+                        const uint32_t pair = bf16_pair(p, __shfl_xor_sync(0xffffffffu, p, 4));
+#pragma unroll
+                        for (int i = 0; i < kRows; ++i) b[i >> 1][i & 1] = __shfl_sync(0xffffffffu, pair, 8 * c + i);
+                    }
                 } else {
                     // row g of each matrix, as it comes out of the products: e4m3 with the keys'
                     // exponents, before the columns' factors
@@ -1055,24 +1092,56 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
                             }
                         }
                     }
+                    bool small = false;
+                    // rows 2c, 2c + 1 of column g: the transpose of what this thread holds
+                    auto weight = [&](int i, int j) {
+                        return E4M3 ? ex2(fmaf(x[i][j], factor(j), value_exp[i]) + (kWeightTop - s.w[j]))
+                                    : ex2(fmaf(x[i][j], factor(j), -s.m[j]));
+                    };
 #pragma unroll
                     for (int i = 0; i < kRows; ++i) {
-                        float p[2];
-#pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            p[j] = ex2(fmaf(x[i][j], factor(j), -s.m[j]));
-                            if constexpr (E4M3) {
-                                s.l[j] += p[j];
-                                p[j] = ex2(fmaf(x[i][j], factor(j), value_exp[i]) + (kWeightTop - s.w[j]));
-                            }
-                        }
+                        const float p[2] = {weight(i, 0), weight(i, 1)};
                         const uint32_t w = E4M3 ? half_pair(p[0], p[1]) : bf16_pair(p[0], p[1]);
-                        if constexpr (!E4M3) {  // (the rounded weights' sum, so that they add up to one)
+                        if constexpr (E4M3) {
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) {
+                                s.l[j] += ex2(fmaf(x[i][j], factor(j), -s.m[j]));
+                                small |= used[j] && small_weight(p[j]);
+                            }
+                        } else {  // (the rounded weights' sum, so that they add up to one)
                             s.l[0] += bf16_lo(w);
                             s.l[1] += bf16_hi(w);
                         }
-                        // rows 2c, 2c + 1 of column g: the transpose of what this thread holds
                         b[i >> 1][i & 1] = transpose_8x8(w);
+                    }
+                    if constexpr (E4M3) {
+                        if (__any_sync(0xffffffffu, small)) {
+                            uint32_t lo[kGroups][2];
+#pragma unroll
+                            for (int i = 0; i < kRows; ++i) {
+                                const float p[2] = {weight(i, 0), weight(i, 1)};
+                                const bool is[2] = {small_weight(p[0]), small_weight(p[1])};
+                                lo[i >> 1][i & 1] = transpose_8x8(
+                                    half_pair(is[0] ? p[0] * kSmallScale : 0.0f, is[1] ? p[1] * kSmallScale : 0.0f));
+                                b[i >> 1][i & 1] =
+                                    transpose_8x8(half_pair(is[0] ? 0.0f : p[0], is[1] ? 0.0f : p[1]));
+                            }
+                            added = true;
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) {
+                                uint32_t w[4], f[4];
+                                float d[4] = {};
+                                ldsm_bytes_trans((values + value_off + step * kWarpBytes) ^ (k << 4), w);
+#pragma unroll
+                                for (int i = 0; i < kGroups; ++i) {
+                                    codes_to_halves(w[2 * i], w[2 * i + 1], f);
+                                    mma<E4M3>(s.o[k], f, b[i][0], b[i][1]);
+                                    mma<E4M3>(d, f, lo[i][0], lo[i][1]);
+                                }
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) s.o[k][j] = fmaf(d[j], 1.0f / kSmallScale, s.o[k][j]);
+                            }
+                        }
                     }
                 }
                 if constexpr (!E4M3) {
@@ -1082,7 +1151,7 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
                         ldsm_x4_trans(((values + value_off + step * kWarpBytes) ^ ((k & 3) << 5)) + (k >> 2) * 4096, f);
                         mma<E4M3>(s.o[k], f, b[0][0], b[0][1]);
                     }
-                } else {
+                } else if (!added) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
                         uint32_t w[4], f[4];
@@ -1099,6 +1168,11 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
             release();
             if (!wait()) return;
         }
+        if constexpr (E4M3 && ONE)
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+#pragma unroll
+                for (int i = 0; i < 4; i += 2) s.o[k][i] = fmaf(s.o[k][i + 1], 1.0f / kSmallScale, s.o[k][i]);
         // what this warp has of the item, into its rows of the stage
         if (a.cols.warps > 1 && !consumers_meet(sh, met, kv.status, a.p.wait_ns)) return;  // (others read them)
 #pragma unroll
