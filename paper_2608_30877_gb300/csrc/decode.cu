@@ -32,7 +32,7 @@
 //    that wraps to zero, adds the parts up in the order of the CTAs, so that the result has
 //    the same bits every time.
 //
-// Measured: 64 rows of 200 to 1024 tokens and 96 heads in pages of 64 tokens 288 us (6.6 TB/s, 97%
+// Measured: 64 rows of 200 to 1024 tokens and 96 heads in pages of 64 tokens 290 us (6.6 TB/s, 97%
 // of the copy bandwidth), in 8 bits 155 (6.2 TB/s, 91%); 37 rows of 1 to 8192 tokens, 12 queries to
 // each of 8 key heads 99 us (88%).  Calls of less than 50 us are bound by the way to the first
 // tile (lengths, table, keys: four loads in a row, 3.5 us), by CTAs that end apart, and by the join
