@@ -132,6 +132,10 @@ __device__ __forceinline__ void each_page(PlanShared& sh, int first, int count, 
     __syncthreads();
 }
 
+// Whether an entry has been found wrong.  All threads call it before each pass over the lists: the pass
+// may set the flag, so no thread begins one before every thread has read it.
+__device__ __forceinline__ bool plan_failed(const PlanShared& sh) { return __syncthreads_or(sh.error) != 0; }
+
 __device__ __forceinline__ void plan_begin(const KvView& kv, PlanShared& sh) {
     for (int i = threadIdx.x; i < (kv.num_slots + 31) / 32; i += kThreads) sh.seen[i] = 0;
     if (threadIdx.x == 0) sh.error = sh.copies = sh.larges = 0;
@@ -307,7 +311,7 @@ __global__ void __launch_bounds__(kThreads)
     }
     __syncthreads();
     // checks every page, then shares them; a chunk of entries at a time
-    for (int pass = 0; pass < 2 && sh.error == 0; ++pass) {
+    for (int pass = 0; pass < 2 && !plan_failed(sh); ++pass) {
         for (int i0 = 0; i0 < n; i0 += kThreads) {
             const int i = i0 + tid;
             int len = 0;
@@ -341,7 +345,7 @@ __global__ void __launch_bounds__(kThreads)
     const int tid = threadIdx.x;
     plan_begin(kv, sh);
     // checks every entry and page, then gives the pages back; a chunk of entries at a time
-    for (int pass = 0; pass < 2 && sh.error == 0; ++pass) {
+    for (int pass = 0; pass < 2 && !plan_failed(sh); ++pass) {
         for (int i0 = 0; i0 < n; i0 += kThreads) {
             const int i = i0 + tid;
             int first = 0, count = 0, slot = -1, left = 0;
