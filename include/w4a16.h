@@ -285,7 +285,8 @@ int w4a16_topk_smallest(const void* scores, int score_bits, int64_t n, int64_t k
  *               sequence's last page mean nothing and are left as they are.
  *   seq_len     int32 [num_slots], tokens of each slot's sequence (0: none)
  *   page_refs   int32 [num_pages], how many sequences have the page; 0: free
- *   scratch     w4a16_kv_scratch_bytes bytes for the page operations, any contents
+ *   scratch     w4a16_kv_scratch_bytes bytes for the page operations, zeroed by the
+ *               caller before its first use
  * Supported: head_dim 128; page_tokens 16, 32, 64 or 128; num_slots <= 65536;
  * num_pages <= 2^24; a layer's rows (2 num_pages kv_heads page_tokens), the page
  * table's entries and a sequence's tokens (max_pages page_tokens) < 2^31.
@@ -307,6 +308,13 @@ int w4a16_topk_smallest(const void* scores, int score_bits, int64_t n, int64_t k
  * operation that records an error changes nothing; kv_write leaves out the rows
  * concerned, and in attention_decode they are zero (a bad page index may show
  * after the row's own key and value were stored).
+ *
+ * A kv_extend that is refused marks its slots (those whose add is not 0): their
+ * sequences are as they were, so that what a step stores next would take the
+ * places of their last tokens, which other sequences may share.  Until a kv_extend
+ * of the slot succeeds (by 0 tokens too), or kv_trim or kv_fork sets its sequence
+ * anew, kv_write and attention_decode treat it as an error (W4A16_ERR_INVALID_ARG,
+ * unless an earlier one is unread): nothing is stored, and its rows are zero.
  */
 typedef struct {
     void* pages;

@@ -302,7 +302,8 @@ __device__ __forceinline__ Row row_of(const DecodeArgs& a, int i, bool* bad) {
     *bad = slot < -1 || slot >= a.kv.num_slots;
     if (*bad || slot < 0) return Row{};
     const int len = a.kv.seq_len[slot];
-    *bad = !length_ok(a, len);
+    const bool refused = growth_refused(a.kv, slot);
+    *bad = refused || !length_ok(a, len);
     return *bad ? Row{} : row_from<E4M3>(a, slot, len);
 }
 // Where tile t of an item starts in its weight.
@@ -374,8 +375,10 @@ __device__ void produce(const DecodeArgs& a, const CacheMaps& maps, Shared& sh, 
             if (rows_from == kNone || from >= rows_from + 32) {
                 rows_from = from;
                 slot_of = from + lane < a.p.n ? __ldcg(a.p.slots + from + lane) : -1;
-                len_of = slot_of >= 0 && slot_of < kv.num_slots ? __ldcg(kv.seq_len + slot_of) : 0;
-                if (!length_ok(a, len_of)) len_of = 0;
+                const bool slot_ok = slot_of >= 0 && slot_of < kv.num_slots;
+                len_of = slot_ok ? __ldcg(kv.seq_len + slot_of) : 0;
+                const bool refused = slot_ok && growth_refused(kv, slot_of);
+                if (refused || !length_ok(a, len_of)) len_of = 0;
             }
             const uint32_t have = __ballot_sync(0xffffffffu, len_of > 0 && rows_from + lane >= from);
             if (have == 0) continue;

@@ -29,13 +29,18 @@ struct KvView {
     int32_t* seq_len;    // [num_slots]
     int32_t* refs;       // [num_pages]
     int32_t* scratch;    // KvScratch
+    int32_t* refused;    // [num_slots], in the scratch buffer: kKvRefused where the last growth failed
     int* status;
     int layers, num_pages, kv_heads, page_shift /* log2 T */, num_slots, max_pages;
     int row_bytes;       // of a token's key: 256 or 128
 };
 
-// The scratch buffer: a header, then kKvScratchLists lists of max(num_pages, num_slots) entries.
+// The scratch buffer: a header, kKvScratchLists lists of max(num_pages, num_slots) entries, and a
+// mark for each slot.
 constexpr int kKvScratchLists = 5;
+// A slot's mark: its last kv_extend was refused, so the tokens that a prompt's write or a step would
+// store were not added and their places are those of its last tokens (which others may share).
+constexpr int32_t kKvRefused = 0x4B565245;
 struct KvScratch {
     int32_t copies;  // entries of src / dst / tokens
     int32_t moved;   // compaction: pages from this index on have moved (a list says where), else -1

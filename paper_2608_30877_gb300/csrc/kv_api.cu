@@ -32,7 +32,7 @@ bool scratch_sizes_ok(int64_t num_pages, int64_t num_slots) {
 }
 int64_t scratch_bytes(int64_t num_pages, int64_t num_slots) {
     const int list = kv_scratch_list(static_cast<int>(num_pages), static_cast<int>(num_slots));
-    return (4 * (kKvScratchHeader + kKvScratchLists * static_cast<int64_t>(list)) + 15) / 16 * 16;
+    return (4 * (kKvScratchHeader + kKvScratchLists * static_cast<int64_t>(list) + num_slots) + 15) / 16 * 16;
 }
 
 // A cache's buffers, for the overlap checks.
@@ -87,6 +87,9 @@ KvView view_of(const w4a16_kv_cache& c, int* status) {
     v.seq_len = static_cast<int32_t*>(c.seq_len);
     v.refs = static_cast<int32_t*>(c.page_refs);
     v.scratch = static_cast<int32_t*>(c.scratch);
+    v.refused = v.scratch + kKvScratchHeader +
+                kKvScratchLists * static_cast<int64_t>(kv_scratch_list(static_cast<int>(c.num_pages),
+                                                                       static_cast<int>(c.num_slots)));
     v.status = status;
     v.layers = static_cast<int>(c.layers);
     v.num_pages = static_cast<int>(c.num_pages);

@@ -244,6 +244,9 @@ __global__ void __launch_bounds__(kThreads)
     }
     __syncthreads();
     if (sh.error != 0 || found < need_all) {
+        // what follows in the same step stores nothing for the sequences that were to grow
+        for (int i = tid; i < n; i += kThreads)
+            if (slots[i] >= 0 && slots[i] < kv.num_slots && add[i] != 0) kv.refused[slots[i]] = kKvRefused;
         if (tid == 0) {
             record_status(kv.status, sh.error != 0 ? sh.error : kCapacity);
             ls.head->copies = 0;
@@ -278,6 +281,7 @@ __global__ void __launch_bounds__(kThreads)
                 sh.large[l] = need;
             }
             kv.seq_len[slot] = to;
+            kv.refused[slot] = 0;
         }
         __syncthreads();
         for (int l = 0; l < sh.larges; ++l)
@@ -314,14 +318,15 @@ __global__ void __launch_bounds__(kThreads)
     for (int pass = 0; pass < 2 && !plan_failed(sh); ++pass) {
         for (int i0 = 0; i0 < n; i0 += kThreads) {
             const int i = i0 + tid;
-            int len = 0;
+            int len = 0, child = -1;
             if (i < n && children[i] != -1) {
                 const int parent = parents[i];
+                child = children[i];
                 // (a parent that is a child of this call)
                 if (sh.seen[parent >> 5] >> (parent & 31) & 1) sh.error = kInvalid;
                 len = kv.seq_len[parent];
                 sh.slot[tid] = parent;
-                sh.other[tid] = children[i];
+                sh.other[tid] = child;
             }
             auto load = [&](int k, int e) { return entries_of(kv, sh.slot[k])[e]; };
             each_page(sh, 0, pages_of(kv, len), min(n - i0, kThreads), load, [&](int k, int e, int page) {
@@ -332,7 +337,10 @@ __global__ void __launch_bounds__(kThreads)
                     atomicAdd(&kv.refs[page], 1);
                 }
             });
-            if (pass == 1 && len > 0) kv.seq_len[children[i]] = len;
+            if (pass == 1 && child >= 0) {
+                kv.seq_len[child] = len;
+                kv.refused[child] = 0;
+            }
         }
     }
     if (sh.error != 0 && tid == 0) record_status(kv.status, sh.error);
@@ -373,7 +381,10 @@ __global__ void __launch_bounds__(kThreads)
                     atomicSub(&kv.refs[page], 1);
                 }
             });
-            if (pass == 1 && slot >= 0) kv.seq_len[slot] = left;
+            if (pass == 1 && slot >= 0) {
+                kv.seq_len[slot] = left;
+                kv.refused[slot] = 0;
+            }
         }
     }
     if (sh.error != 0 && tid == 0) record_status(kv.status, sh.error);

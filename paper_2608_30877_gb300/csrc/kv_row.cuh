@@ -22,6 +22,11 @@ __device__ __forceinline__ int64_t kv_exponent(const KvView& kv, int layer, int 
              << kv.page_shift) + at) * 2 + which;
 }
 
+// Whether nothing is to be stored for the slot: its growth was refused.
+__device__ __forceinline__ bool growth_refused(const KvView& kv, int slot) {
+    return __ldcg(kv.refused + slot) == kKvRefused;
+}
+
 // The 8-bit form takes a power of two per row, not amax / 448: a power of two scales
 // exactly, costs an e4m3 code no relative precision, and takes one byte.
 constexpr int kKvMinExp = -120;

@@ -42,7 +42,8 @@ __device__ __forceinline__ void token_place(const KvView& kv, const KvWriteParam
     *page = -2;
     if (slot < 0 || slot >= kv.num_slots) return;
     const int len = kv.seq_len[slot];
-    if (begin < 0 || end > p.M || m >= end || len < end - begin ||
+    const bool refused = growth_refused(kv, slot);
+    if (refused || begin < 0 || end > p.M || m >= end || len < end - begin ||
         len > static_cast<int64_t>(kv.max_pages) << kv.page_shift)
         return;
     const int pos = len - end + m;

@@ -358,7 +358,7 @@ class KVCache:
         size = lib().w4a16_kv_scratch_bytes(num_pages, num_slots)
         if size == 0:
             raise W4A16Error("w4a16_kv_scratch_bytes", ERR_UNSUPPORTED)
-        self._scratch = torch.empty(size, dtype=torch.uint8, device=pages.device)
+        self._scratch = torch.zeros(size, dtype=torch.uint8, device=pages.device)
         self._workspaces, self._workspace_bytes = {}, {}
         self._struct = KVCacheStruct(
             pages.data_ptr(), None if exponents is None else exponents.data_ptr(), page_table.data_ptr(),
