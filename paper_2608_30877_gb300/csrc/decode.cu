@@ -297,12 +297,12 @@ __device__ __forceinline__ Row row_from(const DecodeArgs& a, int slot, int len) 
     return r;
 }
 template <bool E4M3>
-__device__ __forceinline__ Row row_of(const DecodeArgs& a, int i, bool* bad) {
+__device__ __forceinline__ Row row_of(const DecodeArgs& a, bool any, int i, bool* bad) {
     const int slot = a.p.slots[i];
     *bad = slot < -1 || slot >= a.kv.num_slots;
     if (*bad || slot < 0) return Row{};
     const int len = a.kv.seq_len[slot];
-    const bool refused = growth_refused(a.kv, slot);
+    const bool refused = growth_refused(a.kv, any, slot);
     *bad = refused || !length_ok(a, len);
     return *bad ? Row{} : row_from<E4M3>(a, slot, len);
 }
@@ -369,6 +369,7 @@ __device__ void produce(const DecodeArgs& a, const CacheMaps& maps, Shared& sh, 
     constexpr int kUnknown = -2, kNone = -1;
     int next_index = kUnknown, next_ids = 0, rows_from = kNone, slot_of = -1, len_of = 0;
     Row next{};
+    const bool any = any_refused(kv);
     auto find_next = [&]() {  // the next row with keys
         next_index = kNone;
         for (int from = row + 1; from < a.p.n && next_index == kNone; from = rows_from + 32) {
@@ -377,7 +378,7 @@ __device__ void produce(const DecodeArgs& a, const CacheMaps& maps, Shared& sh, 
                 slot_of = from + lane < a.p.n ? __ldcg(a.p.slots + from + lane) : -1;
                 const bool slot_ok = slot_of >= 0 && slot_of < kv.num_slots;
                 len_of = slot_ok ? __ldcg(kv.seq_len + slot_of) : 0;
-                const bool refused = slot_ok && growth_refused(kv, slot_of);
+                const bool refused = slot_ok && growth_refused(kv, any, slot_of);
                 if (refused || !length_ok(a, len_of)) len_of = 0;
             }
             const uint32_t have = __ballot_sync(0xffffffffu, len_of > 0 && rows_from + lane >= from);
@@ -1251,11 +1252,12 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
     // The batch's weight, this CTA's share of it, and the row where it starts.  (Each load is
     // a microsecond's part: a batch of up to kThreads rows is read once.)
     const int items = a.kv.kv_heads * a.cols.blocks;
+    const bool any = any_refused(a.kv);
     auto weigh = [&](int i, Row* r) -> int64_t {
         *r = Row{};
         if (i >= a.p.n) return 0;
         bool bad;
-        *r = row_of<E4M3>(a, i, &bad);
+        *r = row_of<E4M3>(a, any, i, &bad);
         if (r->tiles == 0 && i % gridDim.x == blockIdx.x) {
             sh.empty_rows = 1;
             if (bad) record_status(a.kv.status, kInvalid);
@@ -1291,7 +1293,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
     if (sh.empty_rows)
         for (int i = blockIdx.x; i < a.p.n; i += gridDim.x) {
             bool bad;
-            if (row_of<E4M3>(a, i, &bad).tiles > 0) continue;
+            if (row_of<E4M3>(a, any, i, &bad).tiles > 0) continue;
             uint4* const out = reinterpret_cast<uint4*>(a.p.out + static_cast<int64_t>(i) * a.p.H * kKvHeadDim);
             for (int j = tid; j < a.p.H * (kKvHeadDim / 8); j += kThreads) out[j] = make_uint4(0, 0, 0, 0);
         }

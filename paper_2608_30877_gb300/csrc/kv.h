@@ -44,7 +44,8 @@ constexpr int32_t kKvRefused = 0x4B565245;
 struct KvScratch {
     int32_t copies;  // entries of src / dst / tokens
     int32_t moved;   // compaction: pages from this index on have moved (a list says where), else -1
-    int32_t pad[14];
+    int32_t refused; // slots with a mark: where there are none no mark is read
+    int32_t pad[13];
 };
 constexpr int kKvScratchHeader = sizeof(KvScratch) / sizeof(int32_t);
 inline __host__ __device__ int kv_scratch_list(int num_pages, int num_slots) {

@@ -162,6 +162,14 @@ __device__ __forceinline__ bool page_ok(const KvView& kv, int page) {
     return page >= 0 && page < kv.num_pages;
 }
 
+// A slot's mark, set or taken away; `any`: whether there was one when the call began.
+__device__ __forceinline__ void mark_refused(const KvView& kv, int slot) {
+    if (atomicExch(&kv.refused[slot], kKvRefused) != kKvRefused) atomicAdd(&lists_of(kv).head->refused, 1);
+}
+__device__ __forceinline__ void unmark(const KvView& kv, bool any, int slot) {
+    if (any && atomicExch(&kv.refused[slot], 0) == kKvRefused) atomicSub(&lists_of(kv).head->refused, 1);
+}
+
 // The slot's last page if the sequence is to get a copy of it, else -1; false for a bad index.
 __device__ __forceinline__ bool shared_last(const KvView& kv, int slot, int len, int add, int* page) {
     *page = -1;
@@ -198,6 +206,7 @@ __global__ void __launch_bounds__(kThreads)
     };
     int4 run[kRun / 4];
     load_run(0, run);
+    const bool any = any_refused(kv);
     // pages that each entry needs, as offsets into the pages to allocate
     int64_t need_all = 0;
     for (int i0 = 0; i0 < n; i0 += kThreads) {
@@ -246,7 +255,7 @@ __global__ void __launch_bounds__(kThreads)
     if (sh.error != 0 || found < need_all) {
         // what follows in the same step stores nothing for the sequences that were to grow
         for (int i = tid; i < n; i += kThreads)
-            if (slots[i] >= 0 && slots[i] < kv.num_slots && add[i] != 0) kv.refused[slots[i]] = kKvRefused;
+            if (slots[i] >= 0 && slots[i] < kv.num_slots && add[i] != 0) mark_refused(kv, slots[i]);
         if (tid == 0) {
             record_status(kv.status, sh.error != 0 ? sh.error : kCapacity);
             ls.head->copies = 0;
@@ -281,7 +290,7 @@ __global__ void __launch_bounds__(kThreads)
                 sh.large[l] = need;
             }
             kv.seq_len[slot] = to;
-            kv.refused[slot] = 0;
+            unmark(kv, any, slot);
         }
         __syncthreads();
         for (int l = 0; l < sh.larges; ++l)
@@ -306,6 +315,7 @@ __global__ void __launch_bounds__(kThreads)
     __shared__ PlanShared sh;
     const int tid = threadIdx.x;
     plan_begin(kv, sh);
+    const bool any = any_refused(kv);
     for (int i = tid; i < n; i += kThreads) {
         if (children[i] == -1) continue;
         const int parent = parents[i];
@@ -339,7 +349,7 @@ __global__ void __launch_bounds__(kThreads)
             });
             if (pass == 1 && child >= 0) {
                 kv.seq_len[child] = len;
-                kv.refused[child] = 0;
+                unmark(kv, any, child);
             }
         }
     }
@@ -352,6 +362,7 @@ __global__ void __launch_bounds__(kThreads)
     __shared__ PlanShared sh;
     const int tid = threadIdx.x;
     plan_begin(kv, sh);
+    const bool any = any_refused(kv);
     // checks every entry and page, then gives the pages back; a chunk of entries at a time
     for (int pass = 0; pass < 2 && !plan_failed(sh); ++pass) {
         for (int i0 = 0; i0 < n; i0 += kThreads) {
@@ -383,7 +394,7 @@ __global__ void __launch_bounds__(kThreads)
             });
             if (pass == 1 && slot >= 0) {
                 kv.seq_len[slot] = left;
-                kv.refused[slot] = 0;
+                unmark(kv, any, slot);
             }
         }
     }

@@ -42,7 +42,7 @@ __device__ __forceinline__ void token_place(const KvView& kv, const KvWriteParam
     *page = -2;
     if (slot < 0 || slot >= kv.num_slots) return;
     const int len = kv.seq_len[slot];
-    const bool refused = growth_refused(kv, slot);
+    const bool refused = growth_refused(kv, true, slot);  // (beside the length: a load of any_refused first takes 0.9 us)
     if (refused || begin < 0 || end > p.M || m >= end || len < end - begin ||
         len > static_cast<int64_t>(kv.max_pages) << kv.page_shift)
         return;
