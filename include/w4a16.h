@@ -397,7 +397,8 @@ int w4a16_kv_write(const w4a16_kv_cache* cache, int64_t layer, const void* qkv_b
  * one (j = len - 1, after w4a16_kv_extend): its key and value come from the row of
  * qkv, are stored in the cache, and count as the cache holds them.
  *   qkv_bf16   [n, (H + 2 kv_heads) * 128] bf16, H a multiple of kv_heads
- *   slots_i32  [n]; a row of slot -1, or of an empty sequence, gives zeros
+ *   slots_i32  [n]; a row of slot -1, or of an empty sequence, gives zeros; with a
+ *              slot twice in the list all rows are zero and nothing is stored
  *   out_bf16   [n, H * 128] bf16, written in full
  *   workspace  w4a16_attention_decode_workspace bytes, zeroed by the caller
  *              before its first use and after a W4A16_ERR_TIMEOUT; calls leave it

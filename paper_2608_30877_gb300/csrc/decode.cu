@@ -151,6 +151,7 @@ struct Shared {
     int start_row, start_item, start_into;
     Row start;
     int empty_rows;
+    int twice;  // a slot is twice in the list
     int abort;
 };
 
@@ -1239,12 +1240,16 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
         mbar_init(smem_u32(&sh.met), kWarps);
         mbar_init(smem_u32(&sh.joined), 1);
         sh.pending[0] = sh.pending[1] = Pending{};
-        sh.start_base = sh.start_row = sh.start_item = sh.start_into = sh.empty_rows = 0;
+        sh.start_base = sh.start_row = sh.start_item = sh.start_into = sh.empty_rows = sh.twice = 0;
         sh.bound[0] = sh.bound[1] = 0;
         sh.start = Row{};
         sh.abort = 0;
         fence_mbar_init();
     }
+    // (a bit for each slot, at most 8 KB, before the stages' first copies)
+    uint32_t* const seen = reinterpret_cast<uint32_t*>(stage_mem);
+    static_assert(kKvMaxSlots / 8 <= kStageBytes);
+    for (int i = tid; i < (a.kv.num_slots + 31) / 32; i += kThreads) seen[i] = 0;
     grid_launch_dependents();
     grid_wait();
     __syncthreads();
@@ -1253,6 +1258,12 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
     // a microsecond's part: a batch of up to kThreads rows is read once.)
     const int items = a.kv.kv_heads * a.cols.blocks;
     const bool any = any_refused(a.kv);
+    auto seen_before = [&](int i) {  // (a list of one has none)
+        const int slot = a.p.n > 1 && i < a.p.n ? a.p.slots[i] : -1;
+        if (slot < 0 || slot >= a.kv.num_slots) return false;
+        const uint32_t bit = 1u << (slot & 31);
+        return (atomicOr(&seen[slot >> 5], bit) & bit) != 0;
+    };
     auto weigh = [&](int i, Row* r) -> int64_t {
         *r = Row{};
         if (i >= a.p.n) return 0;
@@ -1281,23 +1292,33 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
         return v;
     };
     Row r;
-    int64_t all, weight = 0, v = weigh(tid, &r), upto = scan(v, &all);
+    bool again = seen_before(tid);
+    int64_t all, weight = 0, v = weigh(tid, &r);
+    if (again) sh.twice = 1;
+    int64_t upto = scan(v, &all);
     weight = all;
     for (int i0 = kThreads; i0 < a.p.n; i0 += kThreads) {
         __syncthreads();
         Row other;
-        scan(weigh(i0 + tid, &other), &all);
+        again = seen_before(i0 + tid);
+        const int64_t w = weigh(i0 + tid, &other);
+        if (again) sh.twice = 1;
+        scan(w, &all);
         weight += all;
     }
+    if (a.p.n > 1) fence_proxy_async();  // (the slots' bits, before the copies)
+    // Two rows of one slot would both be its last token: nothing is stored, and all rows are zero.
+    const bool twice = sh.twice != 0;
+    if (twice && blockIdx.x == 0 && tid == 0) record_status(a.kv.status, kInvalid);
     // rows without keys are zero
-    if (sh.empty_rows)
+    if (sh.empty_rows || twice)
         for (int i = blockIdx.x; i < a.p.n; i += gridDim.x) {
             bool bad;
-            if (row_of<E4M3>(a, any, i, &bad).tiles > 0) continue;
+            if (!twice && row_of<E4M3>(a, any, i, &bad).tiles > 0) continue;
             uint4* const out = reinterpret_cast<uint4*>(a.p.out + static_cast<int64_t>(i) * a.p.H * kKvHeadDim);
             for (int j = tid; j < a.p.H * (kKvHeadDim / 8); j += kThreads) out[j] = make_uint4(0, 0, 0, 0);
         }
-    if (weight == 0) return;
+    if (weight == 0 || twice) return;
     // as many CTAs as leave each at least the most that lies between two tiles' starts
     const int apart = (E4M3 ? 8 : 4) + a.item_weight;
     const bool full = weight >= static_cast<int64_t>(apart) * gridDim.x;
