@@ -382,7 +382,9 @@ int w4a16_kv_compact(const w4a16_kv_cache* cache, void* stream);
  *                  [seq_start[i], seq_start[i+1]) are the LAST tokens of the
  *                  sequence of slots_i32[i] (after w4a16_kv_extend); a table that
  *                  decreases or leaves [0, M], or a sequence shorter than its rows,
- *                  records W4A16_ERR_INVALID_ARG
+ *                  records W4A16_ERR_INVALID_ARG, and so does a slot that several
+ *                  sequences with rows have (its places then hold rows of any
+ *                  of them).  Of a sequence without rows the slot is not looked at.
  *   layer          0 .. layers - 1
  */
 int w4a16_kv_write(const w4a16_kv_cache* cache, int64_t layer, const void* qkv_bf16,

@@ -68,3 +68,63 @@ def test_attention_over_the_most_slots():
         out = W.attention_decode(c, 0, qkv.neg(), wrong, 1)
         assert W.get_device_error() == W.ERR_INVALID_ARG
         assert (out == 0).all() and torch.equal(before, c.pages)
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("Hkv,lengths,pairs", [
+    (2, [5, 9], [(0, 1)]), (1, [40, 1, 33, 64, 2], [(1, 3), (3, 4)]), (96, [3, 2, 4], [(0, 2)]),
+    (1, [1 + i % 3 for i in range(300)], [(0, 299), (40, 41)]), (4, [1 + i % 20 for i in range(226)], [(3, 225), (100, 101)]),
+    (1, [1 + i % 2 for i in range(1500)], [(7, 8), (2, 1499), (700, 1300)]),
+    (1, [1 + i % 2 for i in range(40000)], [(20000, 39999)]), (1, [1] * 40000, [(33000, 33001), (2, 5)])])
+def test_writes_report_a_slot_twice(bits, Hkv, lengths, pairs):
+    """The status says so, the other sequences' rows are written and what no sequence of the list has
+    is as it was.  A slot that is in the list again for a sequence without rows is no error."""
+    W = _W()
+    n, H, T = len(lengths), 1, 16
+    g = torch.Generator(device="cuda").manual_seed(n + bits)
+
+    def cache():
+        c = W.KVCache(1, sum(-(-x // T) for x in lengths) + 1, Hkv, n + 1, max(-(-x // T) for x in lengths), T,
+                      torch.bfloat16 if bits == 16 else torch.float8_e4m3fn)
+        c.pages.view(torch.uint8).fill_(0x5A)
+        if bits == 8:
+            c.exponents.fill_(0x5A)
+        W.kv_extend(c, R.i32(range(n)), R.i32(lengths))
+        return c
+
+    def rows(c):  # the sequences' rows as the cache has them, one list entry for each
+        raw = c.pages.view(torch.uint8)[0]
+        table = c.page_table.cpu()
+        seq = np.repeat(np.arange(n), lengths)
+        pos = np.concatenate([np.arange(x) for x in lengths])
+        page, at = table[torch.from_numpy(seq), torch.from_numpy(pos // T)].long().cuda(), torch.from_numpy(pos % T).cuda()
+        # [tokens, 2, heads, bytes], [tokens, heads, 2]
+        held = [raw.transpose(0, 1)[page, :, :, at].cpu()] + ([c.exponents[0][page, :, at].cpu()] if bits == 8 else [])
+        return seq, held
+
+    start = np.concatenate([[0], np.cumsum(lengths)])
+    qkv = torch.randn((int(start[-1]) + 3, (H + 2 * Hkv) * D), generator=g, device="cuda").bfloat16()
+    good = cache()
+    slots = R.i32(range(n))
+    W.kv_write(good, 0, qkv, R.i32(start), slots, H)
+    assert W.get_device_error() == W.OK
+    wrong, bad = slots.clone(), set()
+    for a, b in pairs:
+        if lengths[b] > lengths[a]:  # (no more rows than the slot has tokens, which would be an error by itself)
+            a, b = b, a
+        wrong[b] = wrong[a]
+        bad |= {a, b}
+    c = cache()
+    W.kv_write(c, 0, qkv, R.i32(start), wrong, H)
+    assert W.get_device_error() == W.ERR_INVALID_ARG
+    (seq, want), (_, got) = rows(good), rows(c)
+    out = torch.from_numpy(np.isin(seq, sorted(bad)))
+    left = torch.from_numpy(np.isin(seq, sorted(set(range(n)) - set(wrong.tolist()))))  # slots that went out of the list
+    for w, x in zip(want, got):
+        assert torch.equal(x[~out], w[~out])
+        assert bool((x[left] == 0x5A).all())
+    # a sequence of no rows with another's slot, before and after it
+    c = cache()
+    W.kv_write(c, 0, qkv, R.i32([0, 0, *start[1:], start[-1]]), R.i32([n - 1, *range(n), 0]), H)
+    assert W.get_device_error() == W.OK
+    assert all(torch.equal(w, x) for w, x in zip(want, rows(c)[1]))
