@@ -359,6 +359,9 @@ class KVCache:
         if size == 0:
             raise W4A16Error("w4a16_kv_scratch_bytes", ERR_UNSUPPORTED)
         self._scratch = torch.zeros(size, dtype=torch.uint8, device=pages.device)
+        if not torch.cuda.is_current_stream_capturing():
+            # (the first call may be on another stream)
+            torch.cuda.current_stream(pages.device).synchronize()
         self._workspaces, self._workspace_bytes = {}, {}
         self._struct = KVCacheStruct(
             pages.data_ptr(), None if exponents is None else exponents.data_ptr(), page_table.data_ptr(),

@@ -193,3 +193,28 @@ def test_a_refused_growth_of_many():
     assert (W.attention_decode(c, 0, qkv, slots, 1) != 0).any(1).all()
     assert W.get_device_error() == W.OK
     assert np.array_equal(c.seq_len.cpu().numpy()[:n], np.full(n, 6))
+
+
+@pytest.mark.parametrize("make", ["new", "from_tensors"])
+def test_a_cache_is_ready_for_any_stream(make):
+    """A cache that is made while its stream is busy, and used at once on another one: the marks of
+    a refused growth are not wiped out by what the constructor had queued."""
+    W = _W()
+    side = torch.cuda.Stream()
+    one, zero = R.i32([1]), R.i32([0])
+    tensors = [torch.zeros((1, 2, 2, 1, T, D), dtype=torch.bfloat16, device="cuda"),
+               torch.zeros((1, 4), dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda"),
+               torch.zeros(2, dtype=torch.int32, device="cuda")]
+    qkv = torch.randn((1, 3 * D), device="cuda").bfloat16()
+    many = R.i32([33])
+    torch.cuda.synchronize()
+    torch.cuda._sleep(100_000_000)  # 50 ms
+    c = W.KVCache(1, 2, 1, 1, 4, T) if make == "new" else W.KVCache.from_tensors(*tensors)
+    W.kv_extend(c, zero, one, stream=side)
+    W.kv_extend(c, zero, many, stream=side)  # refused
+    side.synchronize()
+    torch.cuda.synchronize()
+    assert W.get_device_error() == W.ERR_CAPACITY
+    assert c.seq_len.tolist() == [1]
+    out = W.attention_decode(c, 0, qkv, zero, 1)
+    assert (out == 0).all() and W.get_device_error() == W.ERR_INVALID_ARG
