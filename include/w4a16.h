@@ -414,7 +414,10 @@ int w4a16_attention_decode(const w4a16_kv_cache* cache, int64_t layer, const voi
                            const void* slots_i32, int64_t n, int64_t H, int64_t window,
                            void* out_bf16, void* workspace, void* stream);
 
-/* Bytes of the workspace on the current device, for any n and any cache of these heads. */
+/*
+ * Bytes of the workspace on the current device, for any n and any cache of these heads;
+ * they do not decrease with H, and calls with other H may use one workspace in turn.
+ */
 int w4a16_attention_decode_workspace(int64_t H, int64_t kv_heads, int64_t* bytes);
 
 /*

@@ -309,7 +309,7 @@ class KVCache:
     """A paged key-value cache (include/w4a16.h): the tensors and the handle that the kv_*
     functions and attention_decode take.  dtype torch.bfloat16, or torch.float8_e4m3fn with
     a power-of-two exponent for each token's key and value of a head.  Calls on one cache
-    are ordered by the caller."""
+    are ordered by the caller, who keeps it until they, and graphs with them, have run."""
 
     def __init__(self, layers: int, num_pages: int, kv_heads: int, num_slots: int, max_pages: int,
                  page_tokens: int = 64, dtype=torch.bfloat16, head_dim: int = 128, device="cuda"):
@@ -358,11 +358,13 @@ class KVCache:
         size = lib().w4a16_kv_scratch_bytes(num_pages, num_slots)
         if size == 0:
             raise W4A16Error("w4a16_kv_scratch_bytes", ERR_UNSUPPORTED)
+        self._workspace_bytes = {}
         self._scratch = torch.zeros(size, dtype=torch.uint8, device=pages.device)
+        self._workspace = None  # for calls that name none
         if not torch.cuda.is_current_stream_capturing():
+            self._workspace = self._largest_workspace()
             # (the first call may be on another stream)
             torch.cuda.current_stream(pages.device).synchronize()
-        self._workspaces, self._workspace_bytes = {}, {}
         self._struct = KVCacheStruct(
             pages.data_ptr(), None if exponents is None else exponents.data_ptr(), page_table.data_ptr(),
             seq_len.data_ptr(), page_refs.data_ptr(), self._scratch.data_ptr(), layers, num_pages, kv_heads,
@@ -373,6 +375,20 @@ class KVCache:
         """A workspace for attention_decode with H query heads, zeroed on `stream`."""
         with _allocating_on(stream):
             return torch.zeros(self.workspace_bytes(H), dtype=torch.uint8, device=self.pages.device)
+
+    def _largest_workspace(self) -> torch.Tensor:
+        """For any number of query heads: the size does not decrease with it."""
+        return self.new_workspace(self.kv_heads * (65535 // self.kv_heads))
+
+    def _own_workspace(self, H: int, stream) -> torch.Tensor:
+        if self._workspace is None:  # the cache was made under capture
+            with _allocating_on(stream):
+                if torch.cuda.is_current_stream_capturing():
+                    # zeroed by the graph whenever it runs, and no other call's
+                    return self.new_workspace(H)
+                self._workspace = self._largest_workspace()
+                torch.cuda.current_stream(self.pages.device).synchronize()
+        return self._workspace
 
     def workspace_bytes(self, H: int) -> int:
         if H not in self._workspace_bytes:
@@ -445,14 +461,12 @@ def attention_decode(cache: KVCache, layer: int, qkv: torch.Tensor, slots: torch
                      workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """Attention of one new token per sequence over the cache, its key and value stored
     (include/w4a16.h): qkv bf16 [n, (H + 2 kv_heads) 128], slots int32 [n] -> out bf16
-    [n, H 128].  Without `workspace` the cache's own is used, made on the first call: calls
-    on several streams at once need one each (KVCache.new_workspace)."""
+    [n, H 128].  Without `workspace` the cache's own is used: calls on several streams at once
+    need one each (KVCache.new_workspace)."""
     _need_qkv(cache, qkv, H)
     n = _need_list(slots, qkv.shape[0])
     if workspace is None:
-        workspace = cache._workspaces.get(H)
-        if workspace is None:
-            workspace = cache._workspaces[H] = cache.new_workspace(H, stream)
+        workspace = cache._own_workspace(H, stream)
     elif not (workspace.is_cuda and workspace.is_contiguous()
               and workspace.numel() * workspace.element_size() >= cache.workspace_bytes(H)):
         raise ValueError("expected a workspace of KVCache.new_workspace(H)")
