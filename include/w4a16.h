@@ -403,9 +403,10 @@ int w4a16_kv_write(const w4a16_kv_cache* cache, int64_t layer, const void* qkv_b
  *              slot twice in the list all rows are zero and nothing is stored
  *   out_bf16   [n, H * 128] bf16, written in full
  *   workspace  w4a16_attention_decode_workspace bytes, zeroed by the caller
- *              before its first use and after a W4A16_ERR_TIMEOUT; calls leave it
- *              ready for the next one.  Calls that may run at the same time need
- *              one each.
+ *              before its first use and after a W4A16_ERR_TIMEOUT (the status word
+ *              keeps the first error, so after any other that may have hidden one);
+ *              calls leave it ready for the next one.  Calls that may run at the
+ *              same time need one each.
  * Scores and sums in fp32; the softmax's weights are rounded to bf16 (kv_bits 16)
  * or fp16 (kv_bits 8) for the product with the values; one bf16 rounding at the
  * store.  Keys outside the range may hold anything, NaN included.

@@ -11,6 +11,7 @@ import contextlib
 import ctypes
 import os
 import re
+import weakref
 
 import torch
 
@@ -25,6 +26,7 @@ OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_ALIGNMENT, ERR_CUDA, ERR_TIMEOUT, ERR_
 ACT_NONE, ACT_SWIGLU, ACT_GELU = range(3)
 
 _lib = None
+_caches = weakref.WeakSet()  # whose own workspaces an error may have left in use
 
 
 class W4A16Error(RuntimeError):
@@ -370,6 +372,7 @@ class KVCache:
             seq_len.data_ptr(), page_refs.data_ptr(), self._scratch.data_ptr(), layers, num_pages, kv_heads,
             page_tokens, head_dim, num_slots, max_pages, 8 if e4m3 else 16)
         self._ref = ctypes.byref(self._struct)
+        _caches.add(self)
 
     def new_workspace(self, H: int, stream=None) -> torch.Tensor:
         """A workspace for attention_decode with H query heads, zeroed on `stream`."""
@@ -510,4 +513,16 @@ def route(M: int, N: int, K: int, g: int = 128, act: int = ACT_NONE, residual: b
 
 
 def get_device_error(stream=None) -> int:
-    return int(lib().w4a16_get_device_error(_stream(stream)))
+    """Synchronises the stream, reads and clears the device status word.  After an error the
+    caches' own workspaces are zeroed, which a call that gave up leaves in use (a workspace
+    that the caller passes is the caller's to zero)."""
+    rc = int(lib().w4a16_get_device_error(_stream(stream)))
+    if rc != OK:  # (the word keeps the first error: any may hide a timeout)
+        used = [c._workspace for c in list(_caches) if c._workspace is not None]
+        if used and rc != ERR_CUDA:
+            torch.cuda.synchronize()
+            with _allocating_on(stream):
+                for workspace in used:
+                    workspace.zero_()
+            torch.cuda.synchronize()
+    return rc

@@ -88,3 +88,59 @@ def test_heads_in_turn():
             x = cases[i]
             assert torch.equal(W.attention_decode(c, 1, x.qkv, x.slots, x.H), want[i])
     assert W.get_device_error() == W.OK
+
+
+@pytest.mark.parametrize("bits,H,Hkv,T,lengths", [(16, 8, 8, 64, [20000, 30000]), (8, 16, 8, 64, [40000, 9])])
+def test_after_a_timeout(bits, H, Hkv, T, lengths):
+    """A call that gave up leaves some of a row's parts counted (here with limits at which some of
+    the CTAs' first copies are in time).  Once its error is read, calls and replayed graphs
+    that use the cache's own workspace are right again.  (Queries differ from call to call, so that
+    a part of another call is not the same.)"""
+    W = _W()
+    case = Case(bits, H, Hkv, T, lengths, 24)
+    c = case.cache
+    rows = [case.qkv, case.qkv.roll(D, 1).mul(-0.5)]
+    want = [W.attention_decode(c, 1, r, case.slots, H) for r in rows]
+    qkv = rows[0].clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = W.attention_decode(c, 1, qkv, case.slots, H)
+    assert W.get_device_error() == W.OK
+    timeouts = 0
+    for limit in [1, 200] + 3 * list(range(600, 2000, 100)):  # ns
+        W.set_wait_limit(limit)
+        try:
+            W.attention_decode(c, 1, case.qkv, case.slots, H)
+            timeouts += W.get_device_error() == W.ERR_TIMEOUT
+        finally:
+            W.set_wait_limit(0)
+        for r, w in zip(rows[::-1], want[::-1]):
+            assert torch.equal(W.attention_decode(c, 1, r, case.slots, H), w), limit
+        for r, w in zip(rows[::-1], want[::-1]):
+            qkv.copy_(r)
+            graph.replay()
+            assert torch.equal(out, w), limit
+        assert W.get_device_error() == W.OK
+    assert timeouts > 0
+
+
+def test_another_error_before_the_timeout():
+    """The status word keeps the first error, which may hide a timeout: reading any of them
+    makes the workspace ready."""
+    W = _W()
+    case = Case(16, 8, 8, 64, [20000, 30000], 25)
+    c, H = case.cache, 8
+    rows = [case.qkv, case.qkv.roll(D, 1).mul(-0.5)]
+    want = [W.attention_decode(c, 1, r, case.slots, H) for r in rows]
+    wrong = torch.full_like(case.slots, c.num_slots)
+    for limit in 3 * list(range(600, 2000, 100)):
+        W.attention_decode(c, 1, rows[0], wrong, H)
+        W.set_wait_limit(limit)
+        try:
+            W.attention_decode(c, 1, rows[0], case.slots, H)
+            assert W.get_device_error() == W.ERR_INVALID_ARG
+        finally:
+            W.set_wait_limit(0)
+        for r, w in zip(rows[::-1], want[::-1]):
+            assert torch.equal(W.attention_decode(c, 1, r, case.slots, H), w), limit
+        assert W.get_device_error() == W.OK
