@@ -558,10 +558,15 @@ __device__ void produce(const DecodeArgs& a, const CacheMaps& maps, Shared& sh, 
 }
 
 // What makes an output of a sum relative to 2^w, with weights whose sum is l relative to 2^m.
+// In two factors, to be multiplied with the sum one after the other: a value's exponent may be -120, and
+// with a sum of weights in the thousands their product would be a subnormal of a few bits.
 template <bool E4M3>
-__device__ __forceinline__ float output_scale(float l, float m, float w) {
-    // (in two steps: an exponent may be -120, and ex2 flushes below 2^-126)
-    return E4M3 ? 1.0f / l * ex2(-kWeightTop) * ex2(w - m) : 1.0f / l;
+__device__ __forceinline__ float2 output_scale(float l, float m, float w) {
+    return E4M3 ? make_float2(1.0f / l * ex2(-kWeightTop), ex2(w - m)) : make_float2(1.0f / l, 1.0f);
+}
+template <bool E4M3>
+__device__ __forceinline__ float scaled(float sum, float2 scale) {
+    return E4M3 ? sum * scale.x * scale.y : sum * scale.x;
 }
 
 // A column of a warp's output lies in the warp's own rows of the stage, which no other warp
@@ -663,9 +668,11 @@ __device__ __noinline__ void join_pending(const float* parts, uint16_t* out, int
         for (int o = 8; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
         bad = (__ballot_sync(0xffffffffu, bad) >> (lane & 16) & 0xFFFFu) != 0;
         if (n == 0) continue;
-        const float scale = output_scale<E4M3>(l, m, top);
-        uint4 o = make_uint4(bf16_pair(sum[0] * scale, sum[1] * scale), bf16_pair(sum[2] * scale, sum[3] * scale),
-                             bf16_pair(sum[4] * scale, sum[5] * scale), bf16_pair(sum[6] * scale, sum[7] * scale));
+        const float2 scale = output_scale<E4M3>(l, m, top);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum[k] = scaled<E4M3>(sum[k], scale);
+        uint4 o = make_uint4(bf16_pair(sum[0], sum[1]), bf16_pair(sum[2], sum[3]), bf16_pair(sum[4], sum[5]),
+                             bf16_pair(sum[6], sum[7]));
         if (bad) {
             o = make_uint4(0, 0, 0, 0);
             if (l16 == 0) record_status(status, kInvalid);
@@ -733,9 +740,11 @@ __device__ void finish(const DecodeArgs& a, Shared& sh, const uint8_t* stage_mem
                     }
                 }
                 if (whole) {
-                    const float f = output_scale<E4M3>(l, m, w);
+                    const float2 f = output_scale<E4M3>(l, m, w);
                     reinterpret_cast<uint2*>(out + col * kKvHeadDim)[lane] =
-                        bad ? make_uint2(0, 0) : make_uint2(bf16_pair(o.x * f, o.y * f), bf16_pair(o.z * f, o.w * f));
+                        bad ? make_uint2(0, 0)
+                            : make_uint2(bf16_pair(scaled<E4M3>(o.x, f), scaled<E4M3>(o.y, f)),
+                                         bf16_pair(scaled<E4M3>(o.z, f), scaled<E4M3>(o.w, f)));
                 } else {
                     reinterpret_cast<float4*>(part + col * kKvHeadDim)[lane] = o;
                     if (lane == 0)  // (a sum is never negative: marks a bad page index)
