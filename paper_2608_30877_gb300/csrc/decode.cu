@@ -109,6 +109,8 @@ __host__ __device__ inline int part_floats(int cols) { return cols * (kKvHeadDim
 // The workspace's counters, one for each CTA.
 __host__ __device__ inline int counter_bytes(int ctas) { return (ctas * 4 + 15) / 16 * 16; }
 
+// (Positions go up to 2^31 - 16, and a tile may end at 2^31: comparisons take from the length, not add to
+// a tile's first key.)
 // What the producer says about a stage.
 struct alignas(16) Unit {
     int row, head, block, key0;       // the tile's first key
@@ -348,6 +350,7 @@ __device__ void produce(const DecodeArgs& a, const CacheMaps& maps, Shared& sh, 
     // (of a group the even lane loads the codes).
     constexpr int kLaneTokens = E4M3 ? 8 : 16;
     const bool has_tokens = lane < kTile / kLaneTokens, has_group = has_tokens && lane * kLaneTokens % 16 == 0;
+    const int lane_key = has_tokens ? lane * kLaneTokens : 0;
     const int group = lane * kLaneTokens / 16, of_box = group & (maps.groups - 1);
     const uint8_t* const exponents = E4M3 ? kv.exponents + kv_exponent(kv, a.p.layer, 0, 0, 0, 0) : nullptr;
 
@@ -442,7 +445,7 @@ __device__ void produce(const DecodeArgs& a, const CacheMaps& maps, Shared& sh, 
         const uint32_t bar = smem_u32(&sh.full[st]);
         // The groups that the row sees, by boxes as large as a page allows, or each by itself at
         // the row's ends.
-        const int key = key0 + lane * kLaneTokens;  // of this lane's tokens
+        const int key = key0 + lane_key;  // of this lane's tokens
         const int id = __shfl_sync(0xffffffffu, ids, ((key >> kv.page_shift) - ids_from) & 31);
         const bool id_ok = id >= 0 && id < kv.num_pages;
         const int32_t row_at = (((id_ok ? id : 0) * kv.kv_heads + head) << kv.page_shift) +
@@ -475,7 +478,7 @@ __device__ void produce(const DecodeArgs& a, const CacheMaps& maps, Shared& sh, 
                           256, bar);
             bytes += q_cols * 256;
         }
-        const bool fresh = key0 + kTile >= r.len;
+        const bool fresh = key0 >= r.len - kTile;
         int page = -1;
         if (fresh) {
             if (lane < 2)
@@ -798,7 +801,7 @@ __device__ __forceinline__ void mend_tile(const DecodeArgs& a, Shared& sh, int s
     const Unit& t = sh.unit[st];
     constexpr int kStep = kTile / kWarps;  // the keys that this warp mends
     const int key = t.key0 + warp * kStep;
-    if (key < t.len && key + kStep > t.low) {
+    if (key < t.len && key > t.low - kStep) {
         for (int i = lane; i < kStep * (E4M3 ? 8 : 16); i += 32) {
             const int r = i >> (E4M3 ? 3 : 4), unit = i & (E4M3 ? 7 : 15);
             if (key + r < t.low || key + r >= t.len)
@@ -927,7 +930,7 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
             tile = stage_mem + st * kStageBytes;
             const uint32_t keys = smem_u32(tile), values = keys + kValueOffset;
             s.bad |= (flags & kBad) != 0;
-            const bool edge = key0 < low || key0 + kTile >= len;
+            const bool edge = key0 < low || key0 >= len - kTile;
             if (edge) {
                 mend_tile<E4M3>(a, sh, st, tile, warp, lane, !s.bad);
                 // others read what this warp mended
@@ -935,7 +938,7 @@ __device__ void consume(const DecodeArgs& a, Shared& sh, uint8_t* stage_mem, uin
             }
             for (int step = key_warp; step < kWarps; step += key_warps) {
                 const int key = key0 + step * kStep;
-                if (key >= len || key + kStep <= low) continue;
+                if (key >= len || key <= low - kStep) continue;
                 // scores of the step's matrices of 8 keys: row g, columns 2c and 2c + 1
                 float acc[2][4];  // e4m3: of two groups; bf16: of even and odd dimensions
 #pragma unroll

@@ -45,3 +45,43 @@ def test_values_of_the_smallest_exponents(H, Hkv):
         err = np.abs(out[i].double().cpu().numpy().reshape(H, D) - ref)
         bound = 1.01 * 2.0 ** -9 * np.abs(ref) + (2.0 ** -8 + 2.0 ** -10) * size
         assert (err <= bound).all(), f"row {i}: worst {np.max(err / bound):.3f} of the bound"
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("before", [0, 1, 17, 40, 120])
+def test_the_last_tokens_below_two_to_the_31(bits, before):
+    """The longest sequence of a table, 2^31 - 16 tokens in pages of 16, seen through a window: its
+    last tile ends where 31 bits do."""
+    W = _W()
+    H, Hkv, T, window, pages = 6, 2, 16, 300, 24
+    entries = (2 ** 31 - 1) // T
+    n = entries * T - before
+    table = torch.zeros((1, entries), dtype=torch.int32, device="cuda")
+    last = (n - 1) // T
+    table[0, last - pages + 1:last + 1] = torch.randperm(pages, device="cuda").to(torch.int32)
+    g = torch.Generator(device="cuda").manual_seed(before + bits)
+    shape = (1, 2, pages, Hkv, T, D)
+    if bits == 16:
+        pool, exps = torch.randn(shape, generator=g, device="cuda").bfloat16(), None
+    else:
+        pool = (torch.randn(shape, generator=g, device="cuda") * 112).clamp(-448, 448).to(torch.float8_e4m3fn)
+        exps = torch.randint(116, 124, (1, pages, Hkv, T, 2), generator=g, device="cuda", dtype=torch.uint8)
+    refs = torch.ones(pages, dtype=torch.int32, device="cuda")
+    c = W.KVCache.from_tensors(pool, table, torch.tensor([n], dtype=torch.int32, device="cuda"), refs, exps)
+    qkv = torch.randn((1, (H + 2 * Hkv) * D), generator=g, device="cuda").bfloat16()
+    out = W.attention_decode(c, 0, qkv, R.i32([0]), H, window=window)
+    assert W.get_device_error() == W.OK
+    pos = torch.arange(n - window, n, device="cuda")
+    page, at = table[0, pos // T].long(), pos % T
+    if bits == 16:
+        kv = torch.stack([pool[0, w][page, :, at] for w in (0, 1)]).double().cpu().numpy()
+    else:
+        codes = np.stack([pool.view(torch.uint8)[0, w][page, :, at].view(torch.float8_e4m3fn).double().cpu().numpy()
+                          for w in (0, 1)])
+        e = exps[0][page, :, at].int().cpu().numpy() - 127
+        kv = np.stack([np.ldexp(codes[w], e[..., w, None]) for w in (0, 1)])
+    row = qkv[0].double().cpu().numpy()
+    assert np.array_equal(kv[:, -1], R.held(row[H * D:].reshape(2, Hkv, D), bits))
+    ref, size = R.attention(row[:H * D].reshape(H, D), kv[0], kv[1])
+    err = np.abs(out[0].double().cpu().numpy().reshape(H, D) - ref)
+    assert (err <= 1.01 * 2.0 ** -9 * np.abs(ref) + (2.0 ** -8 + 2.0 ** -10) * size).all()
