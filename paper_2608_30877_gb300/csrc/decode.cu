@@ -12,8 +12,9 @@
 //    and short rows share a CTA.  Everything follows from the lengths on the device, so
 //    that a captured graph serves growing sequences.
 //  * Stages.  One warp walks the run: it looks pages up in the table, and brings the pieces of
-//    a tile by TMA into a ring of three stages (192 KB in flight on an SM's two CTAs), with
-//    the row's queries and the new token's key and value.
+//    a tile by TMA into a ring of three stages (192 KB in flight on an SM's two CTAs; with 17
+//    and more queries of a key head one CTA fits, 96 KB), with the row's queries and the
+//    new token's key and value.
 //  * Products.  Four warps split a tile's keys, 16 at a time: S^T = K Q^T and O^T += V^T P^T by
 //    warp-level MMAs whose A operand is the cache (16 keys or 16 values' dimensions) and whose
 //    N = 8 columns are the queries of a key head, so that few queries waste few columns.  The
@@ -23,8 +24,10 @@
 //    warp adds them up, stores the result and releases the stage (with the four warps doing
 //    that together, they stood still 1 us per item).
 //  * More than 8 queries of a key head: the warps split the columns before the keys, up to 32
-//    columns, then further items.  (16 columns in a warp passed the registers' limit on the 8-bit
-//    cache: 12 queries of a head 86 us, and 69 with 8, before small weights had products of their own; in bf16 100 either way, 32 queries 71
+//    columns, then further items.  With 32 columns a CTA takes 121856 of an SM's 233472 bytes of shared
+//    memory (108800 with 8, 113152 with 16), so that the grid of two per SM runs as two waves of one.
+//    (16 columns in a warp passed the registers' limit on the 8-bit cache: 12 queries of a head 86 us, and
+//    69 with 8, before small weights had products of their own; in bf16 100 either way, 32 queries 71
 //    and 75, 64 queries 80 and 74.)
 //  * Join.  A CTA's first and last items may continue in other CTAs: each then writes its
 //    part to the workspace, and when all its work is done counts itself present for both
@@ -33,16 +36,23 @@
 //    the same bits every time.
 //
 // Measured: 64 rows of 200 to 1024 tokens and 96 heads in pages of 64 tokens 290 us (6.6 TB/s, 97%
-// of the copy bandwidth), in 8 bits 155 (6.2 TB/s, 91%); 37 rows of 1 to 8192 tokens, 12 queries to
+// of the copy bandwidth), in 8 bits 156 (6.2 TB/s, 91%); 37 rows of 1 to 8192 tokens, 12 queries to
 // each of 8 key heads 99 us (88%).  Calls of less than 50 us are bound by the way to the first
 // tile (lengths, table, keys: four loads in a row, 3.5 us), by CTAs that end apart, and by the join
-// (2 to 4 us): three contexts of 131072 tokens in 8 bits 43.5 us (30 at the copy bandwidth), one
-// row of 333 tokens 9.4 (2.4).
+// (2 to 4 us): three contexts of up to 131072 tokens in 8 bits 43.5 us (30 at the copy bandwidth), one
+// row of 333 tokens 9.6 (2.4).  Far from it, in us of 64 rows of 200 to 1024 tokens: 8 key heads of 12 queries
+// each in 8 bits 39 (12), of 32 queries each 88 (25) and in 8 bits 98 (13).
+//
+// Weights.  They are rounded to bf16 next to bf16 values, since an MMA's operands are of one type, and
+// the sum that divides the output is of the rounded ones: each is off by 2^-9 at most, as the output's
+// own rounding is, and the outputs are off by 0.0021 of their norm where weights in fp32 leave 0.0017 (64
+// pairs, against 64 bits).
 //
 // 8-bit cache.  Keys' and values' codes are converted to fp16, exactly, and multiplied with
-// the queries in fp16 (scaled by a power of two, which keeps all their bits) and the weights in
-// fp16.  (Warp-level MMAs on e4m3 are no way around that: on this machine each takes 2 fp16 MMAs
-// and the conversion of both operands.)  A key's exponent goes to its score, a value's exponent
+// the queries in fp16 (scaled by a power of two, which keeps the bits of all that are 2^-24 of their
+// row's largest or more; smaller ones are off by 2^-32 of that at most) and the weights in fp16.
+// (Warp-level MMAs on e4m3 are no way around that: on this machine each takes 2 fp16 MMAs and the
+// conversion of both operands.)  A key's exponent goes to its score, a value's exponent
 // to its weight, and the weights that multiply the codes are relative to the largest of these
 // products, whose running maximum a column keeps next to its scores'; small ones have MMAs of
 // their own.

@@ -4,7 +4,9 @@
 // A page is free if no sequence refers to it; the free pages are found by scanning the
 // reference counts, lowest index first, so there is no list to keep in step with them and
 // every result is a function of the tables alone (integer atomics commute).  Each
-// operation runs its checks before its first change, so an error leaves the cache as it was.
+// operation runs its checks before its first change, so an error leaves the cache as it was; growth
+// that is refused marks its slots in the scratch buffer, and what would store the tokens
+// that were not added (writes, decode attention) leaves marked slots alone.
 // One CTA plans; what has to be copied (an extend's shared last pages, a compaction's
 // moved pages) goes to a list in the scratch buffer that a second kernel works off over
 // the whole GPU.  Bound by latency but for the copies, which HBM bounds: a thread takes a list

@@ -4,7 +4,7 @@
 // in a page a head's tokens lie in one run.  A CTA takes 1 to 32 tokens (few heads, many tokens);
 // 16 threads move a row of 128 values in 16-byte pieces (and reduce its largest value for the 8-bit
 // form), several rows under way together.  Bound by HBM: each value is read once and written
-// once; 39000 tokens of 96 heads take 561 us (6.8 TB/s, the copy bandwidth), in 8 bits 508 (83%).  Short
+// once; 39000 tokens of 96 heads take 561 us (6.8 TB/s, the copy bandwidth), in 8 bits 509 (83%).  Short
 // calls are bound by the way to a token's place: three loads in a row before the first row (13000
 // tokens of 8 heads in 8 bits 20 us, 13 at the copy bandwidth).  A row's addresses are sums of
 // 32-bit offsets: with divisions and 64-bit products per row the issue slots were the bound.
