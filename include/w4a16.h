@@ -422,6 +422,133 @@ int w4a16_attention_decode(const w4a16_kv_cache* cache, int64_t layer, const voi
 int w4a16_attention_decode_workspace(int64_t H, int64_t kv_heads, int64_t* bytes);
 
 /*
+ * The residual stream between two blocks of a decoder layer, and the norm that the next block
+ * reads, in one pass:
+ *   h = residual_scale * residual + gate * post(block)
+ *   out = pre(h)
+ * with pre and post W4A16_NORM_RMS, v / sqrt(mean(v^2) + eps), or W4A16_NORM_LAYER,
+ * (v - mean(v)) / sqrt(mean((v - mean(v))^2) + eps), over the row's D values, each times
+ * (weight_offset + weight) plus a bias.
+ *   residual          [M, D] bf16 (residual_bits 16) or fp32 (32), device
+ *   block_bf16        [M, D], the block's output; NULL: h = residual_scale * residual
+ *   gate_bf16         [gate_rows, D], gate_rows 1 (the same for every row) or M; NULL: 1
+ *   post_weight_bf16  [D]; NULL: no norm of the block's output.  post_bias_bf16: [D] or NULL
+ *   weight_bf16       [D]; NULL: a factor of 1.  bias_bf16: [D] or NULL
+ *   residual_out      [M, D] as residual, or NULL; it may be residual itself
+ *   out_bf16          [M, D]; NULL: only h
+ * Everything is computed in fp32, with one rounding of h and one of out, which is of h before its
+ * own.  Squares that overflow are scaled; infinities and NaN go where the formula takes
+ * them, in their own row.  1e-12 <= eps <= 1; D <= 49152, and <= 24560 where it is no multiple of 8
+ * (else W4A16_ERR_UNSUPPORTED).
+ */
+typedef enum {
+    W4A16_NORM_RMS = 0,
+    W4A16_NORM_LAYER = 1
+} w4a16_norm;
+int w4a16_residual_norm(const void* residual, int residual_bits, const void* block_bf16,
+                        const void* gate_bf16, int64_t gate_rows, const void* post_weight_bf16,
+                        const void* post_bias_bf16, const void* weight_bf16, const void* bias_bf16,
+                        int64_t M, int64_t D, int norm, float residual_scale, float eps,
+                        float weight_offset, void* residual_out, void* out_bf16, void* stream);
+
+/*
+ * Rotary positions: pair i of a head's first rot_dim values, (a, b), becomes
+ *   (a cos t - b sin t, a sin t + b cos t) * factor,   t = position * theta_i, i < rot_dim / 2,
+ * the pair being values (i, i + rot_dim / 2) of the head (W4A16_ROTARY_HALF) or (2i, 2i + 1)
+ * (W4A16_ROTARY_PAIRS).  Values from rot_dim on stay as they are.
+ *
+ * w4a16_rotary_table (host) gives the frequencies: theta_i = base^(-2i / rot_dim), held as turns
+ * per token, theta / (2 pi), in units of 2^-64, so that an angle is exact modulo a turn at any
+ * position.  Scaled for contexts longer than the trained one:
+ *   LINEAR    theta / factor
+ *   BY_TURNS  theta kept where it makes high_turns turns or more over trained_tokens, theta / factor
+ *             for low_turns or fewer, in between the two weighted linearly in the turns
+ *   BY_INDEX  the same ends, weighted linearly in i between the whole i next to them
+ *   turns     HOST uint64 [rot_dim / 2], which the caller copies to the device
+ * rot_dim a multiple of 16 up to 256; base >= 1; factor >= 1; 0 < low_turns < high_turns.
+ *
+ * w4a16_rotary turns the queries and keys of a fused projection in place:
+ *   qkv_bf16       [M, (H + 2 kv_heads) * d], columns as w4a16_kv_write reads them; the values
+ *                  are not touched.  d a multiple of 8; H or kv_heads may be 0
+ *   seq_start_i32  [nseq + 1] as in w4a16_attention_prefill: row m of sequence s has position
+ *                  first[s] + m - seq_start[s]; NULL: nseq = M sequences of one row each.  A
+ *                  table that decreases or leaves [0, M] records W4A16_ERR_INVALID_ARG; rows outside
+ *                  every sequence are left as they are
+ *   first_i32      [nseq] first positions; negative: the sequence's rows are left as they are.
+ *                  NULL: 0
+ *   turns_u64      [rot_dim / 2] device, rot_dim <= d
+ *
+ * w4a16_kv_rotary takes the positions from a cache: rows [seq_start[i], seq_start[i+1]) are the LAST
+ * tokens of the sequence of slots_i32[i], as w4a16_kv_write has them (after w4a16_kv_extend, before
+ * w4a16_kv_write); seq_start_i32 NULL: row i is the last token of slots_i32[i], as in
+ * w4a16_attention_decode.  Rows of a slot of -1, and of an empty sequence without seq_start, are left as
+ * they are; so are those of a slot or length out of range and of a slot whose growth was refused, which
+ * record W4A16_ERR_INVALID_ARG.  A slot may occur more than once.
+ */
+typedef enum {
+    W4A16_ROTARY_HALF = 0,
+    W4A16_ROTARY_PAIRS = 1
+} w4a16_rotary_layout;
+typedef enum {
+    W4A16_ROTARY_SCALE_NONE = 0,
+    W4A16_ROTARY_SCALE_LINEAR = 1,
+    W4A16_ROTARY_SCALE_BY_TURNS = 2,
+    W4A16_ROTARY_SCALE_BY_INDEX = 3
+} w4a16_rotary_scaling;
+int w4a16_rotary_table(int64_t rot_dim, double base, int scaling, double factor, int64_t trained_tokens,
+                       double low_turns, double high_turns, uint64_t* turns);
+int w4a16_rotary(void* qkv_bf16, const void* seq_start_i32, const void* first_i32, int64_t nseq,
+                 int64_t M, int64_t H, int64_t kv_heads, int64_t d, const void* turns_u64,
+                 int64_t rot_dim, int layout, float factor, void* stream);
+int w4a16_kv_rotary(const w4a16_kv_cache* cache, void* qkv_bf16, const void* seq_start_i32,
+                    const void* slots_i32, int64_t nseq, int64_t M, int64_t H, const void* turns_u64,
+                    int64_t rot_dim, int layout, float factor, void* stream);
+
+/*
+ * Log probabilities from a head's logits: for each row x of V logits, with lse = ln sum_j e^x_j,
+ *   out_logp[m] = x[targets[m]] - lse           (0 where the target is -1)
+ *   out_entropy[m] = -sum_j p_j ln p_j,  p_j = e^(x_j - lse)
+ *   out_index[m, 0..k), out_score[m, 0..k)      the k largest logits' columns and x - lse
+ * The k largest in descending order as w4a16_topk_smallest orders them (+0 before -0, every NaN after
+ * every number), equal ones by ascending column.
+ *   logits         [M] rows of V, row_stride >= V elements apart, bf16 (logit_bits 16) or fp32 (32);
+ *                  the first one 16-byte aligned, the others wherever row_stride puts them
+ *   targets_i32    [M] or NULL; other than -1 outside [0, V): as -1, and W4A16_ERR_INVALID_ARG is
+ *                  recorded in the device status word
+ *   k              0 .. 64, <= V; V <= 2^20
+ *   out_logp_f32   [M], with targets only; out_entropy_f32: [M] or NULL; out_index_i32 and
+ *                  out_score_f32: [M, k], NULL for k = 0
+ * Logits of -infinity have probability 0.  A row of nothing else has log probabilities of -infinity
+ * and entropy 0; one with a NaN or +infinity has NaN for both, and for its scores.
+ * Sums in fp32.
+ */
+int w4a16_log_probs(const void* logits, int logit_bits, int64_t M, int64_t V, int64_t row_stride,
+                    const void* targets_i32, int64_t k, void* out_logp_f32, void* out_entropy_f32,
+                    void* out_index_i32, void* out_score_f32, void* stream);
+
+/*
+ * Low-rank adapters of many sequences at once beside a shared projection:
+ *   out[m] = base[m] + scale[a] * (x[m] A[a]^T) B[a]^T,   a = adapters[s] for the rows m of sequence s
+ *   x_bf16         [M, K], the projection's input; base_bf16 [M, N], its output
+ *   a_bf16         [pool, R, K]; b_bf16 [pool, N, R]; scale_f32 [pool]
+ *   seq_start_i32  [nseq + 1] as in w4a16_attention_prefill; NULL: nseq = M sequences of one row.  Rows
+ *                  outside every sequence have no adapter; a table that decreases or leaves [0, M]
+ *                  records W4A16_ERR_INVALID_ARG
+ *   adapters_i32   [nseq]; -1: none (out = base).  Others outside [0, pool) count as -1 and record
+ *                  W4A16_ERR_INVALID_ARG
+ *   out_bf16       [M, N], written in full; it may be base itself
+ *   workspace      w4a16_add_adapters_workspace bytes; what it holds before or after a call does not
+ *                  matter.  Calls that may run at the same time need one each
+ * K a multiple of 64, R a multiple of 8 up to 64 (W4A16_ERR_UNSUPPORTED).  Sums in fp32; scale (x A^T) is
+ * rounded to bf16 for the product with B, and the sum with base once.
+ */
+int w4a16_add_adapters(const void* x_bf16, const void* a_bf16, const void* b_bf16, const void* scale_f32,
+                       int64_t pool, const void* seq_start_i32, const void* adapters_i32, int64_t nseq,
+                       int64_t M, int64_t N, int64_t K, int64_t R, const void* base_bf16, void* out_bf16,
+                       void* workspace, void* stream);
+int w4a16_add_adapters_workspace(int64_t M, int64_t nseq, int64_t K, int64_t R, int64_t* bytes);
+
+/*
  * Synchronises `stream`, then reads and clears the device status word.
  * Returns W4A16_OK, the first error a kernel recorded since the last read
  * (W4A16_ERR_TIMEOUT from a bounded wait that ran out, W4A16_ERR_INVALID_ARG

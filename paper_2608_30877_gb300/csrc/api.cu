@@ -770,4 +770,4 @@ extern "C" const char* w4a16_status_string(int status) {
     }
 }
 
-extern "C" int w4a16_version(void) { return 200; }
+extern "C" int w4a16_version(void) { return 300; }

@@ -93,7 +93,7 @@ uint64_t wait_limit_ns();  // internal.h
 // A launch that may begin while the kernel before it in the stream ends; the kernel calls
 // grid_wait (ptx.cuh) before it touches global memory.
 template <typename... P, typename... A>
-cudaError_t launch_overlapped(void (*kernel)(P...), int grid, int block, int smem, cudaStream_t stream,
+cudaError_t launch_overlapped(void (*kernel)(P...), dim3 grid, int block, int smem, cudaStream_t stream,
                               const A&... args) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;

@@ -1,6 +1,7 @@
 // C ABI of the paged key-value cache (declared in include/w4a16.h): argument validation and
 // dispatch.
 #include "kv.h"
+#include "layer.h"
 #include "w4a16.h"
 
 #include <cuda.h>
@@ -195,6 +196,47 @@ extern "C" int w4a16_kv_write(const w4a16_kv_cache* cache, int64_t layer, const 
                           static_cast<const int32_t*>(slots_i32), static_cast<int>(layer),
                           static_cast<int>(nseq), static_cast<int>(M), static_cast<int>(H)};
     return status_of(launch_kv_write(view_of(*cache, st.status), p, st.sm_count, static_cast<cudaStream_t>(stream)));
+}
+
+extern "C" int w4a16_kv_rotary(const w4a16_kv_cache* cache, void* qkv_bf16, const void* seq_start_i32,
+                               const void* slots_i32, int64_t nseq, int64_t M, int64_t H, const void* turns_u64,
+                               int64_t rot_dim, int layout, float factor, void* stream) {
+    CacheSpans spans;
+    int rc = check_cache(cache, &spans);
+    if (rc != W4A16_OK) return rc;
+    if (qkv_bf16 == nullptr || slots_i32 == nullptr || turns_u64 == nullptr || nseq <= 0 || M <= 0 || H < 0 ||
+        rot_dim <= 0 || rot_dim > cache->head_dim || !std::isfinite(factor) ||
+        (layout != W4A16_ROTARY_HALF && layout != W4A16_ROTARY_PAIRS) || (seq_start_i32 == nullptr && nseq != M))
+        return W4A16_ERR_INVALID_ARG;
+    if (M > kMaxDim - 16 || nseq > kMaxDim / 2 || H > 65535 || rot_dim % 16 != 0) return W4A16_ERR_UNSUPPORTED;
+    const Span args[4] = {{qkv_bf16, M * (H + 2 * cache->kv_heads) * cache->head_dim * 2},
+                          {seq_start_i32, (nseq + 1) * 4},
+                          {slots_i32, nseq * 4},
+                          {turns_u64, rot_dim / 2 * 8}};
+    for (int i = 0; i < 4; ++i) {
+        rc = check_argument(spans, args[i]);
+        if (rc != W4A16_OK) return rc;
+        if (i > 0 && overlaps(args[0], args[i])) return W4A16_ERR_INVALID_ARG;
+    }
+    LibraryState st;
+    rc = library_state(&st);
+    if (rc != W4A16_OK) return rc;
+    RotaryParams p;
+    p.qkv = static_cast<uint16_t*>(qkv_bf16);
+    p.seq_start = static_cast<const int32_t*>(seq_start_i32);
+    p.first = static_cast<const int32_t*>(slots_i32);
+    p.turns = static_cast<const uint64_t*>(turns_u64);
+    p.status = st.status;
+    p.M = static_cast<int>(M);
+    p.nseq = static_cast<int>(nseq);
+    p.H = static_cast<int>(H);
+    p.kv_heads = static_cast<int>(cache->kv_heads);
+    p.d = kKvHeadDim;
+    p.rot = static_cast<int>(rot_dim);
+    p.factor = factor;
+    p.pairs = layout == W4A16_ROTARY_PAIRS;
+    const KvView view = view_of(*cache, st.status);
+    return status_of(launch_rotary(&view, p, st.sm_count, static_cast<cudaStream_t>(stream)));
 }
 
 extern "C" int w4a16_attention_decode_workspace(int64_t H, int64_t kv_heads, int64_t* bytes) {

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 import os
 import re
 import weakref
@@ -24,6 +25,9 @@ HEADER = os.path.join(os.path.dirname(_PKG), "include", "w4a16.h")
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_ALIGNMENT, ERR_CUDA, ERR_TIMEOUT, ERR_INDEX, \
     ERR_CAPACITY = range(8)
 ACT_NONE, ACT_SWIGLU, ACT_GELU = range(3)
+NORM_RMS, NORM_LAYER = range(2)
+ROTARY_HALF, ROTARY_PAIRS = range(2)
+ROTARY_SCALE_NONE, ROTARY_SCALE_LINEAR, ROTARY_SCALE_BY_TURNS, ROTARY_SCALE_BY_INDEX = range(4)
 
 _lib = None
 _caches = weakref.WeakSet()  # whose own workspaces an error may have left in use
@@ -85,6 +89,14 @@ def lib() -> ctypes.CDLL:
         L.w4a16_kv_write.argtypes = [kv, i64, p, p, p, i64, i64, i64, p]
         L.w4a16_attention_decode.argtypes = [kv, i64, p, p, i64, i64, i64, p, p, p]
         L.w4a16_attention_decode_workspace.argtypes = [i64, i64, ctypes.POINTER(i64)]
+        i32, f32, f64 = ctypes.c_int, ctypes.c_float, ctypes.c_double
+        L.w4a16_residual_norm.argtypes = [p, i32, p, p, i64, p, p, p, p, i64, i64, i32, f32, f32, f32, p, p, p]
+        L.w4a16_rotary_table.argtypes = [i64, f64, i32, f64, i64, f64, f64, p]
+        L.w4a16_rotary.argtypes = [p, p, p, i64, i64, i64, i64, i64, p, i64, i32, f32, p]
+        L.w4a16_kv_rotary.argtypes = [kv, p, p, p, i64, i64, i64, p, i64, i32, f32, p]
+        L.w4a16_log_probs.argtypes = [p, i32, i64, i64, i64, p, i64, p, p, p, p, p]
+        L.w4a16_add_adapters.argtypes = [p, p, p, p, i64, p, p, i64, i64, i64, i64, i64, p, p, p, p]
+        L.w4a16_add_adapters_workspace.argtypes = [i64, i64, i64, i64, ctypes.POINTER(i64)]
         L.w4a16_get_device_error.argtypes = [p]
         L.w4a16_selftest_wait_timeout.argtypes = [i64, p]
         L.w4a16_selftest_set_wait_limit.argtypes = [i64]
@@ -99,6 +111,8 @@ def lib() -> ctypes.CDLL:
                   "w4a16_stack_graph_destroy", "w4a16_dequant", "w4a16_quantize",
                   "w4a16_kv_extend", "w4a16_kv_fork", "w4a16_kv_trim", "w4a16_kv_compact",
                   "w4a16_kv_write", "w4a16_attention_decode", "w4a16_attention_decode_workspace",
+                  "w4a16_residual_norm", "w4a16_rotary_table", "w4a16_rotary", "w4a16_kv_rotary",
+                  "w4a16_log_probs", "w4a16_add_adapters", "w4a16_add_adapters_workspace",
                   "w4a16_get_device_error", "w4a16_selftest_wait_timeout",
                   "w4a16_selftest_set_wait_limit", "w4a16_selftest_route"):
             getattr(L, f).restype = ctypes.c_int
@@ -486,6 +500,208 @@ def attention_decode(cache: KVCache, layer: int, qkv: torch.Tensor, slots: torch
         cache._ref, layer, qkv.data_ptr(), slots.data_ptr(), n, H, int(window), out.data_ptr(),
         workspace.data_ptr(), _stream(stream)))
     return out
+
+
+def _fits(t, dtype, *shape) -> bool:
+    """A contiguous tensor of this type and shape on the current device."""
+    return (t.dtype == dtype and t.shape == shape and t.is_contiguous() and t.is_cuda
+            and t.get_device() == torch.cuda.current_device())
+
+
+def _new(stream, shape, dtype, device) -> torch.Tensor:
+    """An output, allocated on the stream that writes it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with _allocating_on(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def residual_norm(residual: torch.Tensor, weight: torch.Tensor | None = None,
+                  block: torch.Tensor | None = None, *, bias: torch.Tensor | None = None,
+                  gate: torch.Tensor | None = None, post_weight: torch.Tensor | None = None,
+                  post_bias: torch.Tensor | None = None, kind: int = NORM_RMS, eps: float = 1e-5,
+                  weight_offset: float = 0.0, residual_scale: float = 1.0,
+                  residual_out: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                  stream=None):
+    """(out, h): h = residual_scale * residual + gate * post(block), out = norm of h
+    (include/w4a16.h).  residual [M, D] bf16 or fp32, block bf16 [M, D], gate bf16 [1 or M, D], the
+    weights and biases bf16 [D]; post(block) is block without post_weight.  residual_out may be
+    residual.  Without block and residual_out h is not stored (None; residual itself where
+    residual_scale is 1)."""
+    M, D = residual.shape
+    bf16 = torch.bfloat16
+    if residual.dtype not in (bf16, torch.float32) or not _fits(residual, residual.dtype, M, D):
+        raise ValueError("expected a contiguous residual [M, D] in bf16 or fp32 on the current device")
+    for t in (weight, bias, post_weight, post_bias):
+        if t is not None and not _fits(t, bf16, D):
+            raise ValueError("expected contiguous bf16 weights and biases [D] on the current device")
+    if block is not None and not _fits(block, bf16, M, D):
+        raise ValueError("expected a contiguous bf16 block [M, D] on the current device")
+    if gate is not None and not (_fits(gate, bf16, 1, D) or _fits(gate, bf16, M, D)):
+        raise ValueError("expected a contiguous bf16 gate [1, D] or [M, D] on the current device")
+    if residual_out is None:
+        if block is not None:
+            residual_out = _new(stream, (M, D), residual.dtype, residual.device)
+    elif not _fits(residual_out, residual.dtype, M, D):
+        raise ValueError("expected residual_out like residual")
+    if out is None:
+        out = _new(stream, (M, D), bf16, residual.device)
+    elif not _fits(out, bf16, M, D):
+        raise ValueError("expected a contiguous bf16 out [M, D] on the current device")
+    _check("w4a16_residual_norm", lib().w4a16_residual_norm(
+        residual.data_ptr(), 16 if residual.dtype == bf16 else 32, _ptr(block), _ptr(gate),
+        0 if gate is None else gate.shape[0], _ptr(post_weight), _ptr(post_bias), _ptr(weight), _ptr(bias),
+        M, D, kind, residual_scale, eps, weight_offset, _ptr(residual_out), out.data_ptr(), _stream(stream)))
+    if residual_out is None and residual_scale == 1.0:
+        residual_out = residual
+    return out, residual_out
+
+
+class RotaryTable:
+    """Frequencies of rotary positions for the first rot_dim values of a head, on the device
+    (include/w4a16.h).  attention_factor multiplies the turned queries and keys (for BY_INDEX
+    usually 0.1 ln factor + 1)."""
+
+    def __init__(self, rot_dim: int, base: float = 10000.0, scaling: int = ROTARY_SCALE_NONE,
+                 factor: float = 1.0, trained_tokens: int = 0, low_turns: float = 1.0,
+                 high_turns: float = 32.0, layout: int = ROTARY_HALF, attention_factor: float = 1.0,
+                 device="cuda"):
+        if layout not in (ROTARY_HALF, ROTARY_PAIRS):
+            raise ValueError("layout is ROTARY_HALF or ROTARY_PAIRS")
+        host = torch.zeros(max(rot_dim, 2) // 2, dtype=torch.int64)
+        _check("w4a16_rotary_table", lib().w4a16_rotary_table(
+            rot_dim, base, scaling, factor, trained_tokens, low_turns, high_turns, host.data_ptr()))
+        self.rot_dim, self.layout, self.attention_factor = rot_dim, layout, float(attention_factor)
+        self.turns = host.to(device)  # (from pageable memory: the copy has been made)
+
+
+def _rotary_qkv(qkv: torch.Tensor, table: RotaryTable, columns: int) -> int:
+    M = qkv.shape[0]
+    if not _fits(qkv, torch.bfloat16, M, columns):
+        raise ValueError("expected a contiguous bf16 qkv [M, (H + 2 kv_heads) * head_dim] on the current device")
+    if table.turns.get_device() != qkv.get_device():
+        raise ValueError("the table is on another device")
+    return M
+
+
+def _rotary_lists(M: int, seq_start, list_) -> int:
+    """The number of sequences."""
+    if seq_start is None:
+        nseq = M
+    else:
+        nseq = seq_start.shape[0] - 1
+        if not _fits(seq_start, torch.int32, nseq + 1):
+            raise ValueError("expected a contiguous int32 seq_start [nseq + 1] on the current device")
+    if list_ is not None and not _fits(list_, torch.int32, nseq):
+        raise ValueError("expected contiguous int32 lists with an entry for each sequence on the current device")
+    return nseq
+
+
+def rotary(qkv: torch.Tensor, table: RotaryTable, H: int, kv_heads: int | None = None,
+           seq_start: torch.Tensor | None = None, first: torch.Tensor | None = None, head_dim: int = 128,
+           stream=None) -> torch.Tensor:
+    """Turns the queries and keys of qkv bf16 [M, (H + 2 kv_heads) head_dim] by their positions, in
+    place (include/w4a16.h): row m of sequence s has position first[s] + m - seq_start[s] (int32 lists;
+    without seq_start each row is a sequence, without first they begin at 0)."""
+    if kv_heads is None:
+        kv_heads = H
+    M = _rotary_qkv(qkv, table, (H + 2 * kv_heads) * head_dim)
+    nseq = _rotary_lists(M, seq_start, first)
+    _check("w4a16_rotary", lib().w4a16_rotary(
+        qkv.data_ptr(), _ptr(seq_start), _ptr(first), nseq, M, H, kv_heads, head_dim, table.turns.data_ptr(),
+        table.rot_dim, table.layout, table.attention_factor, _stream(stream)))
+    return qkv
+
+
+def kv_rotary(cache: KVCache, qkv: torch.Tensor, slots: torch.Tensor, H: int, table: RotaryTable,
+              seq_start: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """The same with the positions that the cache's sequences have grown to: rows [seq_start[i],
+    seq_start[i+1]) are the last tokens of slots[i]'s sequence (before kv_write), or without seq_start row i
+    is the last one (before attention_decode)."""
+    M = _rotary_qkv(qkv, table, (H + 2 * cache.kv_heads) * cache.pages.shape[5])
+    nseq = _rotary_lists(M, seq_start, slots)
+    _check("w4a16_kv_rotary", lib().w4a16_kv_rotary(
+        cache._ref, qkv.data_ptr(), _ptr(seq_start), slots.data_ptr(), nseq, M, H, table.turns.data_ptr(),
+        table.rot_dim, table.layout, table.attention_factor, _stream(stream)))
+    return qkv
+
+
+def log_probs(logits: torch.Tensor, targets: torch.Tensor | None = None, k: int = 0, entropy: bool = True,
+              stream=None):
+    """(logp [M], entropy [M], index [M, k], score [M, k]) of logits [M, V] in bf16 or fp32, rows
+    contiguous (include/w4a16.h): log probabilities of targets (int32 [M], -1: none, 0), the
+    entropy, and the k largest logits' columns and log probabilities.  None where not asked for."""
+    M, V = logits.shape
+    if (not logits.is_cuda or logits.dtype not in (torch.bfloat16, torch.float32)
+            or logits.get_device() != torch.cuda.current_device() or (V > 1 and logits.stride(1) != 1)):
+        raise ValueError("expected logits [M, V] in bf16 or fp32 with contiguous rows on the current device")
+    stride = logits.stride(0) if M > 1 else V
+    if targets is not None and not _fits(targets, torch.int32, M):
+        raise ValueError("expected contiguous int32 targets [M] on the current device")
+    # one allocation: each part on a 16-byte boundary
+    pad = -(-M // 4) * 4
+    part = -(-M * k // 4) * 4
+    buf = _new(stream, (2 * pad + 2 * part,), torch.float32, logits.device)
+    at = buf.data_ptr()
+    _check("w4a16_log_probs", lib().w4a16_log_probs(
+        logits.data_ptr(), 16 if logits.dtype == torch.bfloat16 else 32, M, V, stride, _ptr(targets), k,
+        None if targets is None else at, at + 4 * pad if entropy else None, at + 8 * pad if k else None,
+        at + 8 * pad + 4 * part if k else None, _stream(stream)))
+    if k:
+        begin = 2 * pad
+        index = buf[begin:begin + M * k].view(torch.int32).view(M, k)
+        score = buf[begin + part:begin + part + M * k].view(M, k)
+    else:
+        index = score = None
+    return (None if targets is None else buf[:M], buf[pad:pad + M] if entropy else None, index, score)
+
+
+def add_adapters(base: torch.Tensor, x: torch.Tensor, A: torch.Tensor, B: torch.Tensor, scale: torch.Tensor,
+                 adapters: torch.Tensor, seq_start: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                 workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """out[m] = base[m] + scale[a] (x[m] A[a]^T) B[a]^T with a = adapters[s] of row m's sequence s
+    (include/w4a16.h): x bf16 [M, K] and base bf16 [M, N], a projection's input and output; A bf16
+    [pool, R, K], B bf16 [pool, N, R], scale fp32 [pool]; adapters int32 [nseq], -1 for none, and
+    seq_start int32 [nseq + 1] (without it each row is a sequence; rows outside every sequence have no
+    adapter).  out may be base.  Without `workspace` (adapters_workspace_bytes) one is allocated."""
+    M, K = x.shape
+    N = base.shape[1]
+    pool, R = A.shape[0], A.shape[1]
+    bf16 = torch.bfloat16
+    if not (_fits(x, bf16, M, K) and _fits(base, bf16, M, N) and _fits(A, bf16, pool, R, K)
+            and _fits(B, bf16, pool, N, R) and _fits(scale, torch.float32, pool)):
+        raise ValueError("expected contiguous bf16 x [M, K], base [M, N], A [pool, R, K], B [pool, N, R] and fp32 "
+                         "scale [pool] on the current device")
+    nseq = _rotary_lists(M, seq_start, adapters)
+    if workspace is None:
+        workspace = _new(stream, (adapters_workspace_bytes(M, nseq, K, R),), torch.uint8, x.device)
+    elif not (workspace.is_cuda and workspace.is_contiguous()
+              and workspace.numel() * workspace.element_size() >= adapters_workspace_bytes(M, nseq, K, R)):
+        raise ValueError("expected a workspace of adapters_workspace_bytes")
+    if out is None:
+        out = _new(stream, (M, N), bf16, x.device)
+    elif not _fits(out, bf16, M, N):
+        raise ValueError("expected a contiguous bf16 out [M, N] on the current device")
+    _check("w4a16_add_adapters", lib().w4a16_add_adapters(
+        x.data_ptr(), A.data_ptr(), B.data_ptr(), scale.data_ptr(), pool, _ptr(seq_start), adapters.data_ptr(),
+        nseq, M, N, K, R, base.data_ptr(), out.data_ptr(), workspace.data_ptr(), _stream(stream)))
+    return out
+
+
+def adapters_workspace_bytes(M: int, nseq: int, K: int, R: int) -> int:
+    """Bytes of a workspace for add_adapters on the current device."""
+    return _adapters_workspace_bytes(torch.cuda.current_device(), M, nseq, K, R)
+
+
+@functools.lru_cache(maxsize=4096)
+def _adapters_workspace_bytes(device: int, M: int, nseq: int, K: int, R: int) -> int:
+    size = ctypes.c_int64()
+    _check("w4a16_add_adapters_workspace", lib().w4a16_add_adapters_workspace(M, nseq, K, R, ctypes.byref(size)))
+    return size.value
 
 
 def selftest_wait_timeout(limit_ns: int, stream=None) -> None:
