@@ -438,8 +438,7 @@ int w4a16_attention_decode_workspace(int64_t H, int64_t kv_heads, int64_t* bytes
  *   out_bf16          [M, D]; NULL: only h
  * Everything is computed in fp32, with one rounding of h and one of out, which is of h before its
  * own.  Squares that overflow are scaled; infinities and NaN go where the formula takes
- * them, in their own row.  1e-12 <= eps <= 1; D <= 49152, and <= 24560 where it is no multiple of 8
- * (else W4A16_ERR_UNSUPPORTED).
+ * them, in their own row.  1e-12 <= eps <= 1; D <= 49152 (else W4A16_ERR_UNSUPPORTED).
  */
 typedef enum {
     W4A16_NORM_RMS = 0,
@@ -546,7 +545,8 @@ int w4a16_add_adapters(const void* x_bf16, const void* a_bf16, const void* b_bf1
                        int64_t pool, const void* seq_start_i32, const void* adapters_i32, int64_t nseq,
                        int64_t M, int64_t N, int64_t K, int64_t R, const void* base_bf16, void* out_bf16,
                        void* workspace, void* stream);
-int w4a16_add_adapters_workspace(int64_t M, int64_t nseq, int64_t K, int64_t R, int64_t* bytes);
+/* Bytes of its workspace; 0 for sizes that are not supported. */
+int64_t w4a16_add_adapters_workspace(int64_t M, int64_t R);
 
 /*
  * Synchronises `stream`, then reads and clears the device status word.

@@ -24,10 +24,11 @@ struct NormParams {
     int M, D;
     float residual_scale, eps, weight_offset;
     bool layer;                   // layer norms, else RMS norms
+    int* status;
+    uint64_t wait_ns;
 };
 constexpr int kNormMaxWidth = 49152;
-constexpr int kNormMaxOdd = 24560;  // widest row that is no multiple of 8
-cudaError_t launch_residual_norm(const NormParams& p, bool fp32, cudaStream_t stream);
+cudaError_t launch_residual_norm(const NormParams& p, bool fp32, int sm_count, cudaStream_t stream);
 
 // Rotary positions (rotary.cu).
 struct RotaryParams {
@@ -69,12 +70,12 @@ struct AdapterParams {
     const int32_t* ids;        // [nseq]
     const uint16_t* base;      // bf16 [M, N]
     uint16_t* out;             // bf16 [M, N]; may be base
-    float* parts;              // workspace: [splits, M, R]
+    uint16_t* t;               // workspace: scale (x A^T), bf16 [M, R]
     int* status;
     int M, N, K, R, pool, nseq;
 };
 constexpr int kAdapterMaxRank = 64;
-int64_t adapters_workspace_bytes(int64_t M, int64_t nseq, int64_t K, int64_t R, int sm_count);
+int64_t adapters_workspace_bytes(int64_t M, int64_t R);
 cudaError_t launch_adapters(const AdapterParams& p, int sm_count, cudaStream_t stream);
 
 }  // namespace w4a16

@@ -65,7 +65,7 @@ extern "C" int w4a16_residual_norm(const void* residual, int residual_bits, cons
     if (post_bias_bf16 != nullptr && post_weight_bf16 == nullptr) return W4A16_ERR_INVALID_ARG;
     if (out_bf16 == nullptr && (weight_bf16 != nullptr || bias_bf16 != nullptr)) return W4A16_ERR_INVALID_ARG;
     if (gate_bf16 != nullptr && gate_rows != 1 && gate_rows != M) return W4A16_ERR_INVALID_ARG;
-    if (M > kMaxDim || D > kNormMaxWidth || (D % 8 != 0 && D > kNormMaxOdd)) return W4A16_ERR_UNSUPPORTED;
+    if (M > kMaxDim || D > kNormMaxWidth) return W4A16_ERR_UNSUPPORTED;
     const int64_t stream_bytes = M * D * (residual_bits / 8);
     const Span in[6] = {{block_bf16, M * D * 2},      {gate_bf16, gate_bf16 != nullptr ? gate_rows * D * 2 : 0},
                         {post_weight_bf16, D * 2},    {post_bias_bf16, D * 2},
@@ -76,6 +76,9 @@ extern "C" int w4a16_residual_norm(const void* residual, int residual_bits, cons
     if (!aligned16(residual)) return W4A16_ERR_ALIGNMENT;
     const Span from{residual, stream_bytes};
     if ((residual_out != residual && overlaps(from, outs[0])) || overlaps(from, outs[1])) return W4A16_ERR_INVALID_ARG;
+    LibraryState st;
+    const int state = library_state(&st);
+    if (state != W4A16_OK) return state;
     NormParams p;
     p.residual = residual;
     p.block = static_cast<const uint16_t*>(block_bf16);
@@ -93,7 +96,9 @@ extern "C" int w4a16_residual_norm(const void* residual, int residual_bits, cons
     p.eps = eps;
     p.weight_offset = weight_offset;
     p.layer = norm == W4A16_NORM_LAYER;
-    return status_of(launch_residual_norm(p, residual_bits == 32, static_cast<cudaStream_t>(stream)));
+    p.status = st.status;
+    p.wait_ns = wait_limit_ns();
+    return status_of(launch_residual_norm(p, residual_bits == 32, st.sm_count, static_cast<cudaStream_t>(stream)));
 }
 
 extern "C" int w4a16_rotary_table(int64_t rot_dim, double base, int scaling, double factor, int64_t trained_tokens,
@@ -208,15 +213,8 @@ int check_adapters(int64_t M, int64_t nseq, int64_t K, int64_t R) {
 
 }  // namespace
 
-extern "C" int w4a16_add_adapters_workspace(int64_t M, int64_t nseq, int64_t K, int64_t R, int64_t* bytes) {
-    if (bytes == nullptr) return W4A16_ERR_INVALID_ARG;
-    int rc = check_adapters(M, nseq, K, R);
-    if (rc != W4A16_OK) return rc;
-    LibraryState st;
-    rc = library_state(&st);
-    if (rc != W4A16_OK) return rc;
-    *bytes = adapters_workspace_bytes(M, nseq, K, R, st.sm_count);
-    return W4A16_OK;
+extern "C" int64_t w4a16_add_adapters_workspace(int64_t M, int64_t R) {
+    return check_adapters(M, 1, 64, R) == W4A16_OK ? adapters_workspace_bytes(M, R) : 0;
 }
 
 extern "C" int w4a16_add_adapters(const void* x_bf16, const void* a_bf16, const void* b_bf16, const void* scale_f32,
@@ -231,21 +229,17 @@ extern "C" int w4a16_add_adapters(const void* x_bf16, const void* a_bf16, const 
     if (rc != W4A16_OK) return rc;
     if (seq_start_i32 == nullptr && nseq != M) return W4A16_ERR_INVALID_ARG;
     if (N > kMaxDim / 64 || pool > kMaxDim / 64) return W4A16_ERR_UNSUPPORTED;
-    Span in[6] = {{x_bf16, M * K * 2},  {a_bf16, pool * R * K * 2},         {b_bf16, pool * N * R * 2},
+    const Span in[6] = {{x_bf16, M * K * 2},  {a_bf16, pool * R * K * 2},         {b_bf16, pool * N * R * 2},
                   {scale_f32, pool * 4}, {seq_start_i32, (nseq + 1) * 4}, {adapters_i32, nseq * 4}};
     const Span base{base_bf16, M * N * 2};
-    Span out[2] = {{out_bf16, M * N * 2}, {workspace, M * R * 4}};  // (at least)
+    const Span out[2] = {{out_bf16, M * N * 2}, {workspace, adapters_workspace_bytes(M, R)}};
     rc = check_spans(in, out);
     if (rc != W4A16_OK) return rc;
     if (!aligned16(base_bf16)) return W4A16_ERR_ALIGNMENT;
-    if (base_bf16 != out_bf16 && overlaps(base, out[0])) return W4A16_ERR_INVALID_ARG;
+    if ((base_bf16 != out_bf16 && overlaps(base, out[0])) || overlaps(base, out[1])) return W4A16_ERR_INVALID_ARG;
     LibraryState st;
     rc = library_state(&st);
     if (rc != W4A16_OK) return rc;
-    out[1].bytes = adapters_workspace_bytes(M, nseq, K, R, st.sm_count);
-    rc = check_spans(in, out);
-    if (rc != W4A16_OK) return rc;
-    if (overlaps(base, out[1])) return W4A16_ERR_INVALID_ARG;
     AdapterParams p;
     p.x = static_cast<const uint16_t*>(x_bf16);
     p.a = static_cast<const uint16_t*>(a_bf16);
@@ -255,7 +249,7 @@ extern "C" int w4a16_add_adapters(const void* x_bf16, const void* a_bf16, const 
     p.ids = static_cast<const int32_t*>(adapters_i32);
     p.base = static_cast<const uint16_t*>(base_bf16);
     p.out = static_cast<uint16_t*>(out_bf16);
-    p.parts = static_cast<float*>(workspace);
+    p.t = static_cast<uint16_t*>(workspace);
     p.status = st.status;
     p.M = static_cast<int>(M);
     p.N = static_cast<int>(N);

@@ -1,15 +1,19 @@
 // Log probabilities of given tokens, entropy and the best alternatives from a head's logits, which are
-// read once:
-//   lse = m + ln s,  s = sum e^(x - m);   H = ln s - (sum e^(x - m) (x - m)) / s,  m the largest;
-// both terms of H are positive, so nothing cancels.  Each thread keeps m, s and the other sum of its
-// part of the row (in base 2), raised to a new m once for 32 logits; the parts are joined in a
-// fixed order.  Few rows are split over a cluster of CTAs and joined in its first one.
+// read once.  In base 2, with y = x log2(e) - m for a whole row's m near its largest:
+//   log2 p = y - log2 s,  s = sum 2^y;   H = (log2 s - (sum 2^y y) / s) ln 2;
+// both terms of H are positive, so nothing cancels, and y is one multiply-add whose rounding of
+// m is the same for every logit.  Each thread keeps m, s and the other sum of its part of the row, raised
+// to a new m once for 32 (fp32: 16) logits; the parts are joined in a fixed order.  Few rows are split over
+// a cluster of CTAs and joined in its first one.  Logits below -2^100 count as that (q y = 0, not
+// NaN, for -infinity); a row of nothing above -1e29, or with one past 1e38, is summed again by the
+// formula in natural logarithms.
 //
 // The k largest: the same pass notes the largest logit of each group of neighbours (up to 1024
 // groups).  With t the k-th largest of those, all of the k largest logits are among the groups above
 // t and the first of those at t, k groups in all: any other group's logits come after k of theirs.
 // Only these groups are read again (k * 512 bytes of a row), their logits from t on are collected
-// and ranked by counting.  Where too many pass, t is raised to the k-th largest logit by
+// and ranked by counting.  t is searched in the upper half of the keys' bits; what has the same upper half is
+// collected as well, unless it is a lot.  Where too many pass, t is raised to the k-th largest logit by
 // bisection; where too many are equal to it, they are taken in order.
 #include <cuda_runtime.h>
 #include <cstdint>
@@ -57,14 +61,61 @@ __device__ __forceinline__ uint4 load_once(const void* p) {
     return v;
 }
 
-// sum e^(x - m) and sum e^(x - m) (x - m), in base 2.
+constexpr float kLeast = -1.2676506002282294e30f;  // -2^100
+constexpr uint32_t kLeast2 = 0xF180F180u;          // two of it in bf16
+
+// Two fp32 in one register pair.
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+    uint64_t p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(a), "f"(b));
+    return p;
+}
+__device__ __forceinline__ float2 both(uint64_t p) {
+    float2 v;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+// The larger; a number beats a NaN / a NaN stays one.
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t max_nan_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
+
+// The largest number of a warp's (a NaN where none is one).
+__device__ __forceinline__ float warp_max(float x) {
+    float d;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(d) : "f"(x));
+    return d;
+}
+
+// sum 2^y and sum 2^y y for y = x log2(e) - m.
 struct Sums {
     float m, s, t;
 
     __device__ __forceinline__ void raise(float to) {
-        const float y = m == -INFINITY ? 0.0f : (m - to) * kLog2e;
-        const float f = m == -INFINITY ? 0.0f : exp2_approx(y);
-        t = f * fmaf(s, fmaxf(y, -1e4f), t);
+        const float y = m - to, f = exp2_approx(y);
+        t = f * fmaf(s, y, t);
         s *= f;
         m = to;
     }
@@ -99,8 +150,8 @@ struct RowOf {
         for (int e = 0; e < N; ++e)
             x[e] = static_cast<unsigned>(c + e) < static_cast<unsigned>(V) ? at(c + e) : absent;
     }
-    static __device__ __forceinline__ void unpack(uint4 v, float (&x)[N]) {
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    __device__ __forceinline__ const void* unit(int u) const { return row + (u * N - shift); }
+    static __device__ __forceinline__ void unpack(const uint32_t (&w)[4], float (&x)[N]) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if constexpr (BF16) {
@@ -111,6 +162,21 @@ struct RowOf {
             }
         }
     }
+    // The largest of a unit as it is in memory (a NaN where all are), and its columns from -2^100 on.
+    static __device__ __forceinline__ float largest(const uint32_t (&w)[4]) {
+        if constexpr (BF16) {
+            const uint32_t v = max_bf16x2(max_bf16x2(w[0], w[1]), max_bf16x2(w[2], w[3]));
+            return fmaxf(__uint_as_float(v << 16), __uint_as_float(v & 0xFFFF0000u));
+        } else {
+            return fmaxf(fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1])),
+                         fmaxf(__uint_as_float(w[2]), __uint_as_float(w[3])));
+        }
+    }
+    static __device__ __forceinline__ void from_least(uint32_t (&w)[4]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            w[i] = BF16 ? max_nan_bf16x2(w[i], kLeast2) : __float_as_uint(max_nan(__uint_as_float(w[i]), kLeast));
+    }
 };
 
 struct Shared {
@@ -119,43 +185,56 @@ struct Shared {
     unsigned long long equal[kCandidates];
     int selected[kGroups];                  // groups, ascending
     Sums warp_sums[kWarps], cta_sums[kMaxCluster];
+    int counts[kWarps], digits[256];
     uint32_t threshold;
+    int low;  // bits that the threshold leaves out
     int num_selected, num_above, num_equal, count;
 };
 
-template <bool BF16>
-__device__ __forceinline__ uint32_t cut(uint32_t key) {
-    // (the low half of a bf16's key follows from its sign)
-    return BF16 ? key >> 16 : key;
-}
 
 // f(column, key) for the logits of the selected groups.
+// (those of key `least` and more; a unit's others are not looked at one by one)
 template <bool BF16, typename F>
-__device__ __forceinline__ void each_selected(const Shared& sh, const RowOf<BF16>& r, int shift, const F& f) {
+__device__ __forceinline__ void each_selected(const Shared& sh, const RowOf<BF16>& r, int shift, uint32_t least, const F& f) {
+    constexpr int kTogether = 4, N = RowOf<BF16>::N;
     const int total = sh.num_selected << shift;
-    for (int i = threadIdx.x; i < total; i += kThreads) {
-        const int u = (sh.selected[i >> shift] << shift) + (i & ((1 << shift) - 1));
-        if (u >= r.units) continue;
-        float x[RowOf<BF16>::N];
-        if (r.whole(u))
-            r.unpack(__ldg(reinterpret_cast<const uint4*>(r.row + (u * RowOf<BF16>::N - r.shift))), x);
-        else
-            r.load_part(u, 0.0f, x);
+    for (int i0 = threadIdx.x; i0 < total; i0 += kThreads * kTogether) {
+        uint4 v[kTogether];
+        int unit[kTogether];
 #pragma unroll
-        for (int e = 0; e < RowOf<BF16>::N; ++e) {
-            const int c = u * RowOf<BF16>::N - r.shift + e;
-            if (static_cast<unsigned>(c) < static_cast<unsigned>(r.V)) f(c, key_of(x[e]));
+        for (int j = 0; j < kTogether; ++j) {
+            const int i = i0 + j * kThreads;
+            unit[j] = i < total ? (sh.selected[i >> shift] << shift) + (i & ((1 << shift) - 1)) : r.units;
+            if (r.whole(unit[j])) v[j] = __ldg(static_cast<const uint4*>(r.unit(unit[j])));
+        }
+#pragma unroll
+        for (int j = 0; j < kTogether; ++j) {
+            if (unit[j] >= r.units) continue;
+            float x[N];
+            if (r.whole(unit[j])) {
+                const uint32_t w[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
+                if (key_of(r.largest(w)) < least) continue;
+                r.unpack(w, x);
+            } else {
+                r.load_part(unit[j], 0.0f, x);
+            }
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const int c = unit[j] * N - r.shift + e;
+                if (static_cast<unsigned>(c) < static_cast<unsigned>(r.V)) f(c, key_of(x[e]));
+            }
         }
     }
 }
 
-// The selected groups' logits above and at the threshold.  All threads.
+// The selected groups' logits whose keys without their low `low` bits are above t, and equal to it.  All
+// threads.
 template <bool BF16>
-__device__ void collect(Shared& sh, const RowOf<BF16>& r, int shift, uint32_t t) {
+__device__ __noinline__ void collect(Shared& sh, const RowOf<BF16>& r, int shift, uint32_t t, int low) {
     if (threadIdx.x == 0) sh.num_above = sh.num_equal = 0;
     __syncthreads();
-    each_selected<BF16>(sh, r, shift, [&](int c, uint32_t key) {
-        const uint32_t q = cut<BF16>(key);
+    each_selected<BF16>(sh, r, shift, t << low, [&](int c, uint32_t key) {
+        const uint32_t q = key >> low;
         if (q < t) return;
         int* const n = q > t ? &sh.num_above : &sh.num_equal;
         unsigned long long* const list = q > t ? sh.above : sh.equal;
@@ -165,9 +244,9 @@ __device__ void collect(Shared& sh, const RowOf<BF16>& r, int shift, uint32_t t)
     __syncthreads();
 }
 
-// The `need` equal ones of the lowest columns, by one warp.
+// The `need` ones of key t of the lowest columns, by one warp.
 template <bool BF16>
-__device__ void collect_in_order(Shared& sh, const RowOf<BF16>& r, int shift, uint32_t t, int need) {
+__device__ __noinline__ void collect_in_order(Shared& sh, const RowOf<BF16>& r, int shift, uint32_t t, int low, int need) {
     constexpr int N = RowOf<BF16>::N;
     const int lane = threadIdx.x;
     const int total = sh.num_selected << shift;
@@ -181,7 +260,7 @@ __device__ void collect_in_order(Shared& sh, const RowOf<BF16>& r, int shift, ui
             r.load_part(u, 0.0f, x);
 #pragma unroll
             for (int e = 0; e < N; ++e)
-                if (static_cast<unsigned>(u * N - r.shift + e) < static_cast<unsigned>(r.V) && cut<BF16>(key_of(x[e])) == t)
+                if (static_cast<unsigned>(u * N - r.shift + e) < static_cast<unsigned>(r.V) && key_of(x[e]) >> low == t)
                     hit |= 1u << e;
         }
         int before = __popc(hit);
@@ -206,86 +285,191 @@ __device__ void collect_in_order(Shared& sh, const RowOf<BF16>& r, int shift, ui
     if (lane == 0) sh.num_equal = found < need ? found : need;
 }
 
-// The k largest of the row, from the groups' keys.  All threads of one CTA.
+// The groups to read again: t (without the keys' low bits), and the list.  All threads; a warp has 128
+// groups.
 template <bool BF16>
-__device__ void top(Shared& sh, const RowOf<BF16>& r, int shift, int groups, int k, float m, float ln_s,
-                    bool none, int32_t* index, float* score) {
-    const int lane = threadIdx.x & 31;
-    if (threadIdx.x < 32) {
-        uint32_t key[kGroups / 32];
+__device__ __forceinline__ void select_groups(Shared& sh, int groups, int k) {
+    constexpr int kMine = kGroups / kThreads;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, first = warp * (32 * kMine) + lane;
+    uint32_t key[kMine];
 #pragma unroll
-        for (int j = 0; j < kGroups / 32; ++j) key[j] = j * 32 < groups ? cut<BF16>(sh.group_key[j * 32 + lane]) : 0u;
-        // the largest t that k groups reach
-        uint32_t t = 0;
-        for (uint32_t bit = BF16 ? 1u << 15 : 1u << 31; bit != 0; bit >>= 1) {
-            int n = 0;
+    for (int j = 0; j < kMine; ++j) key[j] = sh.group_key[first + 32 * j];
+    // the largest t that k groups reach, eight bits at a time: the digits of the groups that have t's bits so
+    // far are counted, and each warp adds the counts up from the top
+    int low = 32, above = 0, equal = 0;  // above: groups past t's bits so far
+    uint32_t t = 0;
+    while (true) {
+        low -= 8;
+        for (int i = threadIdx.x; i < 256; i += kThreads) sh.digits[i] = 0;
+        __syncthreads();
 #pragma unroll
-            for (int j = 0; j < kGroups / 32; ++j)
-                if (j * 32 < groups) n += key[j] >= (t | bit);
-            if (__reduce_add_sync(0xffffffffu, n) >= k) t |= bit;
+        for (int j = 0; j < kMine; ++j)
+            if (first + 32 * j < groups && (low == 24 || key[j] >> (low + 8) == t))
+                atomicAdd(&sh.digits[key[j] >> low & 255u], 1);
+        __syncthreads();
+        // lane l has the digits 255 - 8 l and below
+        int n[8], sum = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            n[i] = sh.digits[255 - 8 * lane - i];
+            sum += n[i];
         }
-        int above = 0;
+        int upto = sum;
 #pragma unroll
-        for (int j = 0; j < kGroups / 32; ++j)
-            if (j * 32 < groups) above += key[j] > t;
-        int equal = k - __reduce_add_sync(0xffffffffu, above);  // to take
-        int n = 0;
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += y;
+        }
+        const uint32_t reach = __ballot_sync(0xffffffffu, above + upto >= k);
+        // (fewer than k groups: all of them, from digit 0)
+        const int at = reach != 0 ? __ffs(reach) - 1 : 31;
+        int digit = 255 - 8 * lane, before = above + upto - sum, here = n[0];
 #pragma unroll
-        for (int j = 0; j < kGroups / 32; ++j) {
-            if (j * 32 >= groups) break;
-            const bool there = j * 32 + lane < groups;
-            const uint32_t same = __ballot_sync(0xffffffffu, there && key[j] == t);
-            const bool take = there && (key[j] > t || (key[j] == t && __popc(same & ((1u << lane) - 1u)) < equal));
-            const uint32_t taken = __ballot_sync(0xffffffffu, take);
-            if (take) sh.selected[n + __popc(taken & ((1u << lane) - 1u))] = j * 32 + lane;
-            n += __popc(taken);
-            equal -= __popc(same);
-        }
-        if (lane == 0) {
-            sh.num_selected = n;
-            sh.threshold = t;
-        }
+        for (int i = 0; i < 7; ++i)
+            if (digit == 255 - 8 * lane - i && before + n[i] < k) {
+                before += n[i];
+                --digit;
+                here = n[i + 1];
+            }
+        digit = __shfl_sync(0xffffffffu, digit, at);
+        above = __shfl_sync(0xffffffffu, before, at);
+        equal = __shfl_sync(0xffffffffu, here, at);
+        t = t << 8 | static_cast<uint32_t>(digit);
+        __syncthreads();
+        // (the low half of a bf16's key follows from its sign)
+        if (low == 0 || (low == 16 && (BF16 || above + equal <= k + 32))) break;
     }
+    // groups at t: the first ones, where t is a whole key
+    const int take = BF16 || low == 0 ? k - above : equal;
+    int both_counts = 0;  // those above t, and 2^16 times those at it
+#pragma unroll
+    for (int j = 0; j < kMine; ++j) {
+        both_counts += key[j] >> low > t;
+        both_counts += (first + 32 * j < groups && key[j] >> low == t) << 16;
+    }
+    both_counts = __reduce_add_sync(0xffffffffu, both_counts);
+    if (lane == 0) sh.counts[warp] = both_counts;
+    __syncthreads();
+    int same_before = 0, place = 0;  // of the warps before
+    for (int w = 0; w < warp; ++w) {
+        const int a = sh.counts[w] & 0xFFFF, e = sh.counts[w] >> 16;
+        place += a + min(max(take - same_before, 0), e);
+        same_before += e;
+    }
+#pragma unroll
+    for (int j = 0; j < kMine; ++j) {
+        const bool there = first + 32 * j < groups;
+        const uint32_t same = __ballot_sync(0xffffffffu, there && key[j] >> low == t), under = (1u << lane) - 1u;
+        const bool mine =
+            there && (key[j] >> low > t || (key[j] >> low == t && same_before + __popc(same & under) < take));
+        const uint32_t taken = __ballot_sync(0xffffffffu, mine);
+        if (mine) sh.selected[place + __popc(taken & under)] = first + 32 * j;
+        place += __popc(taken);
+        same_before += __popc(same);
+    }
+    if (threadIdx.x == kThreads - 1) {
+        sh.num_selected = place;
+        sh.threshold = t;
+        sh.low = low;
+    }
+}
+
+// The k largest of the row, from the groups' keys.  All threads of one CTA.  value(x): x's log probability.
+template <bool BF16, typename F>
+__device__ __forceinline__ void top(Shared& sh, const RowOf<BF16>& r, int shift, int groups, int k, const F& value,
+                                    int32_t* index, float* score) {
+    const int lane = threadIdx.x & 31;
+    select_groups<BF16>(sh, groups, k);
     __syncthreads();
     uint32_t t = sh.threshold;
-    collect<BF16>(sh, r, shift, t);
-    if (sh.num_above > kCandidates) {
+    int low = sh.low;
+    collect<BF16>(sh, r, shift, t, low);
+    if (sh.num_above > kCandidates || (sh.num_equal > kCandidates && low != 0 && !BF16)) {
+        low = BF16 ? 16 : 0;
+        t = 0;
         for (uint32_t bit = BF16 ? 1u << 15 : 1u << 31; bit != 0; bit >>= 1) {
-            // (t's own bits are those of a value that k logits reach)
             if (threadIdx.x == 0) sh.count = 0;
-            if (bit == (BF16 ? 1u << 15 : 1u << 31)) t = 0;
             __syncthreads();
             int n = 0;
-            each_selected<BF16>(sh, r, shift, [&](int, uint32_t key) { n += cut<BF16>(key) >= (t | bit); });
+            each_selected<BF16>(sh, r, shift, (t | bit) << low, [&](int, uint32_t key) { n += key >> low >= (t | bit); });
             n = __reduce_add_sync(0xffffffffu, n);
             if (lane == 0 && n > 0) atomicAdd(&sh.count, n);
             __syncthreads();
             if (sh.count >= k) t |= bit;
             __syncthreads();
         }
-        collect<BF16>(sh, r, shift, t);
+        collect<BF16>(sh, r, shift, t, low);
     }
     if (sh.num_equal > kCandidates) {
-        if (threadIdx.x < 32) collect_in_order<BF16>(sh, r, shift, t, k);
+        if (threadIdx.x < 32) collect_in_order<BF16>(sh, r, shift, t, low, k);
         __syncthreads();
     }
+    // four threads count for a candidate
     const int na = sh.num_above, n = na + sh.num_equal;
-    for (int i = threadIdx.x; i < n; i += kThreads) {
-        const unsigned long long mine = i < na ? sh.above[i] : sh.equal[i - na];
+    for (int i0 = 0; i0 < n; i0 += kThreads / 4) {
+        const int i = i0 + static_cast<int>(threadIdx.x) / 4;
+        const unsigned long long mine = i < na ? sh.above[i] : i < n ? sh.equal[i - na] : 0;
         int rank = 0;
-        for (int j = 0; j < na; ++j) rank += sh.above[j] > mine;
-        if (i >= na)
-            for (int j = 0; j < n - na; ++j) rank += sh.equal[j] > mine;
-        if (rank < k) {
+        if (i < n) {
+            for (int j = threadIdx.x & 3; j < na; j += 4) rank += sh.above[j] > mine;
+            for (int j = threadIdx.x & 3; j < n - na; j += 4) rank += sh.equal[j] > mine;
+        }
+        rank += __shfl_xor_sync(0xffffffffu, rank, 1);
+        rank += __shfl_xor_sync(0xffffffffu, rank, 2);
+        if (i < n && rank < k && (threadIdx.x & 3) == 0) {
             index[rank] = static_cast<int32_t>(~static_cast<uint32_t>(mine));
-            // (without a logit above -infinity no token has a probability)
-            score[rank] = none ? -INFINITY : (value_of(static_cast<uint32_t>(mine >> 32)) - m) - ln_s;
+            score[rank] = value(value_of(static_cast<uint32_t>(mine >> 32)));
         }
     }
 }
 
+// A row's sums about its largest number m, by e^(x - m), for rows that the base-2 form does not hold: all
+// logits below -1e29, or one past 1e38.  m -infinity: no number above that.  All threads of one CTA.
+template <bool BF16>
+__device__ __noinline__ Sums sums_again(Shared& sh, const RowOf<BF16>& r) {
+    constexpr int N = RowOf<BF16>::N;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    Sums all{-INFINITY, 0.0f, 0.0f};
+    for (int pass = 0; pass < 2; ++pass) {
+        Sums mine{-INFINITY, 0.0f, 0.0f};
+        const float m = all.m == -INFINITY ? 0.0f : all.m;
+        for (int u = threadIdx.x; u < r.units; u += kThreads) {
+            float x[N];
+            r.load_part(u, -INFINITY, x);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                if (pass == 0) {
+                    mine.m = fmaxf(mine.m, x[e]);
+                } else {
+                    const float y = (x[e] - m) * kLog2e, q = exp2_approx(y);
+                    mine.s += q;
+                    mine.t = fmaf(q, fmaxf(y, -1e4f), mine.t);
+                }
+            }
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            mine.m = fmaxf(mine.m, __shfl_xor_sync(0xffffffffu, mine.m, o));
+            mine.s += __shfl_xor_sync(0xffffffffu, mine.s, o);
+            mine.t += __shfl_xor_sync(0xffffffffu, mine.t, o);
+        }
+        __syncthreads();
+        if (lane == 0) sh.warp_sums[warp] = mine;
+        __syncthreads();
+        if (pass == 0) {
+            for (int w = 0; w < kWarps; ++w) all.m = fmaxf(all.m, sh.warp_sums[w].m);
+        } else {
+            for (int w = 0; w < kWarps; ++w) {
+                all.s += sh.warp_sums[w].s;
+                all.t += sh.warp_sums[w].t;
+            }
+        }
+    }
+    return all;
+}
+
 template <bool BF16, bool TOP>
-__global__ void __launch_bounds__(kThreads) log_probs_kernel(const LogProbsParams p, const int shift, const int ctas) {
+__global__ void __launch_bounds__(kThreads, TOP ? 4 : 6) log_probs_kernel(const LogProbsParams p, const int shift, const int ctas) {
     constexpr int N = RowOf<BF16>::N;
     __shared__ Shared sh;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -303,62 +487,94 @@ __global__ void __launch_bounds__(kThreads) log_probs_kernel(const LogProbsParam
     grid_wait();
     __syncthreads();
     if (ctas > 1) cluster_sync();  // (the first CTA's keys are ready for the others')
-    Sums mine{-INFINITY, 0.0f, 0.0f};
+    Sums mine{kLeast * kLog2e, 0.0f, 0.0f};
     // a warp's 128 units at a time, the warps of all CTAs side by side
+    const int ends = r.shift == 0 && p.V % N == 0 ? 0 : 1;  // units that may be in part the row's
     for (int u0 = (rank * kWarps + warp) * 32 * kAhead; u0 < r.units; u0 += ctas * kThreads * kAhead) {
-        float x[kAhead][N], most[kAhead];
-        uint4 v[kAhead];
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const int u = u0 + 32 * i + lane;
-            if (r.whole(u)) v[i] = load_once(r.row + (u * N - r.shift));
-        }
-        float high = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const int u = u0 + 32 * i + lane;
-            if (r.whole(u)) {
-                r.unpack(v[i], x[i]);
-                most[i] = x[i][0];
-#pragma unroll
-                for (int e = 1; e < N; ++e) most[i] = fmaxf(most[i], x[i][e]);
-            } else {
-                r.load_part(u, -INFINITY, x[i]);
-                most[i] = __uint_as_float(0x7FFFFFFFu);  // no number
-#pragma unroll
-                for (int e = 0; e < N; ++e)
-                    if (static_cast<unsigned>(u * N - r.shift + e) < static_cast<unsigned>(r.V))
-                        most[i] = fmaxf(most[i], x[i][e]);
-            }
-            high = fmaxf(high, most[i]);
-        }
-        if (high > mine.m) mine.raise(high);
-        const float m = mine.m == -INFINITY ? 0.0f : mine.m;
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i)
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const float y = (x[i][e] - m) * kLog2e, q = exp2_approx(y);
-                mine.s += q;
-                mine.t = fmaf(q, fmaxf(y, -1e4f), mine.t);  // (-infinity: 0 times a number)
-            }
-        if constexpr (TOP) {
+        uint32_t w[kAhead][4];
+        float most[kAhead];
+        if (u0 >= ends && u0 + 32 * kAhead <= r.units - ends) {
+            const uint4* const from = static_cast<const uint4*>(r.unit(u0 + lane));
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
-                uint32_t key = key_of(most[i]);
-                if (shift >= 5) {
-                    key = __reduce_max_sync(0xffffffffu, key);
-                } else {
-                    for (int o = 1; o < 1 << shift; o <<= 1) key = max(key, __shfl_xor_sync(0xffffffffu, key, o));
-                }
+                const uint4 v = load_once(from + 32 * i);
+                w[i][0] = v.x, w[i][1] = v.y, w[i][2] = v.z, w[i][3] = v.w;
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) most[i] = r.largest(w[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
                 const int u = u0 + 32 * i + lane;
-                if ((u & ((1 << min(shift, 5)) - 1)) == 0 && u < r.units && key != 0) {
-                    if (rank == 0) {
-                        atomicMax(&sh.group_key[u >> shift], key);
-                    } else {
-                        const uint32_t to = mapa_shared(smem_u32(&sh.group_key[u >> shift]), 0);
-                        asm volatile("red.relaxed.cluster.shared::cluster.max.u32 [%0], %1;" ::"r"(to), "r"(key) : "memory");
-                    }
+                if (r.whole(u)) {
+                    const uint4 v = load_once(r.unit(u));
+                    w[i][0] = v.x, w[i][1] = v.y, w[i][2] = v.z, w[i][3] = v.w;
+                    most[i] = r.largest(w[i]);
+                } else {
+                    float x[N];
+                    r.load_part(u, -INFINITY, x);
+                    most[i] = __uint_as_float(0x7FFFFFFFu);  // no number
+#pragma unroll
+                    for (int e = 0; e < N; ++e)
+                        if (static_cast<unsigned>(u * N - r.shift + e) < static_cast<unsigned>(r.V))
+                            most[i] = fmaxf(most[i], x[e]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        w[i][j] = BF16 ? (__float_as_uint(x[(BF16 ? 2 : 1) * j]) >> 16) |
+                                             (__float_as_uint(x[BF16 ? 2 * j + 1 : j]) & 0xFFFF0000u)
+                                       : __float_as_uint(x[j]);
+                }
+            }
+        }
+        float high = most[0];
+#pragma unroll
+        for (int i = 1; i < kAhead; ++i) high = fmaxf(high, most[i]);
+        high *= kLog2e;
+        if (high > mine.m) mine.raise(high);
+        const uint64_t log2e = pair(kLog2e, kLog2e), minus = pair(-mine.m, -mine.m);
+        uint64_t s2 = pair(mine.s, 0.0f), t2 = pair(mine.t, 0.0f);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            float x[N];
+            r.from_least(w[i]);
+            r.unpack(w[i], x);
+#pragma unroll
+            for (int e = 0; e < N; e += 2) {
+                const uint64_t y = fma2(pair(x[e], x[e + 1]), log2e, minus);
+                const float2 v = both(y);
+                const uint64_t q = pair(exp2_approx(v.x), exp2_approx(v.y));
+                s2 = add2(s2, q);
+                t2 = fma2(q, y, t2);
+            }
+        }
+        mine.s = both(s2).x + both(s2).y;
+        mine.t = both(t2).x + both(t2).y;
+        if constexpr (TOP) {
+            auto note = [&](int group, uint32_t key) {
+                if (key == 0) return;
+                if (rank == 0) {
+                    atomicMax(&sh.group_key[group], key);
+                } else {
+                    const uint32_t to = mapa_shared(smem_u32(&sh.group_key[group]), 0);
+                    asm volatile("red.relaxed.cluster.shared::cluster.max.u32 [%0], %1;" ::"r"(to), "r"(key) : "memory");
+                }
+            };
+            if (shift >= 5) {  // a lane's number is one of the warp's four
+                float v = 0.0f;
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) {
+                    const float all = warp_max(most[i]);
+                    if (lane == i) v = all;
+                }
+                const int u = u0 + 32 * lane;
+                if (lane < kAhead && u < r.units) note(u >> shift, key_of(v));
+            } else {
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) {
+                    uint32_t key = key_of(most[i]);
+                    for (int o = 1; o < 1 << shift; o <<= 1) key = max(key, __shfl_xor_sync(0xffffffffu, key, o));
+                    const int u = u0 + 32 * i + lane;
+                    if ((u & ((1 << shift) - 1)) == 0 && u < r.units) note(u >> shift, key);
                 }
             }
         }
@@ -387,21 +603,29 @@ __global__ void __launch_bounds__(kThreads) log_probs_kernel(const LogProbsParam
         if (rank != 0) return;
         for (int c = 1; c < ctas; ++c) mine.join(sh.cta_sums[c]);
     }
-    const float m = mine.m, ln_s = logf(mine.s);
+    const bool again = !(mine.m > -1e29f && mine.m < 1e38f);
+    if (again) mine = sums_again<BF16>(sh, r);
+    const float m = mine.m, log2_s = log2f(mine.s);
     const bool none = mine.s == 0.0f;  // every logit -infinity
+    // (far below the others, x - lse is x)
+    const auto value = [=](float x) {
+        if (none) return -INFINITY;
+        if (again) return fmaf(-kLn2, log2_s, x - m);
+        return (x < -1e37f ? x : (fmaf(x, kLog2e, -m) - log2_s) * kLn2) + 0.0f * mine.s;  // (NaN where s is)
+    };
     if (threadIdx.x == 0) {
-        if (p.entropy != nullptr) p.entropy[row] = none ? 0.0f : fmaf(-kLn2, mine.t / mine.s, ln_s);
+        if (p.entropy != nullptr) p.entropy[row] = none ? 0.0f : (log2_s - mine.t / mine.s) * kLn2;
         if (p.targets != nullptr) {
             const int target = p.targets[row];
             float logp = 0.0f;
             if (target >= 0 && target < p.V)
-                logp = none ? -INFINITY : (r.at(target) - m) - ln_s;
+                logp = value(r.at(target));
             else if (target != -1)
                 record_status(p.status, 1 /* W4A16_ERR_INVALID_ARG */);
             p.logp[row] = logp;
         }
     }
-    if constexpr (TOP) top<BF16>(sh, r, shift, groups, p.k, m, ln_s, none, p.index + row * p.k, p.score + row * p.k);
+    if constexpr (TOP) top<BF16>(sh, r, shift, groups, p.k, value, p.index + row * p.k, p.score + row * p.k);
 }
 
 template <bool BF16, bool TOP>
@@ -412,7 +636,7 @@ cudaError_t launch(const LogProbsParams& p, int sm_count, cudaStream_t stream) {
     while (units > kGroups << shift) ++shift;
     while (shift > 0 && units >> shift < 8 * p.k) --shift;
     int ctas = 1;
-    while (ctas < kMaxCluster && static_cast<int64_t>(p.M) * ctas * 2 <= 8 * sm_count && ctas * kThreads * kAhead < units)
+    while (ctas < kMaxCluster && static_cast<int64_t>(p.M) * ctas * 2 <= 4 * sm_count && ctas * kThreads * kAhead < units)
         ctas *= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(p.M) * ctas);

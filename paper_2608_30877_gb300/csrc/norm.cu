@@ -19,7 +19,7 @@ namespace w4a16 {
 
 namespace {
 
-constexpr int kMaxWarps = 16;
+constexpr int kMaxWarps = 32;
 
 __device__ __forceinline__ float bf16_low(uint32_t v) { return __uint_as_float(v << 16); }
 __device__ __forceinline__ float bf16_high(uint32_t v) { return __uint_as_float(v & 0xFFFF0000u); }
@@ -104,12 +104,14 @@ struct Raw<float> {
 
 // Vectors that every row reads, through L1.
 template <bool ODD>
-__device__ __forceinline__ void load_vector(const uint16_t* vec, int c, const Row<ODD>& r, float (&x)[8]) {
+__device__ __forceinline__ uint4 load_vector(const uint16_t* vec, int c, const Row<ODD>& r) {
     if constexpr (!ODD) {
-        unpack8(r.whole(c) ? __ldg(reinterpret_cast<const uint4*>(vec + c)) : make_uint4(0, 0, 0, 0), x);
+        return r.whole(c) ? __ldg(reinterpret_cast<const uint4*>(vec + c)) : make_uint4(0, 0, 0, 0);
     } else {
+        uint32_t w[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = r.has(c, e) ? bf16_low(__ldg(vec + c + e)) : 0.0f;
+        for (int e = 0; e < 8; ++e) w[e] = r.has(c, e) ? __ldg(vec + c + e) : 0u;
+        return make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
     }
 }
 
@@ -156,36 +158,36 @@ struct Reducer {
         ++turn;
         if ((threadIdx.x & 31) == 0) p[threadIdx.x >> 5] = x;
         __syncthreads();
-        x = p[0];
-        for (int w = 1; w < warps; ++w) x = MAX ? fmaxf(x, p[w]) : x + p[w];
+        // (entries past the last warp's are 0, which changes neither sums nor maxima of magnitudes)
+        x = 0.0f;
+        for (int w = 0; w < warps; w += 4) {
+            const float4 v = *reinterpret_cast<const float4*>(p + w);
+            x = MAX ? fmaxf(fmaxf(fmaxf(x, v.x), fmaxf(v.y, v.z)), v.w) : x + ((v.x + v.y) + (v.z + v.w));
+        }
         return x;
     }
 };
 
-// The mean (layer norm; else 0) and 1 / sqrt(mean square about it + eps) of a row.
-template <int NV, bool ODD>
-__device__ __forceinline__ void statistics(const float (&x)[NV][8], bool layer, const Row<ODD>& r, float inv_d, float eps,
-                                           Reducer& red, float* mean, float* rstd) {
+// The entries past a CTA's last warp; the first reduction's barrier is behind it.
+__device__ __forceinline__ void clear(float (&parts)[2][kMaxWarps]) {
+    const int t = threadIdx.x;
+    if (t < 2 * kMaxWarps && t % kMaxWarps >= static_cast<int>(blockDim.x >> 5)) parts[t / kMaxWarps][t % kMaxWarps] = 0.0f;
+}
+
+// The mean (layer norm; else 0) and 1 / sqrt(mean square about it + eps) of a row.  each(f): f(value) for the
+// thread's values.
+template <typename Each>
+__device__ __forceinline__ void statistics(const Each& each, bool layer, float inv_d, float eps, Reducer& red, float* mean,
+                                           float* rstd) {
     float m = 0.0f;
     if (layer) {
         // (a sum of x / D: one of x could overflow)
         float sum = 0.0f;
-#pragma unroll
-        for (int v = 0; v < NV; ++v)
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (r.has(r.first(v), e)) sum = fmaf(x[v][e], inv_d, sum);
+        each([&](float x) { sum = fmaf(x, inv_d, sum); });
         m = red.reduce<false>(sum);
     }
     float ss = 0.0f;
-#pragma unroll
-    for (int v = 0; v < NV; ++v)
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (r.has(r.first(v), e)) {
-                const float c = x[v][e] - m;
-                ss = fmaf(c, c, ss);
-            }
+    each([&](float x) { ss = fmaf(x - m, x - m, ss); });
     const float total = red.reduce<false>(ss);
     *mean = m;
     *rstd = rsqrtf(fmaf(total, inv_d, eps));
@@ -194,112 +196,76 @@ __device__ __forceinline__ void statistics(const float (&x)[NV][8], bool layer, 
     // branch is the same for all threads of the row.  An infinity or a NaN gives 0 or NaN, as the
     // formula has it.)
     float top = 0.0f;
-#pragma unroll
-    for (int v = 0; v < NV; ++v)
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (r.has(r.first(v), e)) top = fmaxf(top, fabsf(x[v][e] - m));
+    each([&](float x) { top = fmaxf(top, fabsf(x - m)); });
     top = red.reduce<true>(top);
     if (!(top < INFINITY) || total != total) return;
     const float s = __uint_as_float((253u << 23) - (__float_as_uint(top) & 0x7F800000u));  // 2^-exponent / 2
     ss = 0.0f;
-#pragma unroll
-    for (int v = 0; v < NV; ++v)
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (r.has(r.first(v), e)) {
-                const float c = (x[v][e] - m) * s;
-                ss = fmaf(c, c, ss);
-            }
+    each([&](float x) { ss = fmaf((x - m) * s, (x - m) * s, ss); });
     *rstd = s * rsqrtf(red.reduce<false>(ss) * inv_d);  // (eps s^2 is far below half a step)
 }
 
-template <typename R, int NV, bool ODD>
-__global__ void __launch_bounds__(NV > 8 ? 384 : 512) residual_norm_kernel(const NormParams p, const int group) {
-    // (with more pieces than that the stream's values are read after the block's norm: registers)
-    constexpr bool kAhead = NV <= 6;
-    __shared__ float parts[2][kMaxWarps];
-    const int64_t row = group == 32 ? static_cast<int64_t>(blockIdx.x) * (blockDim.x >> 5) + (threadIdx.x >> 5)
-                                    : blockIdx.x;
-    grid_launch_dependents();
-    grid_wait();
-    if (row >= p.M) return;  // (a whole warp; a CTA's row always exists)
-    Reducer red{parts, group >> 5, 0};
-    const int D = p.D;
-    const int64_t at = row * D;
-    const Row<ODD> r{static_cast<int>(group == 32 ? threadIdx.x & 31 : threadIdx.x), group, D,
-                     static_cast<int>(at & 7)};
-    const float inv_d = 1.0f / static_cast<float>(D);
-    const R* const residual = static_cast<const R*>(p.residual) + at;
-    float x[NV][8];
+template <int NV, bool ODD>
+__device__ __forceinline__ void statistics(const float (&x)[NV][8], bool layer, const Row<ODD>& r, float inv_d, float eps,
+                                           Reducer& red, float* mean, float* rstd) {
+    statistics(
+        [&](const auto& f) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (r.has(r.first(v), e)) f(x[v][e]);
+        },
+        layer, inv_d, eps, red, mean, rstd);
+}
+
+// x[v][e] = f(x[v][e], vec[column]), a vector's loads together.
+template <int NV, bool ODD, typename F>
+__device__ __forceinline__ void with_vector(float (&x)[NV][8], const uint16_t* vec, const Row<ODD>& r, const F& f) {
+    uint4 raw[NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) raw[v] = load_vector(vec, r.first(v), r);
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        float w[8];
+        unpack8(raw[v], w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[v][e] = f(x[v][e], w[e]);
+    }
+}
+
+// The rest of a row whose block output is x (its scaled stream values without a block): `stream` and
+// `gate` give a piece's values.
+template <typename R, int NV, bool ODD, typename Stream, typename Gate>
+__device__ __forceinline__ void finish_row(const NormParams& p, const Row<ODD>& r, int64_t at, float inv_d, Reducer& red,
+                                           float (&x)[NV][8], const Stream& stream, const Gate& gate) {
+    const float offset = p.weight_offset;
+    float mean, rstd;
     if (p.block != nullptr) {
-        Raw<R> stream[kAhead ? NV : 1];
-        constexpr int kTogether = kAhead ? NV : 4;
-        static_assert(NV % kTogether == 0, "a row's pieces in whole batches");
-#pragma unroll
-        for (int v0 = 0; v0 < NV; v0 += kTogether) {
-            Raw<uint16_t> block[kTogether];
-#pragma unroll
-            for (int v = 0; v < kTogether; ++v) block[v].load(p.block + at, r.first(v0 + v), r);
-            if constexpr (kAhead) {
-#pragma unroll
-                for (int v = 0; v < NV; ++v) stream[v].load(residual, r.first(v), r);
-            }
-#pragma unroll
-            for (int v = 0; v < kTogether; ++v) block[v].values(x[v0 + v]);
-        }
         if (p.post_weight != nullptr) {
-            float mean, rstd;
             statistics<NV, ODD>(x, p.layer, r, inv_d, p.eps, red, &mean, &rstd);
-#pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                float w[8];
-                load_vector(p.post_weight, r.first(v), r, w);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[v][e] = (x[v][e] - mean) * rstd * (p.weight_offset + w[e]);
-                if (p.post_bias != nullptr) {
-                    load_vector(p.post_bias, r.first(v), r, w);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[v][e] += w[e];
-                }
-            }
+            with_vector(x, p.post_weight, r, [=](float v, float w) { return (v - mean) * rstd * (offset + w); });
+            if (p.post_bias != nullptr) with_vector(x, p.post_bias, r, [](float v, float w) { return v + w; });
         }
         if (p.gate != nullptr) {
+            if (p.gate_stride == 0) {
+                with_vector(x, p.gate, r, [](float v, float w) { return v * w; });
+            } else {
 #pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                float w[8];
-                if (p.gate_stride == 0) {
-                    load_vector(p.gate, r.first(v), r, w);
-                } else {
-                    Raw<uint16_t> g;
-                    g.load(p.gate + at, r.first(v), r);
-                    g.values(w);
+                for (int v = 0; v < NV; ++v) {
+                    float w[8];
+                    gate(v, w);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[v][e] *= w[e];
                 }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[v][e] *= w[e];
             }
         }
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             float w[8];
-            if constexpr (!kAhead) stream[0].load(residual, r.first(v), r);
-            stream[kAhead ? v : 0].values(w);
+            stream(v, w);
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[v][e] = fmaf(p.residual_scale, w[e], x[v][e]);
-        }
-    } else {
-        constexpr int kTogether = kAhead ? NV : 2;
-#pragma unroll
-        for (int v0 = 0; v0 < NV; v0 += kTogether) {
-            Raw<R> stream[kTogether];
-#pragma unroll
-            for (int v = 0; v < kTogether; ++v) stream[v].load(residual, r.first(v0 + v), r);
-#pragma unroll
-            for (int v = 0; v < kTogether; ++v) {
-                stream[v].values(x[v0 + v]);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[v0 + v][e] *= p.residual_scale;
-            }
         }
     }
     if (p.residual_out != nullptr) {
@@ -308,25 +274,315 @@ __global__ void __launch_bounds__(NV > 8 ? 384 : 512) residual_norm_kernel(const
         for (int v = 0; v < NV; ++v) store8(to, r.first(v), r, x[v]);
     }
     if (p.out == nullptr) return;
-    float mean, rstd;
     statistics<NV, ODD>(x, p.layer, r, inv_d, p.eps, red, &mean, &rstd);
+    if (p.weight != nullptr) {
+        with_vector(x, p.weight, r, [=](float v, float w) { return (v - mean) * rstd * (offset + w); });
+    } else {
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        float w[8], y[8];
+        for (int v = 0; v < NV; ++v)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = (x[v][e] - mean) * rstd;
+            for (int e = 0; e < 8; ++e) x[v][e] = (x[v][e] - mean) * rstd;
+    }
+    if (p.bias != nullptr) with_vector(x, p.bias, r, [](float v, float w) { return v + w; });
+#pragma unroll
+    for (int v = 0; v < NV; ++v) store8(p.out + at, r.first(v), r, x[v]);
+}
+
+// A warp or a CTA to a row, which it holds in registers from the first load on: few rows, rows of odd or
+// of large width.
+template <typename R, int NV, bool ODD>
+__global__ void __launch_bounds__(512, NV <= 3 && !ODD ? 2 : 1) residual_norm_kernel(const NormParams p, const int group) {
+    __shared__ __align__(16) float parts[2][kMaxWarps];
+    const int64_t row = group == 32 ? static_cast<int64_t>(blockIdx.x) * (blockDim.x >> 5) + (threadIdx.x >> 5)
+                                    : blockIdx.x;
+    grid_launch_dependents();
+    grid_wait();
+    if (row >= p.M) return;  // (a whole warp; a CTA's row always exists)
+    Reducer red{parts, group >> 5, 0};
+    clear(parts);
+    const int64_t at = row * p.D;
+    const Row<ODD> r{static_cast<int>(group == 32 ? threadIdx.x & 31 : threadIdx.x), group, p.D,
+                     static_cast<int>(at & 7)};
+    const float inv_d = 1.0f / static_cast<float>(p.D);
+    const R* const residual = static_cast<const R*>(p.residual) + at;
+    float x[NV][8];
+    Raw<R> stream[NV];
+    if (p.block != nullptr) {
+        Raw<uint16_t> block[NV];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) block[v].load(p.block + at, r.first(v), r);
+#pragma unroll
+        for (int v = 0; v < NV; ++v) stream[v].load(residual, r.first(v), r);
+#pragma unroll
+        for (int v = 0; v < NV; ++v) block[v].values(x[v]);
+    } else {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) stream[v].load(residual, r.first(v), r);
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            stream[v].values(x[v]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[v][e] *= p.residual_scale;
+        }
+    }
+    finish_row<R, NV, ODD>(
+        p, r, at, inv_d, red, x, [&](int v, float (&w)[8]) { stream[v].values(w); },
+        [&](int v, float (&w)[8]) {
+            Raw<uint16_t> g;
+            g.load(p.gate + at, r.first(v), r);
+            g.values(w);
+        });
+}
+
+// Many rows of whole 16-byte units: as many CTAs as are resident, each with a ring of rows in shared
+// memory that bulk copies fill while it is at a row before (the reductions leave the memory idle
+// otherwise: two rows an SM in registers, 4097 rows of 8200 with both layer norms and an fp32 stream 159 us).
+constexpr int kRingThreads = 384;
+constexpr int kRingRows = 4;  // at most
+
+__device__ __forceinline__ void copy_row(uint32_t to, const void* from, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from),
+                 "r"(bytes), "r"(bar)
+                 : "memory");
+}
+
+template <typename R>
+__device__ __forceinline__ void ring_values(const uint8_t* row, int c, float (&w)[8]) {
+    Raw<R> raw;
+    const uint4* const at = reinterpret_cast<const uint4*>(row + c * sizeof(R));
+    if constexpr (sizeof(R) == 2) {
+        raw.u = at[0];
+    } else {
+        raw.a = at[0];
+        raw.b = at[1];
+    }
+    raw.values(w);
+}
+
+template <typename R, int NV>
+__global__ void __launch_bounds__(kRingThreads, 2) residual_norm_ring_kernel(const NormParams p, const int depth) {
+    extern __shared__ __align__(16) uint8_t ring[];
+    __shared__ __align__(16) float parts[2][kMaxWarps];
+    __shared__ __align__(8) uint64_t full[kRingRows];
+    __shared__ int abort_flag;
+    const int D = p.D;
+    const uint32_t stream_bytes = D * static_cast<uint32_t>(sizeof(R)), block_bytes = p.block != nullptr ? D * 2u : 0u,
+                   gate_bytes = p.gate != nullptr && p.gate_stride != 0 ? D * 2u : 0u;
+    const uint32_t row_bytes = stream_bytes + block_bytes + gate_bytes;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < depth; ++i) mbar_init(smem_u32(&full[i]), 1);
+        abort_flag = 0;
+        fence_mbar_init();
+    }
+    grid_launch_dependents();
+    grid_wait();
+    __syncthreads();
+    auto fetch = [&](int slot, int64_t row) {  // one thread
+        const uint32_t bar = smem_u32(&full[slot]), to = smem_u32(ring) + slot * row_bytes;
+        mbar_arrive_expect_tx(bar, row_bytes);
+        if (block_bytes != 0) copy_row(to, p.block + row * D, block_bytes, bar);
+        copy_row(to + block_bytes, static_cast<const R*>(p.residual) + row * D, stream_bytes, bar);
+        if (gate_bytes != 0) copy_row(to + block_bytes + stream_bytes, p.gate + row * D, gate_bytes, bar);
+    };
+    bool ok = true;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < depth; ++i) {
+            const int64_t row = blockIdx.x + static_cast<int64_t>(i) * gridDim.x;
+            if (row < p.M) fetch(i, row);
+        }
+        ok = short_limit_ok(smem_u32(&full[0]), 0, &abort_flag, p.status, p.wait_ns);
+    }
+    Reducer red{parts, static_cast<int>(blockDim.x) >> 5, 0};
+    clear(parts);
+    const Row<false> r{static_cast<int>(threadIdx.x), static_cast<int>(blockDim.x), D, 0};
+    const float inv_d = 1.0f / static_cast<float>(D);
+    const int64_t step = gridDim.x;
+    int slot = 0;
+    uint32_t parity = 0;
+    for (int64_t row = blockIdx.x; row < p.M; row += step) {
+        ok = wait_warp(smem_u32(&full[slot]), parity, &abort_flag, p.status, p.wait_ns) && ok;
+        const bool begun = row != blockIdx.x;
+        if (__syncthreads_or(!ok)) {
+            if (threadIdx.x == 0)  // the copies under way land before the CTA ends
+                for (int i = 0; i < depth - begun && row + i * step < p.M; ++i) {
+                    settle(smem_u32(&full[slot]), parity);
+                    slot = slot + 1 == depth ? 0 : slot + 1;
+                    parity ^= slot == 0;
+                }
+            return;
+        }
+        // every thread is done with the row before: its place takes the next one
+        if (threadIdx.x == 0 && begun && row + (depth - 1) * step < p.M)
+            fetch(slot == 0 ? depth - 1 : slot - 1, row + (depth - 1) * step);
+        const uint8_t* const from = ring + slot * row_bytes;
+        float x[NV][8];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int c = r.first(v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[v][e] = 0.0f;
+            if (c < D) {
+                if (block_bytes != 0) {
+                    ring_values<uint16_t>(from, c, x[v]);
+                } else {
+                    ring_values<R>(from, c, x[v]);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[v][e] *= p.residual_scale;
+                }
+            }
+        }
+        auto values = [&](const uint8_t* part, auto type, int v, float (&w)[8]) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = 0.0f;
+            if (r.first(v) < D) ring_values<decltype(type)>(part, r.first(v), w);
+        };
+        finish_row<R, NV, false>(
+            p, r, row * D, inv_d, red, x, [&](int v, float (&w)[8]) { values(from + block_bytes, R{}, v, w); },
+            [&](int v, float (&w)[8]) { values(from + block_bytes + stream_bytes, uint16_t{}, v, w); });
+        slot = slot + 1 == depth ? 0 : slot + 1;
+        parity ^= slot == 0;
+    }
+}
+
+template <typename R>
+cudaError_t launch_ring(const NormParams& p, int depth, int row_bytes, int ctas, int sm_count, cudaStream_t stream) {
+    const int pieces = p.D / 8, least = (pieces + kRingThreads - 1) / kRingThreads;
+    const int nv = least <= 2 ? 2 : least;
+    auto kernel = nv == 2   ? residual_norm_ring_kernel<R, 2>
+                  : nv == 3 ? residual_norm_ring_kernel<R, 3>
+                            : residual_norm_ring_kernel<R, 4>;
+    const cudaError_t e =
+        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, depth * row_bytes);
+    if (e != cudaSuccess) return e;
+    const int threads = ((pieces + nv - 1) / nv + 31) / 32 * 32;
+    return launch_overlapped(kernel, dim3(ctas * sm_count), threads, depth * row_bytes, stream, p, depth);
+}
+
+// Rows wider than registers hold: one CTA to a row, whose values are in shared memory in fp32 between the
+// passes; a thread works on its own units alone.
+constexpr int kWideThreads = 1024;
+
+template <typename R, bool ODD>
+__global__ void __launch_bounds__(kWideThreads) residual_norm_wide_kernel(const NormParams p) {
+    extern __shared__ __align__(16) float values[];
+    __shared__ __align__(16) float parts[2][kMaxWarps];
+    const int64_t row = blockIdx.x, at = row * p.D;
+    grid_launch_dependents();
+    grid_wait();
+    Reducer red{parts, kWideThreads / 32, 0};
+    const Row<ODD> r{static_cast<int>(threadIdx.x), kWideThreads, p.D, static_cast<int>(at & 7)};
+    const float inv_d = 1.0f / static_cast<float>(p.D), offset = p.weight_offset;
+    const int pieces = (p.D + (ODD ? r.shift : 0) + 7) / 8;
+    const R* const residual = static_cast<const R*>(p.residual) + at;
+    const int own = static_cast<int>(threadIdx.x) < pieces ? (pieces - 1 - threadIdx.x) / kWideThreads + 1 : 0;
+    auto get = [&](int v, float (&x)[8]) {
+        const float4* const from = reinterpret_cast<const float4*>(values + (v * kWideThreads + threadIdx.x) * 8);
+        const float4 a = from[0], b = from[1];
+        x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+    };
+    auto put = [&](int v, const float (&x)[8]) {
+        float4* const to = reinterpret_cast<float4*>(values + (v * kWideThreads + threadIdx.x) * 8);
+        to[0] = make_float4(x[0], x[1], x[2], x[3]);
+        to[1] = make_float4(x[4], x[5], x[6], x[7]);
+    };
+    auto stats = [&](float* mean, float* rstd) {
+        statistics(
+            [&](const auto& f) {
+                for (int v = 0; v < own; ++v) {
+                    float x[8];
+                    get(v, x);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (r.has(r.first(v), e)) f(x[e]);
+                }
+            },
+            p.layer, inv_d, p.eps, red, mean, rstd);
+    };
+    float mean, rstd;
+    if (p.block != nullptr && p.post_weight != nullptr) {
+#pragma unroll 2
+        for (int v = 0; v < own; ++v) {
+            Raw<uint16_t> raw;
+            raw.load(p.block + at, r.first(v), r);
+            float x[8];
+            raw.values(x);
+            put(v, x);
+        }
+        stats(&mean, &rstd);
+    }
+#pragma unroll 2
+    for (int v = 0; v < own; ++v) {
+        const int c = r.first(v);
+        float x[8], h[8], w[8];
+        Raw<R> raw;
+        raw.load(residual, c, r);
+        raw.values(h);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[e] *= p.residual_scale;
+        if (p.block != nullptr) {
+            if (p.post_weight != nullptr) {
+                get(v, x);
+                unpack8(load_vector(p.post_weight, c, r), w);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = (x[e] - mean) * rstd * (offset + w[e]);
+                if (p.post_bias != nullptr) {
+                    unpack8(load_vector(p.post_bias, c, r), w);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] += w[e];
+                }
+            } else {
+                Raw<uint16_t> block;
+                block.load(p.block + at, c, r);
+                block.values(x);
+            }
+            if (p.gate != nullptr) {
+                if (p.gate_stride == 0) {
+                    unpack8(load_vector(p.gate, c, r), w);
+                } else {
+                    Raw<uint16_t> gate;
+                    gate.load(p.gate + at, c, r);
+                    gate.values(w);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] *= w[e];
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) h[e] += x[e];
+        }
+        if (p.residual_out != nullptr) store8(static_cast<R*>(p.residual_out) + at, c, r, h);
+        put(v, h);
+    }
+    if (p.out == nullptr) return;
+    stats(&mean, &rstd);
+#pragma unroll 2
+    for (int v = 0; v < own; ++v) {
+        const int c = r.first(v);
+        float x[8], w[8];
+        get(v, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = (x[e] - mean) * rstd;
         if (p.weight != nullptr) {
-            load_vector(p.weight, r.first(v), r, w);
+            unpack8(load_vector(p.weight, c, r), w);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] *= p.weight_offset + w[e];
+            for (int e = 0; e < 8; ++e) x[e] *= offset + w[e];
         }
         if (p.bias != nullptr) {
-            load_vector(p.bias, r.first(v), r, w);
+            unpack8(load_vector(p.bias, c, r), w);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] += w[e];
+            for (int e = 0; e < 8; ++e) x[e] += w[e];
         }
-        store8(p.out + at, r.first(v), r, y);
+        store8(p.out + at, c, r, x);
     }
+}
+
+template <typename R, bool ODD>
+cudaError_t launch_wide(const NormParams& p, cudaStream_t stream) {
+    const int units = (p.D + (ODD ? 14 : 7)) / 8;
+    const int smem = (units + kWideThreads - 1) / kWideThreads * kWideThreads * 32;
+    auto kernel = residual_norm_wide_kernel<R, ODD>;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    return launch_overlapped(kernel, dim3(p.M), kWideThreads, smem, stream, p);
 }
 
 template <typename R, bool ODD>
@@ -342,14 +598,11 @@ cudaError_t launch(const NormParams& p, cudaStream_t stream) {
                            : residual_norm_kernel<R, 4, ODD>;
     } else {
         const int least = (pieces + 511) / 512;
-        const int nv = least <= 2 ? 2 : least <= 4 ? least : least <= 6 ? 6 : least <= 8 ? 8 : 16;
-        if (ODD && nv > 6) return cudaErrorInvalidValue;  // (refused before: kNormMaxOdd)
+        if (least > 4) return launch_wide<R, ODD>(p, stream);
+        const int nv = least <= 2 ? 2 : least;
         kernel = nv == 2   ? residual_norm_kernel<R, 2, ODD>
                  : nv == 3 ? residual_norm_kernel<R, 3, ODD>
-                 : nv == 4 ? residual_norm_kernel<R, 4, ODD>
-                 : nv == 6 ? residual_norm_kernel<R, 6, ODD>
-                 : nv == 8 ? residual_norm_kernel<R, ODD ? 6 : 8, ODD>
-                           : residual_norm_kernel<R, ODD ? 6 : 16, ODD>;
+                           : residual_norm_kernel<R, 4, ODD>;
         group = threads = ((pieces + nv - 1) / nv + 31) / 32 * 32;
     }
     const int rows = threads / group;
@@ -358,8 +611,18 @@ cudaError_t launch(const NormParams& p, cudaStream_t stream) {
 
 }  // namespace
 
-cudaError_t launch_residual_norm(const NormParams& p, bool fp32, cudaStream_t stream) {
+cudaError_t launch_residual_norm(const NormParams& p, bool fp32, int sm_count, cudaStream_t stream) {
     const bool whole = p.D % 8 == 0;  // rows of 16-byte units (bases are 16-byte aligned)
+    // (a plain bf16 RMS norm is at the copy bandwidth from registers: 39004 rows of 12288 551 us, 613 with the
+    // ring; 4097 of 8200 with both layer norms and an fp32 stream 128, 99 with it)
+    if (whole && p.D > 1024 && p.D <= 4 * 8 * kRingThreads) {
+        const int row_bytes = p.D * ((fp32 ? 4 : 2) + (p.block != nullptr ? 2 : 0) +
+                                     (p.gate != nullptr && p.gate_stride != 0 ? 2 : 0));
+        const int depth = 112 * 1024 / row_bytes < kRingRows ? 112 * 1024 / row_bytes : kRingRows;
+        if (depth >= 2 && p.M >= 4 * sm_count && (fp32 || p.layer || p.post_weight != nullptr))
+            return fp32 ? launch_ring<float>(p, depth, row_bytes, 2, sm_count, stream)
+                        : launch_ring<uint16_t>(p, depth, row_bytes, 2, sm_count, stream);
+    }
     return fp32 ? (whole ? launch<float, false>(p, stream) : launch<float, true>(p, stream))
                 : (whole ? launch<uint16_t, false>(p, stream) : launch<uint16_t, true>(p, stream));
 }

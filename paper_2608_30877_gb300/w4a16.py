@@ -9,7 +9,6 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
-import functools
 import os
 import re
 import weakref
@@ -96,7 +95,8 @@ def lib() -> ctypes.CDLL:
         L.w4a16_kv_rotary.argtypes = [kv, p, p, p, i64, i64, i64, p, i64, i32, f32, p]
         L.w4a16_log_probs.argtypes = [p, i32, i64, i64, i64, p, i64, p, p, p, p, p]
         L.w4a16_add_adapters.argtypes = [p, p, p, p, i64, p, p, i64, i64, i64, i64, i64, p, p, p, p]
-        L.w4a16_add_adapters_workspace.argtypes = [i64, i64, i64, i64, ctypes.POINTER(i64)]
+        L.w4a16_add_adapters_workspace.argtypes = [i64, i64]
+        L.w4a16_add_adapters_workspace.restype = i64
         L.w4a16_get_device_error.argtypes = [p]
         L.w4a16_selftest_wait_timeout.argtypes = [i64, p]
         L.w4a16_selftest_set_wait_limit.argtypes = [i64]
@@ -112,7 +112,7 @@ def lib() -> ctypes.CDLL:
                   "w4a16_kv_extend", "w4a16_kv_fork", "w4a16_kv_trim", "w4a16_kv_compact",
                   "w4a16_kv_write", "w4a16_attention_decode", "w4a16_attention_decode_workspace",
                   "w4a16_residual_norm", "w4a16_rotary_table", "w4a16_rotary", "w4a16_kv_rotary",
-                  "w4a16_log_probs", "w4a16_add_adapters", "w4a16_add_adapters_workspace",
+                  "w4a16_log_probs", "w4a16_add_adapters",
                   "w4a16_get_device_error", "w4a16_selftest_wait_timeout",
                   "w4a16_selftest_set_wait_limit", "w4a16_selftest_route"):
             getattr(L, f).restype = ctypes.c_int
@@ -502,18 +502,33 @@ def attention_decode(cache: KVCache, layer: int, qkv: torch.Tensor, slots: torch
     return out
 
 
-def _fits(t, dtype, *shape) -> bool:
-    """A contiguous tensor of this type and shape on the current device."""
-    return (t.dtype == dtype and t.shape == shape and t.is_contiguous() and t.is_cuda
-            and t.get_device() == torch.cuda.current_device())
+# (what a call checks takes as long as a small kernel: one look at the current device, and shapes
+# as they are)
+def _fits(t, dtype, shape, device: int) -> bool:
+    """A contiguous tensor of this type and shape on the device."""
+    return t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == device
 
 
-def _new(stream, shape, dtype, device) -> torch.Tensor:
+def _device_of(t: torch.Tensor) -> int:
+    """The tensor's device, which has to be the current one (the library launches there)."""
+    device = t.get_device()
+    if device < 0 or device != torch.cuda.current_device():
+        raise ValueError("expected CUDA tensors on the current device")
+    return device
+
+
+def _stream_on(stream, device: int) -> int:
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(device)
+    return _stream(stream)
+
+
+def _new(stream, shape, dtype, like) -> torch.Tensor:
     """An output, allocated on the stream that writes it."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
     with _allocating_on(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
 
 
 def _ptr(t):
@@ -532,30 +547,32 @@ def residual_norm(residual: torch.Tensor, weight: torch.Tensor | None = None,
     weights and biases bf16 [D]; post(block) is block without post_weight.  residual_out may be
     residual.  Without block and residual_out h is not stored (None; residual itself where
     residual_scale is 1)."""
-    M, D = residual.shape
-    bf16 = torch.bfloat16
-    if residual.dtype not in (bf16, torch.float32) or not _fits(residual, residual.dtype, M, D):
+    bf16, shape, device = torch.bfloat16, residual.shape, _device_of(residual)
+    M, D = shape
+    vector = shape[1:]
+    if not (_fits(residual, residual.dtype, shape, device) and (residual.dtype is bf16 or residual.dtype is torch.float32)):
         raise ValueError("expected a contiguous residual [M, D] in bf16 or fp32 on the current device")
     for t in (weight, bias, post_weight, post_bias):
-        if t is not None and not _fits(t, bf16, D):
+        if t is not None and not _fits(t, bf16, vector, device):
             raise ValueError("expected contiguous bf16 weights and biases [D] on the current device")
-    if block is not None and not _fits(block, bf16, M, D):
+    if block is not None and not _fits(block, bf16, shape, device):
         raise ValueError("expected a contiguous bf16 block [M, D] on the current device")
-    if gate is not None and not (_fits(gate, bf16, 1, D) or _fits(gate, bf16, M, D)):
+    if gate is not None and not (_fits(gate, bf16, (1, D), device) or _fits(gate, bf16, shape, device)):
         raise ValueError("expected a contiguous bf16 gate [1, D] or [M, D] on the current device")
     if residual_out is None:
         if block is not None:
-            residual_out = _new(stream, (M, D), residual.dtype, residual.device)
-    elif not _fits(residual_out, residual.dtype, M, D):
+            residual_out = _new(stream, shape, residual.dtype, residual)
+    elif not _fits(residual_out, residual.dtype, shape, device):
         raise ValueError("expected residual_out like residual")
     if out is None:
-        out = _new(stream, (M, D), bf16, residual.device)
-    elif not _fits(out, bf16, M, D):
+        out = _new(stream, shape, bf16, residual)
+    elif not _fits(out, bf16, shape, device):
         raise ValueError("expected a contiguous bf16 out [M, D] on the current device")
     _check("w4a16_residual_norm", lib().w4a16_residual_norm(
-        residual.data_ptr(), 16 if residual.dtype == bf16 else 32, _ptr(block), _ptr(gate),
+        residual.data_ptr(), 16 if residual.dtype is bf16 else 32, _ptr(block), _ptr(gate),
         0 if gate is None else gate.shape[0], _ptr(post_weight), _ptr(post_bias), _ptr(weight), _ptr(bias),
-        M, D, kind, residual_scale, eps, weight_offset, _ptr(residual_out), out.data_ptr(), _stream(stream)))
+        M, D, kind, residual_scale, eps, weight_offset, _ptr(residual_out), out.data_ptr(),
+        _stream_on(stream, device)))
     if residual_out is None and residual_scale == 1.0:
         residual_out = residual
     return out, residual_out
@@ -579,24 +596,24 @@ class RotaryTable:
         self.turns = host.to(device)  # (from pageable memory: the copy has been made)
 
 
-def _rotary_qkv(qkv: torch.Tensor, table: RotaryTable, columns: int) -> int:
+def _rotary_qkv(qkv: torch.Tensor, table: RotaryTable, columns: int, device: int) -> int:
     M = qkv.shape[0]
-    if not _fits(qkv, torch.bfloat16, M, columns):
+    if not _fits(qkv, torch.bfloat16, (M, columns), device):
         raise ValueError("expected a contiguous bf16 qkv [M, (H + 2 kv_heads) * head_dim] on the current device")
-    if table.turns.get_device() != qkv.get_device():
+    if table.turns.get_device() != device:
         raise ValueError("the table is on another device")
     return M
 
 
-def _rotary_lists(M: int, seq_start, list_) -> int:
-    """The number of sequences."""
+def _sequences(M: int, seq_start, list_, device: int) -> int:
+    """The number of sequences: of the table, or a row each; list_ has an entry for each."""
     if seq_start is None:
         nseq = M
     else:
         nseq = seq_start.shape[0] - 1
-        if not _fits(seq_start, torch.int32, nseq + 1):
+        if not _fits(seq_start, torch.int32, (nseq + 1,), device):
             raise ValueError("expected a contiguous int32 seq_start [nseq + 1] on the current device")
-    if list_ is not None and not _fits(list_, torch.int32, nseq):
+    if list_ is not None and not _fits(list_, torch.int32, (nseq,), device):
         raise ValueError("expected contiguous int32 lists with an entry for each sequence on the current device")
     return nseq
 
@@ -609,11 +626,12 @@ def rotary(qkv: torch.Tensor, table: RotaryTable, H: int, kv_heads: int | None =
     without seq_start each row is a sequence, without first they begin at 0)."""
     if kv_heads is None:
         kv_heads = H
-    M = _rotary_qkv(qkv, table, (H + 2 * kv_heads) * head_dim)
-    nseq = _rotary_lists(M, seq_start, first)
+    device = _device_of(qkv)
+    M = _rotary_qkv(qkv, table, (H + 2 * kv_heads) * head_dim, device)
+    nseq = _sequences(M, seq_start, first, device)
     _check("w4a16_rotary", lib().w4a16_rotary(
         qkv.data_ptr(), _ptr(seq_start), _ptr(first), nseq, M, H, kv_heads, head_dim, table.turns.data_ptr(),
-        table.rot_dim, table.layout, table.attention_factor, _stream(stream)))
+        table.rot_dim, table.layout, table.attention_factor, _stream_on(stream, device)))
     return qkv
 
 
@@ -622,11 +640,12 @@ def kv_rotary(cache: KVCache, qkv: torch.Tensor, slots: torch.Tensor, H: int, ta
     """The same with the positions that the cache's sequences have grown to: rows [seq_start[i],
     seq_start[i+1]) are the last tokens of slots[i]'s sequence (before kv_write), or without seq_start row i
     is the last one (before attention_decode)."""
-    M = _rotary_qkv(qkv, table, (H + 2 * cache.kv_heads) * cache.pages.shape[5])
-    nseq = _rotary_lists(M, seq_start, slots)
+    device = _device_of(qkv)
+    M = _rotary_qkv(qkv, table, (H + 2 * cache.kv_heads) * 128, device)
+    nseq = _sequences(M, seq_start, slots, device)
     _check("w4a16_kv_rotary", lib().w4a16_kv_rotary(
         cache._ref, qkv.data_ptr(), _ptr(seq_start), slots.data_ptr(), nseq, M, H, table.turns.data_ptr(),
-        table.rot_dim, table.layout, table.attention_factor, _stream(stream)))
+        table.rot_dim, table.layout, table.attention_factor, _stream_on(stream, device)))
     return qkv
 
 
@@ -636,28 +655,21 @@ def log_probs(logits: torch.Tensor, targets: torch.Tensor | None = None, k: int 
     contiguous (include/w4a16.h): log probabilities of targets (int32 [M], -1: none, 0), the
     entropy, and the k largest logits' columns and log probabilities.  None where not asked for."""
     M, V = logits.shape
-    if (not logits.is_cuda or logits.dtype not in (torch.bfloat16, torch.float32)
-            or logits.get_device() != torch.cuda.current_device() or (V > 1 and logits.stride(1) != 1)):
+    device = _device_of(logits)
+    bf16 = logits.dtype is torch.bfloat16
+    if not (bf16 or logits.dtype is torch.float32) or (V > 1 and logits.stride(1) != 1):
         raise ValueError("expected logits [M, V] in bf16 or fp32 with contiguous rows on the current device")
-    stride = logits.stride(0) if M > 1 else V
-    if targets is not None and not _fits(targets, torch.int32, M):
+    if targets is not None and not _fits(targets, torch.int32, (M,), device):
         raise ValueError("expected contiguous int32 targets [M] on the current device")
-    # one allocation: each part on a 16-byte boundary
-    pad = -(-M // 4) * 4
-    part = -(-M * k // 4) * 4
-    buf = _new(stream, (2 * pad + 2 * part,), torch.float32, logits.device)
-    at = buf.data_ptr()
+    f32 = torch.float32
+    logp = None if targets is None else _new(stream, (M,), f32, logits)
+    h = _new(stream, (M,), f32, logits) if entropy else None
+    index = _new(stream, (M, k), torch.int32, logits) if k else None
+    score = _new(stream, (M, k), f32, logits) if k else None
     _check("w4a16_log_probs", lib().w4a16_log_probs(
-        logits.data_ptr(), 16 if logits.dtype == torch.bfloat16 else 32, M, V, stride, _ptr(targets), k,
-        None if targets is None else at, at + 4 * pad if entropy else None, at + 8 * pad if k else None,
-        at + 8 * pad + 4 * part if k else None, _stream(stream)))
-    if k:
-        begin = 2 * pad
-        index = buf[begin:begin + M * k].view(torch.int32).view(M, k)
-        score = buf[begin + part:begin + part + M * k].view(M, k)
-    else:
-        index = score = None
-    return (None if targets is None else buf[:M], buf[pad:pad + M] if entropy else None, index, score)
+        logits.data_ptr(), 16 if bf16 else 32, M, V, logits.stride(0) if M > 1 else V, _ptr(targets), k, _ptr(logp),
+        _ptr(h), _ptr(index), _ptr(score), _stream_on(stream, device)))
+    return logp, h, index, score
 
 
 def add_adapters(base: torch.Tensor, x: torch.Tensor, A: torch.Tensor, B: torch.Tensor, scale: torch.Tensor,
@@ -671,37 +683,31 @@ def add_adapters(base: torch.Tensor, x: torch.Tensor, A: torch.Tensor, B: torch.
     M, K = x.shape
     N = base.shape[1]
     pool, R = A.shape[0], A.shape[1]
-    bf16 = torch.bfloat16
-    if not (_fits(x, bf16, M, K) and _fits(base, bf16, M, N) and _fits(A, bf16, pool, R, K)
-            and _fits(B, bf16, pool, N, R) and _fits(scale, torch.float32, pool)):
+    bf16, device = torch.bfloat16, _device_of(x)
+    if not (_fits(x, bf16, (M, K), device) and _fits(base, bf16, (M, N), device)
+            and _fits(A, bf16, (pool, R, K), device) and _fits(B, bf16, (pool, N, R), device)
+            and _fits(scale, torch.float32, (pool,), device)):
         raise ValueError("expected contiguous bf16 x [M, K], base [M, N], A [pool, R, K], B [pool, N, R] and fp32 "
                          "scale [pool] on the current device")
-    nseq = _rotary_lists(M, seq_start, adapters)
+    nseq = _sequences(M, seq_start, adapters, device)
     if workspace is None:
-        workspace = _new(stream, (adapters_workspace_bytes(M, nseq, K, R),), torch.uint8, x.device)
-    elif not (workspace.is_cuda and workspace.is_contiguous()
-              and workspace.numel() * workspace.element_size() >= adapters_workspace_bytes(M, nseq, K, R)):
+        workspace = _new(stream, (M, R), bf16, x)
+    elif not (workspace.get_device() == device and workspace.is_contiguous()
+              and workspace.numel() * workspace.element_size() >= adapters_workspace_bytes(M, R)):
         raise ValueError("expected a workspace of adapters_workspace_bytes")
     if out is None:
-        out = _new(stream, (M, N), bf16, x.device)
-    elif not _fits(out, bf16, M, N):
+        out = _new(stream, (M, N), bf16, x)
+    elif not _fits(out, bf16, (M, N), device):
         raise ValueError("expected a contiguous bf16 out [M, N] on the current device")
     _check("w4a16_add_adapters", lib().w4a16_add_adapters(
         x.data_ptr(), A.data_ptr(), B.data_ptr(), scale.data_ptr(), pool, _ptr(seq_start), adapters.data_ptr(),
-        nseq, M, N, K, R, base.data_ptr(), out.data_ptr(), workspace.data_ptr(), _stream(stream)))
+        nseq, M, N, K, R, base.data_ptr(), out.data_ptr(), workspace.data_ptr(), _stream_on(stream, device)))
     return out
 
 
-def adapters_workspace_bytes(M: int, nseq: int, K: int, R: int) -> int:
-    """Bytes of a workspace for add_adapters on the current device."""
-    return _adapters_workspace_bytes(torch.cuda.current_device(), M, nseq, K, R)
-
-
-@functools.lru_cache(maxsize=4096)
-def _adapters_workspace_bytes(device: int, M: int, nseq: int, K: int, R: int) -> int:
-    size = ctypes.c_int64()
-    _check("w4a16_add_adapters_workspace", lib().w4a16_add_adapters_workspace(M, nseq, K, R, ctypes.byref(size)))
-    return size.value
+def adapters_workspace_bytes(M: int, R: int) -> int:
+    """Bytes of a workspace for add_adapters; 0 for sizes that are not supported."""
+    return lib().w4a16_add_adapters_workspace(M, R)
 
 
 def selftest_wait_timeout(limit_ns: int, stream=None) -> None:

@@ -88,7 +88,7 @@ def test_in_place_and_workspaces():
         ids = [i % 4 for i in range(M if starts is None else 3)]
         want = check(given, ids, starts)
         seq = None if starts is None else i32(starts)
-        w = torch.full((W.adapters_workspace_bytes(M, len(ids), 256, 16) // 4,), float("nan"), device="cuda")
+        w = torch.full((W.adapters_workspace_bytes(M, 16) // 4,), float("nan"), device="cuda")
         out = torch.full_like(want, 7)
         got = W.add_adapters(**given, adapters=i32(ids), seq_start=seq, workspace=w, out=out)
         assert got is out and torch.equal(out, want)

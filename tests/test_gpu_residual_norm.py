@@ -85,7 +85,7 @@ def check(given, layer=False, eps=EPS, offset=1.0, scale=1.0, **more):
     return out, h
 
 
-WIDTHS = [1, 7, 8, 64, 100, 255, 256, 1000, 1016, 1024, 1025, 1032, 2047, 4096, 8193, 12288, 16392, 24560, 32768, 32776, 49152]
+WIDTHS = [1, 7, 8, 64, 100, 255, 256, 1000, 1016, 1024, 1025, 1032, 2047, 4096, 8193, 12288, 16392, 24560, 32768, 32775, 49151, 49152]
 
 
 @pytest.mark.parametrize("D", WIDTHS)

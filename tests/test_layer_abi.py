@@ -39,7 +39,7 @@ NORM = dict(residual=A, bits=16, block=2 * A, gate=3 * A, gate_rows=1, post_weig
     (dict(scale=math.inf), BAD), (dict(scale=math.nan), BAD), (dict(offset=math.nan), BAD),
     (dict(residual_out=None, out=None), BAD), (dict(block=None), BAD), (dict(block=None, gate=None), BAD),
     (dict(post_weight=None), BAD), (dict(out=None), BAD),
-    (dict(M=1 << 31), UNSUPPORTED), (dict(D=49160), UNSUPPORTED), (dict(D=24561), UNSUPPORTED), (dict(D=24562), UNSUPPORTED),
+    (dict(M=1 << 31), UNSUPPORTED), (dict(D=49153), UNSUPPORTED),
     *((dict([(n, NORM[n] + 8)]), ALIGNMENT) for n in ("residual", "block", "gate", "post_weight", "post_bias", "weight",
                                                      "bias", "residual_out", "out")),
     (dict(residual_out=A + 16), BAD), (dict(out=A + 16), BAD), (dict(out=A), BAD), (dict(out=8 * A + 16), BAD),
@@ -114,19 +114,17 @@ ADAPTERS = dict(x=A, a=2 * A, b=3 * A, scale=4 * A, pool=3, seq_start=5 * A, ids
     (dict(seq_start=None), BAD), (dict(pool=0), BAD), (dict(nseq=0), BAD), (dict(M=0), BAD), (dict(N=0), BAD),
     (dict(K=0), BAD), (dict(R=0), BAD), (dict(K=100), UNSUPPORTED), (dict(K=32), UNSUPPORTED), (dict(R=12), UNSUPPORTED),
     *((dict([(n, ADAPTERS[n] + 8)]), ALIGNMENT) for n in ("x", "a", "b", "scale", "seq_start", "ids", "base", "out", "workspace")),
-    (dict(out=A + 16), BAD), (dict(out=7 * A + 16), BAD), (dict(workspace=8 * A + 1008), BAD), (dict(out=3 * A), BAD),
+    (dict(out=A + 16), BAD), (dict(out=7 * A + 16), BAD), (dict(workspace=8 * A + 1984), BAD), (dict(out=3 * A), BAD),
     (dict(workspace=6 * A), BAD), (dict(R=72), UNSUPPORTED), (dict(M=1 << 26), UNSUPPORTED), (dict(N=1 << 26), UNSUPPORTED), (dict(pool=1 << 26), UNSUPPORTED),
 ])
 def test_adapters_arguments(L, change, want):
     assert call(L.w4a16_add_adapters, ADAPTERS, change) == want
 
 
-def test_adapters_workspace_arguments(L):
-    n = ctypes.c_int64()
-    assert L.w4a16_add_adapters_workspace(4, 4, 128, 16, None) == BAD
-    assert L.w4a16_add_adapters_workspace(0, 4, 128, 16, ctypes.byref(n)) == BAD
-    assert L.w4a16_add_adapters_workspace(4, 4, 100, 16, ctypes.byref(n)) == UNSUPPORTED
-    assert L.w4a16_add_adapters_workspace(4, 4, 128, 80, ctypes.byref(n)) == UNSUPPORTED
+def test_adapters_workspace(L):
+    assert L.w4a16_add_adapters_workspace(4, 16) == 128
+    for M, R in ((0, 16), (4, 0), (4, 12), (4, 72), (1 << 26, 16)):
+        assert L.w4a16_add_adapters_workspace(M, R) == 0
 
 
 @pytest.mark.parametrize("change,want", [
