@@ -1,15 +1,18 @@
 // Low-rank adapters of many sequences beside a shared projection:
 //   out = base + t B_a^T,  t = scale_a (x A_a^T),  a the adapter of the row's sequence.
 //
-// Two kernels.  The first reads x and gives t: warp-level MMAs with the adapter's rows as the 16-row
-// operand and eight tokens as columns, K split over warps and over the CTAs of a cluster, whose fp32
-// sums are added up in order through distributed shared memory; t is rounded to bf16 (2^-8 of each, of an
-// update beside a sum that a bf16 store rounds as much) into the workspace.  The second streams base and
+// Two kernels.  The first reads x and gives t.  Long sequences: 128 tokens of x and the tile's adapters by
+// TMA into a ring of stages, tcgen05 MMAs (tokens as rows, an adapter's rank as columns) into tensor memory.
+// Short ones: warp-level MMAs with the adapter's rows as the 16-row operand and eight tokens as columns.
+// K is split over the CTAs of a cluster, whose fp32 sums are added up in order through distributed shared
+// memory; t is rounded to bf16 (2^-8 of each, of an update beside a sum that a bf16 store rounds as much)
+// into the workspace.  The second streams base and
 // out, with tokens as rows and 32 features as columns of its MMAs, arranged so that a thread has eight
 // neighbours: the accumulators begin as base and are stored as out, 16 bytes a thread.
 // Rows of a tile that share an adapter are done together; x is zero in the others' columns.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
+#include <algorithm>
 #include <cstdint>
 #include <type_traits>
 
@@ -36,17 +39,18 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                          uint32_t b1) {
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
         "{%0, %1, %2, %3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// The rows of a tile: each one's adapter, and the list of those that occur.
+// The rows of a tile: each one's adapter, the list of those that occur, and each row's place in it (-1: no
+// adapter).
 template <int ROWS>
 struct Tile {
     int id[ROWS];
+    int slot[ROWS];
     int list[ROWS];
     int count;
 };
@@ -132,43 +136,31 @@ __device__ __forceinline__ void find_adapters(Tile<ROWS>& tile, const AdapterPar
         if (lane == 0) tile.count = n;
     }
     __syncthreads();
+    if (t < ROWS) {
+        int slot = -1;
+        if (tile.id[t] >= 0)
+            for (slot = 0; slot < tile.count - 1 && tile.list[slot] != tile.id[t]; ++slot) {}  // (it is in the list)
+        tile.slot[t] = slot;
+    }
+    __syncthreads();
 }
 
 __device__ __forceinline__ uint4 load16(const uint16_t* p) { return __ldg(reinterpret_cast<const uint4*>(p)); }
-
-__device__ __forceinline__ void copy_async16(uint32_t to, const void* from) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
-}
-__device__ __forceinline__ void store_shared_zero16(uint32_t at) {
-    asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0) : "memory");
-}
-__device__ __forceinline__ void copy_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copy_async_wait() {
-    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
-__device__ __forceinline__ uint4 load_shared16(uint32_t at) {
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
-    return v;
-}
 
 // 32 k of 16 MT rows of an adapter with eight tokens: a lane has 16 bytes of its rows g and g + 8 of
 // each 16 and of its token g, of which each MMA takes half; the order of k is the same on both sides.
 template <int MT>
 __device__ __forceinline__ void mma_step(float (&acc)[MT][4], const uint4 (&a)[MT][2], const uint4& x) {
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-        mma_bf16(acc[i], a[i][0].x, a[i][1].x, a[i][0].y, a[i][1].y, x.x, x.y);
-        mma_bf16(acc[i], a[i][0].z, a[i][1].z, a[i][0].w, a[i][1].w, x.z, x.w);
-    }
+    for (int i = 0; i < MT; ++i) mma_bf16(acc[i], a[i][0].x, a[i][1].x, a[i][0].y, a[i][1].y, x.x, x.y);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) mma_bf16(acc[i], a[i][0].z, a[i][1].z, a[i][0].w, a[i][1].w, x.z, x.w);
 }
 
-// A slice of K for a split: steps of 32.
+// This CTA's slice of the steps that K takes.
 struct Slice {
     int from, to;
-    __device__ __forceinline__ explicit Slice(int K) {
-        const int64_t steps = K / 32;
+    __device__ __forceinline__ explicit Slice(int64_t steps) {
         from = static_cast<int>(steps * blockIdx.y / gridDim.y);
         to = static_cast<int>(steps * (blockIdx.y + 1) / gridDim.y);
     }
@@ -180,27 +172,29 @@ __device__ __forceinline__ float load_cluster(uint32_t at) {
     return v;
 }
 
-// The warps' sums [WARPS][ROWS][16 MT + 4] added up, in order, then those of the cluster's CTAs (gridDim.y
-// of them), for the tokens with the adapter.  All threads; the sums may be overwritten after it.
-template <int WARPS, int ROWS, int MT>
-__device__ __forceinline__ void store_t(float* sums, const Tile<ROWS>& tile, const AdapterParams& p, int64_t m0, int a) {
+// PARTS sums [ROWS][16 MT + 4] added up, in order, then those of the cluster's CTAs (gridDim.y of them), for
+// the tokens of the adapters first .. last - 1 of the tile's list.  All threads; the sums may be overwritten
+// after it.
+template <int THREADS, int PARTS, int ROWS, int MT>
+__device__ __forceinline__ void store_t(float* sums, const Tile<ROWS>& tile, const AdapterParams& p, int64_t m0, int first,
+                                        int last) {
     constexpr int kPitch = 16 * MT + 4, kAll = ROWS * 16 * MT;
     const int ctas = static_cast<int>(gridDim.y);
     __syncthreads();
-    for (int i = threadIdx.x; i < kAll; i += WARPS * 32) {
-        float* const at = sums + i / (16 * MT) * kPitch + i % (16 * MT);
-        float sum = at[0];
+    if constexpr (PARTS > 1)
+        for (int i = threadIdx.x; i < kAll; i += THREADS) {
+            float* const at = sums + i / (16 * MT) * kPitch + i % (16 * MT);
+            float sum = at[0];
 #pragma unroll
-        for (int w = 1; w < WARPS; ++w) sum += at[w * ROWS * kPitch];
-        at[0] = sum;
-    }
-    if (ctas > 1) cluster_sync(); else __syncthreads();
+            for (int w = 1; w < PARTS; ++w) sum += at[w * ROWS * kPitch];
+            at[0] = sum;
+        }
+    if (ctas > 1) cluster_sync(); else if (PARTS > 1) __syncthreads();
     // each CTA adds up a part of the tokens
-    const float scale = p.scale[a];
     uint16_t* const out = p.t + m0 * p.R;
-    for (int i = blockIdx.y * (WARPS * 32) + threadIdx.x; i < kAll; i += ctas * WARPS * 32) {
-        const int token = i / (16 * MT), r = i % (16 * MT);
-        if (tile.id[token] != a || r >= p.R) continue;
+    for (int i = blockIdx.y * THREADS + threadIdx.x; i < kAll; i += ctas * THREADS) {
+        const int token = i / (16 * MT), r = i % (16 * MT), slot = tile.slot[token];
+        if (slot < first || slot >= last || r >= p.R) continue;
         const float* const at = sums + token * kPitch + r;
         float sum = 0.0f;
         if (ctas > 1) {
@@ -209,91 +203,172 @@ __device__ __forceinline__ void store_t(float* sums, const Tile<ROWS>& tile, con
         } else {
             sum = at[0];
         }
-        out[static_cast<int64_t>(token) * p.R + r] = __bfloat16_as_ushort(__float2bfloat16_rn(sum * scale));
+        out[static_cast<int64_t>(token) * p.R + r] =
+            __bfloat16_as_ushort(__float2bfloat16_rn(sum * p.scale[tile.id[token]]));
     }
     if (ctas > 1) cluster_sync(); else __syncthreads();
 }
 
-// t of 64 tokens (blockIdx.x) over a slice of K (blockIdx.y), for each of the tile's adapters; K between
-// the warps.  What a lane needs of x and of the adapter it copies itself, kStages steps ahead, into its
-// own places of shared memory: no barrier, and 96 KB an SM under way.
-constexpr int kDownWarps = 4;
+// D[tmem] (+)= A[smem] * B[smem]^T, kind::f16 (bf16 inputs, fp32 accumulator).
+__device__ __forceinline__ void tc_mma_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                          uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
+// t of 128 tokens (blockIdx.x) over a slice of K (blockIdx.y), for up to kGroup of the tile's adapters at
+// once.  A stage of the ring: 64 k of the tokens, and of each adapter's rank (rounded up to 16: what the
+// last rows hold is another adapter's, and not looked at).  Warps 0 to 3 take the sums out of tensor
+// memory, one thread of warp 4 copies, one of warp 5 issues the MMAs.
+constexpr int kTcRows = 128, kTcThreads = 192;
 template <int MT>
-constexpr int kStages = MT == 4 ? 3 : 4;
+struct TcLayout {
+    static constexpr int kRank = 16 * MT, kGroup = MT <= 2 ? 4 : 2;
+    static constexpr int kTokens = kTcRows * 128, kAdapter = kRank * 128;  // bytes
+    static constexpr int kStage = kTokens + kGroup * kAdapter, kStages = MT == 1 ? 4 : 3;
+    static constexpr int kColumns = kGroup * kRank <= 64 ? 64 : 128;       // of tensor memory
+    static constexpr int kSums = kTcRows * (kRank + 4) * 4;
+    static constexpr int kSmem = kStages * kStage + 1024;                  // (the ring begins on 1024 bytes)
+    static_assert(kSums <= kStages * kStage, "the sums take the ring's place");
+};
 
 template <int MT>
-__global__ void __launch_bounds__(kDownWarps * 32, 2) adapters_down_kernel(const AdapterParams p) {
-    constexpr int kRows = 64, NB = kRows / 8, ST = kStages<MT>, kPieces = NB + 2 * MT;
-    __shared__ Tile<kRows> tile;
-    extern __shared__ __align__(16) uint8_t ring[];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
-    const int64_t m0 = static_cast<int64_t>(blockIdx.x) * kRows;
-    grid_launch_dependents();
-    grid_wait();
-    find_adapters<kRows>(tile, p, m0, blockIdx.y == 0);
-    if (p.seq_start != nullptr && blockIdx.y == 0) check_starts(p.seq_start, p.nseq, p.M, p.status);
-    const Slice k(p.K);
-    const uint32_t mine_at = smem_u32(ring) + (warp * ST * kPieces * 32 + lane) * 16;
-    for (int l = 0; l < tile.count; ++l) {
-        const int a = tile.list[l];
-        uint32_t mine = 0;  // blocks in which this lane's token has the adapter
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) mine |= static_cast<uint32_t>(tile.id[nb * 8 + g] == a) << nb;
-        const uint32_t any = __reduce_or_sync(0xffffffffu, mine);
-        // the places of rows that are not copied hold zeros
-        for (int stage = 0; stage < ST; ++stage)
-#pragma unroll
-            for (int i = 0; i < kPieces; ++i)
-                if (i < NB ? !(mine >> i & 1u) : (i - NB) * 8 + g >= p.R)
-                    store_shared_zero16(mine_at + (stage * kPieces + i) * 512);
-        const uint8_t* const x = reinterpret_cast<const uint8_t*>(p.x + (m0 + g) * p.K + 8 * q);
-        const uint8_t* const w =
-            reinterpret_cast<const uint8_t*>(p.a + (static_cast<int64_t>(a) * p.R + g) * p.K + 8 * q);
-        const uint32_t rows8 = 16u * static_cast<uint32_t>(p.K);  // bytes of eight rows (K < 2^25)
-        auto fetch = [&](int stage, int s) {
-            if (s < k.to) {
-                const uint32_t at = mine_at + stage * (kPieces * 512);
-                const uint8_t* const xs = x + static_cast<int64_t>(s) * 64;
-                const uint8_t* const ws = w + static_cast<int64_t>(s) * 64;
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb)
-                    if (mine >> nb & 1u) copy_async16(at + nb * 512, xs + rows8 * nb);
-#pragma unroll
-                for (int i = 0; i < 2 * MT; ++i)
-                    if (i * 8 + g < p.R) copy_async16(at + (NB + i) * 512, ws + rows8 * i);
-            }
-            copy_async_commit();
-        };
-        float acc[NB][MT][4] = {};
-        int s = k.from + warp;
-#pragma unroll
-        for (int i = 0; i < ST - 1; ++i) fetch(i, s + i * kDownWarps);
-        for (int stage = 0; s < k.to; s += kDownWarps) {
-            copy_async_wait<ST - 2>();
-            const uint32_t at = mine_at + stage * (kPieces * 512);
-            uint4 av[MT][2];
-#pragma unroll
-            for (int i = 0; i < 2 * MT; ++i) av[i / 2][i % 2] = load_shared16(at + (NB + i) * 512);
-            // (its place was read a turn ago)
-            fetch(stage == 0 ? ST - 1 : stage - 1, s + (ST - 1) * kDownWarps);
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
-                if (any >> nb & 1u) mma_step<MT>(acc[nb], av, load_shared16(at + nb * 512));
-            stage = stage == ST - 1 ? 0 : stage + 1;
+__global__ void __launch_bounds__(kTcThreads, 2)
+    adapters_down_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_a,
+                         const AdapterParams p) {
+    using L = TcLayout<MT>;
+    __shared__ Tile<kTcRows> tile;
+    __shared__ __align__(8) uint64_t full[L::kStages], empty[L::kStages], done, drain;
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_flag;
+    extern __shared__ uint8_t dynamic[];
+    const uint32_t ring = (smem_u32(dynamic) + 1023u) & ~1023u;
+    float* const sums = reinterpret_cast<float*>(dynamic + (ring - smem_u32(dynamic)));
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t m0 = static_cast<int64_t>(blockIdx.x) * kTcRows;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < L::kStages; ++i) {
+            mbar_init(smem_u32(&full[i]), 1);
+            mbar_init(smem_u32(&empty[i]), 1);
         }
-        copy_async_wait<0>();
-        __syncthreads();
-        float* const sums = reinterpret_cast<float*>(ring);
-        constexpr int kPitch = 16 * MT + 4;
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    sums[(warp * kRows + nb * 8 + 2 * q + (e & 1)) * kPitch + i * 16 + g + (e & 2) * 4] = acc[nb][i][e];
-        store_t<kDownWarps, kRows, MT>(sums, tile, p, m0, a);
+        mbar_init(smem_u32(&done), 1);
+        mbar_init(smem_u32(&drain), 1);
+        abort_flag = 0;
+        fence_mbar_init();
     }
+    if (warp == 5) {
+        tmem_alloc(smem_u32(&tmem_slot), L::kColumns);
+        tmem_relinquish();
+    }
+    grid_wait();
+    find_adapters<kTcRows>(tile, p, m0, blockIdx.y == 0);
+    if (p.seq_start != nullptr && blockIdx.y == 0) check_starts(p.seq_start, p.nseq, p.M, p.status);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+    const Slice k(p.K / 64);
+    uint32_t it = 0;    // stages so far
+    bool alive = true;  // no wait of this CTA ran out: else only the cluster's barriers are kept
+    for (int l = 0, turn = 0; l < tile.count; l += L::kGroup, ++turn) {
+        const int n = min(L::kGroup, tile.count - l);
+        bool ok = true;
+        if (alive && warp == 4) {
+            if (lane == 0) {
+                for (int s = k.from; s < k.to; ++s, ++it) {
+                    const uint32_t stage = it % L::kStages, at = ring + stage * L::kStage, bar = smem_u32(&full[stage]);
+                    if (it >= L::kStages && !wait_one(smem_u32(&empty[stage]), (it / L::kStages - 1) & 1u, &abort_flag,
+                                                      p.status, p.wait_ns)) {
+                        ok = false;
+                        break;
+                    }
+                    mbar_arrive_expect_tx(bar, L::kTokens + n * L::kAdapter);
+                    tma_load_2d(at, &map_x, bar, s * 64, static_cast<int32_t>(m0));
+                    for (int i = 0; i < n; ++i)
+                        tma_load_2d(at + L::kTokens + i * L::kAdapter, &map_a, bar, s * 64, tile.list[l + i] * p.R);
+                    if (it == 0 && !short_limit_ok(bar, 0, &abort_flag, p.status, p.wait_ns)) {
+                        ++it;
+                        ok = false;
+                        break;
+                    }
+                }
+                if (!ok)  // its copies land before the CTA goes on
+                    for (uint32_t i = it > L::kStages ? it - L::kStages : 0; i < it; ++i)
+                        settle(smem_u32(&full[i % L::kStages]), (i / L::kStages) & 1u);
+            }
+            __syncwarp();
+            it = __shfl_sync(0xffffffffu, it, 0);
+        } else if (alive && warp == 5) {
+            constexpr uint32_t kIdesc = idesc_bf16_f32(kTcRows, L::kRank);
+            for (int s = k.from; s < k.to; ++s, ++it) {
+                const uint32_t stage = it % L::kStages, at = ring + stage * L::kStage;
+                if (!wait_warp(smem_u32(&full[stage]), (it / L::kStages) & 1u, &abort_flag, p.status, p.wait_ns)) {
+                    ok = false;
+                    break;
+                }
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint64_t x = sdesc_kmajor_sw128(at);
+#pragma unroll
+                    for (int kk = 0; kk < 4; ++kk)  // 16 k: 32 bytes
+                        for (int i = 0; i < n; ++i)
+                            tc_mma_ss(tmem + i * L::kRank, x + 2 * kk,
+                                      sdesc_kmajor_sw128(at + L::kTokens + i * L::kAdapter) + 2 * kk, kIdesc,
+                                      s > k.from || kk > 0);
+                    tc_commit(smem_u32(&empty[stage]));
+                }
+                __syncwarp();
+            }
+            if (elect_one()) {
+                if (ok) {
+                    tc_commit(smem_u32(&done));
+                } else {
+                    tc_commit(smem_u32(&drain));
+                    settle(smem_u32(&drain), 0);
+                }
+            }
+            __syncwarp();
+        } else if (alive && warp < 4) {
+            ok = wait_warp<false, 64>(smem_u32(&done), turn & 1, &abort_flag, p.status, p.wait_ns);
+            if (ok) {
+                tc_fence_after();
+                const int token = warp * 32 + lane, mine = tile.slot[token] - l;
+                for (int i = 0; i < n; ++i)
+#pragma unroll
+                    for (int c = 0; c < MT; ++c) {
+                        uint32_t v[16];
+                        tmem_ld_32x32b_x16(tmem + (static_cast<uint32_t>(warp * 32) << 16) + i * L::kRank + c * 16, v);
+                        tmem_ld_wait_x16(v);
+                        if (mine == i) {
+                            float4* const to = reinterpret_cast<float4*>(sums + token * (L::kRank + 4) + c * 16);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                to[e] = make_float4(__uint_as_float(v[4 * e]), __uint_as_float(v[4 * e + 1]),
+                                                    __uint_as_float(v[4 * e + 2]), __uint_as_float(v[4 * e + 3]));
+                        }
+                    }
+                tc_fence_before();
+            }
+        }
+        alive = !__syncthreads_or(alive && !ok) && alive;
+        store_t<kTcThreads, 1, kTcRows, MT>(sums, tile, p, m0, l, l + n);
+        // (the next copies into the ring come behind what was read and written here)
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        tc_fence_before();
+        __syncthreads();
+        tc_fence_after();
+    }
+    // (not before: the second kernel's CTAs would come to wait beside these, on SMs whose shared memory is laid out
+    // for the ring, and run there by a few an SM: 39004 rows 654 us, 467 so)
+    grid_launch_dependents();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 5) tmem_dealloc(tmem, L::kColumns);
 }
 
 // The same for short sequences: 8 tokens (blockIdx.x), one of the tile's adapters (blockIdx.z), a slice of
@@ -310,7 +385,7 @@ __global__ void __launch_bounds__(kThreads) adapters_down_few_kernel(const Adapt
     grid_wait();
     find_adapters<kRows>(tile, p, m0, blockIdx.y == 0 && blockIdx.z == 0);
     if (p.seq_start != nullptr && blockIdx.y == 0 && blockIdx.z == 0) check_starts(p.seq_start, p.nseq, p.M, p.status);
-    const Slice k(p.K);
+    const Slice k(p.K / 32);
     for (int l = blockIdx.z; l < tile.count; l += gridDim.z) {
         const int a = tile.list[l];
         const bool mine = tile.id[g] == a;
@@ -339,7 +414,7 @@ __global__ void __launch_bounds__(kThreads) adapters_down_few_kernel(const Adapt
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 sums[(warp * kRows + 2 * q + (e & 1)) * kPitch + i * 16 + g + (e & 2) * 4] = acc[i][e];
-        store_t<kWarps, kRows, MT>(sums, tile, p, m0, a);
+        store_t<kThreads, kWarps, kRows, MT>(sums, tile, p, m0, l, l + 1);
     }
 }
 
@@ -388,7 +463,7 @@ struct UpFragments {
 // adapters blockIdx.z, + gridDim.z, ...; a warp has FB blocks under way.  MB: 16s of tokens; 0: eight, in
 // the upper half of one.  EXACT: the rank is 16 or 32 CH.  WHOLE: rows of 16-byte units.
 template <int CH, int MB, int FB, bool EXACT, bool WHOLE>
-__global__ void __launch_bounds__(kThreads, !WHOLE || CH == 2 ? 1 : CH == 0 && MB == 0 ? 3 : 2)
+__global__ void __launch_bounds__(kThreads, !WHOLE ? 1 : CH == 0 && MB == 0 ? 3 : 2)
     adapters_up_kernel(const AdapterParams p, const int chunk) {
     constexpr int kRows = MB == 0 ? 8 : 16 * MB, kHalves = MB == 0 ? 1 : 2 * MB;  // rows of a lane
     constexpr int kWords = CH == 0 ? 8 : 16 * CH, kPitch = kWords + 4;            // (pairs of bf16)
@@ -429,10 +504,10 @@ __global__ void __launch_bounds__(kThreads, !WHOLE || CH == 2 ? 1 : CH == 0 && M
         // are then its eight neighbours
         const uint16_t* const b_rows = p.b + static_cast<int64_t>(a < 0 ? 0 : a) * p.N * R;
         const int feature = (g >> 1) * 8 + (g & 1);
-        // `blocks` blocks from f on: FB with every column there, or one that is checked
-        auto batch = [&](int f, auto blocks) __attribute__((always_inline)) {
-            constexpr int NB = decltype(blocks)::value;
-            constexpr bool kInside = NB == FB && FB > 1;
+        // blocks from f on: FB with every column there, or one that is checked
+        auto batch = [&](int f, auto inside) __attribute__((always_inline)) {
+            constexpr bool kInside = decltype(inside)::value;
+            constexpr int NB = kInside ? FB : 1;
             uint4 c[NB][kHalves];
             const int n0 = f * 32 + 8 * q;
 #pragma unroll
@@ -507,11 +582,11 @@ __global__ void __launch_bounds__(kThreads, !WHOLE || CH == 2 ? 1 : CH == 0 && M
             }
         };
         for (int f = first + FB * warp; f < last; f += FB * kWarps) {
-            if (FB > 1 && (f + FB) * 32 <= columns) {
-                batch(f, std::integral_constant<int, FB>{});
+            if ((f + FB) * 32 <= columns) {
+                batch(f, std::true_type{});
             } else {
 #pragma unroll 1
-                for (int u = f; u < min(f + FB, last); ++u) batch(u, std::integral_constant<int, 1>{});
+                for (int u = f; u < min(f + FB, last); ++u) batch(u, std::false_type{});
             }
         }
     }
@@ -522,19 +597,30 @@ bool short_sequences(int64_t M, int64_t nseq) { return M < 16 * nseq; }
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// CTAs of a cluster that share K: a power of two up to 16 (8 where adapters are few tokens each: 28.7 against 32.4 us
-// with 64 requests), while that leaves each of them something and SMs
-// would be idle otherwise.
+// CTAs of a cluster that share K: a power of two up to 16.  Few tokens of an adapter each: while there is K for
+// every warp and SMs would be idle (8 at most: 28.7 against 32.4 us with 64 requests).  Tiles of 128 tokens: by the
+// turns that 2 CTAs an SM take, each of its K and some start and end (in steps of 64 k).
 int cluster_of(const AdapterParams& p, bool few, int sm_count) {
-    const int64_t ctas = few ? ceil_div(p.M, 8) * (p.M < 8 ? p.M : 8) : ceil_div(p.M, 64);
-    const int64_t least = few ? kWarps * 32 : kDownWarps * 128;  // of K
     int s = 1;
-    while (s < (few ? 8 : 16) && s * ctas < 4 * sm_count && 2 * s * least <= p.K) s *= 2;
+    if (few) {
+        const int64_t ctas = ceil_div(p.M, 8) * (p.M < 8 ? p.M : 8);
+        while (s < 8 && s * ctas < 4 * sm_count && 2 * s * kWarps * 32 <= p.K) s *= 2;
+        return s;
+    }
+    const int64_t tiles = ceil_div(p.M, kTcRows), steps = p.K / 64;
+    int64_t least = -1;
+    for (int c = 1; c <= 16 && c <= steps; c *= 2) {
+        const int64_t cost = ceil_div(tiles * c, 2 * sm_count) * (ceil_div(steps, c) + 8);
+        if (least < 0 || cost < least) {
+            least = cost;
+            s = c;
+        }
+    }
     return s;
 }
 
-template <typename Kernel>
-cudaError_t launch_cluster(Kernel kernel, dim3 grid, int block, int smem, cudaStream_t stream, const AdapterParams& p) {
+template <typename... P, typename... A>
+cudaError_t launch_cluster(void (*kernel)(P...), dim3 grid, int block, int smem, cudaStream_t stream, const A&... args) {
     cudaError_t e = cudaSuccess;
     if (smem > 0) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e == cudaSuccess && grid.y > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
@@ -552,7 +638,7 @@ cudaError_t launch_cluster(Kernel kernel, dim3 grid, int block, int smem, cudaSt
     attr[1].val.clusterDim.y = grid.y;
     cfg.attrs = attr;
     cfg.numAttrs = grid.y > 1 ? 2 : 1;
-    e = cudaLaunchKernelEx(&cfg, kernel, p);
+    e = cudaLaunchKernelEx(&cfg, kernel, P(args)...);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
@@ -562,26 +648,29 @@ cudaError_t launch_down(const AdapterParams& p, bool few, int sm_count, cudaStre
     if (few)
         return launch_cluster(adapters_down_few_kernel<MT>, dim3((p.M + 7) / 8, ctas, p.M < 8 ? p.M : 8), kThreads, 0,
                               stream, p);
-    constexpr int kRing = kDownWarps * kStages<MT> * (8 + 2 * MT) * 512;
-    constexpr int kSums = kDownWarps * 64 * (16 * MT + 4) * 4;
-    return launch_cluster(adapters_down_kernel<MT>, dim3((p.M + 63) / 64, ctas), kDownWarps * 32,
-                          kRing > kSums ? kRing : kSums, stream, p);
+    alignas(64) CUtensorMap x, a;
+    if (encode_rows(&x, p.x, p.K, p.M, kTcRows) != 0 ||
+        encode_rows(&a, p.a, p.K, static_cast<int64_t>(p.pool) * p.R, TcLayout<MT>::kRank) != 0)
+        return cudaErrorInvalidValue;
+    return launch_cluster(adapters_down_kernel<MT>, dim3((p.M + kTcRows - 1) / kTcRows, ctas), kTcThreads,
+                          TcLayout<MT>::kSmem, stream, x, a, p);
 }
 
 template <int CH, bool EXACT, bool WHOLE>
 cudaError_t launch_up(const AdapterParams& p, bool few, int sm_count, cudaStream_t stream) {
-    constexpr int FB = CH == 2 ? 2 : 4;  // few rows
-    const int rows = few ? 8 : 32, z = few ? (p.M < 8 ? p.M : 8) : 1;
-    const int64_t tiles = ceil_div(p.M, rows) * z, blocks = ceil_div(p.N, 32);
-    // as many features to a CTA as leave every SM several CTAs
-    int64_t y = ceil_div((few ? 4 : 16) * static_cast<int64_t>(sm_count), tiles);
-    const int64_t unit = kWarps * (!WHOLE ? 1 : few ? FB : 2);  // blocks that a CTA has under way
-    const int64_t chunk = ceil_div(ceil_div(blocks, y), unit) * unit;
-    y = ceil_div(blocks, chunk);
-    const dim3 grid(static_cast<unsigned>(ceil_div(p.M, rows)), static_cast<unsigned>(y), z);
-    auto kernel = few ? adapters_up_kernel<CH, 0, WHOLE ? FB : 1, EXACT, WHOLE>
-                      : adapters_up_kernel<CH, 2, WHOLE ? 2 : 1, EXACT, WHOLE>;
-    return launch_overlapped(kernel, grid, kThreads, 0, stream, p, static_cast<int>(chunk));
+    // blocks that a warp has under way
+    constexpr int kFew = !WHOLE || CH == 2 ? 1 : 4, kMany = !WHOLE || CH == 2 ? 1 : 2;
+    const int rows = few ? 8 : 32, z = few ? (p.M < 8 ? p.M : 8) : 1, unit = kWarps * (few ? kFew : kMany);
+    const int64_t tiles = ceil_div(p.M, rows) * z, units = ceil_div(ceil_div(p.N, 32), unit);
+    // Few tokens: the CTAs that are resident, at most, as each starts with four loads in a row.  Many: several
+    // turns of them, but four units each at least.
+    int64_t y = few ? (CH == 0 ? 3 : 2) * static_cast<int64_t>(sm_count) / tiles
+                    : std::min(ceil_div(16 * static_cast<int64_t>(sm_count), tiles), units / 4);
+    if (y < 1) y = 1;
+    const int64_t chunk = ceil_div(units, y);
+    const dim3 grid(static_cast<unsigned>(ceil_div(p.M, rows)), static_cast<unsigned>(ceil_div(units, chunk)), z);
+    auto kernel = few ? adapters_up_kernel<CH, 0, kFew, EXACT, WHOLE> : adapters_up_kernel<CH, 2, kMany, EXACT, WHOLE>;
+    return launch_overlapped(kernel, grid, kThreads, 0, stream, p, static_cast<int>(chunk * unit));
 }
 
 template <int CH>
@@ -600,6 +689,7 @@ cudaError_t launch_adapters(const AdapterParams& p, int sm_count, cudaStream_t s
     const bool few = short_sequences(p.M, p.nseq);
     const cudaError_t e = p.R <= 16   ? launch_down<1>(p, few, sm_count, stream)
                           : p.R <= 32 ? launch_down<2>(p, few, sm_count, stream)
+                          : p.R <= 48 ? launch_down<3>(p, few, sm_count, stream)
                                       : launch_down<4>(p, few, sm_count, stream);
     if (e != cudaSuccess) return e;
     return p.R <= 16   ? launch_up<0>(p, few, sm_count, stream)

@@ -2,6 +2,7 @@
 // TMA descriptor encoding, kernel dispatch and the device status word.
 #include "internal.h"
 #include "kv.h"
+#include "layer.h"
 #include "ptx.cuh"
 #include "w4a16.h"
 
@@ -406,6 +407,11 @@ int library_state(LibraryState* out) {
     if (rc != W4A16_OK) return rc;
     *out = {st->sm_count, st->status};
     return W4A16_OK;
+}
+
+int encode_rows(CUtensorMap* map, const void* base, int64_t columns, int64_t rows, int box_rows) {
+    return encode_2d(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, columns, rows, columns * 2, 64, box_rows,
+                     CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 int encode_5d(CUtensorMap* map, CUtensorMapDataType dtype, const void* base, const uint64_t dims[5],

@@ -2,6 +2,7 @@
 // kv_api.cu hand to the kernel translation units.  Not part of the public ABI.
 #pragma once
 
+#include <cuda.h>
 #include <cuda_runtime.h>
 #include <cstdint>
 
@@ -73,8 +74,11 @@ struct AdapterParams {
     uint16_t* t;               // workspace: scale (x A^T), bf16 [M, R]
     int* status;
     int M, N, K, R, pool, nseq;
+    uint64_t wait_ns;
 };
 constexpr int kAdapterMaxRank = 64;
+// api.cu: a tensor map of bf16 rows, in boxes of 64 columns (128-byte swizzle) and box_rows rows
+int encode_rows(CUtensorMap* map, const void* base, int64_t columns, int64_t rows, int box_rows);
 int64_t adapters_workspace_bytes(int64_t M, int64_t R);
 cudaError_t launch_adapters(const AdapterParams& p, int sm_count, cudaStream_t stream);
 

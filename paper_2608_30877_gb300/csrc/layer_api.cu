@@ -257,5 +257,6 @@ extern "C" int w4a16_add_adapters(const void* x_bf16, const void* a_bf16, const 
     p.R = static_cast<int>(R);
     p.pool = static_cast<int>(pool);
     p.nseq = static_cast<int>(nseq);
+    p.wait_ns = wait_limit_ns();
     return status_of(launch_adapters(p, st.sm_count, static_cast<cudaStream_t>(stream)));
 }

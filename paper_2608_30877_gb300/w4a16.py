@@ -524,11 +524,11 @@ def _stream_on(stream, device: int) -> int:
 
 
 def _new(stream, shape, dtype, like) -> torch.Tensor:
-    """An output, allocated on the stream that writes it."""
+    """An output, allocated on the stream that writes it.  (torch.empty 1.6 us, new_empty 2.9)"""
     if stream is None:
-        return like.new_empty(shape, dtype=dtype)
+        return torch.empty(shape, dtype=dtype, device=like.device)
     with _allocating_on(stream):
-        return like.new_empty(shape, dtype=dtype)
+        return torch.empty(shape, dtype=dtype, device=like.device)
 
 
 def _ptr(t):
