@@ -483,9 +483,13 @@ __global__ void __launch_bounds__(kThreads, !WHOLE ? 1 : CH == 0 && MB == 0 ? 3 
     const int first = static_cast<int>(blockIdx.y) * chunk, last = min(first + chunk, (p.N + 31) / 32);
     const int columns = min(p.N, last * 32);
     const int R = EXACT ? (CH == 0 ? 16 : 32 * CH) : p.R;
-    UpFragments<CH> tf[kHalves];  // of the lane's rows
+    // the lane's rows of t: in registers, but for the largest ranks
+    constexpr bool kHeld = CH < 2 || MB == 0;
+    UpFragments<CH> tf[kHeld ? kHalves : 1];
+    if constexpr (kHeld) {
 #pragma unroll
-    for (int i = 0; i < kHalves; ++i) tf[i].load_t(t[i * 8 + g], q);
+        for (int i = 0; i < kHalves; ++i) tf[i].load_t(t[i * 8 + g], q);
+    }
     // (rows without an adapter come last: they are copied)
     const int passes = tile.count + (p.out != p.base);
     for (int l = blockIdx.z; l < passes; l += gridDim.z) {
@@ -539,8 +543,14 @@ __global__ void __launch_bounds__(kThreads, !WHOLE ? 1 : CH == 0 && MB == 0 ? 3 
 #pragma unroll
             for (int m = 0; m < (MB == 0 ? 1 : MB); ++m) {
                 if (MB > 1 && !(any >> (2 * m) & 3u)) continue;
-                UpFragments<CH> tb;
-                if (MB == 0) tb.zero(); else tb = tf[MB == 0 ? 0 : 2 * m + 1];
+                UpFragments<CH> ta, tb;
+                if constexpr (!kHeld) {
+                    ta.load_t(t[m * 16 + g], q);
+                    tb.load_t(t[m * 16 + g + 8], q);
+                } else {
+                    ta = tf[2 * m];
+                    if constexpr (MB == 0) tb.zero(); else tb = tf[2 * m + 1];
+                }
 #pragma unroll
                 for (int u = 0; u < NB; ++u) {
                     float acc[4][4];
@@ -557,7 +567,7 @@ __global__ void __launch_bounds__(kThreads, !WHOLE ? 1 : CH == 0 && MB == 0 ? 3 
                         for (int s = 0; s < UpFragments<CH>::kSteps; ++s)
 #pragma unroll
                             for (int j = 0; j < 4; ++j)
-                                mma_bf16(acc[j], tf[2 * m].w[s][0], tb.w[s][0], tf[2 * m].w[s][1], tb.w[s][1],
+                                mma_bf16(acc[j], ta.w[s][0], tb.w[s][0], ta.w[s][1], tb.w[s][1],
                                          b[u][j].w[s][0], b[u][j].w[s][1]);
                     }
                     const int n = n0 + u * 32;

@@ -185,19 +185,19 @@ struct Shared {
     unsigned long long equal[kCandidates];
     int selected[kGroups];                  // groups, ascending
     Sums warp_sums[kWarps], cta_sums[kMaxCluster];
-    int counts[kWarps], digits[256];
+    int counts[32], digits[4][256], found[3];
     uint32_t threshold;
     int low;  // bits that the threshold leaves out
     int num_selected, num_above, num_equal, count;
 };
 
 
-// f(column, key) for the logits of the selected groups.
-// (those of key `least` and more; a unit's others are not looked at one by one)
+// f(column, key) for the logits of the selected groups from key `least` on, and for NaNs.
 template <bool BF16, typename F>
 __device__ __forceinline__ void each_selected(const Shared& sh, const RowOf<BF16>& r, int shift, uint32_t least, const F& f) {
     constexpr int kTogether = 4, N = RowOf<BF16>::N;
     const int total = sh.num_selected << shift;
+    const float bound = value_of(least);  // (0: a NaN, below which nothing is)
     for (int i0 = threadIdx.x; i0 < total; i0 += kThreads * kTogether) {
         uint4 v[kTogether];
         int unit[kTogether];
@@ -209,19 +209,27 @@ __device__ __forceinline__ void each_selected(const Shared& sh, const RowOf<BF16
         }
 #pragma unroll
         for (int j = 0; j < kTogether; ++j) {
-            if (unit[j] >= r.units) continue;
+            const int c0 = unit[j] * N - r.shift;
             float x[N];
+            uint32_t hits = 0;
             if (r.whole(unit[j])) {
                 const uint32_t w[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
-                if (key_of(r.largest(w)) < least) continue;
                 r.unpack(w, x);
-            } else {
-                r.load_part(unit[j], 0.0f, x);
-            }
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const int c = unit[j] * N - r.shift + e;
-                if (static_cast<unsigned>(c) < static_cast<unsigned>(r.V)) f(c, key_of(x[e]));
+                for (int e = 0; e < N; ++e) hits |= x[e] < bound ? 0u : 1u << e;
+            } else if (unit[j] < r.units) {
+                r.load_part(unit[j], 0.0f, x);
+#pragma unroll
+                for (int e = 0; e < N; ++e)
+                    hits |= static_cast<unsigned>(c0 + e) >= static_cast<unsigned>(r.V) || x[e] < bound ? 0u : 1u << e;
+            }
+            // (few: not worth code for each of the columns)
+            for (; hits != 0; hits &= hits - 1) {
+                const int e = __ffs(hits) - 1;
+                float y = x[0];
+#pragma unroll
+                for (int i = 1; i < N; ++i) y = e == i ? x[i] : y;
+                f(c0 + e, key_of(y));
             }
         }
     }
@@ -285,90 +293,104 @@ __device__ __noinline__ void collect_in_order(Shared& sh, const RowOf<BF16>& r, 
     if (lane == 0) sh.num_equal = found < need ? found : need;
 }
 
-// The groups to read again: t (without the keys' low bits), and the list.  All threads; a warp has 128
-// groups.
+// The groups to read again: t (without the keys' low bits), and the list.  All threads; a thread has the
+// groups of its number, that plus 256, ...
 template <bool BF16>
 __device__ __forceinline__ void select_groups(Shared& sh, int groups, int k) {
     constexpr int kMine = kGroups / kThreads;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, first = warp * (32 * kMine) + lane;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tid = threadIdx.x;
     uint32_t key[kMine];
 #pragma unroll
-    for (int j = 0; j < kMine; ++j) key[j] = sh.group_key[first + 32 * j];
+    for (int j = 0; j < kMine; ++j) key[j] = sh.group_key[tid + kThreads * j];
+    sh.digits[0][tid] = sh.digits[1][tid] = sh.digits[2][tid] = sh.digits[3][tid] = 0;
+    __syncthreads();
     // the largest t that k groups reach, eight bits at a time: the digits of the groups that have t's bits so
-    // far are counted, and each warp adds the counts up from the top
+    // far are counted, and one warp adds the counts up from the top
     int low = 32, above = 0, equal = 0;  // above: groups past t's bits so far
     uint32_t t = 0;
     while (true) {
         low -= 8;
-        for (int i = threadIdx.x; i < 256; i += kThreads) sh.digits[i] = 0;
-        __syncthreads();
+        int* const digits = sh.digits[low >> 3];
 #pragma unroll
-        for (int j = 0; j < kMine; ++j)
-            if (first + 32 * j < groups && (low == 24 || key[j] >> (low + 8) == t))
-                atomicAdd(&sh.digits[key[j] >> low & 255u], 1);
-        __syncthreads();
-        // lane l has the digits 255 - 8 l and below
-        int n[8], sum = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            n[i] = sh.digits[255 - 8 * lane - i];
-            sum += n[i];
-        }
-        int upto = sum;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int y = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += y;
-        }
-        const uint32_t reach = __ballot_sync(0xffffffffu, above + upto >= k);
-        // (fewer than k groups: all of them, from digit 0)
-        const int at = reach != 0 ? __ffs(reach) - 1 : 31;
-        int digit = 255 - 8 * lane, before = above + upto - sum, here = n[0];
-#pragma unroll
-        for (int i = 0; i < 7; ++i)
-            if (digit == 255 - 8 * lane - i && before + n[i] < k) {
-                before += n[i];
-                --digit;
-                here = n[i + 1];
+        for (int j = 0; j < kMine; ++j) {
+            if (kThreads * j >= groups) break;
+            // (one addition for a warp's equal digits: the first ones are nearly all the same)
+            const bool in = tid + kThreads * j < groups && (low == 24 || key[j] >> (low + 8) == t);
+            const uint32_t who = __ballot_sync(0xffffffffu, in), digit = key[j] >> low & 255u;
+            if (in) {
+                const uint32_t same = __match_any_sync(who, digit);
+                if (lane == __ffs(same) - 1) atomicAdd(&digits[digit], __popc(same));
             }
-        digit = __shfl_sync(0xffffffffu, digit, at);
-        above = __shfl_sync(0xffffffffu, before, at);
-        equal = __shfl_sync(0xffffffffu, here, at);
-        t = t << 8 | static_cast<uint32_t>(digit);
+        }
         __syncthreads();
+        if (warp == 0) {  // lane l has the digits 255 - 8 l and below
+            int n[8], sum = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                n[i] = digits[255 - 8 * lane - i];
+                sum += n[i];
+            }
+            int upto = sum;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += y;
+            }
+            const uint32_t reach = __ballot_sync(0xffffffffu, above + upto >= k);
+            // (fewer than k groups: all of them, from digit 0)
+            if (lane == (reach != 0 ? __ffs(reach) - 1 : 31)) {
+                int digit = 255 - 8 * lane, before = above + upto - sum, here = n[0];
+#pragma unroll
+                for (int i = 0; i < 7; ++i)
+                    if (digit == 255 - 8 * lane - i && before + n[i] < k) {
+                        before += n[i];
+                        --digit;
+                        here = n[i + 1];
+                    }
+                sh.found[0] = digit;
+                sh.found[1] = before;
+                sh.found[2] = here;
+            }
+        }
+        __syncthreads();
+        t = t << 8 | static_cast<uint32_t>(sh.found[0]);
+        above = sh.found[1];
+        equal = sh.found[2];
         // (the low half of a bf16's key follows from its sign)
         if (low == 0 || (low == 16 && (BF16 || above + equal <= k + 32))) break;
     }
-    // groups at t: the first ones, where t is a whole key
+    // the list, ascending; of the groups at t the first ones, where t is a whole key
     const int take = BF16 || low == 0 ? k - above : equal;
-    int both_counts = 0;  // those above t, and 2^16 times those at it
 #pragma unroll
     for (int j = 0; j < kMine; ++j) {
-        both_counts += key[j] >> low > t;
-        both_counts += (first + 32 * j < groups && key[j] >> low == t) << 16;
+        const bool there = tid + kThreads * j < groups;
+        const uint32_t more = __ballot_sync(0xffffffffu, there && key[j] >> low > t);
+        const uint32_t same = __ballot_sync(0xffffffffu, there && key[j] >> low == t);
+        if (lane == 0) sh.counts[j * kWarps + warp] = __popc(more) | __popc(same) << 16;
     }
-    both_counts = __reduce_add_sync(0xffffffffu, both_counts);
-    if (lane == 0) sh.counts[warp] = both_counts;
     __syncthreads();
-    int same_before = 0, place = 0;  // of the warps before
-    for (int w = 0; w < warp; ++w) {
-        const int a = sh.counts[w] & 0xFFFF, e = sh.counts[w] >> 16;
-        place += a + min(max(take - same_before, 0), e);
-        same_before += e;
+    static_assert(kMine * kWarps == 32, "a count for each lane");
+    int upto = sh.counts[lane];
+    const int own = upto;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += y;
     }
+    const int before = upto - own;  // of the groups before the lane's 32: above t, and 2^16 times those at it
 #pragma unroll
     for (int j = 0; j < kMine; ++j) {
-        const bool there = first + 32 * j < groups;
-        const uint32_t same = __ballot_sync(0xffffffffu, there && key[j] >> low == t), under = (1u << lane) - 1u;
-        const bool mine =
-            there && (key[j] >> low > t || (key[j] >> low == t && same_before + __popc(same & under) < take));
+        if (kThreads * j >= groups) break;
+        const int b = __shfl_sync(0xffffffffu, before, j * kWarps + warp), same_before = b >> 16;
+        const bool there = tid + kThreads * j < groups;
+        const uint32_t under = (1u << lane) - 1u;
+        const uint32_t same = __ballot_sync(0xffffffffu, there && key[j] >> low == t);
+        const bool mine = there && (key[j] >> low > t || (key[j] >> low == t && same_before + __popc(same & under) < take));
         const uint32_t taken = __ballot_sync(0xffffffffu, mine);
-        if (mine) sh.selected[place + __popc(taken & under)] = first + 32 * j;
-        place += __popc(taken);
-        same_before += __popc(same);
+        if (mine) sh.selected[(b & 0xFFFF) + min(same_before, max(take, 0)) + __popc(taken & under)] = tid + kThreads * j;
     }
-    if (threadIdx.x == kThreads - 1) {
-        sh.num_selected = place;
+    if (tid == 0) {
+        sh.num_selected = min(above + max(take, 0), groups);
         sh.threshold = t;
         sh.low = low;
     }
@@ -551,7 +573,6 @@ __global__ void __launch_bounds__(kThreads, TOP ? 4 : 6) log_probs_kernel(const 
         mine.t = both(t2).x + both(t2).y;
         if constexpr (TOP) {
             auto note = [&](int group, uint32_t key) {
-                if (key == 0) return;
                 if (rank == 0) {
                     atomicMax(&sh.group_key[group], key);
                 } else {
@@ -567,7 +588,10 @@ __global__ void __launch_bounds__(kThreads, TOP ? 4 : 6) log_probs_kernel(const 
                     if (lane == i) v = all;
                 }
                 const int u = u0 + 32 * lane;
-                if (lane < kAhead && u < r.units) note(u >> shift, key_of(v));
+                if (lane < kAhead && u < r.units) {
+                    if (shift == 5 && rank == 0) sh.group_key[u >> 5] = key_of(v);  // (no other warp's)
+                    else note(u >> shift, key_of(v));
+                }
             } else {
 #pragma unroll
                 for (int i = 0; i < kAhead; ++i) {

@@ -72,7 +72,7 @@ template <bool PAIRS, bool CACHE>
 __global__ void __launch_bounds__(kThreads) rotary_kernel(const KvView kv, const RotaryParams p, const int tokens,
                                                           const int heads_per_cta) {
     __shared__ int64_t position[kTokens];
-    __shared__ float2 turned[kTokens][kMaxPairs];  // cosine and sine, times the factor
+    __shared__ __align__(16) float2 turned[kTokens][kMaxPairs];  // cosine and sine, times the factor
     const int pairs = p.rot / 2;
     const int64_t m0 = static_cast<int64_t>(blockIdx.x) * tokens;
     grid_launch_dependents();
@@ -94,59 +94,54 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const KvView kv, const
         }
     }
     __syncthreads();
-    // a unit: eight pairs of a head, in two pieces of 16 bytes
+    // a unit: eight pairs of a head, in two pieces of 16 bytes; the tokens, and heads of each, side by side
     const int units = pairs / 8;
-    const int side = kThreads / units;  // heads side by side
-    const int u = threadIdx.x % units, h0 = threadIdx.x / units;
-    if (h0 >= side) return;
+    const int side = kThreads / units / tokens;  // heads of a token
+    const int u = threadIdx.x % units, t = threadIdx.x / units / side, h0 = threadIdx.x / units - t * side;
+    if (t >= tokens || position[t] < 0) return;
     const int heads = p.H + p.kv_heads;
     const int begin = static_cast<int>(blockIdx.y) * heads_per_cta, end = min(begin + heads_per_cta, heads);
     const int64_t width = static_cast<int64_t>(heads + p.kv_heads) * p.d;
     const int low = PAIRS ? 16 * u : 8 * u, high = PAIRS ? low + 8 : low + pairs;
-    for (int t = 0; t < tokens; ++t) {
-        if (position[t] < 0) continue;
-        float c[8], s[8];
+    float c[8], s[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float2 cs = turned[t][8 * u + e];
-            c[e] = cs.x;
-            s[e] = cs.y;
-        }
-        uint16_t* const row = p.qkv + (m0 + t) * width;
-        constexpr int kAhead = 4;
-        for (int h = begin + h0; h < end; h += kAhead * side) {
-            uint4 a[kAhead], b[kAhead];
+    for (int e = 0; e < 8; ++e) {
+        const float2 cs = turned[t][8 * u + e];
+        c[e] = cs.x;
+        s[e] = cs.y;
+    }
+    uint16_t* const row = p.qkv + (m0 + t) * width;
+    constexpr int kAhead = 4;
+    for (int h = begin + h0; h < end; h += kAhead * side) {
+        uint4 a[kAhead], b[kAhead];
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k)
-                if (h + k * side < end) {
-                    const uint16_t* const head = row + (h + k * side) * p.d;
-                    a[k] = __ldcs(reinterpret_cast<const uint4*>(head + low));
-                    b[k] = __ldcs(reinterpret_cast<const uint4*>(head + high));
-                }
+        for (int k = 0; k < kAhead; ++k)
+            if (h + k * side < end) {
+                const uint16_t* const head = row + (h + k * side) * p.d;
+                a[k] = __ldcs(reinterpret_cast<const uint4*>(head + low));
+                b[k] = __ldcs(reinterpret_cast<const uint4*>(head + high));
+            }
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k)
-                if (h + k * side < end) {
-                    uint32_t x[4] = {a[k].x, a[k].y, a[k].z, a[k].w}, y[4] = {b[k].x, b[k].y, b[k].z, b[k].w};
+        for (int k = 0; k < kAhead; ++k)
+            if (h + k * side < end) {
+                uint32_t x[4] = {a[k].x, a[k].y, a[k].z, a[k].w}, y[4] = {b[k].x, b[k].y, b[k].z, b[k].w};
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if constexpr (PAIRS) {
-                            const float x0 = bf16_low(x[i]), x1 = bf16_high(x[i]);
-                            const float y0 = bf16_low(y[i]), y1 = bf16_high(y[i]);
-                            x[i] = pack_bf16(x0 * c[i] - x1 * s[i], x0 * s[i] + x1 * c[i]);
-                            y[i] = pack_bf16(y0 * c[4 + i] - y1 * s[4 + i], y0 * s[4 + i] + y1 * c[4 + i]);
-                        } else {
-                            const float x0 = bf16_low(x[i]), x1 = bf16_high(x[i]);
-                            const float y0 = bf16_low(y[i]), y1 = bf16_high(y[i]);
-                            const int e = 2 * i;
-                            x[i] = pack_bf16(x0 * c[e] - y0 * s[e], x1 * c[e + 1] - y1 * s[e + 1]);
-                            y[i] = pack_bf16(x0 * s[e] + y0 * c[e], x1 * s[e + 1] + y1 * c[e + 1]);
-                        }
+                for (int i = 0; i < 4; ++i) {
+                    const float x0 = bf16_low(x[i]), x1 = bf16_high(x[i]);
+                    const float y0 = bf16_low(y[i]), y1 = bf16_high(y[i]);
+                    if constexpr (PAIRS) {
+                        x[i] = pack_bf16(x0 * c[i] - x1 * s[i], x0 * s[i] + x1 * c[i]);
+                        y[i] = pack_bf16(y0 * c[4 + i] - y1 * s[4 + i], y0 * s[4 + i] + y1 * c[4 + i]);
+                    } else {
+                        const int e = 2 * i;
+                        x[i] = pack_bf16(x0 * c[e] - y0 * s[e], x1 * c[e + 1] - y1 * s[e + 1]);
+                        y[i] = pack_bf16(x0 * s[e] + y0 * c[e], x1 * s[e + 1] + y1 * c[e + 1]);
                     }
-                    uint16_t* const head = row + (h + k * side) * p.d;
-                    *reinterpret_cast<uint4*>(head + low) = make_uint4(x[0], x[1], x[2], x[3]);
-                    *reinterpret_cast<uint4*>(head + high) = make_uint4(y[0], y[1], y[2], y[3]);
                 }
-        }
+                uint16_t* const head = row + (h + k * side) * p.d;
+                *reinterpret_cast<uint4*>(head + low) = make_uint4(x[0], x[1], x[2], x[3]);
+                *reinterpret_cast<uint4*>(head + high) = make_uint4(y[0], y[1], y[2], y[3]);
+            }
     }
 }
 
