@@ -28,6 +28,33 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     return *reinterpret_cast<const uint32_t*>(&p);
 }
 
+// Two fp32 in one register pair, an instruction for both.
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+    uint64_t p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(a), "f"(b));
+    return p;
+}
+__device__ __forceinline__ float2 both(uint64_t p) {
+    float2 v;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+
 // Rows are read once: they leave L1 to the weights, which every row reads.
 __device__ __forceinline__ uint4 load_row16(const void* p) {
     uint4 v;
@@ -174,21 +201,30 @@ __device__ __forceinline__ void clear(float (&parts)[2][kMaxWarps]) {
     if (t < 2 * kMaxWarps && t % kMaxWarps >= static_cast<int>(blockDim.x >> 5)) parts[t / kMaxWarps][t % kMaxWarps] = 0.0f;
 }
 
-// The mean (layer norm; else 0) and 1 / sqrt(mean square about it + eps) of a row.  each(f): f(value) for the
-// thread's values.
-template <typename Each>
-__device__ __forceinline__ void statistics(const Each& each, bool layer, float inv_d, float eps, Reducer& red, float* mean,
-                                           float* rstd) {
+// The mean (layer norm; else 0) and 1 / sqrt(mean square about it + eps) of a row.  pairs(f): f(two values) for the
+// thread's, in register pairs; a column that the row has not counts as `absent`.
+template <bool PACKED, typename Pairs>
+__device__ __forceinline__ void statistics(const Pairs& pairs, bool layer, float inv_d, float eps, Reducer& red,
+                                           float* mean, float* rstd) {
     float m = 0.0f;
     if (layer) {
         // (a sum of x / D: one of x could overflow)
-        float sum = 0.0f;
-        each([&](float x) { sum = fmaf(x, inv_d, sum); });
-        m = red.reduce<false>(sum);
+        uint64_t sum = 0;
+        pairs(0.0f, [&](uint64_t x) { sum = fma2(x, pair(inv_d, inv_d), sum); });
+        m = red.reduce<false>(both(sum).x + both(sum).y);
     }
-    float ss = 0.0f;
-    each([&](float x) { ss = fmaf(x - m, x - m, ss); });
-    const float total = red.reduce<false>(ss);
+    uint64_t ss = 0;
+    if (PACKED || layer) {
+        pairs(m, [&](uint64_t x) {
+            const uint64_t c = add2(x, pair(-m, -m));
+            ss = fma2(c, c, ss);
+        });
+    } else {
+        float sum = 0.0f;
+        pairs(0.0f, [&](uint64_t x) { sum = fmaf(both(x).x, both(x).x, fmaf(both(x).y, both(x).y, sum)); });
+        ss = pair(sum, 0.0f);
+    }
+    const float total = red.reduce<false>(both(ss).x + both(ss).y);
     *mean = m;
     *rstd = rsqrtf(fmaf(total, inv_d, eps));
     if (total < 1e38f) return;
@@ -196,60 +232,132 @@ __device__ __forceinline__ void statistics(const Each& each, bool layer, float i
     // branch is the same for all threads of the row.  An infinity or a NaN gives 0 or NaN, as the
     // formula has it.)
     float top = 0.0f;
-    each([&](float x) { top = fmaxf(top, fabsf(x - m)); });
+    pairs(m, [&](uint64_t x) { top = fmaxf(top, fmaxf(fabsf(both(x).x - m), fabsf(both(x).y - m))); });
     top = red.reduce<true>(top);
     if (!(top < INFINITY) || total != total) return;
     const float s = __uint_as_float((253u << 23) - (__float_as_uint(top) & 0x7F800000u));  // 2^-exponent / 2
-    ss = 0.0f;
-    each([&](float x) { ss = fmaf((x - m) * s, (x - m) * s, ss); });
-    *rstd = s * rsqrtf(red.reduce<false>(ss) * inv_d);  // (eps s^2 is far below half a step)
+    ss = 0;
+    pairs(m, [&](uint64_t x) {
+        const uint64_t c = mul2(add2(x, pair(-m, -m)), pair(s, s));
+        ss = fma2(c, c, ss);
+    });
+    *rstd = s * rsqrtf(red.reduce<false>(both(ss).x + both(ss).y) * inv_d);  // (eps s^2 is far below half a step)
 }
 
-template <int NV, bool ODD>
+// f(two values) for a piece's pairs, with `absent` where the row has no column.
+template <bool ODD, typename F>
+__device__ __forceinline__ void piece_pairs(const float (&x)[8], int c, const Row<ODD>& r, float absent, const F& f) {
+    if (ODD) {
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) f(pair(r.has(c, e) ? x[e] : absent, r.has(c, e + 1) ? x[e + 1] : absent));
+    } else if (r.whole(c)) {
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) f(pair(x[e], x[e + 1]));
+    } else {
+        const uint64_t none = pair(absent, absent);
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) f(none);
+    }
+}
+
+template <bool PACKED, int NV, bool ODD>
 __device__ __forceinline__ void statistics(const float (&x)[NV][8], bool layer, const Row<ODD>& r, float inv_d, float eps,
                                            Reducer& red, float* mean, float* rstd) {
-    statistics(
-        [&](const auto& f) {
+    statistics<PACKED>(
+        [&](float absent, const auto& f) {
 #pragma unroll
-            for (int v = 0; v < NV; ++v)
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (r.has(r.first(v), e)) f(x[v][e]);
+            for (int v = 0; v < NV; ++v) piece_pairs(x[v], r.first(v), r, absent, f);
         },
         layer, inv_d, eps, red, mean, rstd);
 }
 
-// x[v][e] = f(x[v][e], vec[column]), a vector's loads together.
-template <int NV, bool ODD, typename F>
-__device__ __forceinline__ void with_vector(float (&x)[NV][8], const uint16_t* vec, const Row<ODD>& r, const F& f) {
-    uint4 raw[NV];
+// x = (x - mean) rstd (offset + weight) + bias; no weight: a factor of 1.  PACKED: in register pairs, which
+// take more registers.
+template <bool PACKED>
+__device__ __forceinline__ void normalise8(float (&x)[8], float mean, float rstd, float offset, bool weighted, uint4 weight,
+                                           bool biased, uint4 bias) {
+    float w[8], b[8];
+    unpack8(weight, w);
+    unpack8(bias, b);
+    if constexpr (PACKED) {
+        const uint64_t minus = pair(-mean, -mean), scale = pair(rstd, rstd), more = pair(offset, offset);
 #pragma unroll
-    for (int v = 0; v < NV; ++v) raw[v] = load_vector(vec, r.first(v), r);
+        for (int e = 0; e < 8; e += 2) {
+            const uint64_t c = add2(pair(x[e], x[e + 1]), minus);
+            const uint64_t factor = weighted ? mul2(add2(pair(w[e], w[e + 1]), more), scale) : scale;
+            const float2 y = both(biased ? fma2(c, factor, pair(b[e], b[e + 1])) : mul2(c, factor));
+            x[e] = y.x;
+            x[e + 1] = y.y;
+        }
+    } else {
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        float w[8];
-        unpack8(raw[v], w);
+        for (int e = 0; e < 8; ++e) {
+            const float c = x[e] - mean, factor = weighted ? (w[e] + offset) * rstd : rstd;
+            x[e] = biased ? fmaf(c, factor, b[e]) : c * factor;
+        }
+    }
+}
+
+// The same for a row; the weights' loads together.
+template <bool PACKED, int NV, bool ODD>
+__device__ __forceinline__ void normalise(float (&x)[NV][8], const uint16_t* weight, const uint16_t* bias, const Row<ODD>& r,
+                                          float mean, float rstd, float offset) {
+    const uint4 none = make_uint4(0, 0, 0, 0);
+    uint4 w[NV];
+    if (PACKED && weight != nullptr && bias != nullptr) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[v][e] = f(x[v][e], w[e]);
+        for (int v = 0; v < NV; ++v) w[v] = load_vector(weight, r.first(v), r);
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+            normalise8<PACKED>(x[v], mean, rstd, offset, true, w[v], true, load_vector(bias, r.first(v), r));
+        return;
+    }
+    if (weight != nullptr) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) w[v] = load_vector(weight, r.first(v), r);
+#pragma unroll
+        for (int v = 0; v < NV; ++v) normalise8<PACKED>(x[v], mean, rstd, offset, true, w[v], false, none);
+    } else {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) normalise8<PACKED>(x[v], mean, rstd, offset, false, none, false, none);
+    }
+    if (bias != nullptr) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) w[v] = load_vector(bias, r.first(v), r);
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            float b[8];
+            unpack8(w[v], b);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[v][e] += b[e];
+        }
     }
 }
 
 // The rest of a row whose block output is x (its scaled stream values without a block): `stream` and
 // `gate` give a piece's values.
-template <typename R, int NV, bool ODD, typename Stream, typename Gate>
+template <bool PACKED, typename R, int NV, bool ODD, typename Stream, typename Gate>
 __device__ __forceinline__ void finish_row(const NormParams& p, const Row<ODD>& r, int64_t at, float inv_d, Reducer& red,
                                            float (&x)[NV][8], const Stream& stream, const Gate& gate) {
     const float offset = p.weight_offset;
     float mean, rstd;
     if (p.block != nullptr) {
         if (p.post_weight != nullptr) {
-            statistics<NV, ODD>(x, p.layer, r, inv_d, p.eps, red, &mean, &rstd);
-            with_vector(x, p.post_weight, r, [=](float v, float w) { return (v - mean) * rstd * (offset + w); });
-            if (p.post_bias != nullptr) with_vector(x, p.post_bias, r, [](float v, float w) { return v + w; });
+            statistics<PACKED>(x, p.layer, r, inv_d, p.eps, red, &mean, &rstd);
+            normalise<PACKED>(x, p.post_weight, p.post_bias, r, mean, rstd, offset);
         }
         if (p.gate != nullptr) {
             if (p.gate_stride == 0) {
-                with_vector(x, p.gate, r, [](float v, float w) { return v * w; });
+                uint4 raw[NV];
+#pragma unroll
+                for (int v = 0; v < NV; ++v) raw[v] = load_vector(p.gate, r.first(v), r);
+#pragma unroll
+                for (int v = 0; v < NV; ++v) {
+                    float w[8];
+                    unpack8(raw[v], w);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[v][e] *= w[e];
+                }
             } else {
 #pragma unroll
                 for (int v = 0; v < NV; ++v) {
@@ -274,16 +382,8 @@ __device__ __forceinline__ void finish_row(const NormParams& p, const Row<ODD>& 
         for (int v = 0; v < NV; ++v) store8(to, r.first(v), r, x[v]);
     }
     if (p.out == nullptr) return;
-    statistics<NV, ODD>(x, p.layer, r, inv_d, p.eps, red, &mean, &rstd);
-    if (p.weight != nullptr) {
-        with_vector(x, p.weight, r, [=](float v, float w) { return (v - mean) * rstd * (offset + w); });
-    } else {
-#pragma unroll
-        for (int v = 0; v < NV; ++v)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[v][e] = (x[v][e] - mean) * rstd;
-    }
-    if (p.bias != nullptr) with_vector(x, p.bias, r, [](float v, float w) { return v + w; });
+    statistics<PACKED>(x, p.layer, r, inv_d, p.eps, red, &mean, &rstd);
+    normalise<PACKED>(x, p.weight, p.bias, r, mean, rstd, offset);
 #pragma unroll
     for (int v = 0; v < NV; ++v) store8(p.out + at, r.first(v), r, x[v]);
 }
@@ -325,7 +425,7 @@ __global__ void __launch_bounds__(512, NV <= 3 && !ODD ? 2 : 1) residual_norm_ke
             for (int e = 0; e < 8; ++e) x[v][e] *= p.residual_scale;
         }
     }
-    finish_row<R, NV, ODD>(
+    finish_row<false, R, NV, ODD>(
         p, r, at, inv_d, red, x, [&](int v, float (&w)[8]) { stream[v].values(w); },
         [&](int v, float (&w)[8]) {
             Raw<uint16_t> g;
@@ -436,7 +536,7 @@ __global__ void __launch_bounds__(kRingThreads, 2) residual_norm_ring_kernel(con
             for (int e = 0; e < 8; ++e) w[e] = 0.0f;
             if (r.first(v) < D) ring_values<decltype(type)>(part, r.first(v), w);
         };
-        finish_row<R, NV, false>(
+        finish_row<true, R, NV, false>(
             p, r, row * D, inv_d, red, x, [&](int v, float (&w)[8]) { values(from + block_bytes, R{}, v, w); },
             [&](int v, float (&w)[8]) { values(from + block_bytes + stream_bytes, uint16_t{}, v, w); });
         slot = slot + 1 == depth ? 0 : slot + 1;
@@ -445,22 +545,31 @@ __global__ void __launch_bounds__(kRingThreads, 2) residual_norm_ring_kernel(con
 }
 
 template <typename R>
-cudaError_t launch_ring(const NormParams& p, int depth, int row_bytes, int ctas, int sm_count, cudaStream_t stream) {
+bool launch_ring(const NormParams& p, int sm_count, cudaStream_t stream, cudaError_t* e) {
+    const int row_bytes = p.D * (static_cast<int>(sizeof(R)) + (p.block != nullptr ? 2 : 0) +
+                                 (p.gate != nullptr && p.gate_stride != 0 ? 2 : 0));
     const int pieces = p.D / 8, least = (pieces + kRingThreads - 1) / kRingThreads;
     const int nv = least <= 2 ? 2 : least;
+    const int threads = ((pieces + nv - 1) / nv + 31) / 32 * 32;
+    // as many CTAs an SM as have registers (80 a thread), with two rows each at least
+    int ctas = 65536 / (80 * threads);
+    if (ctas > 4) ctas = 4;
+    while (ctas > 2 && 224 * 1024 / ctas / row_bytes < 2) --ctas;
+    int depth = 224 * 1024 / ctas / row_bytes;
+    if (depth > kRingRows) depth = kRingRows;
+    if (depth < 2 || p.M < 2 * ctas * sm_count) return false;
     auto kernel = nv == 2   ? residual_norm_ring_kernel<R, 2>
                   : nv == 3 ? residual_norm_ring_kernel<R, 3>
                             : residual_norm_ring_kernel<R, 4>;
-    const cudaError_t e =
-        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, depth * row_bytes);
-    if (e != cudaSuccess) return e;
-    const int threads = ((pieces + nv - 1) / nv + 31) / 32 * 32;
-    return launch_overlapped(kernel, dim3(ctas * sm_count), threads, depth * row_bytes, stream, p, depth);
+    *e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, depth * row_bytes);
+    if (*e == cudaSuccess)
+        *e = launch_overlapped(kernel, dim3(ctas * sm_count), threads, depth * row_bytes, stream, p, depth);
+    return true;
 }
 
-// Rows wider than registers hold: one CTA to a row, whose values are in shared memory in fp32 between the
-// passes; a thread works on its own units alone.
-constexpr int kWideThreads = 1024;
+// Rows wider than registers hold, and rows of odd width past a warp's: one CTA to a row, whose values are in
+// shared memory in fp32 between the passes; a thread works on its own units alone.
+constexpr int kWideThreads = 1024;  // at most
 
 template <typename R, bool ODD>
 __global__ void __launch_bounds__(kWideThreads) residual_norm_wide_kernel(const NormParams p) {
@@ -469,31 +578,31 @@ __global__ void __launch_bounds__(kWideThreads) residual_norm_wide_kernel(const 
     const int64_t row = blockIdx.x, at = row * p.D;
     grid_launch_dependents();
     grid_wait();
-    Reducer red{parts, kWideThreads / 32, 0};
-    const Row<ODD> r{static_cast<int>(threadIdx.x), kWideThreads, p.D, static_cast<int>(at & 7)};
+    const int threads = static_cast<int>(blockDim.x);
+    Reducer red{parts, threads >> 5, 0};
+    clear(parts);
+    const Row<ODD> r{static_cast<int>(threadIdx.x), threads, p.D, static_cast<int>(at & 7)};
     const float inv_d = 1.0f / static_cast<float>(p.D), offset = p.weight_offset;
     const int pieces = (p.D + (ODD ? r.shift : 0) + 7) / 8;
     const R* const residual = static_cast<const R*>(p.residual) + at;
-    const int own = static_cast<int>(threadIdx.x) < pieces ? (pieces - 1 - threadIdx.x) / kWideThreads + 1 : 0;
+    const int own = static_cast<int>(threadIdx.x) < pieces ? (pieces - 1 - static_cast<int>(threadIdx.x)) / threads + 1 : 0;
     auto get = [&](int v, float (&x)[8]) {
-        const float4* const from = reinterpret_cast<const float4*>(values + (v * kWideThreads + threadIdx.x) * 8);
+        const float4* const from = reinterpret_cast<const float4*>(values + (v * threads + static_cast<int>(threadIdx.x)) * 8);
         const float4 a = from[0], b = from[1];
         x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
     };
     auto put = [&](int v, const float (&x)[8]) {
-        float4* const to = reinterpret_cast<float4*>(values + (v * kWideThreads + threadIdx.x) * 8);
+        float4* const to = reinterpret_cast<float4*>(values + (v * threads + static_cast<int>(threadIdx.x)) * 8);
         to[0] = make_float4(x[0], x[1], x[2], x[3]);
         to[1] = make_float4(x[4], x[5], x[6], x[7]);
     };
     auto stats = [&](float* mean, float* rstd) {
-        statistics(
-            [&](const auto& f) {
+        statistics<true>(
+            [&](float absent, const auto& f) {
                 for (int v = 0; v < own; ++v) {
                     float x[8];
                     get(v, x);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (r.has(r.first(v), e)) f(x[e]);
+                    piece_pairs(x, r.first(v), r, absent, f);
                 }
             },
             p.layer, inv_d, p.eps, red, mean, rstd);
@@ -522,14 +631,8 @@ __global__ void __launch_bounds__(kWideThreads) residual_norm_wide_kernel(const 
         if (p.block != nullptr) {
             if (p.post_weight != nullptr) {
                 get(v, x);
-                unpack8(load_vector(p.post_weight, c, r), w);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = (x[e] - mean) * rstd * (offset + w[e]);
-                if (p.post_bias != nullptr) {
-                    unpack8(load_vector(p.post_bias, c, r), w);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] += w[e];
-                }
+                normalise8<true>(x, mean, rstd, offset, true, load_vector(p.post_weight, c, r), p.post_bias != nullptr,
+                           p.post_bias != nullptr ? load_vector(p.post_bias, c, r) : make_uint4(0, 0, 0, 0));
             } else {
                 Raw<uint16_t> block;
                 block.load(p.block + at, c, r);
@@ -557,20 +660,11 @@ __global__ void __launch_bounds__(kWideThreads) residual_norm_wide_kernel(const 
 #pragma unroll 2
     for (int v = 0; v < own; ++v) {
         const int c = r.first(v);
-        float x[8], w[8];
+        float x[8];
         get(v, x);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = (x[e] - mean) * rstd;
-        if (p.weight != nullptr) {
-            unpack8(load_vector(p.weight, c, r), w);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] *= offset + w[e];
-        }
-        if (p.bias != nullptr) {
-            unpack8(load_vector(p.bias, c, r), w);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] += w[e];
-        }
+        const uint4 none = make_uint4(0, 0, 0, 0);
+        normalise8<true>(x, mean, rstd, offset, p.weight != nullptr, p.weight != nullptr ? load_vector(p.weight, c, r) : none,
+                   p.bias != nullptr, p.bias != nullptr ? load_vector(p.bias, c, r) : none);
         store8(p.out + at, c, r, x);
     }
 }
@@ -578,11 +672,13 @@ __global__ void __launch_bounds__(kWideThreads) residual_norm_wide_kernel(const 
 template <typename R, bool ODD>
 cudaError_t launch_wide(const NormParams& p, cudaStream_t stream) {
     const int units = (p.D + (ODD ? 14 : 7)) / 8;
-    const int smem = (units + kWideThreads - 1) / kWideThreads * kWideThreads * 32;
+    int threads = 256;  // with two to four units each, as far as that goes
+    while (threads < kWideThreads && units > 4 * threads) threads *= 2;
+    const int smem = (units + threads - 1) / threads * threads * 32;
     auto kernel = residual_norm_wide_kernel<R, ODD>;
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
-    return launch_overlapped(kernel, dim3(p.M), kWideThreads, smem, stream, p);
+    return launch_overlapped(kernel, dim3(p.M), threads, smem, stream, p);
 }
 
 template <typename R, bool ODD>
@@ -598,11 +694,11 @@ cudaError_t launch(const NormParams& p, cudaStream_t stream) {
                            : residual_norm_kernel<R, 4, ODD>;
     } else {
         const int least = (pieces + 511) / 512;
-        if (least > 4) return launch_wide<R, ODD>(p, stream);
+        if (ODD || least > 4) return launch_wide<R, ODD>(p, stream);
         const int nv = least <= 2 ? 2 : least;
-        kernel = nv == 2   ? residual_norm_kernel<R, 2, ODD>
-                 : nv == 3 ? residual_norm_kernel<R, 3, ODD>
-                           : residual_norm_kernel<R, 4, ODD>;
+        kernel = nv == 2   ? residual_norm_kernel<R, 2, false>
+                 : nv == 3 ? residual_norm_kernel<R, 3, false>
+                           : residual_norm_kernel<R, 4, false>;
         group = threads = ((pieces + nv - 1) / nv + 31) / 32 * 32;
     }
     const int rows = threads / group;
@@ -615,13 +711,9 @@ cudaError_t launch_residual_norm(const NormParams& p, bool fp32, int sm_count, c
     const bool whole = p.D % 8 == 0;  // rows of 16-byte units (bases are 16-byte aligned)
     // (a plain bf16 RMS norm is at the copy bandwidth from registers: 39004 rows of 12288 551 us, 613 with the
     // ring; 4097 of 8200 with both layer norms and an fp32 stream 128, 99 with it)
-    if (whole && p.D > 1024 && p.D <= 4 * 8 * kRingThreads) {
-        const int row_bytes = p.D * ((fp32 ? 4 : 2) + (p.block != nullptr ? 2 : 0) +
-                                     (p.gate != nullptr && p.gate_stride != 0 ? 2 : 0));
-        const int depth = 112 * 1024 / row_bytes < kRingRows ? 112 * 1024 / row_bytes : kRingRows;
-        if (depth >= 2 && p.M >= 4 * sm_count && (fp32 || p.layer || p.post_weight != nullptr))
-            return fp32 ? launch_ring<float>(p, depth, row_bytes, 2, sm_count, stream)
-                        : launch_ring<uint16_t>(p, depth, row_bytes, 2, sm_count, stream);
+    if (whole && p.D > 1024 && p.D <= 4 * 8 * kRingThreads && (fp32 || p.layer || p.post_weight != nullptr)) {
+        cudaError_t e = cudaSuccess;
+        if (fp32 ? launch_ring<float>(p, sm_count, stream, &e) : launch_ring<uint16_t>(p, sm_count, stream, &e)) return e;
     }
     return fp32 ? (whole ? launch<float, false>(p, stream) : launch<float, true>(p, stream))
                 : (whole ? launch<uint16_t, false>(p, stream) : launch<uint16_t, true>(p, stream));
