@@ -9,7 +9,11 @@ attention over the cache (attention_decode).  The step is captured once as a CUD
 replayed; ligands that have ended are padding.  The affinity head reads each ligand's last
 state, and topk_smallest sorts the predictions.  Freed pages are compacted at the end.
 
-    python examples/screen_ligands.py [--ligands 64] [--protein 700] [--e4m3]
+With --whole the layers have what decoders have around their linears: norms of the residual stream
+(residual_norm), rotary positions (kv_rotary by the cache's lengths, rotary without a cache) and a low-rank
+adapter of the target on the QKV projection (add_adapters).
+
+    python examples/screen_ligands.py [--ligands 64] [--protein 700] [--e4m3] [--whole]
 
 Weights and token states are random: the model's are not available.
 """
@@ -31,19 +35,28 @@ HEAD_DIM = 128
 
 
 @dataclasses.dataclass
+class Around:
+    """What a layer has around its linears."""
+    norms: list      # weights, of each layer before attention and before the MLP, and the last one
+    table: W.RotaryTable
+    adapters: list   # of each layer's QKV projection: A [targets, rank, width], B, scale
+
+
+@dataclasses.dataclass
 class Decoder:
-    """int4 decoder layers (QKV, attention, output, SwiGLU MLP; no norms, as the library
-    has none: the outputs that are added to the stream are scaled down instead)."""
+    """int4 decoder layers (QKV, attention, output, SwiGLU MLP).  Without `around` they have no
+    norms: the outputs that are added to the stream are scaled down instead."""
     heads: int
     layers: list
     head: tuple  # affinity head: packed, scales, bias
+    around: Around | None = None
 
     @property
     def width(self):
         return self.heads * HEAD_DIM
 
     @classmethod
-    def random(cls, heads: int, n_layers: int, seed: int = 0):
+    def random(cls, heads: int, n_layers: int, seed: int = 0, whole: bool = False, targets: int = 4, rank: int = 16):
         d = heads * HEAD_DIM
 
         def weights(n, k, seed, scale=1.0):
@@ -52,15 +65,41 @@ class Decoder:
         layers = [(weights(3 * d, d, seed + 10 * i), weights(d, d, seed + 10 * i + 1, 0.5),
                    weights(8 * d, d, seed + 10 * i + 2), weights(d, 4 * d, seed + 10 * i + 3, 0.5))
                   for i in range(n_layers)]
-        return cls(heads, layers, (*weights(1, d, seed + 7), torch.zeros(1, dtype=torch.bfloat16, device="cuda")))
+        head = (*weights(1, d, seed + 7), torch.zeros(1, dtype=torch.bfloat16, device="cuda"))
+        if not whole:
+            return cls(heads, layers, head)
+        gen = torch.Generator(device="cuda").manual_seed(seed + 8)
 
-    def forward(self, x, attend):
-        """x [tokens, width]; attend(layer, qkv) -> [tokens, width]."""
+        def rnd(*shape, scale):
+            return (torch.randn(shape, generator=gen, device="cuda") * scale).bfloat16()
+
+        norms = [1 + rnd(d, scale=0.1) for _ in range(2 * n_layers + 1)]
+        adapters = [(rnd(targets, rank, d, scale=d ** -0.5), rnd(targets, 3 * d, rank, scale=rank ** -0.5),
+                     torch.full((targets,), 0.5, device="cuda")) for _ in range(n_layers)]
+        return cls(heads, layers, head, Around(norms, W.RotaryTable(HEAD_DIM), adapters))
+
+    def forward(self, x, attend, turn=None, target=None, start=None):
+        """x [tokens, width]; attend(layer, qkv) -> [tokens, width].  Whole layers: turn(qkv) gives the
+        queries and keys their positions, target is each sequence's adapter and start their table."""
+        if self.around is not None:
+            return self._forward_whole(x, attend, turn, target, start)
         for i, (qkv, o, up, down) in enumerate(self.layers):
             a = attend(i, W.linear(x, *qkv))
             x = W.linear_fused(a, *o, residual=x)
             x = W.linear_fused(W.linear_fused(x, *up, act=W.ACT_SWIGLU), *down, residual=x)
         return x
+
+    def _forward_whole(self, x, attend, turn, target, start):
+        norms, block = self.around.norms, None
+        for i, (qkv, o, up, down) in enumerate(self.layers):
+            y, x = W.residual_norm(x, norms[2 * i], block)  # (x takes in the block before)
+            p = W.linear(y, *qkv)
+            W.add_adapters(p, y, *self.around.adapters[i], target, seq_start=start, out=p)
+            turn(p)
+            block = W.linear(attend(i, p), *o)
+            y, x = W.residual_norm(x, norms[2 * i + 1], block)
+            block = W.linear(W.linear_fused(y, *up, act=W.ACT_SWIGLU), *down)
+        return W.residual_norm(x, norms[-1], block)[0]
 
     def affinities(self, states):
         return W.linear_fused(states, self.head[0], self.head[1], bias=self.head[2])[:, 0].contiguous()
@@ -71,9 +110,9 @@ def _i32(values):
 
 
 def screen(model: Decoder, protein: torch.Tensor, ligands: list[torch.Tensor], page_tokens: int = 16,
-           dtype=torch.bfloat16):
+           dtype=torch.bfloat16, target: int = 0):
     """Affinities [len(ligands)] of the protein (token states [tokens, width]) with each
-    ligand ([tokens, width]), and the cache that was used."""
+    ligand ([tokens, width]), and the cache that was used.  target: the adapter of a whole decoder."""
     n, H = len(ligands), model.heads
     lengths = [x.shape[0] for x in ligands]
     steps = max(lengths)
@@ -89,7 +128,9 @@ def screen(model: Decoder, protein: torch.Tensor, ligands: list[torch.Tensor], p
         W.kv_write(cache, layer, qkv, start, slot0, H)
         return W.attention_prefill(qkv, start, H)
 
-    model.forward(protein, prefill)
+    whole = model.around is not None
+    model.forward(protein, prefill, *((lambda qkv: W.kv_rotary(cache, qkv, slot0, H, model.around.table, seq_start=start),
+                                       _i32([target]), start) if whole else ()))
 
     # every ligand goes on from it
     slots = _i32(range(1, n + 1))
@@ -100,10 +141,13 @@ def screen(model: Decoder, protein: torch.Tensor, ligands: list[torch.Tensor], p
     active, one = slots.clone(), torch.ones_like(slots)
     workspace = cache.new_workspace(H)
 
+    more = (lambda qkv: W.kv_rotary(cache, qkv, active, H, model.around.table),
+            torch.full_like(slots, target)) if whole else ()
+
     def step():
         W.kv_extend(cache, active, one)
         return model.forward(token, lambda layer, qkv: W.attention_decode(cache, layer, qkv, active, H,
-                                                                          workspace=workspace))
+                                                                          workspace=workspace), *more)
 
     inputs = torch.zeros((steps, n, model.width), dtype=torch.bfloat16, device="cuda")
     left = torch.full((steps, n), -1, dtype=torch.int32)
@@ -130,12 +174,14 @@ def screen(model: Decoder, protein: torch.Tensor, ligands: list[torch.Tensor], p
     return affinities, cache
 
 
-def screen_without_cache(model: Decoder, protein: torch.Tensor, ligands: list[torch.Tensor]):
+def screen_without_cache(model: Decoder, protein: torch.Tensor, ligands: list[torch.Tensor], target: int = 0):
     """The same by prefilling every pair."""
     pairs = [torch.cat([protein, x]) for x in ligands]
     ends = torch.tensor([p.shape[0] for p in pairs]).cumsum(0)
     start = _i32([0, *ends.tolist()])
-    states = model.forward(torch.cat(pairs), lambda layer, qkv: W.attention_prefill(qkv, start, model.heads))
+    more = (lambda qkv: W.rotary(qkv, model.around.table, model.heads, seq_start=start), _i32([target] * len(pairs)),
+            start) if model.around is not None else ()
+    states = model.forward(torch.cat(pairs), lambda layer, qkv: W.attention_prefill(qkv, start, model.heads), *more)
     return model.affinities(W.gather_rows(states, (start[1:] - 1).contiguous()))
 
 
@@ -151,8 +197,9 @@ def main():
     ap.add_argument("--layers", type=int, default=4)
     ap.add_argument("--best", type=int, default=5)
     ap.add_argument("--e4m3", action="store_true", help="an 8-bit cache")
+    ap.add_argument("--whole", action="store_true", help="norms, rotary positions and a target's adapter")
     a = ap.parse_args()
-    model = Decoder.random(a.heads, a.layers)
+    model = Decoder.random(a.heads, a.layers, whole=a.whole)
     protein = random_states(a.protein, model.width, 1)
     ligands = [random_states(20 + 7 * i % 41, model.width, 100 + i) for i in range(a.ligands)]
     dtype = torch.float8_e4m3fn if a.e4m3 else torch.bfloat16

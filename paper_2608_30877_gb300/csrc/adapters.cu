@@ -203,6 +203,7 @@ __device__ __forceinline__ void store_t(float* sums, const Tile<ROWS>& tile, con
         } else {
             sum = at[0];
         }
+        if (!dbg_check(m0 + token < p.M, p.status)) continue;
         out[static_cast<int64_t>(token) * p.R + r] =
             __bfloat16_as_ushort(__float2bfloat16_rn(sum * p.scale[tile.id[token]]));
     }
@@ -287,9 +288,14 @@ __global__ void __launch_bounds__(kTcThreads, 2)
                         break;
                     }
                     mbar_arrive_expect_tx(bar, L::kTokens + n * L::kAdapter);
-                    tma_load_2d(at, &map_x, bar, s * 64, static_cast<int32_t>(m0));
-                    for (int i = 0; i < n; ++i)
-                        tma_load_2d(at + L::kTokens + i * L::kAdapter, &map_a, bar, s * 64, tile.list[l + i] * p.R);
+                    const uint32_t end = ring + L::kStages * L::kStage;
+                    if (dbg_check(tma_box_ok(at, L::kTokens, 1024, ring, end, s * 64, 2), p.status))
+                        tma_load_2d(at, &map_x, bar, s * 64, static_cast<int32_t>(m0));
+                    for (int i = 0; i < n; ++i) {
+                        const uint32_t to = at + L::kTokens + i * L::kAdapter;
+                        if (dbg_check(tma_box_ok(to, L::kAdapter, 1024, ring, end, s * 64, 2), p.status))
+                            tma_load_2d(to, &map_a, bar, s * 64, tile.list[l + i] * p.R);
+                    }
                     if (it == 0 && !short_limit_ok(bar, 0, &abort_flag, p.status, p.wait_ns)) {
                         ++it;
                         ok = false;
@@ -520,7 +526,7 @@ __global__ void __launch_bounds__(kThreads, !WHOLE ? 1 : CH == 0 && MB == 0 ? 3 
                 for (int u = 0; u < NB; ++u) {
                     const int n = n0 + u * 32;
                     if constexpr (WHOLE) {
-                        c[u][i] = __ldcs(reinterpret_cast<const uint4*>(from[i] + (kInside ? n : min(n, p.N - 8))));
+                        c[u][i] = *reinterpret_cast<const uint4*>(from[i] + (kInside ? n : min(n, p.N - 8)));
                     } else {
                         uint32_t w[8];
 #pragma unroll
@@ -579,6 +585,9 @@ __global__ void __launch_bounds__(kThreads, !WHOLE ? 1 : CH == 0 && MB == 0 ? 3 
                                                pack_bf16(acc[2][2 * h], acc[2][2 * h + 1]),
                                                pack_bf16(acc[3][2 * h], acc[3][2 * h + 1])};
                         uint16_t* const to = const_cast<uint16_t*>(from[2 * m + h]) + to_out + n;
+                        if (!dbg_check(to >= p.out && to - p.out + (WHOLE && (kInside || n < columns) ? 8 : 0) <=
+                                                          static_cast<int64_t>(p.M) * p.N, p.status))
+                            continue;
                         if constexpr (WHOLE) {
                             if (kInside || n < columns) *reinterpret_cast<uint4*>(to) = make_uint4(v[0], v[1], v[2], v[3]);
                         } else {

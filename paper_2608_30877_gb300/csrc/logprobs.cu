@@ -119,11 +119,23 @@ struct Sums {
         s *= f;
         m = to;
     }
-    __device__ __forceinline__ void join(Sums o) {
-        if (o.m > m) raise(o.m);
-        if (o.m < m) o.raise(m);
-        s += o.s;
-        t += o.t;
+};
+
+// Sums of several threads: of the one with the largest logit as it has them, and of the others apart, so that
+// what is far smaller is not lost in a sum near one.
+struct Joined {
+    float m, big, big_t, s, t;
+    int owner;
+
+    __device__ __forceinline__ void join(Joined o) {
+        if (o.m > m || (o.m == m && o.owner < owner)) {  // (the same on both sides of an exchange)
+            const Joined mine = *this;
+            *this = o;
+            o = mine;
+        }
+        const float y = o.m - m, f = exp2_approx(y), n = o.big + o.s;
+        s = fmaf(f, n, s);
+        t = fmaf(f, fmaf(n, y, o.big_t + o.t), t);
     }
 };
 
@@ -184,7 +196,8 @@ struct Shared {
     unsigned long long above[kCandidates];  // key << 32 | ~column
     unsigned long long equal[kCandidates];
     int selected[kGroups];                  // groups, ascending
-    Sums warp_sums[kWarps], cta_sums[kMaxCluster];
+    Joined warp_sums[kWarps], cta_sums[kMaxCluster];
+    float refined[kWarps][3];
     int counts[32], digits[4][256], found[3];
     uint32_t threshold;
     int low;  // bits that the threshold leaves out
@@ -399,7 +412,7 @@ __device__ __forceinline__ void select_groups(Shared& sh, int groups, int k) {
 // The k largest of the row, from the groups' keys.  All threads of one CTA.  value(x): x's log probability.
 template <bool BF16, typename F>
 __device__ __forceinline__ void top(Shared& sh, const RowOf<BF16>& r, int shift, int groups, int k, const F& value,
-                                    int32_t* index, float* score) {
+                                    int32_t* index, float* score, int* status) {
     const int lane = threadIdx.x & 31;
     select_groups<BF16>(sh, groups, k);
     __syncthreads();
@@ -438,8 +451,9 @@ __device__ __forceinline__ void top(Shared& sh, const RowOf<BF16>& r, int shift,
         }
         rank += __shfl_xor_sync(0xffffffffu, rank, 1);
         rank += __shfl_xor_sync(0xffffffffu, rank, 2);
-        if (i < n && rank < k && (threadIdx.x & 3) == 0) {
-            index[rank] = static_cast<int32_t>(~static_cast<uint32_t>(mine));
+        const uint32_t column = ~static_cast<uint32_t>(mine);
+        if (i < n && rank < k && (threadIdx.x & 3) == 0 && dbg_check(column < static_cast<uint32_t>(r.V), status)) {
+            index[rank] = static_cast<int32_t>(column);
             score[rank] = value(value_of(static_cast<uint32_t>(mine >> 32)));
         }
     }
@@ -476,18 +490,75 @@ __device__ __noinline__ Sums sums_again(Shared& sh, const RowOf<BF16>& r) {
             mine.t += __shfl_xor_sync(0xffffffffu, mine.t, o);
         }
         __syncthreads();
-        if (lane == 0) sh.warp_sums[warp] = mine;
+        if (lane == 0) {
+            sh.refined[warp][0] = mine.m;
+            sh.refined[warp][1] = mine.s;
+            sh.refined[warp][2] = mine.t;
+        }
         __syncthreads();
-        if (pass == 0) {
-            for (int w = 0; w < kWarps; ++w) all.m = fmaxf(all.m, sh.warp_sums[w].m);
-        } else {
-            for (int w = 0; w < kWarps; ++w) {
-                all.s += sh.warp_sums[w].s;
-                all.t += sh.warp_sums[w].t;
+        for (int w = 0; w < kWarps; ++w) {
+            if (pass == 0) {
+                all.m = fmaxf(all.m, sh.refined[w][0]);
+            } else {
+                all.s += sh.refined[w][1];
+                all.t += sh.refined[w][2];
             }
         }
     }
     return all;
+}
+
+// One logit stands far above the others: what its thread added to a sum that has it lost its low bits.  That
+// thread's logits are added up again without it, by all threads of one CTA; d: the y of that logit, which m's
+// rounding keeps from being 0.
+template <bool BF16>
+__device__ __noinline__ Sums sums_without_largest(Shared& sh, const RowOf<BF16>& r, const Joined& all, int ctas, float* d) {
+    constexpr int N = RowOf<BF16>::N;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int from = (all.owner >> 5) * 32 * kAhead + (all.owner & 31), step = ctas * kThreads * kAhead;
+    float s = 0.0f, t = 0.0f, top = -INFINITY;
+    for (int i = threadIdx.x;; i += kThreads) {
+        const int64_t u = from + 32 * (i % kAhead) + static_cast<int64_t>(i / kAhead) * step;
+        if (u - 32 * (i % kAhead) >= r.units) break;
+        float x[N];
+        r.load_part(static_cast<int>(u < r.units ? u : r.units), -INFINITY, x);
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float y = fmaf(fmaxf(x[e], kLeast), kLog2e, -all.m);
+            if (y > -1.0f) {  // (the others are below 2^-4)
+                top = y;
+            } else {
+                const float q = exp2_approx(y);
+                s += q;
+                t = fmaf(q, y, t);
+            }
+        }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        s += __shfl_xor_sync(0xffffffffu, s, o);
+        t += __shfl_xor_sync(0xffffffffu, t, o);
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    }
+    __syncthreads();
+    if (lane == 0) {
+        sh.refined[warp][0] = s;
+        sh.refined[warp][1] = t;
+        sh.refined[warp][2] = top;
+    }
+    __syncthreads();
+    s = all.s;
+    t = all.t;
+    top = sh.refined[0][2];
+    for (int w = 0; w < kWarps; ++w) {
+        s += sh.refined[w][0];
+        t += sh.refined[w][1];
+        top = fmaxf(top, sh.refined[w][2]);
+    }
+    // from m to that logit
+    const float f = exp2_approx(-top);
+    *d = top;
+    return {0.0f, s * f, fmaf(-top, s, t) * f};
 }
 
 template <bool BF16, bool TOP>
@@ -603,42 +674,54 @@ __global__ void __launch_bounds__(kThreads, TOP ? 4 : 6) log_probs_kernel(const 
             }
         }
     }
+    Joined all{mine.m, mine.s, mine.t, 0.0f, 0.0f, (rank * kWarps + warp) * 32 + lane};
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
-        Sums other;
-        other.m = __shfl_xor_sync(0xffffffffu, mine.m, o);
-        other.s = __shfl_xor_sync(0xffffffffu, mine.s, o);
-        other.t = __shfl_xor_sync(0xffffffffu, mine.t, o);
-        mine.join(other);
+        Joined other;
+        other.m = __shfl_xor_sync(0xffffffffu, all.m, o);
+        other.big = __shfl_xor_sync(0xffffffffu, all.big, o);
+        other.big_t = __shfl_xor_sync(0xffffffffu, all.big_t, o);
+        other.s = __shfl_xor_sync(0xffffffffu, all.s, o);
+        other.t = __shfl_xor_sync(0xffffffffu, all.t, o);
+        other.owner = __shfl_xor_sync(0xffffffffu, all.owner, o);
+        all.join(other);
     }
-    if (lane == 0) sh.warp_sums[warp] = mine;
+    if (lane == 0) sh.warp_sums[warp] = all;
     __syncthreads();
-    mine = sh.warp_sums[0];
+    all = sh.warp_sums[0];
 #pragma unroll
-    for (int w = 1; w < kWarps; ++w) mine.join(sh.warp_sums[w]);
+    for (int w = 1; w < kWarps; ++w) all.join(sh.warp_sums[w]);
     if (ctas > 1) {
         if (threadIdx.x == 0 && rank != 0) {
             const uint32_t to = mapa_shared(smem_u32(&sh.cta_sums[rank]), 0);
-            st_shared_cluster_u32(to, __float_as_uint(mine.m));
-            st_shared_cluster_u32(to + 4, __float_as_uint(mine.s));
-            st_shared_cluster_u32(to + 8, __float_as_uint(mine.t));
+            st_shared_cluster_u32(to, __float_as_uint(all.m));
+            st_shared_cluster_u32(to + 4, __float_as_uint(all.big));
+            st_shared_cluster_u32(to + 8, __float_as_uint(all.big_t));
+            st_shared_cluster_u32(to + 12, __float_as_uint(all.s));
+            st_shared_cluster_u32(to + 16, __float_as_uint(all.t));
+            st_shared_cluster_u32(to + 20, static_cast<uint32_t>(all.owner));
         }
         cluster_sync();
         if (rank != 0) return;
-        for (int c = 1; c < ctas; ++c) mine.join(sh.cta_sums[c]);
+        for (int c = 1; c < ctas; ++c) all.join(sh.cta_sums[c]);
     }
-    const bool again = !(mine.m > -1e29f && mine.m < 1e38f);
+    mine = {all.m, all.big + all.s, all.big_t + all.t};
+    const bool again = !(mine.m > -1e29f && mine.m < 1e38f), sure = !again && mine.s < 1.0625f;
+    float d = 0.0f;
     if (again) mine = sums_again<BF16>(sh, r);
-    const float m = mine.m, log2_s = log2f(mine.s);
-    const bool none = mine.s == 0.0f;  // every logit -infinity
+    if (sure) mine = sums_without_largest<BF16>(sh, r, all, ctas, &d);
+    const float m = mine.m, ln_s = sure ? log1pf(mine.s) : log2f(mine.s) * kLn2;  // (m: of `again` alone)
+    const bool none = mine.s == 0.0f && !sure;  // every logit -infinity
     // (far below the others, x - lse is x)
     const auto value = [=](float x) {
         if (none) return -INFINITY;
-        if (again) return fmaf(-kLn2, log2_s, x - m);
-        return (x < -1e37f ? x : (fmaf(x, kLog2e, -m) - log2_s) * kLn2) + 0.0f * mine.s;  // (NaN where s is)
+        if (again) return (x - m) - ln_s;
+        const float y = fmaf(x, kLog2e, -all.m);
+        return (x < -1e37f ? x : sure ? fmaf(y - d, kLn2, -ln_s) : fmaf(y, kLn2, -ln_s)) + 0.0f * mine.s;  // (NaN where s is)
     };
     if (threadIdx.x == 0) {
-        if (p.entropy != nullptr) p.entropy[row] = none ? 0.0f : (log2_s - mine.t / mine.s) * kLn2;
+        if (p.entropy != nullptr)
+            p.entropy[row] = none ? 0.0f : sure ? ln_s - kLn2 * mine.t / (1.0f + mine.s) : ln_s - kLn2 * (mine.t / mine.s);
         if (p.targets != nullptr) {
             const int target = p.targets[row];
             float logp = 0.0f;
@@ -649,7 +732,7 @@ __global__ void __launch_bounds__(kThreads, TOP ? 4 : 6) log_probs_kernel(const 
             p.logp[row] = logp;
         }
     }
-    if constexpr (TOP) top<BF16>(sh, r, shift, groups, p.k, value, p.index + row * p.k, p.score + row * p.k);
+    if constexpr (TOP) top<BF16>(sh, r, shift, groups, p.k, value, p.index + row * p.k, p.score + row * p.k, p.status);
 }
 
 template <bool BF16, bool TOP>

@@ -376,6 +376,7 @@ __device__ __forceinline__ void finish_row(const NormParams& p, const Row<ODD>& 
             for (int e = 0; e < 8; ++e) x[v][e] = fmaf(p.residual_scale, w[e], x[v][e]);
         }
     }
+    if (!dbg_check(at >= 0 && at + p.D <= static_cast<int64_t>(p.M) * p.D, p.status)) return;
     if (p.residual_out != nullptr) {
         R* const to = static_cast<R*>(p.residual_out) + at;
 #pragma unroll
@@ -479,6 +480,7 @@ __global__ void __launch_bounds__(kRingThreads, 2) residual_norm_ring_kernel(con
     __syncthreads();
     auto fetch = [&](int slot, int64_t row) {  // one thread
         const uint32_t bar = smem_u32(&full[slot]), to = smem_u32(ring) + slot * row_bytes;
+        if (!dbg_check(slot < depth && (to & 15u) == 0 && row < p.M, p.status)) return;
         mbar_arrive_expect_tx(bar, row_bytes);
         if (block_bytes != 0) copy_row(to, p.block + row * D, block_bytes, bar);
         copy_row(to + block_bytes, static_cast<const R*>(p.residual) + row * D, stream_bytes, bar);
@@ -596,6 +598,7 @@ __global__ void __launch_bounds__(kWideThreads) residual_norm_wide_kernel(const 
         to[0] = make_float4(x[0], x[1], x[2], x[3]);
         to[1] = make_float4(x[4], x[5], x[6], x[7]);
     };
+    if (!dbg_check(at + p.D <= static_cast<int64_t>(p.M) * p.D, p.status)) return;
     auto stats = [&](float* mean, float* rstd) {
         statistics<true>(
             [&](float absent, const auto& f) {

@@ -111,6 +111,7 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const KvView kv, const
         s[e] = cs.y;
     }
     uint16_t* const row = p.qkv + (m0 + t) * width;
+    if (!dbg_check(m0 + t < p.M && end <= heads && high + 8 <= p.rot, p.status)) return;
     constexpr int kAhead = 4;
     for (int h = begin + h0; h < end; h += kAhead * side) {
         uint4 a[kAhead], b[kAhead];

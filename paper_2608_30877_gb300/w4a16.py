@@ -643,6 +643,8 @@ def kv_rotary(cache: KVCache, qkv: torch.Tensor, slots: torch.Tensor, H: int, ta
     device = _device_of(qkv)
     M = _rotary_qkv(qkv, table, (H + 2 * cache.kv_heads) * 128, device)
     nseq = _sequences(M, seq_start, slots, device)
+    if cache.pages.get_device() != device:
+        raise ValueError("the cache is on another device")
     _check("w4a16_kv_rotary", lib().w4a16_kv_rotary(
         cache._ref, qkv.data_ptr(), _ptr(seq_start), slots.data_ptr(), nseq, M, H, table.turns.data_ptr(),
         table.rot_dim, table.layout, table.attention_factor, _stream_on(stream, device)))

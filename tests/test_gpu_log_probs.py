@@ -160,6 +160,34 @@ def test_sure_and_even(dtype):
     check(x.to(dtype), [17, 17, 4, 5, 3, 29999], 20)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M", [1, 7, 400])
+@pytest.mark.parametrize("V,at", [(300, 299), (32000, 17), (50001, 50000), (131072, 70001)])
+def test_almost_certain(V, at, M, dtype):
+    """One logit far above the others: its log probability is minus the others' sum S, and the entropy about S times
+    their distance, each to S's relative error: 2^-22 + 2^-23 |y| of a term (|y| < 64 bits here) and the chain of
+    additions of `check`, twice for the function's and the products'."""
+    W = _W()
+    gaps = [4.0, 6.0, 9.0, 14.0, 20.0, 30.0, 43.0][:M]
+    x = logits(M, V, dtype, spread=1.0)
+    for i in range(M):
+        x[i, at] = x[i].float().logsumexp(0) + gaps[i % len(gaps)]
+    x[:, at] = x[:, at].float() + (300.0 if dtype is torch.float32 else 0.0)
+    if dtype is torch.float32:
+        x[:, :at] += 300.0
+        x[:, at + 1:] += 300.0
+    t = torch.full((M,), at, dtype=torch.int32, device="cuda")
+    logp, entropy, index, score = W.log_probs(x, t, 2)
+    a = x.double().cpu().numpy()
+    others = np.delete(a - a[:, at:at + 1], at, axis=1)
+    S = np.exp(others).sum(1)
+    H = np.log1p(S) - (np.exp(others) * others).sum(1) / (1 + S)
+    rel = 2 * (2.0 ** -22 + 64 * 2.0 ** -23 + (V / 256 + 50) * 2.0 ** -24)
+    assert (np.abs(f64(logp) + np.log1p(S)) <= rel * S).all()
+    assert (np.abs(f64(entropy) - H) <= 2 * rel * H).all()
+    assert (index[:, 0] == at).all() and torch.equal(score[:, 0], logp)
+
+
 def test_bad_targets():
     W = _W()
     x = logits(4, 1000, torch.bfloat16)
