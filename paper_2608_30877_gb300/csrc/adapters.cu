@@ -585,15 +585,14 @@ __global__ void __launch_bounds__(kThreads, !WHOLE ? 1 : CH == 0 && MB == 0 ? 3 
                                                pack_bf16(acc[2][2 * h], acc[2][2 * h + 1]),
                                                pack_bf16(acc[3][2 * h], acc[3][2 * h + 1])};
                         uint16_t* const to = const_cast<uint16_t*>(from[2 * m + h]) + to_out + n;
-                        if (!dbg_check(to >= p.out && to - p.out + (WHOLE && (kInside || n < columns) ? 8 : 0) <=
-                                                          static_cast<int64_t>(p.M) * p.N, p.status))
-                            continue;
+                        const int64_t end = to - p.out + (WHOLE ? 8 : 1), all = static_cast<int64_t>(p.M) * p.N;
                         if constexpr (WHOLE) {
-                            if (kInside || n < columns) *reinterpret_cast<uint4*>(to) = make_uint4(v[0], v[1], v[2], v[3]);
+                            if ((kInside || n < columns) && dbg_check(to >= p.out && end <= all, p.status))
+                                *reinterpret_cast<uint4*>(to) = make_uint4(v[0], v[1], v[2], v[3]);
                         } else {
 #pragma unroll
                             for (int e = 0; e < 8; ++e)
-                                if (kInside || n + e < columns)
+                                if ((kInside || n + e < columns) && dbg_check(to >= p.out && end + e <= all, p.status))
                                     to[e] = static_cast<uint16_t>(e & 1 ? v[e / 2] >> 16 : v[e / 2]);
                         }
                     }

@@ -562,7 +562,7 @@ __device__ __noinline__ Sums sums_without_largest(Shared& sh, const RowOf<BF16>&
 }
 
 template <bool BF16, bool TOP>
-__global__ void __launch_bounds__(kThreads, TOP ? 4 : 6) log_probs_kernel(const LogProbsParams p, const int shift, const int ctas) {
+__global__ void __launch_bounds__(kThreads, 4) log_probs_kernel(const LogProbsParams p, const int shift, const int ctas) {
     constexpr int N = RowOf<BF16>::N;
     __shared__ Shared sh;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;

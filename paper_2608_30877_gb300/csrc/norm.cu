@@ -439,7 +439,9 @@ __global__ void __launch_bounds__(512, NV <= 3 && !ODD ? 2 : 1) residual_norm_ke
 // memory that bulk copies fill while it is at a row before (the reductions leave the memory idle
 // otherwise: two rows an SM in registers, 4097 rows of 8200 with both layer norms and an fp32 stream 159 us).
 constexpr int kRingThreads = 384;
-constexpr int kRingRows = 4;  // at most
+constexpr int kRingRows = 4;               // at most
+constexpr int kSmBytes = 224 * 1024;       // of an SM's shared memory, for all its rings
+constexpr int kRingBytes = 114 * 1024;     // of one: two CTAs an SM at least
 
 __device__ __forceinline__ void copy_row(uint32_t to, const void* from, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from),
@@ -556,14 +558,16 @@ bool launch_ring(const NormParams& p, int sm_count, cudaStream_t stream, cudaErr
     // as many CTAs an SM as have registers (80 a thread), with two rows each at least
     int ctas = 65536 / (80 * threads);
     if (ctas > 4) ctas = 4;
-    while (ctas > 2 && 224 * 1024 / ctas / row_bytes < 2) --ctas;
-    int depth = 224 * 1024 / ctas / row_bytes;
+    while (ctas > 2 && kSmBytes / ctas / row_bytes < 2) --ctas;
+    int depth = kSmBytes / ctas / row_bytes;
     if (depth > kRingRows) depth = kRingRows;
+    if (depth * row_bytes > kRingBytes) depth = kRingBytes / row_bytes;
     if (depth < 2 || p.M < 2 * ctas * sm_count) return false;
     auto kernel = nv == 2   ? residual_norm_ring_kernel<R, 2>
                   : nv == 3 ? residual_norm_ring_kernel<R, 3>
                             : residual_norm_ring_kernel<R, 4>;
-    *e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, depth * row_bytes);
+    // (the same limit for every size: calls of several threads set it at the same time)
+    *e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes);
     if (*e == cudaSuccess)
         *e = launch_overlapped(kernel, dim3(ctas * sm_count), threads, depth * row_bytes, stream, p, depth);
     return true;
@@ -678,8 +682,9 @@ cudaError_t launch_wide(const NormParams& p, cudaStream_t stream) {
     int threads = 256;  // with two to four units each, as far as that goes
     while (threads < kWideThreads && units > 4 * threads) threads *= 2;
     const int smem = (units + threads - 1) / threads * threads * 32;
+    constexpr int kMost = ((kNormMaxWidth + 14) / 8 + kWideThreads - 1) / kWideThreads * kWideThreads * 32;
     auto kernel = residual_norm_wide_kernel<R, ODD>;
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
     if (e != cudaSuccess) return e;
     return launch_overlapped(kernel, dim3(p.M), threads, smem, stream, p);
 }

@@ -96,10 +96,11 @@ def test_largest():
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("V,k", [(300, 64), (5000, 20), (40000, 64), (100003, 64)])
 def test_ties_and_order(V, k, dtype):
-    """Equal logits by column: all of them, few values, sorted both ways, one value more than k times."""
+    """Equal logits by column: all of them, subnormal ones, few values, sorted both ways, one value more than k times."""
     i = torch.arange(V, device="cuda")
     rows = [torch.zeros(V, device="cuda"), (i % 3).float(), (i % 7 == 6).float() * 5, -(i.float()) / V * 8, i.float() / V * 8,
             torch.where(i >= V - 10, 3.0, 1.0), torch.where(i < k - 1, 9.0, 2.0), torch.where(i % 1000 == 999, 4.0, -4.0),
+            i * 1e-40, -(i * 1e-40),  # (less than the smallest normal numbers)
             torch.where(i == V - 1, 0.0, -0.0), torch.where(i % 2 == 0, -0.0, 0.0), (i // 300).float().remainder(11)]
     check(torch.stack(rows).to(dtype), [0] * len(rows), k)
 
