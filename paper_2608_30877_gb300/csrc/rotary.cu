@@ -75,46 +75,19 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const KvView kv, const
     __shared__ __align__(16) float2 turned[kTokens][kMaxPairs];  // cosine and sine, times the factor
     const int pairs = p.rot / 2;
     const int64_t m0 = static_cast<int64_t>(blockIdx.x) * tokens;
-    grid_launch_dependents();
-    grid_wait();
-    if (threadIdx.x < tokens)
-        position[threadIdx.x] =
-            m0 + threadIdx.x < p.M ? position_of<CACHE>(kv, p, static_cast<int>(m0 + threadIdx.x)) : -1;
-    if (p.seq_start != nullptr && blockIdx.y == 0) check_starts(p.seq_start, p.nseq, p.M, p.status);
-    __syncthreads();
-    for (int i = threadIdx.x; i < tokens * pairs; i += kThreads) {
-        const int t = i / pairs, j = i - t * pairs;
-        const int64_t pos = position[t];
-        if (pos >= 0) {
-            const uint64_t turns = static_cast<uint64_t>(pos) * p.turns[j];
-            float s, c;
-            sincospif(static_cast<float>(static_cast<int32_t>(turns >> 32)) * 4.656612873077393e-10f /* 2^-31 */, &s,
-                      &c);
-            turned[t][j] = make_float2(c * p.factor, s * p.factor);
-        }
-    }
-    __syncthreads();
     // a unit: eight pairs of a head, in two pieces of 16 bytes; the tokens, and heads of each, side by side
     const int units = pairs / 8;
     const int side = kThreads / units / tokens;  // heads of a token
     const int u = threadIdx.x % units, t = threadIdx.x / units / side, h0 = threadIdx.x / units - t * side;
-    if (t >= tokens || position[t] < 0) return;
     const int heads = p.H + p.kv_heads;
     const int begin = static_cast<int>(blockIdx.y) * heads_per_cta, end = min(begin + heads_per_cta, heads);
     const int64_t width = static_cast<int64_t>(heads + p.kv_heads) * p.d;
     const int low = PAIRS ? 16 * u : 8 * u, high = PAIRS ? low + 8 : low + pairs;
-    float c[8], s[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float2 cs = turned[t][8 * u + e];
-        c[e] = cs.x;
-        s[e] = cs.y;
-    }
-    uint16_t* const row = p.qkv + (m0 + t) * width;
-    if (!dbg_check(m0 + t < p.M && end <= heads && high + 8 <= p.rot, p.status)) return;
+    const bool there = t < tokens && m0 + t < p.M;
+    uint16_t* const row = p.qkv + (m0 + (there ? t : 0)) * width;
     constexpr int kAhead = 4;
-    for (int h = begin + h0; h < end; h += kAhead * side) {
-        uint4 a[kAhead], b[kAhead];
+    uint4 a[kAhead], b[kAhead];
+    auto load = [&](int h) {
 #pragma unroll
         for (int k = 0; k < kAhead; ++k)
             if (h + k * side < end) {
@@ -122,6 +95,40 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const KvView kv, const
                 a[k] = __ldcs(reinterpret_cast<const uint4*>(head + low));
                 b[k] = __ldcs(reinterpret_cast<const uint4*>(head + high));
             }
+    };
+    grid_launch_dependents();
+    grid_wait();
+    // (the first heads are on their way while the positions are looked up, a chain of four loads: 46 us of three
+    // long contexts of shared heads without this)
+    if (there) load(begin + h0);
+    if (threadIdx.x < tokens)
+        position[threadIdx.x] =
+            m0 + threadIdx.x < p.M ? position_of<CACHE>(kv, p, static_cast<int>(m0 + threadIdx.x)) : -1;
+    if (p.seq_start != nullptr && blockIdx.y == 0) check_starts(p.seq_start, p.nseq, p.M, p.status);
+    __syncthreads();
+    for (int i = threadIdx.x; i < tokens * pairs; i += kThreads) {
+        const int of = i / pairs, j = i - of * pairs;
+        const int64_t pos = position[of];
+        if (pos >= 0) {
+            const uint64_t turns = static_cast<uint64_t>(pos) * p.turns[j];
+            float s, c;
+            sincospif(static_cast<float>(static_cast<int32_t>(turns >> 32)) * 4.656612873077393e-10f /* 2^-31 */, &s,
+                      &c);
+            turned[of][j] = make_float2(c * p.factor, s * p.factor);
+        }
+    }
+    __syncthreads();
+    if (!there || position[t] < 0) return;
+    if (!dbg_check(end <= heads && high + 8 <= p.rot, p.status)) return;
+    float c[8], s[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float2 cs = turned[t][8 * u + e];
+        c[e] = cs.x;
+        s[e] = cs.y;
+    }
+    for (int h = begin + h0; h < end; h += kAhead * side) {
+        if (h != begin + h0) load(h);
 #pragma unroll
         for (int k = 0; k < kAhead; ++k)
             if (h + k * side < end) {
