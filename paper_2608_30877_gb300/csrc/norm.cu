@@ -3,10 +3,17 @@
 // with post and pre RMS norms v / sqrt(mean v^2 + eps) or layer norms (v - mean) / sqrt(var + eps),
 // each times (offset + weight) plus a bias.
 //
-// A row's values stay in registers between the reductions and the store, so that each is read
-// once and written once, and a variance is the mean of squares about a mean that is known (no
-// difference of large sums).  Up to 1024 columns a warp has a row, else a CTA; a thread has up to
-// kMost pieces of eight columns.  The norm is of h as computed, not as rounded for the store.
+// A row is read once and written once; between the reductions and the store its values stay on the SM, so that a
+// variance is the mean of squares about a mean that is known (no difference of large sums).  The norm is of h as
+// computed, not as rounded for the store.  Bound by HBM.  Where they stay:
+//   registers, a warp to a row up to 1024 columns, else a CTA to a row: 39004 bf16 rows of 12288, RMS, 555 us (6.9 TB/s,
+//     the copy bandwidth);
+//   shared memory filled ahead by bulk copies, for what takes long between load and store (post norms, layer norms, an
+//     fp32 stream): 4097 rows of 8200 with both layer norms, gate and biases on an fp32 stream 93 us (4.3 TB/s; 128
+//     from registers), 20000 of 12288 with layer norms 95% of the copy bandwidth;
+//   shared memory in fp32, a unit of eight columns at a time, for rows wider than 16384 and rows of odd width past a
+//     warp's: 49152 columns 60%, 4099 columns 45% (the vectors' elements load one by one).
+// One row is latency: 2.9 us on the device, the call's host side 13.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <cstdint>
@@ -436,8 +443,9 @@ __global__ void __launch_bounds__(512, NV <= 3 && !ODD ? 2 : 1) residual_norm_ke
 }
 
 // Many rows of whole 16-byte units: as many CTAs as are resident, each with a ring of rows in shared
-// memory that bulk copies fill while it is at a row before (the reductions leave the memory idle
-// otherwise: two rows an SM in registers, 4097 rows of 8200 with both layer norms and an fp32 stream 159 us).
+// memory that bulk copies fill while it is at a row before (the reductions leave the memory idle otherwise).  What is
+// left is issue slots (42%) and the vectors, which the rings leave no room for in L1: five of them come from L2 for every
+// row.  Register pairs (half the arithmetic instructions) took 99 us to 93.
 constexpr int kRingThreads = 384;
 constexpr int kRingRows = 4;               // at most
 constexpr int kSmBytes = 224 * 1024;       // of an SM's shared memory, for all its rings
