@@ -4,9 +4,9 @@
 // both terms of H are positive, so nothing cancels, and y is one multiply-add whose rounding of
 // m is the same for every logit.  Each thread keeps m, s and the other sum of its part of the row, raised
 // to a new m once for 32 (fp32: 16) logits; the parts are joined in a fixed order.  Few rows are split over
-// a cluster of CTAs and joined in its first one.  Logits below -2^100 count as that (q y = 0, not
-// NaN, for -infinity); a row of nothing above -1e29, or with one past 1e38, is summed again by the
-// formula in natural logarithms.
+// a cluster of CTAs and joined in its first one.  Logits below -2^17 count as that (2^y y = 0, not NaN, for
+// -infinity); a row of nothing above -124000, or with one past 726000, is summed again by the formula in natural
+// logarithms.
 //
 // The k largest: the same pass notes the largest logit of each group of neighbours (up to 1024
 // groups).  With t the k-th largest of those, all of the k largest logits are among the groups above
@@ -67,8 +67,12 @@ __device__ __forceinline__ uint4 load_once(const void* p) {
     return v;
 }
 
-constexpr float kLeast = -1.2676506002282294e30f;  // -2^100
-constexpr uint32_t kLeast2 = 0xF180F180u;          // two of it in bf16
+// Logits below count as this: small enough that m's rounding is far below one (a thread may see masked logits
+// alone, of any size), and a power of two, whose own m is exact.
+constexpr float kLeast = -131072.0f;
+constexpr uint32_t kLeast2 = 0xC800C800u;  // two of it in bf16
+// m of rows that the base-2 form holds: what counts as kLeast has no weight there
+constexpr float kFrom = -180000.0f, kTo = 1048576.0f;
 
 // Two fp32 in one register pair.
 __device__ __forceinline__ uint64_t pair(float a, float b) {
@@ -180,7 +184,7 @@ struct RowOf {
             }
         }
     }
-    // The largest of a unit as it is in memory (a NaN where all are), and its columns from -2^100 on.
+    // The largest of a unit as it is in memory (a NaN where all are), and its columns from kLeast on.
     static __device__ __forceinline__ float largest(const uint32_t (&w)[4]) {
         if constexpr (BF16) {
             const uint32_t v = max_bf16x2(max_bf16x2(w[0], w[1]), max_bf16x2(w[2], w[3]));
@@ -465,8 +469,7 @@ __device__ __forceinline__ void top(Shared& sh, const RowOf<BF16>& r, int shift,
     }
 }
 
-// A row's sums about its largest number m, by e^(x - m), for rows that the base-2 form does not hold: all
-// logits below -1e29, or one past 1e38.  m -infinity: no number above that.  All threads of one CTA.
+// A row's sums about its largest number m, by e^(x - m), for rows that the base-2 form does not hold.  m -infinity: no number above that.  All threads of one CTA.
 template <bool BF16>
 __device__ __noinline__ Sums sums_again(Shared& sh, const RowOf<BF16>& r) {
     constexpr int N = RowOf<BF16>::N;
@@ -712,7 +715,7 @@ __global__ void __launch_bounds__(kThreads, 4) log_probs_kernel(const LogProbsPa
         for (int c = 1; c < ctas; ++c) all.join(sh.cta_sums[c]);
     }
     mine = {all.m, all.big + all.s, all.big_t + all.t};
-    const bool again = !(mine.m > -1e29f && mine.m < 1e38f), sure = !again && mine.s < 1.0625f;
+    const bool again = !(mine.m > kFrom && mine.m < kTo), sure = !again && mine.s < 1.0625f;
     float d = 0.0f;
     if (again) mine = sums_again<BF16>(sh, r);
     if (sure) mine = sums_without_largest<BF16>(sh, r, all, ctas, &d);

@@ -208,8 +208,8 @@ __device__ __forceinline__ void clear(float (&parts)[2][kMaxWarps]) {
     if (t < 2 * kMaxWarps && t % kMaxWarps >= static_cast<int>(blockDim.x >> 5)) parts[t / kMaxWarps][t % kMaxWarps] = 0.0f;
 }
 
-// The mean (layer norm; else 0) and 1 / sqrt(mean square about it + eps) of a row.  pairs(f): f(two values) for the
-// thread's, in register pairs; a column that the row has not counts as `absent`.
+// The mean (layer norm; else 0) and 1 / sqrt(mean square about it + eps) of a row.  pairs(absent, f): f(two values) for
+// the thread's, in register pairs; a column that the row has not counts as `absent`.
 template <bool PACKED, typename Pairs>
 __device__ __forceinline__ void statistics(const Pairs& pairs, bool layer, float inv_d, float eps, Reducer& red,
                                            float* mean, float* rstd) {
@@ -396,8 +396,7 @@ __device__ __forceinline__ void finish_row(const NormParams& p, const Row<ODD>& 
     for (int v = 0; v < NV; ++v) store8(p.out + at, r.first(v), r, x[v]);
 }
 
-// A warp or a CTA to a row, which it holds in registers from the first load on: few rows, rows of odd or
-// of large width.
+// A warp (up to 1024 columns) or a CTA to a row, which it holds in registers from the first load on.
 template <typename R, int NV, bool ODD>
 __global__ void __launch_bounds__(512, NV <= 3 && !ODD ? 2 : 1) residual_norm_kernel(const NormParams p, const int group) {
     __shared__ __align__(16) float parts[2][kMaxWarps];

@@ -132,6 +132,24 @@ def test_masks(V, k, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M", [1, 40, 700])
+@pytest.mark.parametrize("size", [1e4, 1.2e5, 1.4e5, 3e5, 1e6, 1e9, 1e10, 1e20, 1e30, 3e38])
+def test_magnitudes(size, M, dtype):
+    """Masks of finite values: where whole runs of logits, as a thread sees them, hold nothing else; whole rows at
+    such a value; and logits as large."""
+    V = 20000
+    x = logits(M, V, dtype)
+    kinds = [lambda r: r[2000:].fill_(-size), lambda r: r[:-3].fill_(-size), lambda r: r.fill_(-size),
+             lambda r: r[5:].sub_(size), lambda r: r.sub_(size), lambda r: r.add_(size), lambda r: r[777:900].add_(size),
+             lambda r: r[3:4].fill_(size), lambda r: r.mul_(size / 8), lambda r: r[::2].fill_(-size)]
+    for i in range(M):
+        kinds[i % len(kinds)](x[i])
+    x.clamp_(torch.finfo(dtype).min, torch.finfo(dtype).max)
+    check(x, [(7 * i) % V for i in range(M)], 5)
+    check(x[:1].clone(), [3], 64)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("V,k", [(90, 20), (5000, 64), (50001, 20)])
 def test_nan_and_infinity(V, k, dtype):
     """They stay in their rows; a NaN comes after every number."""
