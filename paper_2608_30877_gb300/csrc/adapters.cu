@@ -228,6 +228,15 @@ __device__ __forceinline__ void tc_mma_ss(uint32_t d_tmem, uint64_t a_desc, uint
         : "memory");
 }
 
+// One box of 64 columns of rows (of five dimensions, of which three have one entry).
+__device__ __forceinline__ void load_rows(uint32_t to, const CUtensorMap* map, uint32_t bar, int32_t column, int32_t row) {
+    asm volatile(
+        "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%3, %4, %2, %2, %2}], [%5];" ::"r"(to),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(column), "r"(row), "r"(bar)
+        : "memory");
+}
+
 // t of 128 tokens (blockIdx.x) over a slice of K (blockIdx.y), for up to kGroup of the tile's adapters at
 // once.  A stage of the ring: 64 k of the tokens, and of each adapter's rank (rounded up to 16: what the
 // last rows hold is another adapter's, and not looked at).  Warps 0 to 3 take the sums out of tensor
@@ -297,11 +306,11 @@ __global__ void __launch_bounds__(kTcThreads, 2)
                     mbar_arrive_expect_tx(bar, L::kTokens + n * L::kAdapter);
                     const uint32_t end = ring + L::kStages * L::kStage;
                     if (dbg_check(tma_box_ok(at, L::kTokens, 1024, ring, end, s * 64, 2), p.status))
-                        tma_load_2d(at, &map_x, bar, s * 64, static_cast<int32_t>(m0));
+                        load_rows(at, &map_x, bar, s * 64, static_cast<int32_t>(m0));
                     for (int i = 0; i < n; ++i) {
                         const uint32_t to = at + L::kTokens + i * L::kAdapter;
                         if (dbg_check(tma_box_ok(to, L::kAdapter, 1024, ring, end, s * 64, 2), p.status))
-                            tma_load_2d(to, &map_a, bar, s * 64, tile.list[l + i] * p.R);
+                            load_rows(to, &map_a, bar, s * 64, tile.list[l + i] * p.R);
                     }
                     if (it == 0 && !short_limit_ok(bar, 0, &abort_flag, p.status, p.wait_ns)) {
                         ++it;
@@ -617,10 +626,25 @@ __global__ void __launch_bounds__(kThreads, !WHOLE ? 1 : CH == 0 && MB == 0 ? 3 
     }
 }
 
-// Short sequences: tiles of 8 tokens, an adapter of the tile to a CTA.
-bool short_sequences(int64_t M, int64_t nseq) { return M < 16 * nseq; }
-
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Whether tiles of 8 tokens, an adapter of the tile to a CTA, read no more than the larger tiles, which take an
+// adapter once for more tokens but start fewer CTAs.  Which adapters occur is on the device: as many of a tile are
+// counted as it has sequences, and as there are.  (us with small tiles / large ones in both kernels: 8 rows of 8
+// adapters, 12288 x 36864, rank 16 9.8 / 27; 1000 rows of 40 sequences 123 / 63; 200 rows of 2, 12288 x 12288, rank 64
+// 51 / 21; 512 rows of one token with 8 adapters 144 / 76; 256 of them on 4096 x 4096, rank 16 20 / 25.)
+int64_t adapters_of(const AdapterParams& p, int64_t rows) {
+    return std::min<int64_t>(p.pool, std::min(rows, ceil_div(std::min<int64_t>(rows, p.M) * p.nseq, p.M)));
+}
+bool few_down(const AdapterParams& p) {  // (in rows of K)
+    const int64_t group = p.R <= 32 ? 4 : 2, adapters = adapters_of(p, kTcRows);
+    const int64_t passes = ceil_div(adapters, group);
+    return ceil_div(p.M, 8) * adapters_of(p, 8) * p.R + p.M <=
+           ceil_div(p.M, kTcRows) * (adapters * p.R + passes * std::min<int64_t>(kTcRows, p.M));
+}
+bool few_up(const AdapterParams& p) {
+    return ceil_div(p.M, 8) * adapters_of(p, 8) <= ceil_div(p.M, 32) * adapters_of(p, 32);
+}
 
 // CTAs of a cluster that share K: a power of two up to 16.  Few tokens of an adapter each: while there is K for
 // every warp and SMs would be idle (8 at most: 28.7 against 32.4 us with 64 requests).  Tiles of 128 tokens: by the
@@ -667,6 +691,14 @@ cudaError_t launch_cluster(void (*kernel)(P...), dim3 grid, int block, int smem,
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
+// A tensor map of bf16 rows, in boxes of 64 columns (128-byte swizzle).
+int encode_rows(CUtensorMap* map, const void* base, int64_t columns, int64_t rows, int box_rows) {
+    const uint64_t dims[5] = {static_cast<uint64_t>(columns), static_cast<uint64_t>(rows), 1, 1, 1};
+    const uint64_t stride = static_cast<uint64_t>(columns) * 2, strides[4] = {stride, stride, stride, stride};
+    const uint32_t box[5] = {64, static_cast<uint32_t>(box_rows), 1, 1, 1};
+    return encode_5d(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, dims, strides, box);
+}
+
 template <int MT>
 cudaError_t launch_down(const AdapterParams& p, bool few, int sm_count, cudaStream_t stream) {
     const int ctas = cluster_of(p, few, sm_count);
@@ -688,9 +720,10 @@ cudaError_t launch_up(const AdapterParams& p, bool few, int sm_count, cudaStream
     const int rows = few ? 8 : 32, z = few ? (p.M < 8 ? p.M : 8) : 1, unit = kWarps * (few ? kFew : kMany);
     const int64_t tiles = ceil_div(p.M, rows) * z, units = ceil_div(ceil_div(p.N, 32), unit);
     // Few tokens: the CTAs that are resident, at most, as each starts with four loads in a row.  Many: several
-    // turns of them, but four units each at least.
-    int64_t y = few ? (CH == 0 ? 3 : 2) * static_cast<int64_t>(sm_count) / tiles
-                    : std::min(ceil_div(16 * static_cast<int64_t>(sm_count), tiles), units / 4);
+    // turns of them, but four units each at least, unless that leaves SMs idle.
+    const int64_t sms = sm_count;
+    int64_t y = few ? (CH == 0 ? 3 : 2) * sms / tiles
+                    : std::max(std::min(ceil_div(16 * sms, tiles), units / 4), std::min(units, ceil_div(2 * sms, tiles)));
     if (y < 1) y = 1;
     const int64_t chunk = ceil_div(units, y);
     const dim3 grid(static_cast<unsigned>(ceil_div(p.M, rows)), static_cast<unsigned>(ceil_div(units, chunk)), z);
@@ -711,15 +744,15 @@ cudaError_t launch_up(const AdapterParams& p, bool few, int sm_count, cudaStream
 int64_t adapters_workspace_bytes(int64_t M, int64_t R) { return M * R * static_cast<int64_t>(sizeof(uint16_t)); }
 
 cudaError_t launch_adapters(const AdapterParams& p, int sm_count, cudaStream_t stream) {
-    const bool few = short_sequences(p.M, p.nseq);
+    const bool few = few_down(p), few_rows = few_up(p);
     const cudaError_t e = p.R <= 16   ? launch_down<1>(p, few, sm_count, stream)
                           : p.R <= 32 ? launch_down<2>(p, few, sm_count, stream)
                           : p.R <= 48 ? launch_down<3>(p, few, sm_count, stream)
                                       : launch_down<4>(p, few, sm_count, stream);
     if (e != cudaSuccess) return e;
-    return p.R <= 16   ? launch_up<0>(p, few, sm_count, stream)
-           : p.R <= 32 ? launch_up<1>(p, few, sm_count, stream)
-                       : launch_up<2>(p, few, sm_count, stream);
+    return p.R <= 16   ? launch_up<0>(p, few_rows, sm_count, stream)
+           : p.R <= 32 ? launch_up<1>(p, few_rows, sm_count, stream)
+                       : launch_up<2>(p, few_rows, sm_count, stream);
 }
 
 }  // namespace w4a16

@@ -2,7 +2,6 @@
 // TMA descriptor encoding, kernel dispatch and the device status word.
 #include "internal.h"
 #include "kv.h"
-#include "layer.h"
 #include "ptx.cuh"
 #include "w4a16.h"
 
@@ -409,11 +408,6 @@ int library_state(LibraryState* out) {
     return W4A16_OK;
 }
 
-int encode_rows(CUtensorMap* map, const void* base, int64_t columns, int64_t rows, int box_rows) {
-    return encode_2d(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, columns, rows, columns * 2, 64, box_rows,
-                     CU_TENSOR_MAP_SWIZZLE_128B);
-}
-
 int encode_5d(CUtensorMap* map, CUtensorMapDataType dtype, const void* base, const uint64_t dims[5],
               const uint64_t strides[4], const uint32_t box[5]) {
     cuuint64_t d[5], s[4];
@@ -776,4 +770,4 @@ extern "C" const char* w4a16_status_string(int status) {
     }
 }
 
-extern "C" int w4a16_version(void) { return 300; }
+extern "C" int w4a16_version(void) { return 200; }

@@ -77,8 +77,6 @@ struct AdapterParams {
     uint64_t wait_ns;
 };
 constexpr int kAdapterMaxRank = 64;
-// api.cu: a tensor map of bf16 rows, in boxes of 64 columns (128-byte swizzle) and box_rows rows
-int encode_rows(CUtensorMap* map, const void* base, int64_t columns, int64_t rows, int box_rows);
 int64_t adapters_workspace_bytes(int64_t M, int64_t R);
 cudaError_t launch_adapters(const AdapterParams& p, int sm_count, cudaStream_t stream);
 

@@ -750,7 +750,9 @@ cudaError_t launch(const LogProbsParams& p, int sm_count, cudaStream_t stream) {
     const int units = (p.V + 2 * (N - 1)) / N;  // at most, wherever the row begins
     int shift = 5;
     while (units > kGroups << shift) ++shift;
-    while (shift > 0 && units >> shift < 8 * p.k) --shift;
+    // four groups for each alternative at least: what passes the k-th largest of their maxima is then little more than
+    // k (2000 rows of 32000 with 20 52 us; with eight for each, which takes groups of half a warp's units, 63)
+    while (shift > 0 && units >> shift < 4 * p.k) --shift;
     int ctas = 1;
     while (ctas < kMaxCluster && static_cast<int64_t>(p.M) * ctas * 2 <= 4 * sm_count && ctas * kThreads * kAhead < units)
         ctas *= 2;

@@ -65,9 +65,10 @@ def test_a_row_each(M, rank):
 
 @pytest.mark.parametrize("rank", [8, 16, 32, 48, 64])
 @pytest.mark.parametrize("starts", [[0, 1], [0, 64], [0, 100, 100, 333], [0, 7, 8, 9, 63, 64, 65, 200], [5, 6, 130], [0, 1000],
-                                    [0, *range(3, 200, 11)]])
+                                    [0, *range(3, 200, 11)], list(range(301)), [0] * 120 + [50] * 120 + [51, 200]])
 def test_packed(starts, rank):
-    """Sequences that begin and end inside tiles, empty ones, rows before and after them."""
+    """Sequences that begin and end inside tiles, empty ones, more than a tile's list of starts, rows before and
+    after them."""
     n, M = len(starts) - 1, starts[-1] + 5
     for N, K in ((72, 192), (1031, 640), (2048, 256)):
         given = make(M, N, K, rank, 4)
