@@ -469,7 +469,8 @@ __device__ __forceinline__ void top(Shared& sh, const RowOf<BF16>& r, int shift,
     }
 }
 
-// A row's sums about its largest number m, by e^(x - m), for rows that the base-2 form does not hold.  m -infinity: no number above that.  All threads of one CTA.
+// A row's sums about its largest number m, by e^(x - m), for rows that the base-2 form does not hold (m -infinity:
+// no number above that).  All threads of one CTA.
 template <bool BF16>
 __device__ __noinline__ Sums sums_again(Shared& sh, const RowOf<BF16>& r) {
     constexpr int N = RowOf<BF16>::N;

@@ -183,7 +183,7 @@ def test_of_a_cache_refusals():
         assert torch.equal(qkv[-bad:], before[-bad:])
     # a refused growth: the step's rows are left alone
     W.kv_extend(c, KV.i32([0]), KV.i32([100000]))
-    assert W.get_device_error() == W.ERR_CAPACITY or True
+    assert W.get_device_error() != W.OK
     qkv = make(2, 4, 2)
     before = qkv.clone()
     W.kv_rotary(c, qkv, KV.i32([0, 1]), 4, table)
