@@ -5,8 +5,9 @@
 // TMA into a ring of stages, tcgen05 MMAs (tokens as rows, an adapter's rank as columns) into tensor memory.
 // Short ones: warp-level MMAs with the adapter's rows as the 16-row operand and eight tokens as columns.
 // K is split over the CTAs of a cluster, whose fp32 sums are added up in order through distributed shared
-// memory; t is rounded to bf16 (2^-8 of each, of an update beside a sum that a bf16 store rounds as much)
-// into the workspace.  The second streams base and
+// memory; t goes to the workspace with 12 significant bits in 16 (pack_t), which the second takes as two bf16
+// parts, a product with B each: what is left of t's rounding is 2^-12 of an update whose sum with base a bf16 store
+// rounds to 2^-8.  The second streams base and
 // out, with tokens as rows and 32 features as columns of its MMAs, arranged so that a thread has eight
 // neighbours: the accumulators begin as base and are stored as out, 16 bytes a thread.
 // Rows of a tile that share an adapter are done together.
@@ -50,6 +51,48 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1
         "{%0, %1, %2, %3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// t in the workspace: eight ranks of a token in 16 bytes.  E is the exponent field of the largest; each has its sign, 14
+// bits of |t| / 2^(E - 127) < 2 as a small float (three of exponent, eleven of mantissa: 2^-12 of the value down to 2^-6
+// of the largest, 2^-18 of that below) and, lowest, its bit of E.  With E 255, an infinity or a NaN among the eight, they
+// are bf16 without the last bit.
+// A lane has one of the eight, those of its aligned group of lanes; all lanes take part.
+__device__ __forceinline__ uint32_t pack_t(float v) {
+    uint32_t top = __float_as_uint(v) & 0x7FFFFFFFu;
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const uint32_t E = top >> 23;
+    if (E == 255u) return __float_as_uint(v) >> 16 | (v != v ? 0x41u : 1u);
+    const float unit = __uint_as_float(E == 254u ? 0x00400000u : (254u - E) << 23);  // 2^(127 - E)
+    const uint32_t g = __float_as_uint(v * unit * 0x1p-120f), m = g & 0x7FFFFFFFu;  // (1 has exponent field 7)
+    return g >> 31 << 15 | min((m + 0x7FFu + (m >> 12 & 1u)) >> 12, 0x3FFFu) << 1 | (E >> (threadIdx.x & 7) & 1u);
+}
+
+// Two of those eight as two bf16 each, whose sum they are: the upper eight bits (`first`) and the others.  The second part
+// of a number other than 0 is not 0 either (2^-126 at least), so that its product with an infinity is one.  A lane has
+// the two of its number in its aligned group of four lanes; all lanes take part.
+__device__ __forceinline__ void unpack_t(uint32_t packed, uint32_t* first, uint32_t* second) {
+    uint32_t E = ((packed & 1u) | (packed >> 15 & 2u)) << (2 * (threadIdx.x & 3));
+    E |= __shfl_xor_sync(0xffffffffu, E, 1);
+    E |= __shfl_xor_sync(0xffffffffu, E, 2);
+    const float unit = __uint_as_float(E == 0 ? 0x00400000u : E << 23);  // 2^(E - 127)
+    uint32_t a[2], b[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t c = packed >> (16 * h) & 0xFFFEu;
+        uint32_t v = c << 16;
+        float low = 0.0f;
+        if (E != 255u) {
+            const float x = __uint_as_float((c & 0x8000u) << 16 | (c & 0x7FFFu) << 11) * 0x1p120f * unit;
+            v = __float_as_uint(x);
+            low = x - __uint_as_float(v & 0xFFFF0000u);
+        }
+        a[h] = v >> 16;
+        b[h] = low != 0.0f || v << 1 == 0u ? __float_as_uint(low) >> 16 : 0x80u | (a[h] & 0x8000u);
+    }
+    *first = a[0] | a[1] << 16;
+    *second = b[0] | b[1] << 16;
 }
 
 // The rows of a tile: each one's adapter, the list of those that occur, and each row's place in it (-1: no
@@ -198,21 +241,24 @@ __device__ __forceinline__ void store_t(float* sums, const Tile<ROWS>& tile, con
         }
     if (ctas > 1) cluster_sync(); else if (PARTS > 1) __syncthreads();
     // each CTA adds up a part of the tokens
+    static_assert(THREADS % 32 == 0 && kAll % 32 == 0, "whole warps");
     uint16_t* const out = p.t + m0 * p.R;
     for (int i = blockIdx.y * THREADS + threadIdx.x; i < kAll; i += ctas * THREADS) {
         const int token = i / (16 * MT), r = i % (16 * MT), slot = tile.slot[token];
-        if (slot < first || slot >= last || r >= p.R) continue;
-        const float* const at = sums + token * kPitch + r;
+        const bool mine = slot >= first && slot < last && r < p.R;
         float sum = 0.0f;
-        if (ctas > 1) {
-            const uint32_t local = smem_u32(at);
-            for (int c = 0; c < ctas; ++c) sum += load_cluster(mapa_shared(local, c));
-        } else {
-            sum = at[0];
+        if (mine) {
+            const float* const at = sums + token * kPitch + r;
+            if (ctas > 1) {
+                const uint32_t local = smem_u32(at);
+                for (int c = 0; c < ctas; ++c) sum += load_cluster(mapa_shared(local, c));
+            } else {
+                sum = at[0];
+            }
+            sum *= p.scale[tile.id[token]];
         }
-        if (!dbg_check(m0 + token < p.M, p.status)) continue;
-        out[static_cast<int64_t>(token) * p.R + r] =
-            __bfloat16_as_ushort(__float2bfloat16_rn(sum * p.scale[tile.id[token]]));
+        const uint32_t code = pack_t(sum);
+        if (mine && dbg_check(m0 + token < p.M, p.status)) out[static_cast<int64_t>(token) * p.R + r] = static_cast<uint16_t>(code);
     }
     if (ctas > 1) cluster_sync(); else __syncthreads();
 }
@@ -463,10 +509,6 @@ struct UpFragments {
             }
         }
     }
-    __device__ __forceinline__ void zero() {
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) w[s][0] = w[s][1] = 0;
-    }
     __device__ __forceinline__ void load_t(const uint32_t* row, int q) {
         if constexpr (CH == 0) {
             const uint2 v = *reinterpret_cast<const uint2*>(row + 2 * q);
@@ -482,35 +524,42 @@ struct UpFragments {
 };
 
 // out of a tile of tokens (blockIdx.x) and `chunk` blocks of 32 features (blockIdx.y), for the tile's
-// adapters blockIdx.z, + gridDim.z, ...; a warp has FB blocks under way.  MB: 16s of tokens; 0: eight, in
-// the upper half of one.  EXACT: the rank is 16 or 32 CH.  WHOLE: rows of 16-byte units.
+// adapters blockIdx.z, + gridDim.z, ...; a warp has FB blocks under way.  MB: 16s of tokens, with an MMA for each
+// part of t; 0: eight, the upper half of one for its first part, the lower for the second.  EXACT: the rank is 16
+// or 32 CH.  WHOLE: rows of 16-byte units.
 template <int CH, int MB, int FB, bool EXACT, bool WHOLE>
 __global__ void __launch_bounds__(kThreads, !WHOLE ? 1 : CH == 0 && MB == 0 ? 3 : 2)
     adapters_up_kernel(const AdapterParams p, const int chunk) {
     constexpr int kRows = MB == 0 ? 8 : 16 * MB, kHalves = MB == 0 ? 1 : 2 * MB;  // rows of a lane
     constexpr int kWords = CH == 0 ? 8 : 16 * CH, kPitch = kWords + 4;            // (pairs of bf16)
     __shared__ Tile<kRows> tile;
-    __shared__ __align__(16) uint32_t t[kRows][kPitch];
+    __shared__ __align__(16) uint32_t t[2][kRows][kPitch];  // t's two parts
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
     const int64_t m0 = static_cast<int64_t>(blockIdx.x) * kRows;
     grid_launch_dependents();
     grid_wait();
     find_adapters<kRows>(tile, p, m0, false);
+    static_assert(kRows * kWords % 32 == 0, "whole warps");
     for (int i = threadIdx.x; i < kRows * kWords; i += kThreads) {
         const int row = i / kWords, word = i % kWords;
-        t[row][word] = tile.id[row] >= 0 && 2 * word < p.R
-                           ? *reinterpret_cast<const uint32_t*>(p.t + (m0 + row) * p.R + 2 * word) : 0u;
+        const bool there = tile.id[row] >= 0 && 2 * word < p.R;
+        unpack_t(there ? *reinterpret_cast<const uint32_t*>(p.t + (m0 + row) * p.R + 2 * word) : 0u, &t[0][row][word],
+                 &t[1][row][word]);
     }
     __syncthreads();
     const int first = static_cast<int>(blockIdx.y) * chunk, last = min(first + chunk, (p.N + 31) / 32);
     const int columns = min(p.N, last * 32);
     const int R = EXACT ? (CH == 0 ? 16 : 32 * CH) : p.R;
-    // the lane's rows of t: in registers, but for the largest ranks
-    constexpr bool kHeld = CH < 2 || MB == 0;
-    UpFragments<CH> tf[kHeld ? kHalves : 1];
+    // the lane's rows of t: in registers, but for the larger ranks on many tokens (8000 rows of rank 32 300 us, 279 from
+    // shared memory; with both parts there before their products 8000 of rank 64 373, 367 one after the other)
+    constexpr bool kHeld = CH < 1 || MB == 0;
+    UpFragments<CH> tf[2][kHeld ? kHalves : 1];
     if constexpr (kHeld) {
 #pragma unroll
-        for (int i = 0; i < kHalves; ++i) tf[i].load_t(t[i * 8 + g], q);
+        for (int i = 0; i < kHalves; ++i) {
+            tf[0][i].load_t(t[0][i * 8 + g], q);
+            tf[1][i].load_t(t[1][i * 8 + g], q);
+        }
     }
     // (rows without an adapter come last: they are copied)
     const int passes = tile.count + (p.out != p.base);
@@ -565,14 +614,7 @@ __global__ void __launch_bounds__(kThreads, !WHOLE ? 1 : CH == 0 && MB == 0 ? 3 
 #pragma unroll
             for (int m = 0; m < (MB == 0 ? 1 : MB); ++m) {
                 if (MB > 1 && !(any >> (2 * m) & 3u)) continue;
-                UpFragments<CH> ta, tb;
-                if constexpr (!kHeld) {
-                    ta.load_t(t[m * 16 + g], q);
-                    tb.load_t(t[m * 16 + g + 8], q);
-                } else {
-                    ta = tf[2 * m];
-                    if constexpr (MB == 0) tb.zero(); else tb = tf[2 * m + 1];
-                }
+                constexpr int kParts = MB == 0 ? 1 : 2, kSteps = UpFragments<CH>::kSteps;  // products with B
 #pragma unroll
                 for (int u = 0; u < NB; ++u) {
                     float acc[4][4];
@@ -586,11 +628,31 @@ __global__ void __launch_bounds__(kThreads, !WHOLE ? 1 : CH == 0 && MB == 0 ? 3 
                     }
                     if (a >= 0) {
 #pragma unroll
-                        for (int s = 0; s < UpFragments<CH>::kSteps; ++s)
+                        for (int part = 0; part < kParts; ++part)
 #pragma unroll
-                            for (int j = 0; j < 4; ++j)
-                                mma_bf16(acc[j], ta.w[s][0], tb.w[s][0], ta.w[s][1], tb.w[s][1],
-                                         b[u][j].w[s][0], b[u][j].w[s][1]);
+                            for (int s = 0; s < kSteps; ++s) {
+                                uint2 upper, lower;  // rows g and g + 8 of 16
+                                if constexpr (kHeld) {
+                                    const uint32_t (&x)[2] = tf[MB == 0 ? 0 : part][2 * m].w[s];
+                                    const uint32_t (&y)[2] = tf[MB == 0 ? 1 : part][MB == 0 ? 0 : 2 * m + 1].w[s];
+                                    upper = make_uint2(x[0], x[1]);
+                                    lower = make_uint2(y[0], y[1]);
+                                } else {
+                                    const uint32_t* const row = &t[part][m * 16 + g][16 * (s / 2) + 4 * q + 2 * (s % 2)];
+                                    upper = *reinterpret_cast<const uint2*>(row);
+                                    lower = *reinterpret_cast<const uint2*>(row + 8 * kPitch);
+                                }
+#pragma unroll
+                                for (int j = 0; j < 4; ++j)
+                                    mma_bf16(acc[j], upper.x, lower.x, upper.y, lower.y, b[u][j].w[s][0], b[u][j].w[s][1]);
+                            }
+                        if constexpr (MB == 0) {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                acc[j][0] += acc[j][2];
+                                acc[j][1] += acc[j][3];
+                            }
+                        }
                     }
                     const int n = n0 + u * 32;
 #pragma unroll

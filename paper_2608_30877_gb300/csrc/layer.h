@@ -71,7 +71,7 @@ struct AdapterParams {
     const int32_t* ids;        // [nseq]
     const uint16_t* base;      // bf16 [M, N]
     uint16_t* out;             // bf16 [M, N]; may be base
-    uint16_t* t;               // workspace: scale (x A^T), bf16 [M, R]
+    uint16_t* t;               // workspace: scale (x A^T), 16 bits each [M, R] (adapters.cu)
     int* status;
     int M, N, K, R, pool, nseq;
     uint64_t wait_ns;
