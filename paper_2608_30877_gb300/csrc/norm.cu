@@ -180,23 +180,19 @@ struct Reducer {
     int warps;  // of the row; 1: no shared memory
     int turn;
 
-    template <bool MAX>
-    __device__ __forceinline__ float reduce(float x) {
+    __device__ __forceinline__ float sum(float x) {
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            const float y = __shfl_xor_sync(0xffffffffu, x, o);
-            x = MAX ? fmaxf(x, y) : x + y;
-        }
+        for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
         if (warps == 1) return x;
         float* const p = parts[turn & 1];
         ++turn;
         if ((threadIdx.x & 31) == 0) p[threadIdx.x >> 5] = x;
         __syncthreads();
-        // (entries past the last warp's are 0, which changes neither sums nor maxima of magnitudes)
+        // (entries past the last warp's are 0)
         x = 0.0f;
         for (int w = 0; w < warps; w += 4) {
             const float4 v = *reinterpret_cast<const float4*>(p + w);
-            x = MAX ? fmaxf(fmaxf(fmaxf(x, v.x), fmaxf(v.y, v.z)), v.w) : x + ((v.x + v.y) + (v.z + v.w));
+            x += (v.x + v.y) + (v.z + v.w);
         }
         return x;
     }
@@ -209,17 +205,18 @@ __device__ __forceinline__ void clear(float (&parts)[2][kMaxWarps]) {
 }
 
 // The mean (layer norm; else 0) and 1 / sqrt(mean square about it + eps) of a row.  pairs(absent, f): f(two values) for
-// the thread's, in register pairs; a column that the row has not counts as `absent`.
-template <bool PACKED, typename Pairs>
-__device__ __forceinline__ void statistics(const Pairs& pairs, bool layer, float inv_d, float eps, Reducer& red,
-                                           float* mean, float* rstd) {
-    float m = 0.0f;
-    if (layer) {
+// the thread's, in register pairs; a column that the row has not counts as `absent`.  scale(s): the thread's values
+// times s, in their place.
+template <bool PACKED, typename Pairs, typename Scale>
+__device__ __forceinline__ void statistics(const Pairs& pairs, const Scale& scale, bool layer, float inv_d, float eps,
+                                           Reducer& red, float* mean, float* rstd) {
+    const auto mean_of = [&]() {
         // (a sum of x / D: one of x could overflow)
         uint64_t sum = 0;
         pairs(0.0f, [&](uint64_t x) { sum = fma2(x, pair(inv_d, inv_d), sum); });
-        m = red.reduce<false>(both(sum).x + both(sum).y);
-    }
+        return red.sum(both(sum).x + both(sum).y);
+    };
+    float m = layer ? mean_of() : 0.0f;
     uint64_t ss = 0;
     if (PACKED || layer) {
         pairs(m, [&](uint64_t x) {
@@ -231,24 +228,25 @@ __device__ __forceinline__ void statistics(const Pairs& pairs, bool layer, float
         pairs(0.0f, [&](uint64_t x) { sum = fmaf(both(x).x, both(x).x, fmaf(both(x).y, both(x).y, sum)); });
         ss = pair(sum, 0.0f);
     }
-    const float total = red.reduce<false>(both(ss).x + both(ss).y);
+    float total = red.sum(both(ss).x + both(ss).y);
     *mean = m;
     *rstd = rsqrtf(fmaf(total, inv_d, eps));
     if (total < 1e38f) return;
-    // Squares that overflow, of values that do not: divided by a power of two near the largest.  (The
-    // branch is the same for all threads of the row.  An infinity or a NaN gives 0 or NaN, as the
-    // formula has it.)
-    float top = 0.0f;
-    pairs(m, [&](uint64_t x) { top = fmaxf(top, fmaxf(fabsf(both(x).x - m), fabsf(both(x).y - m))); });
-    top = red.reduce<true>(top);
-    if (!(top < INFINITY) || total != total) return;
-    const float s = __uint_as_float((253u << 23) - (__float_as_uint(top) & 0x7F800000u));  // 2^-exponent / 2
+    // Squares that overflow, of values that may not (and differences from the mean, and the mean's sum, of the largest
+    // finite ones): the row is taken again times 2^-76, which leaves its norm as it is.  The root mean square was 2^55
+    // at least, so that what counts stays a normal number and rstd below 2^22, as eps has it elsewhere; 49152 squares of
+    // 2^(129 - 76) are far from overflow.  (The branch is the same for all threads of the row.  An infinity or a NaN gives
+    // 0 or NaN, as the formula has it.)
+    scale(0x1p-76f);
+    m = layer ? mean_of() : 0.0f;
     ss = 0;
     pairs(m, [&](uint64_t x) {
-        const uint64_t c = mul2(add2(x, pair(-m, -m)), pair(s, s));
+        const uint64_t c = add2(x, pair(-m, -m));
         ss = fma2(c, c, ss);
     });
-    *rstd = s * rsqrtf(red.reduce<false>(both(ss).x + both(ss).y) * inv_d);  // (eps s^2 is far below half a step)
+    total = red.sum(both(ss).x + both(ss).y);
+    *mean = m;
+    *rstd = rsqrtf(fmaf(total, inv_d, 1e-37f));  // (eps is far below half a step; not 1 / 0 where all are equal)
 }
 
 // f(two values) for a piece's pairs, with `absent` where the row has no column.
@@ -268,12 +266,18 @@ __device__ __forceinline__ void piece_pairs(const float (&x)[8], int c, const Ro
 }
 
 template <bool PACKED, int NV, bool ODD>
-__device__ __forceinline__ void statistics(const float (&x)[NV][8], bool layer, const Row<ODD>& r, float inv_d, float eps,
+__device__ __forceinline__ void statistics(float (&x)[NV][8], bool layer, const Row<ODD>& r, float inv_d, float eps,
                                            Reducer& red, float* mean, float* rstd) {
     statistics<PACKED>(
         [&](float absent, const auto& f) {
 #pragma unroll
             for (int v = 0; v < NV; ++v) piece_pairs(x[v], r.first(v), r, absent, f);
+        },
+        [&](float s) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[v][e] *= s;
         },
         layer, inv_d, eps, red, mean, rstd);
 }
@@ -617,6 +621,15 @@ __global__ void __launch_bounds__(kWideThreads) residual_norm_wide_kernel(const 
                     float x[8];
                     get(v, x);
                     piece_pairs(x, r.first(v), r, absent, f);
+                }
+            },
+            [&](float s) {
+                for (int v = 0; v < own; ++v) {
+                    float x[8];
+                    get(v, x);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] *= s;
+                    put(v, x);
                 }
             },
             p.layer, inv_d, p.eps, red, mean, rstd);
