@@ -339,7 +339,7 @@ __global__ void __launch_bounds__(kTcThreads, 2)
     bool alive = true;  // no wait of this CTA ran out: else only the cluster's barriers are kept
     for (int l = 0, turn = 0; l < tile.count; l += L::kGroup, ++turn) {
         const int n = min(L::kGroup, tile.count - l);
-        bool ok = true;
+        bool ok = true, drained = false;  // drained: the MMAs' last commit is to `drain`
         if (alive && warp == 4) {
             if (lane == 0) {
                 for (int s = k.from; s < k.to; ++s, ++it) {
@@ -364,9 +364,6 @@ __global__ void __launch_bounds__(kTcThreads, 2)
                         break;
                     }
                 }
-                if (!ok)  // its copies land before the CTA goes on
-                    for (uint32_t i = it > L::kStages ? it - L::kStages : 0; i < it; ++i)
-                        settle(smem_u32(&full[i % L::kStages]), (i / L::kStages) & 1u);
             }
             __syncwarp();
             it = __shfl_sync(0xffffffffu, it, 0);
@@ -391,15 +388,9 @@ __global__ void __launch_bounds__(kTcThreads, 2)
                 }
                 __syncwarp();
             }
-            if (elect_one()) {
-                if (ok) {
-                    tc_commit(smem_u32(&done));
-                } else {
-                    tc_commit(smem_u32(&drain));
-                    settle(smem_u32(&drain), 0);
-                }
-            }
+            if (elect_one()) tc_commit(smem_u32(ok ? &done : &drain));
             __syncwarp();
+            drained = !ok;
         } else if (alive && warp < 4) {
             ok = wait_warp<false, 64>(smem_u32(&done), turn & 1, &abort_flag, p.status, p.wait_ns);
             if (ok) {
@@ -422,7 +413,17 @@ __global__ void __launch_bounds__(kTcThreads, 2)
                 tc_fence_before();
             }
         }
-        alive = !__syncthreads_or(alive && !ok) && alive;
+        // A CTA in which any role gave up lets all that it has in flight end, whatever the others' own waits said (a
+        // producer with a stage for every copy waits for none, and MMAs may all have been issued): the last copy into each
+        // stage, and the commit behind the MMAs.
+        if (__syncthreads_or(alive && !ok) && alive) {
+            alive = false;
+            if (warp == 4 && lane == 0)
+                for (uint32_t i = it > L::kStages ? it - L::kStages : 0; i < it; ++i)
+                    settle(smem_u32(&full[i % L::kStages]), (i / L::kStages) & 1u);
+            if (warp == 5) settle(smem_u32(drained ? &drain : &done), drained ? 0 : turn & 1);
+            __syncthreads();
+        }
         store_t<kTcThreads, 1, kTcRows, MT>(sums, tile, p, m0, l, l + n);
         // (the next copies into the ring come behind what was read and written here)
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
