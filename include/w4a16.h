@@ -598,7 +598,10 @@ int w4a16_selftest_route(int64_t M, int64_t N, int64_t K, int64_t g, int activat
 /* Static text for a status code; never NULL. */
 const char* w4a16_status_string(int status);
 
-/* Library version as major*10000 + minor*100 + patch. */
+/*
+ * Library version as major*10000 + minor*100 + patch: 200 has no w4a16_residual_norm, w4a16_rotary_table, w4a16_rotary,
+ * w4a16_kv_rotary, w4a16_log_probs and w4a16_add_adapters, 300 does.
+ */
 int w4a16_version(void);
 
 #ifdef __cplusplus

@@ -769,5 +769,3 @@ extern "C" const char* w4a16_status_string(int status) {
         default: return "unknown status";
     }
 }
-
-extern "C" int w4a16_version(void) { return 200; }
