@@ -510,26 +510,23 @@ struct UpFragments {
             }
         }
     }
-    __device__ __forceinline__ void load_t(const uint32_t* row, int q) {
-        if constexpr (CH == 0) {
-            const uint2 v = *reinterpret_cast<const uint2*>(row + 2 * q);
-            w[0][0] = v.x, w[0][1] = v.y;
-        } else {
-#pragma unroll
-            for (int c = 0; c < CH; ++c) {
-                const uint4 v = *reinterpret_cast<const uint4*>(row + 16 * c + 4 * q);
-                w[2 * c][0] = v.x, w[2 * c][1] = v.y, w[2 * c + 1][0] = v.z, w[2 * c + 1][1] = v.w;
-            }
-        }
-    }
 };
+
+// 16 rows and 16 k of t's parts in shared memory, as an MMA takes them: lanes 8 i .. 8 i + 7 have the rows' addresses of
+// piece i.
+__device__ __forceinline__ void load_t(uint32_t (&w)[4], const uint32_t* row) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                 : "r"(smem_u32(row))
+                 : "memory");
+}
 
 // out of a tile of tokens (blockIdx.x) and `chunk` blocks of 32 features (blockIdx.y), for the tile's
 // adapters blockIdx.z, + gridDim.z, ...; a warp has FB blocks under way.  MB: 16s of tokens, with an MMA for each
 // part of t; 0: eight, the upper half of one for its first part, the lower for the second.  EXACT: the rank is 16
 // or 32 CH.  WHOLE: rows of 16-byte units.
 template <int CH, int MB, int FB, bool EXACT, bool WHOLE>
-__global__ void __launch_bounds__(kThreads, !WHOLE ? 1 : CH == 0 && MB == 0 ? 3 : 2)
+__global__ void __launch_bounds__(kThreads, !WHOLE ? 1 : 2)
     adapters_up_kernel(const AdapterParams p, const int chunk) {
     constexpr int kRows = MB == 0 ? 8 : 16 * MB, kHalves = MB == 0 ? 1 : 2 * MB;  // rows of a lane
     constexpr int kWords = CH == 0 ? 8 : 16 * CH, kPitch = kWords + 4;            // (pairs of bf16)
@@ -544,23 +541,29 @@ __global__ void __launch_bounds__(kThreads, !WHOLE ? 1 : CH == 0 && MB == 0 ? 3 
     for (int i = threadIdx.x; i < kRows * kWords; i += kThreads) {
         const int row = i / kWords, word = i % kWords;
         const bool there = tile.id[row] >= 0 && 2 * word < p.R;
-        unpack_t(there ? *reinterpret_cast<const uint32_t*>(p.t + (m0 + row) * p.R + 2 * word) : 0u, &t[0][row][word],
-                 &t[1][row][word]);
+        // (in the order in which the products take them: a lane's pieces of B are k in a row of several MMAs)
+        const int at = CH == 0 ? word % 2 * 4 + word / 2 : word / 16 * 16 + word % 4 * 4 + word / 4 % 4;
+        unpack_t(there ? *reinterpret_cast<const uint32_t*>(p.t + (m0 + row) * p.R + 2 * word) : 0u, &t[0][row][at],
+                 &t[1][row][at]);
     }
     __syncthreads();
     const int first = static_cast<int>(blockIdx.y) * chunk, last = min(first + chunk, (p.N + 31) / 32);
     const int columns = min(p.N, last * 32);
     const int R = EXACT ? (CH == 0 ? 16 : 32 * CH) : p.R;
-    // the lane's rows of t: in registers, but for the larger ranks on many tokens (8000 rows of rank 32 300 us, 279 from
-    // shared memory; with both parts there before their products 8000 of rank 64 373, 367 one after the other)
+    // t: in registers, but for the larger ranks on many tokens (8000 rows of rank 32 303 us, 242 from shared memory)
+    constexpr int kSteps = UpFragments<CH>::kSteps, kTiles = MB == 0 ? 1 : MB, kParts = MB == 0 ? 1 : 2;
     constexpr bool kHeld = CH < 1 || MB == 0;
-    UpFragments<CH> tf[2][kHeld ? kHalves : 1];
+    const uint32_t* const t_lane =
+        MB == 0 ? &t[lane >> 3 & 1][lane & 7][lane >> 4 << 2] : &t[0][lane & 15][lane >> 4 << 2];
+    auto load_step = [&](uint32_t (&w)[4], int m, int part, int s) { load_t(w, t_lane + (part * kRows + m * 16) * kPitch + 8 * s); };
+    uint32_t tf[kHeld ? kTiles : 1][kParts][kSteps][4];
     if constexpr (kHeld) {
 #pragma unroll
-        for (int i = 0; i < kHalves; ++i) {
-            tf[0][i].load_t(t[0][i * 8 + g], q);
-            tf[1][i].load_t(t[1][i * 8 + g], q);
-        }
+        for (int m = 0; m < kTiles; ++m)
+#pragma unroll
+            for (int part = 0; part < kParts; ++part)
+#pragma unroll
+                for (int s = 0; s < kSteps; ++s) load_step(tf[m][part][s], m, part, s);
     }
     // (rows without an adapter come last: they are copied)
     const int passes = tile.count + (p.out != p.base);
@@ -613,9 +616,8 @@ __global__ void __launch_bounds__(kThreads, !WHOLE ? 1 : CH == 0 && MB == 0 ? 3 
                     }
             }
 #pragma unroll
-            for (int m = 0; m < (MB == 0 ? 1 : MB); ++m) {
+            for (int m = 0; m < kTiles; ++m) {
                 if (MB > 1 && !(any >> (2 * m) & 3u)) continue;
-                constexpr int kParts = MB == 0 ? 1 : 2, kSteps = UpFragments<CH>::kSteps;  // products with B
 #pragma unroll
                 for (int u = 0; u < NB; ++u) {
                     float acc[4][4];
@@ -632,20 +634,12 @@ __global__ void __launch_bounds__(kThreads, !WHOLE ? 1 : CH == 0 && MB == 0 ? 3 
                         for (int part = 0; part < kParts; ++part)
 #pragma unroll
                             for (int s = 0; s < kSteps; ++s) {
-                                uint2 upper, lower;  // rows g and g + 8 of 16
-                                if constexpr (kHeld) {
-                                    const uint32_t (&x)[2] = tf[MB == 0 ? 0 : part][2 * m].w[s];
-                                    const uint32_t (&y)[2] = tf[MB == 0 ? 1 : part][MB == 0 ? 0 : 2 * m + 1].w[s];
-                                    upper = make_uint2(x[0], x[1]);
-                                    lower = make_uint2(y[0], y[1]);
-                                } else {
-                                    const uint32_t* const row = &t[part][m * 16 + g][16 * (s / 2) + 4 * q + 2 * (s % 2)];
-                                    upper = *reinterpret_cast<const uint2*>(row);
-                                    lower = *reinterpret_cast<const uint2*>(row + 8 * kPitch);
-                                }
+                                uint32_t w[4];
+                                if constexpr (!kHeld) load_step(w, m, part, s);
+                                const uint32_t (&x)[4] = kHeld ? tf[kHeld ? m : 0][part][s] : w;
 #pragma unroll
                                 for (int j = 0; j < 4; ++j)
-                                    mma_bf16(acc[j], upper.x, lower.x, upper.y, lower.y, b[u][j].w[s][0], b[u][j].w[s][1]);
+                                    mma_bf16(acc[j], x[0], x[1], x[2], x[3], b[u][j].w[s][0], b[u][j].w[s][1]);
                             }
                         if constexpr (MB == 0) {
 #pragma unroll
@@ -693,9 +687,10 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Whether tiles of 8 tokens, an adapter of the tile to a CTA, read no more than the larger tiles, which take an
 // adapter once for more tokens but start fewer CTAs.  Which adapters occur is on the device: as many of a tile are
-// counted as it has sequences, and as there are.  (us with small tiles / large ones in both kernels: 8 rows of 8
-// adapters, 12288 x 36864, rank 16 9.8 / 27; 1000 rows of 40 sequences 123 / 63; 200 rows of 2, 12288 x 12288, rank 64
-// 51 / 21; 512 rows of one token with 8 adapters 144 / 76; 256 of them on 4096 x 4096, rank 16 20 / 25.)
+// counted as it has sequences, and as there are.  (us with small tiles / large ones in both kernels, 12288 x 36864 of
+// rank 16: 8 rows of 8 adapters 9.8 / 27, 64 of 48 24 / 129, 1000 of 40 sequences 93 / 69; 12288 x 12288 of rank 64: 200 rows
+// of 2 sequences 71 / 24, 512 of one token with 8 adapters 173 / 86.  Where the bytes are few the rule misses: 256 rows of one
+// token with 8 adapters of rank 16, 4096 x 4096, 17 / 25, of which it takes the large ones.)
 int64_t adapters_of(const AdapterParams& p, int64_t rows) {
     return std::min<int64_t>(p.pool, std::min(rows, ceil_div(std::min<int64_t>(rows, p.M) * p.nseq, p.M)));
 }
@@ -785,7 +780,7 @@ cudaError_t launch_up(const AdapterParams& p, bool few, int sm_count, cudaStream
     // Few tokens: the CTAs that are resident, at most, as each starts with four loads in a row.  Many: several
     // turns of them, but four units each at least, unless that leaves SMs idle.
     const int64_t sms = sm_count;
-    int64_t y = few ? (CH == 0 ? 3 : 2) * sms / tiles
+    int64_t y = few ? 2 * sms / tiles
                     : std::max(std::min(ceil_div(16 * sms, tiles), units / 4), std::min(units, ceil_div(2 * sms, tiles)));
     if (y < 1) y = 1;
     const int64_t chunk = ceil_div(units, y);
