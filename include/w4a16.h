@@ -534,7 +534,7 @@ int w4a16_log_probs(const void* logits, int logit_bits, int64_t M, int64_t V, in
  *                  outside every sequence have no adapter; a table that decreases or leaves [0, M]
  *                  records W4A16_ERR_INVALID_ARG
  *   adapters_i32   [nseq]; -1: none (out = base).  Others outside [0, pool) count as -1 and record
- *                  W4A16_ERR_INVALID_ARG
+ *                  W4A16_ERR_INVALID_ARG.  Of a sequence without rows the entry is not looked at
  *   out_bf16       [M, N], written in full; it may be base itself
  *   workspace      w4a16_add_adapters_workspace bytes; what it holds before or after a call does not
  *                  matter.  Calls that may run at the same time need one each

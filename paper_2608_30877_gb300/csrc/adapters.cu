@@ -13,11 +13,12 @@
 // Rows of a tile that share an adapter are done together.
 //
 // Bound by HBM: the rank gives a product 2 R FLOPs a byte of x.  39004 tokens, 12288 x 12288, eight adapters of rank
-// 16: 135 us (x at 6.4 TB/s) and 314 (base and out at 6.1), 453 together.  Before: mma.sync on x through registers
+// 16: 136 us (x at 6.4 TB/s) and 313 (base and out at 6.1), 457 together.  Before: mma.sync on x through registers
 // 240 us, through shared memory by 16-byte copies 195; the second kernel with an address computed for every load
-// 340.  1363 tokens on 49152 x 12288, rank 64: 38 + 27 us, 70 together (33 at the copy bandwidth): one turn of 176 CTAs, and
-// an adapter's rows that come from L2 for every tile, as many bytes as x.  64 requests of one token with 48 adapters,
-// 12288 x 36864: 21 us (11.3): each kernel starts with the adapters' numbers, a list of them, and only then loads.
+// 340.  1363 tokens on 49152 x 12288, rank 64: 40 + 32 us cold, 70 together (33 at the copy bandwidth): one turn of 176 CTAs,
+// and an adapter's rows that come from L2 for every tile, as many bytes as x.  64 requests of one token with 48 adapters,
+// 12288 x 36864: 21 us (11.3): each kernel starts with the adapters' numbers, a list of them, and only then loads, and the
+// second waits for the first before that.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <algorithm>

@@ -447,7 +447,7 @@ __global__ void __launch_bounds__(512, NV <= 3 && !ODD ? 2 : 1) residual_norm_ke
 
 // Many rows of whole 16-byte units: as many CTAs as are resident, each with a ring of rows in shared
 // memory that bulk copies fill while it is at a row before (the reductions leave the memory idle otherwise).  What is
-// left is issue slots (42%) and the vectors, which the rings leave no room for in L1: five of them come from L2 for every
+// left is issue slots (44%) and the vectors, which the rings leave no room for in L1: five of them come from L2 for every
 // row.  Register pairs (half the arithmetic instructions) took 99 us to 93.
 constexpr int kRingThreads = 384;
 constexpr int kRingRows = 4;               // at most
@@ -738,7 +738,7 @@ cudaError_t launch(const NormParams& p, cudaStream_t stream) {
 cudaError_t launch_residual_norm(const NormParams& p, bool fp32, int sm_count, cudaStream_t stream) {
     const bool whole = p.D % 8 == 0;  // rows of 16-byte units (bases are 16-byte aligned)
     // (a plain bf16 RMS norm is at the copy bandwidth from registers: 39004 rows of 12288 551 us, 613 with the
-    // ring; 4097 of 8200 with both layer norms and an fp32 stream 128, 99 with it)
+    // ring; 4097 of 8200 with both layer norms and an fp32 stream 128, 93 with it)
     if (whole && p.D > 1024 && p.D <= 4 * 8 * kRingThreads && (fp32 || p.layer || p.post_weight != nullptr)) {
         cudaError_t e = cudaSuccess;
         if (fp32 ? launch_ring<float>(p, sm_count, stream, &e) : launch_ring<uint16_t>(p, sm_count, stream, &e)) return e;
