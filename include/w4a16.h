@@ -540,7 +540,7 @@ int w4a16_log_probs(const void* logits, int logit_bits, int64_t M, int64_t V, in
  *                  matter.  Calls that may run at the same time need one each
  * K a multiple of 64, R a multiple of 8 up to 64 (W4A16_ERR_UNSUPPORTED).  Sums in fp32; t = scale (x A^T) is
  * rounded to 12 significant bits for the product with B (those below 2^-6 of the largest of their eight ranks 8i ..
- * 8i + 7 to 2^-17 of it), and the sum with base once.
+ * 8i + 7 to steps of 2^-17 of it), and the sum with base once.
  */
 int w4a16_add_adapters(const void* x_bf16, const void* a_bf16, const void* b_bf16, const void* scale_f32,
                        int64_t pool, const void* seq_start_i32, const void* adapters_i32, int64_t nseq,
